@@ -146,6 +146,67 @@ int w2l_logsoftmax_fwd(const void *z, float *lp, long long rows, int C, int z_dt
 int w2l_logsoftmax_bwd(const float *lp, const float *dlp, float *dz, long long rows, int C,
                        void *stream);
 
+/* ---- reading a frame's scores: log-probabilities of given tokens, entropy, best classes --------------
+ * What a program reads from network output without writing the whole log-softmax: scores of an alignment,
+ * confidences, alternatives for a decoder, the classes that a smaller network is trained on (w2l_distill_fwd_bwd).
+ * For frame (b,t) with scores x = z[b,t,:], m = max x, s = sum_c exp(x_c - m), lp_c = x_c - m - log s, p_c = exp(lp_c):
+ *   logprob[b,t,j]     = lp_{tokens[b,t,j]}                     0 where the token is -1 (none)
+ *   entropy[b,t]       = - sum_c p_c lp_c                       in nats
+ *   top_ids[b,t,k], top_logprob[b,t,k]: the K classes of the largest scores, largest first, equal scores by class,
+ *                        and their lp
+ *   stats[b,t,0..3]    = m, log s, entropy, 0                   what w2l_token_logprob_bwd reads (0, -inf, 0, 0 where s = 0)
+ * z: [B,Tp,C] (z_dtype);  tokens [B,Tp,S] int32;  in_len [B] int32 (0..Tp) or NULL: all frames;  logprob [B,Tp,S],
+ * entropy [B,Tp], top_logprob [B,Tp,K], stats [B,Tp,4] fp32;  top_ids [B,Tp,K] int32.  tokens and logprob are NULL if
+ * S = 0, top_ids and top_logprob if K = 0; entropy and stats are nullable.
+ * Frames t >= in_len[b] are not read: log-probabilities, entropy and stats 0, top_ids -1, top_logprob -inf.
+ * A score of -inf is probability zero (log-probability -inf, no share of the entropy); a frame of nothing else has
+ * entropy 0 and log-probabilities -inf.  A frame that holds NaN or +inf has no distribution: all its outputs are NaN,
+ * its top_ids -1; so have all frames of an utterance whose in_len is outside its range.  A token other than -1
+ * outside [0,C) gives NaN.  (w2l_frame_ids_check_host() validates host copies.)
+ * Limits: C <= 262144, S <= 64, K <= 64, K <= C, B * Tp < 2^31.  Workspace: 256-byte aligned, the queried bytes (0: NULL will do).
+ * Results do not depend on the batch a frame is in, apart from the rounding of fp32 sums, and are bit-reproducible. */
+size_t w2l_token_logprob_workspace_bytes(int B, int Tp, int C, int K, int z_dtype);
+int w2l_token_logprob_fwd(const void *z, const int *tokens, const int *in_len, float *logprob, float *entropy,
+                          int *top_ids, float *top_logprob, float *stats, int B, int Tp, int C, int S, int K,
+                          int z_dtype, void *workspace, size_t ws_bytes, void *stream);
+/* Gradient with respect to the scores, given dlogprob [B,Tp,S], dentropy [B,Tp] (NULL: 0) and dtop [B,Tp,K]
+ * (gradient with respect to top_logprob), all fp32.  With G = sum_j dlogprob_j + sum_k dtop_k over the entries that are there:
+ *   dz_c = -p_c (G + dentropy (lp_c + entropy)) + sum_{j: tokens_j = c} dlogprob_j + sum_{k: top_ids_k = c} dtop_k
+ * z, tokens, in_len as for the forward call, stats and top_ids as it wrote them; dz: [B,Tp,C], dz_dtype W2L_F32, or
+ * W2L_BF16 where z is bf16.  accumulate = 0 overwrites dz, 1 adds to it (the sum is rounded once).  tokens and dlogprob are NULL
+ * if S = 0; top_ids and dtop if K = 0.  The gradient of a frame that is not there (t >= in_len[b], bad in_len) or has no
+ * distribution (NaN, +inf, nothing but -inf) is 0, of entries that are not (token or top_ids outside [0,C)) as well.  No workspace. */
+int w2l_token_logprob_bwd(const void *z, const float *stats, const int *tokens, const float *dlogprob,
+                          const float *dentropy, const int *top_ids, const float *dtop, const int *in_len, void *dz,
+                          int B, int Tp, int C, int S, int K, int z_dtype, int dz_dtype, int accumulate, void *stream);
+
+/* ---- distillation from a teacher's best classes ------------------------------------------------------
+ * A criterion that trains a network on what a larger one gave each frame: ids t_ids[b,t,k] and scores
+ * t_scores[b,t,k] (logits or log-probabilities, such as w2l_token_logprob_fwd's top_logprob) of its K best classes.  At
+ * temperature tau, with q the softmax of t_scores / tau over the entries that are there and p that of z / tau over
+ * all classes:
+ *   frame_loss[b,t] = weight[b,t] * tau^2 * sum_k q_k (log q_k - log p_{id_k})
+ *   loss[b]         = sum_{t < in_len[b]} frame_loss[b,t]
+ *   dz[b,t,c]       = grad_scale * d(sum_b loss_b)/d z = grad_scale * weight[b,t] * tau * (p_c - sum_{k: id_k = c} q_k)
+ * z: [B,Tp,C] (z_dtype);  t_ids [B,Tp,K] int32, t_scores [B,Tp,K] fp32;  in_len [B] int32 (0..Tp) or NULL: all
+ * frames;  weight [B,Tp] fp32 or NULL: 1;  frame_loss [B,Tp] and loss [B] fp32 (loss nullable);  dz [B,Tp,C] or NULL
+ * (losses alone), dz_dtype W2L_F32, or W2L_BF16 where z is bf16.  accumulate = 0 overwrites dz, 1 adds to it, rounding
+ * the sum once (to the gradient that w2l_ctc_fwd_bwd left there, say).
+ * An id of -1 or a score of -inf is an entry that is not there; the same id in two entries counts twice.  Frames t >=
+ * in_len[b] and frames of weight 0 are not read, and like frames with no entry they have loss 0 and zero gradient.
+ * A class of probability zero (z = -inf) that the teacher gives weight to: frame_loss +inf.  NaN or +inf in the frame's
+ * z or t_scores, an id other than -1 outside [0,C), an in_len outside its range: frame_loss NaN (the whole utterance in the last
+ * case).  A frame whose loss is no finite fp32 number has zero gradient.
+ * 0 < temperature, both scales finite.  Limits and workspace as above; 1 <= K. */
+size_t w2l_distill_workspace_bytes(int B, int Tp, int C, int K, int z_dtype);
+int w2l_distill_fwd_bwd(const void *z, const int *t_ids, const float *t_scores, const int *in_len, const float *weight,
+                        float *frame_loss, float *loss, void *dz, int B, int Tp, int C, int K, float temperature,
+                        float grad_scale, int z_dtype, int dz_dtype, int accumulate,
+                        void *workspace, size_t ws_bytes, void *stream);
+/* HOST pointers: ids [B,Tp,n] (tokens or t_ids), in_len [B] or NULL.  Returns W2L_ERR_TARGET for an in_len outside [0,Tp] or, in
+ * a frame t < in_len[b], an id other than -1 outside [0,C). */
+int w2l_frame_ids_check_host(const int *ids, const int *in_len, int B, int Tp, int C, int n);
+
 /* ---- SGD with momentum (Sec. 4.1: the optimiser of every run in the paper) ---------
  * The paper names the optimiser and does not write the update out; this is the classical
  * heavy-ball form with optional L2 weight decay, elementwise over n values:

@@ -192,6 +192,105 @@ def logsoftmax_bwd(lp, dlp):
     return dz
 
 
+# ----------------------------------------------------------------------------- frame scores
+def _log_probs(x):
+    """lp[..., C] of scores x (fp64), nothing but -inf where a row holds nothing but -inf; and which rows hold NaN or +inf."""
+    odd = (np.isnan(x) | (x == np.inf)).any(-1)
+    x = np.where(odd[..., None], 0.0, x)
+    m = x.max(-1, keepdims=True)
+    m = np.where(np.isfinite(m), m, 0.0)
+    with np.errstate(divide="ignore"):
+        lse = np.log(np.exp(x - m).sum(-1, keepdims=True))
+    return x - m - np.where(np.isfinite(lse), lse, 0.0), odd
+
+
+def _frame_kind(in_len, B, T):
+    """(live, bad) [B,T] of the frames: bad where the utterance's length is out of range."""
+    n = np.full(B, T) if in_len is None else np.asarray(in_len)
+    bad = np.repeat(((n < 0) | (n > T))[:, None], T, 1)
+    return (np.arange(T)[None] < n[:, None]) & ~bad, bad
+
+
+def token_logprob(z, tokens, K=0, in_len=None):
+    """Log-probabilities of tokens[B,T,S], entropy[B,T] and the K largest scores' classes and log-probabilities of every frame of
+    z[B,T,C]: equal scores by class.  Frames beyond in_len: 0, -1, -inf; rows with NaN or +inf, and utterances whose length is out of
+    range: NaN and -1; token -1: 0, others outside the classes: NaN.  Returns a dict; "lp" holds all log-probabilities."""
+    z = np.asarray(z, dtype=np.float64)
+    B, T, Cc = z.shape
+    tokens = np.asarray(tokens)
+    live, bad = _frame_kind(in_len, B, T)
+    lp, odd = _log_probs(z)
+    bad |= live & odd
+    live &= ~odd
+    p = np.exp(lp)
+    H = -(p * np.where(p > 0, lp, 0.0)).sum(-1)
+    pick = lambda ok, v, rest: np.where(ok, v, np.where(bad, np.nan, rest))
+    here = (tokens >= 0) & (tokens < Cc)
+    t = np.take_along_axis(lp, np.where(here, tokens, 0), 2)
+    t = np.where(here, t, np.where(tokens == -1, 0.0, np.nan))
+    top = np.argsort(-np.where(odd[..., None], 0.0, z), axis=-1, kind="stable")[..., :K]
+    return dict(lp=lp, logprob=np.where(live[..., None], t, np.where(bad, np.nan, 0.0)[..., None]),
+                entropy=pick(live, H, 0.0), live=live,
+                top_ids=np.where(live[..., None], top, -1),
+                top_logprob=np.where(live[..., None], np.take_along_axis(lp, top, 2), np.where(bad, np.nan, -np.inf)[..., None]))
+
+
+def token_logprob_bwd(z, tokens, dlogprob, dentropy=None, top_ids=None, dtop=None, in_len=None):
+    """Gradient [B,T,C] of sum(dlogprob * logprob) + sum(dentropy * entropy) + sum(dtop * top_logprob) with respect to z; 0 in
+    frames that are not there or hold nothing but -inf, and for entries outside the classes."""
+    z = np.asarray(z, dtype=np.float64)
+    B, T, Cc = z.shape
+    f = token_logprob(z, np.zeros((B, T, 0), int), 0, in_len)
+    lp, p = f["lp"], np.exp(f["lp"])
+    direct = np.zeros((B * T, Cc))                # gradient with respect to the log-probabilities
+    for ids, g in ((tokens, dlogprob), (top_ids, dtop)):
+        if g is not None:
+            ids, g = np.asarray(ids).reshape(B * T, -1), np.asarray(g, dtype=np.float64).reshape(B * T, -1)
+            ok = (ids >= 0) & (ids < Cc)
+            rows = np.broadcast_to(np.arange(B * T)[:, None], ids.shape)
+            np.add.at(direct, (rows[ok], ids[ok]), g[ok])
+    direct = direct.reshape(B, T, Cc)
+    dz = direct - p * direct.sum(-1, keepdims=True)
+    if dentropy is not None:
+        H = np.where(f["live"], f["entropy"], 0.0)[..., None]
+        dz -= np.asarray(dentropy, dtype=np.float64)[..., None] * p * (np.where(p > 0, lp, 0.0) + H)
+    return np.where((f["live"] & (z > -np.inf).any(-1))[..., None], dz, 0.0)
+
+
+def distill(z, t_ids, t_scores, tau=1.0, weight=None, in_len=None, grad_scale=1.0):
+    """(frame_loss[B,T], loss[B], dz[B,T,C]) of weight * tau^2 * KL(softmax(t_scores / tau) || softmax(z / tau) at t_ids).  An id of
+    -1 or a score of -inf is no entry; bad ids, NaN, +inf: NaN; no entry or weight 0: 0; a loss that is no finite
+    fp32 number has no gradient."""
+    z = np.asarray(z, dtype=np.float64)
+    B, T, Cc = z.shape
+    live, badlen = _frame_kind(in_len, B, T)
+    frame = np.where(badlen, np.nan, 0.0)
+    dz = np.zeros(z.shape)
+    lp, odd = _log_probs(z / tau)
+    for b in range(B):
+        for t in range(T):
+            w = 1.0 if weight is None else float(weight[b, t])
+            if not live[b, t] or w == 0.0:
+                continue
+            ids = np.asarray(t_ids[b, t])
+            s = np.where(ids == -1, -np.inf, np.asarray(t_scores[b, t], dtype=np.float64)) / tau
+            if odd[b, t] or np.any((ids < -1) | (ids >= Cc)) or np.any(np.isnan(s) | (s == np.inf)):
+                frame[b, t] = np.nan
+                continue
+            s, ids = s[s > -np.inf], ids[s > -np.inf]
+            if len(ids) == 0:
+                continue
+            logq = s - s.max()
+            logq = logq - np.log(np.exp(logq).sum())
+            q = np.exp(logq)
+            frame[b, t] = w * tau * tau * (q * (logq - lp[b, t, ids])).sum()
+            if np.abs(frame[b, t]) <= np.finfo(np.float32).max:
+                g = np.exp(lp[b, t])
+                np.add.at(g, ids, -q)
+                dz[b, t] = grad_scale * w * tau * g
+    return frame, frame.sum(1), dz
+
+
 # ----------------------------------------------------------------------------- optimiser
 def sgd_momentum(w, v, g, lr, momentum, weight_decay=0.0):
     """One SGD-with-momentum update (Sec. 4.1; heavy-ball form): returns (w', v') with

@@ -24,6 +24,8 @@ __all__ = [
     "w2l_logsoftmax_fwd", "w2l_logsoftmax_bwd", "w2l_ctc_workspace_bytes", "w2l_ctc_fwd_bwd", "w2l_ctc_fwd_bwd_noalloc",
     "w2l_ctc_check_targets_host", "w2l_ctc_launch_config", "w2l_asg_launch_config", "w2l_asg_workspace_bytes", "w2l_asg_fwd_bwd", "w2l_asg_check_targets_host",
     "w2l_logmel_num_frames", "w2l_logmel_fwd",
+    "w2l_token_logprob_workspace_bytes", "w2l_token_logprob_fwd", "w2l_token_logprob_bwd",
+    "w2l_distill_workspace_bytes", "w2l_distill_fwd_bwd", "w2l_frame_ids_check_host",
     "w2l_train_step_workspace_bytes", "w2l_train_step", "w2l_train_step_asg_workspace_bytes", "w2l_train_step_asg",
     "w2l_train_step_launch_config", "w2l_train_step_layer_config", "w2l_sgd_momentum_step",
     "w2l_probe_mfma", "raw",
@@ -68,6 +70,12 @@ def _load():
         "w2l_glu_bwd": (i, [vp, vp, vp, ll, i, i, vp]),
         "w2l_logsoftmax_fwd": (i, [vp, vp, ll, i, i, vp]),
         "w2l_logsoftmax_bwd": (i, [vp, vp, vp, ll, i, vp]),
+        "w2l_token_logprob_workspace_bytes": (sz, [i] * 5),
+        "w2l_token_logprob_fwd": (i, [vp] * 8 + [i] * 6 + [vp, sz, vp]),
+        "w2l_token_logprob_bwd": (i, [vp] * 9 + [i] * 8 + [vp]),
+        "w2l_distill_workspace_bytes": (sz, [i] * 5),
+        "w2l_distill_fwd_bwd": (i, [vp] * 8 + [i] * 4 + [f, f] + [i] * 3 + [vp, sz, vp]),
+        "w2l_frame_ids_check_host": (i, [vp, vp] + [i] * 4),
         "w2l_ctc_workspace_bytes": (sz, [i] * 4),
         "w2l_ctc_fwd_bwd": (i, [vp, i, vp, vp, vp, vp, vp, i, i, i, i, i, f, vp, sz, vp]),
         "w2l_ctc_fwd_bwd_noalloc": (i, [vp, i, vp, vp, vp, vp, vp, i, i, i, i, i, f, vp]),
@@ -232,6 +240,118 @@ def w2l_logsoftmax_bwd(lp, dlp, dz, stream=None):
     _check(raw.w2l_logsoftmax_bwd(_p(lp), _p(dlp), _p(dz), lp.numel() // Cc, Cc, _stream(stream)),
            "w2l_logsoftmax_bwd")
     return dz
+
+
+def _frames(t, shape, dtype, z, name):
+    """Device pointer of an operand that has to be `shape` of `dtype` beside the scores z (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+    if tuple(t.shape) != shape:
+        raise ValueError("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
+    if t.device != z.device:
+        raise ValueError("%s is on %s, the scores are on %s" % (name, t.device, z.device))
+    return _p(t)
+
+
+def _scores(z):
+    if z.dim() != 3:
+        raise ValueError("scores must be [B, T, C], not %s" % (tuple(z.shape),))
+    if not z.is_cuda:
+        raise ValueError("scores must be on a GPU")
+    return tuple(z.shape)
+
+
+def _grad_of(dz, z):
+    if dz is not None and dz.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("unsupported tensor dtype %s" % dz.dtype)
+    return _frames(dz, tuple(z.shape), dz.dtype, z, "dz") if dz is not None else None
+
+
+def _on_device(z, stream, workspace, call):
+    """call(workspace pointer, its bytes, stream) with the device of z current; its current stream unless one is given."""
+    if workspace is not None and workspace.device != z.device:
+        raise ValueError("workspace is on %s, the scores are on %s" % (workspace.device, z.device))
+    wp, wn = _ws(workspace)
+    if z.device.index == torch.cuda.current_device():
+        return call(wp, wn, _stream(stream))
+    with torch.cuda.device(z.device):
+        return call(wp, wn, _stream(stream))
+
+
+def w2l_token_logprob_workspace_bytes(B, Tp, Cc, K, dtype) -> int:
+    return raw.w2l_token_logprob_workspace_bytes(B, Tp, Cc, K, dtype)
+
+
+def w2l_token_logprob_fwd(z, tokens=None, logprob=None, entropy=None, top_ids=None, top_logprob=None, stats=None, in_len=None,
+                          workspace=None, stream=None):
+    """Scores z[B,T,C] -> log-probabilities of tokens[B,T,S], entropy[B,T], the K best classes (top_ids, top_logprob [B,T,K])
+    and what the backward call reads (stats [B,T,4]); outputs that are None are not wanted."""
+    B, T, Cc = _scores(z)
+    S = 0 if tokens is None else tokens.shape[-1]
+    K = 0 if top_ids is None else top_ids.shape[-1]
+    f, n = torch.float32, torch.int32
+    ptr = (_p(z), _frames(tokens, (B, T, S), n, z, "tokens"), _frames(in_len, (B,), n, z, "in_len"),
+           _frames(logprob, (B, T, S), f, z, "logprob"), _frames(entropy, (B, T), f, z, "entropy"),
+           _frames(top_ids, (B, T, K), n, z, "top_ids"), _frames(top_logprob, (B, T, K), f, z, "top_logprob"),
+           _frames(stats, (B, T, 4), f, z, "stats"))
+    dt = _dt(z)
+    _check(_on_device(z, stream, workspace, lambda wp, wn, st: raw.w2l_token_logprob_fwd(*ptr, B, T, Cc, S, K, dt, wp, wn, st)),
+           "w2l_token_logprob_fwd")
+    return logprob, entropy, top_ids, top_logprob, stats
+
+
+def w2l_token_logprob_bwd(z, stats, dz, tokens=None, dlogprob=None, dentropy=None, top_ids=None, dtop=None, in_len=None,
+                          accumulate=False, stream=None):
+    """dz[B,T,C] (accumulate: added to it) from the gradients of the forward call's outputs; those that are None are 0."""
+    B, T, Cc = _scores(z)
+    if dlogprob is None:
+        tokens = None
+    if dtop is None:
+        top_ids = None
+    S = 0 if tokens is None else tokens.shape[-1]
+    K = 0 if top_ids is None else top_ids.shape[-1]
+    f, n = torch.float32, torch.int32
+    ptr = (_p(z), _frames(stats, (B, T, 4), f, z, "stats"), _frames(tokens, (B, T, S), n, z, "tokens"),
+           _frames(dlogprob, (B, T, S), f, z, "dlogprob"), _frames(dentropy, (B, T), f, z, "dentropy"),
+           _frames(top_ids, (B, T, K), n, z, "top_ids"), _frames(dtop, (B, T, K), f, z, "dtop"),
+           _frames(in_len, (B,), n, z, "in_len"), _grad_of(dz, z))
+    dt, gt = _dt(z), _dt(dz)
+    _check(_on_device(z, stream, None, lambda wp, wn, st: raw.w2l_token_logprob_bwd(*ptr, B, T, Cc, S, K, dt, gt, int(bool(accumulate)), st)),
+           "w2l_token_logprob_bwd")
+    return dz
+
+
+def w2l_distill_workspace_bytes(B, Tp, Cc, K, dtype) -> int:
+    return raw.w2l_distill_workspace_bytes(B, Tp, Cc, K, dtype)
+
+
+def w2l_distill_fwd_bwd(z, t_ids, t_scores, frame_loss, loss=None, dz=None, in_len=None, weight=None, temperature=1.0,
+                        grad_scale=1.0, accumulate=False, workspace=None, stream=None):
+    """Loss of a student's scores z[B,T,C] against a teacher's best classes (t_ids, t_scores [B,T,K]) and its gradient dz."""
+    B, T, Cc = _scores(z)
+    K = t_ids.shape[-1]
+    f, n = torch.float32, torch.int32
+    ptr = (_p(z), _frames(t_ids, (B, T, K), n, z, "t_ids"), _frames(t_scores, (B, T, K), f, z, "t_scores"),
+           _frames(in_len, (B,), n, z, "in_len"), _frames(weight, (B, T), f, z, "weight"),
+           _frames(frame_loss, (B, T), f, z, "frame_loss"), _frames(loss, (B,), f, z, "loss"), _grad_of(dz, z))
+    dt = _dt(z)
+    gt = dt if dz is None else _dt(dz)
+    _check(_on_device(z, stream, workspace,
+                      lambda wp, wn, st: raw.w2l_distill_fwd_bwd(*ptr, B, T, Cc, K, float(temperature), float(grad_scale), dt, gt,
+                                                                 int(bool(accumulate)), wp, wn, st)),
+           "w2l_distill_fwd_bwd")
+    return frame_loss, loss, dz
+
+
+def w2l_frame_ids_check_host(ids, in_len, Cc) -> int:
+    """numpy int32 host arrays ids[B,T,n], in_len[B] or None; returns the status instead of raising."""
+    import numpy as np
+    t = np.ascontiguousarray(ids, dtype=np.int32)
+    il = None if in_len is None else np.ascontiguousarray(in_len, dtype=np.int32)
+    B, T, n = t.shape
+    return raw.w2l_frame_ids_check_host(t.ctypes.data, None if il is None else il.ctypes.data, B, T, Cc, n)
 
 
 def w2l_sgd_momentum_step(w, v, grad, w_lowp, lr, momentum, weight_decay=0.0, stream=None):
