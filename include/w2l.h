@@ -163,7 +163,7 @@ int w2l_logsoftmax_bwd(const float *lp, const float *dlp, float *dz, long long r
  * entropy 0 and log-probabilities -inf.  A frame that holds NaN or +inf has no distribution: all its outputs are NaN,
  * its top_ids -1; so have all frames of an utterance whose in_len is outside its range.  A token other than -1
  * outside [0,C) gives NaN.  (w2l_frame_ids_check_host() validates host copies.)
- * Limits: C <= 262144, S <= 64, K <= 64, K <= C, B * Tp < 2^31.  Workspace: 256-byte aligned, the queried bytes (0: NULL will do).
+ * Limits: C <= 262144, S <= 64, K <= 64, K <= C, B * Tp < 2^31, B * Tp * C <= 2^40.  Workspace: 256-byte aligned, the queried bytes (0: NULL will do).
  * Results do not depend on the batch a frame is in, apart from the rounding of fp32 sums, and are bit-reproducible. */
 size_t w2l_token_logprob_workspace_bytes(int B, int Tp, int C, int K, int z_dtype);
 int w2l_token_logprob_fwd(const void *z, const int *tokens, const int *in_len, float *logprob, float *entropy,

@@ -13,7 +13,8 @@ using namespace w2l;
 namespace {
 
 constexpr int MAX_CLASSES = 262144, MAX_ENTRIES = 64;
-constexpr int THREADS = 256;
+constexpr int THREADS = 256, MAX_GROUPS = 16;
+constexpr float LOG2E = 1.44269504088896f;
 enum Frame { LIVE = 0, PADDING = 1, BAD = 2 };
 
 __device__ __forceinline__ Frame frame_of(const int* __restrict__ in_len, unsigned r, unsigned Tp)
@@ -24,214 +25,930 @@ __device__ __forceinline__ Frame frame_of(const int* __restrict__ in_len, unsign
     return n < 0 || n > (int)Tp ? BAD : (int)(r - b * Tp) < n ? LIVE : PADDING;
 }
 
-// reductions over the workgroup, the same value in every thread
+
+// ---- reductions over lanes ----------------------------------------------------------------------------
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float lane_of(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+struct Min { __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); } };
+struct Sum { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+// over the sixteen lanes of a DPP row, the same bits in each of them
 template <typename F>
-__device__ __forceinline__ float block_reduce(float v, F f, float* lds)
+__device__ __forceinline__ float row16(float v, F f)
 {
+    v = f(v, lane_of<0xB1>(v));   // quad_perm [1,0,3,2]
+    v = f(v, lane_of<0x4E>(v));   // quad_perm [2,3,0,1]
+    v = f(v, lane_of<0x141>(v));  // row_half_mirror
+    return f(v, lane_of<0x140>(v));  // row_mirror
+}
+// over the wavefront, uniform
+template <typename F>
+__device__ __forceinline__ float wave64(float v, F f)
+{
+    v = row16(v, f);
+    v = f(v, lane_of<0x142, 0xa>(v));  // row_bcast:15 into rows 1 and 3 (lanes that receive nothing hold what nobody reads)
+    v = f(v, lane_of<0x143, 0xc>(v));  // row_bcast:31 into rows 2 and 3
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+// LDS written by some lanes of a wavefront (MULTI: a workgroup) and read by others after this
+template <bool MULTI>
+__device__ __forceinline__ void exchange()
+{
+    if (MULTI) __syncthreads();
+    else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// ---- rows in registers ---------------------------------------------------------------------------------
+// A row lies in 16-byte vectors on the grid of the whole tensor (rows of odd length begin inside one): nv of them, `head`
+// elements before the row's first.  They are dealt out in slots of 64, a vector a lane, in turn over the row's wavefronts
+// (those of a workgroup, and of several workgroups where there are few rows), so that the row is read once, with whole loads, and stays in
+// registers: V slots at most a wavefront.  Lanes beyond the row, and elements of a vector that belong to its neighbours, are -inf.
+template <typename T> constexpr int LANE_VALUES = 16 / sizeof(T);
+
+struct Row {
+    size_t first;    // element of the tensor that vector 0 begins with
+    int head, nv;
+};
+template <typename T>
+__device__ __forceinline__ Row row_at(unsigned r, int C)
+{
+    constexpr int N = LANE_VALUES<T>;
+    const size_t i = (size_t)r * C;
+    const int head = (int)(i & (N - 1));
+    return {i - head, head, (head + C + N - 1) / N};
+}
+
+__device__ __forceinline__ void unpack(uint4 q, float (&x)[4])
+{
+    x[0] = __uint_as_float(q.x); x[1] = __uint_as_float(q.y); x[2] = __uint_as_float(q.z); x[3] = __uint_as_float(q.w);
+}
+__device__ __forceinline__ void unpack(uint4 q, float (&x)[8])
+{
+    const unsigned w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
-    for (int w = 1; w < THREADS / 64; ++w) v = f(v, lds[w]);
-    __syncthreads();
-    return v;
+    for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(w[j] << 16); x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
 }
-__device__ __forceinline__ float add(float a, float b) { return a + b; }
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
-
-// class `c` at score `v` comes before class `d` at score `w`
-__device__ __forceinline__ bool before(float v, int c, float w, int d) { return v > w || (v == w && c < d); }
-
-struct RowStats { float m, s, u; bool ok; };  // ok: no NaN and no +inf; m is finite (0 where every score is -inf, and then s = 0)
-template <typename T>
-__device__ RowStats row_stats(const T* __restrict__ x, int C, float inv_tau, float* lds)
+__device__ __forceinline__ uint4 pack(const float (&x)[4])
 {
-    RowStats q;
-    float m = -INFINITY, bad = 0.f;
-    for (int c = threadIdx.x; c < C; c += THREADS) {
-        const float v = Elem<T>::load(x, c);
-        if (!(v < INFINITY)) bad = 1.f;
-        m = fmaxf(m, v);
-    }
-    q.ok = block_reduce(bad, larger, lds) == 0.f;
-    m = block_reduce(m, larger, lds);
-    q.m = m == -INFINITY ? 0.f : m;
-    float s = 0.f, u = 0.f;
-    for (int c = threadIdx.x; c < C; c += THREADS) {
-        const float d = (Elem<T>::load(x, c) - q.m) * inv_tau, e = expf(d);
-        s += e;
-        u += e * fmaxf(d, -1000.f);  // 0 * -inf is no share of the entropy
-    }
-    q.s = block_reduce(s, add, lds);
-    q.u = block_reduce(u, add, lds);
-    return q;
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[8])
+{
+    unsigned w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = (unsigned)f32_to_bf16(x[2 * j]) | (unsigned)f32_to_bf16(x[2 * j + 1]) << 16;
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// vector n of the row.  A vector that reaches past the tensor's last element is put together from single loads
 template <typename T>
-__global__ __launch_bounds__(THREADS) void token_fwd_k(const T* __restrict__ z, const int* __restrict__ tokens, const int* __restrict__ in_len,
-                                                       float* __restrict__ logprob, float* __restrict__ entropy, int* __restrict__ top_ids,
-                                                       float* __restrict__ top_logprob, float* __restrict__ stats, unsigned rows, unsigned Tp, int C,
-                                                       int S, int K)
+__device__ __forceinline__ uint4 load_vector(const T* __restrict__ z, size_t total, const Row& row, int n, int C)
 {
-    __shared__ float lds[THREADS / 64];
-    __shared__ int lds_c[THREADS / 64];
-    for (unsigned r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T* x = z + (size_t)r * C;
-        const int tid = threadIdx.x;
-        const Frame f = frame_of(in_len, r, Tp);
-        RowStats q{0.f, 0.f, 0.f, false};
-        if (f == LIVE) q = row_stats(x, C, 1.f, lds);
-        if (f != LIVE || !q.ok) {
-            const float v = f == PADDING ? 0.f : NAN;
-            if (tid < S) logprob[(size_t)r * S + tid] = v;
-            if (tid < K) {
-                top_ids[(size_t)r * K + tid] = -1;
-                top_logprob[(size_t)r * K + tid] = f == PADDING ? -INFINITY : NAN;
+    constexpr int N = LANE_VALUES<T>;
+    float x[N];
+    const int c0 = n * N - row.head;
+    if (n >= row.nv) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = -INFINITY;
+        return pack(x);
+    }
+    const size_t i = row.first + (size_t)n * N;
+    if (c0 >= 0 && c0 + N <= C) return *reinterpret_cast<const uint4*>(z + i);
+    if (i + N <= total) unpack(*reinterpret_cast<const uint4*>(z + i), x);
+    else
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = i + e < total ? Elem<T>::load(z, i + e) : -INFINITY;
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = (unsigned)(c0 + e) < (unsigned)C ? x[e] : -INFINITY;
+    return pack(x);
+}
+
+// ---- the K largest of a row --------------------------------------------------------------------------------
+// Scores in the order of their bits, as unsigned integers; and a score with its class as one integer that orders by score, then by
+// the lower class.  (+ 0.f: the two zeros are equal.)
+__device__ __forceinline__ unsigned key_of(float x)
+{
+    const unsigned u = __float_as_uint(x + 0.f);
+    return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float of_key(unsigned k) { return __uint_as_float(k ^ ((unsigned)((int)~k >> 31) | 0x80000000u)); }
+typedef unsigned long long ranked_t;
+__device__ __forceinline__ ranked_t ranked(float x, int c) { return (ranked_t)key_of(x) << 32 | ~(unsigned)c; }
+__device__ __forceinline__ int class_of(ranked_t k) { return (int)~(unsigned)k; }
+__device__ __forceinline__ float score_of(ranked_t k) { return of_key((unsigned)(k >> 32)); }
+
+__device__ __forceinline__ int below(unsigned long long mask)  // bits of the mask in lanes below this one
+{
+    return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
+}
+
+// A threshold that at least `need` (<= 64) values of the wavefront reach, and not many more: each lane brings the largest of four
+// groups of its values, and the threshold is bisected (over the order of the bits) until about `need` of these 256 reach it.
+// least: the smallest of the lanes' largest, which 64 values reach; most: the largest of all.
+__device__ __forceinline__ float wave_threshold(const float (&group)[4], float least, float most, int need)
+{
+    unsigned lo = key_of(least), hi = key_of(most) + 1;
+    while (hi - lo > 1) {
+        const unsigned mid = lo + (hi - lo) / 2;
+        const float t = of_key(mid);
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) n += __popcll(__ballot(group[j] >= t));
+        if (n >= need) {
+            lo = mid;
+            if (n <= need + 4) break;
+        } else
+            hi = mid;
+    }
+    return of_key(lo);
+}
+
+// The wavefront's K largest classes, exactly, into list[0 .. K) in any order (fewer, if it holds fewer classes); returns how many.
+// For rows where thresholds leave too many: equal scores, or fewer finite ones than K.  The K-th score is bisected over
+// the registers, and of the scores equal to it the lowest classes are taken.
+template <typename T, int V>
+__device__ int exact_largest(const uint4 (&q)[V], int ns, int step, int n0, const Row& row, int C, int K, ranked_t* list)
+{
+    constexpr int N = LANE_VALUES<T>;
+    float least = INFINITY, most = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (v < ns) {
+            float x[N];
+            unpack(q[v], x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) { least = fminf(least, x[e]); most = fmaxf(most, x[e]); }
+        }
+    least = wave64(least, Min());
+    most = wave64(most, Max());
+    unsigned lo = key_of(least), hi = key_of(most) + 1, mid = lo + 1;  // first: are more equal to the least than are wanted?
+    while (hi - lo > 1) {
+        const float t = of_key(mid);
+        int n = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < ns) {
+                float x[N];
+                unpack(q[v], x);
+                const int c0 = (n0 + v * step) * N - row.head;
+#pragma unroll
+                for (int e = 0; e < N; ++e) n += __popcll(__ballot(x[e] >= t && (unsigned)(c0 + e) < (unsigned)C));
             }
-            if (tid == 0 && entropy) entropy[r] = v;
-            if (tid == 0 && stats) reinterpret_cast<float4*>(stats)[r] = make_float4(v, v, v, 0.f);
+        (n >= K ? lo : hi) = mid;
+        mid = lo + (hi - lo) / 2;
+    }
+    const float t = of_key(lo);
+    int n = 0;
+#pragma unroll 1
+    for (int equal = 0; equal < 2; ++equal)   // those above the threshold, then those at it, in the order of their classes
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < ns && n < K) {
+                float x[N];
+                unpack(q[v], x);
+                const int c0 = (n0 + v * step) * N - row.head;
+                int before = n, mine = 0;  // of the slot's takers, those in lower lanes come first, then those before in this one
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const unsigned long long b = __ballot((equal ? x[e] == t : x[e] > t) && (unsigned)(c0 + e) < (unsigned)C);
+                    before += below(b);
+                    n += __popcll(b);
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if ((equal ? x[e] == t : x[e] > t) && (unsigned)(c0 + e) < (unsigned)C) {
+                        if (before + mine < K) list[before + mine] = ranked(x[e], c0 + e);
+                        ++mine;
+                    }
+            }
+    return n < K ? n : K;
+}
+
+// list[0 .. n) of a wavefront (n <= 128) or a workgroup (MULTI: n <= its threads), all different: calls out(rank, entry) for the K first
+template <bool MULTI, typename F>
+__device__ __forceinline__ void rank_list(const ranked_t* list, int n, int K, int thread, F out)
+{
+    if (MULTI) {
+        if (thread >= n) return;
+        const ranked_t a = list[thread];
+        int before = 0;
+        for (int j = 0; j < n; ++j) before += list[j] > a;
+        if (before < K) out(before, a);
+    } else {
+        const bool on = thread < n, on2 = thread + 64 < n;
+        const ranked_t a = on ? list[thread] : 0, a2 = on2 ? list[thread + 64] : 0;
+        int before = 0, before2 = 0;
+        for (int j = 0; j < n; ++j) {
+            const ranked_t w = list[j];
+            before += w > a;
+            before2 += w > a2;
+        }
+        if (on && before < K) out(before, a);
+        if (on2 && before2 < K) out(before2, a2);
+    }
+}
+
+// ---- log-probabilities, entropy, best classes --------------------------------------------------------
+struct TokenOut {
+    float *logprob, *entropy;
+    int* top_ids;
+    float *top_logprob, *stats;
+    int S, K;
+};
+__device__ __forceinline__ void write_absent(const TokenOut& o, unsigned r, Frame f, int i, int step)
+{
+    const float v = f == PADDING ? 0.f : NAN;
+    for (int j = i; j < o.S; j += step) o.logprob[(size_t)r * o.S + j] = v;
+    for (int j = i; j < o.K; j += step) {
+        o.top_ids[(size_t)r * o.K + j] = -1;
+        o.top_logprob[(size_t)r * o.K + j] = f == PADDING ? -INFINITY : NAN;
+    }
+    if (i == 0 && o.entropy) o.entropy[r] = v;
+    if (i == 0 && o.stats) reinterpret_cast<float4*>(o.stats)[r] = make_float4(v, v, v, 0.f);
+}
+struct Dist { float m, logs, H; };  // s = 0, nothing but -inf: m = 0, and logs is taken as 0
+__device__ __forceinline__ Dist dist_of(float m, float s, float u)
+{
+    const bool any = s > 0.f;
+    const float logs = any ? logf(s) : 0.f;
+    return {m, logs, any ? logs - u / s : 0.f};
+}
+__device__ __forceinline__ void write_dist(const TokenOut& o, unsigned r, const Dist& d, bool any)
+{
+    if (o.entropy) o.entropy[r] = d.H;
+    if (o.stats) reinterpret_cast<float4*>(o.stats)[r] = make_float4(d.m, any ? d.logs : -INFINITY, d.H, 0.f);
+}
+
+// Partial results of a row that several workgroups share: [rows][G] of (m or -inf, s, u, 0), then [rows][G][K] best classes, largest
+// first, 0 where there are fewer
+struct Parts {
+    float4* sums;
+    ranked_t* best;
+};
+
+// One row by a wavefront (!MULTI, four rows a workgroup), by a workgroup, or by G workgroups, which leave partial results (PARTS) for
+// token_join_k.  kscale = log2 e / temperature.
+template <typename T, int V, bool MULTI>
+__global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
+                                                                                    const int* __restrict__ in_len, TokenOut o, Parts parts,
+                                                                                    unsigned rows, unsigned Tp, int C, int G, float kscale)
+{
+    constexpr int N = LANE_VALUES<T>;
+    constexpr int ROWS = MULTI ? 1 : 4, CAP = MULTI ? 1024 : 128;
+    __shared__ ranked_t lists[ROWS][CAP];
+    __shared__ float red[MULTI ? 4 : 1][16];
+    __shared__ int count, exact;  // entries of the list; where they did not fit, those of all wavefronts' own best
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = MULTI ? blockDim.x >> 6 : 1;
+    const size_t total = (size_t)rows * C;
+    ranked_t* const list = lists[MULTI ? 0 : wave];
+    const int thread = MULTI ? (int)threadIdx.x : lane;
+    const unsigned tasks = rows * G, stride = gridDim.x * ROWS;
+    for (unsigned task = blockIdx.x * ROWS + (MULTI ? 0 : wave); task < tasks; task += stride) {
+        const unsigned r = task / G;
+        const int g = task - r * G;
+        const Frame f = frame_of(in_len, r, Tp);
+        if (f != LIVE) {
+            if (G == 1) write_absent(o, r, f, thread, MULTI ? blockDim.x : 64);
             continue;
         }
-        const float logs = q.s > 0.f ? logf(q.s) : 0.f, H = q.s > 0.f ? logs - q.u / q.s : 0.f;
-        if (tid == 0 && entropy) entropy[r] = H;
-        if (tid == 0 && stats) reinterpret_cast<float4*>(stats)[r] = make_float4(q.m, q.s > 0.f ? logs : -INFINITY, H, 0.f);
-        if (tid < S) {
-            const int c = tokens[(size_t)r * S + tid];
-            logprob[(size_t)r * S + tid] = c == -1 ? 0.f : c < 0 || c >= C ? NAN : (Elem<T>::load(x, c) - q.m) - logs;
-        }
-        float pv = INFINITY;
-        int pc = -1;
-        for (int k = 0; k < K; ++k) {
-            float v = -INFINITY;
-            int c = MAX_CLASSES;
-            for (int j = tid; j < C; j += THREADS) {
-                const float w = Elem<T>::load(x, j);
-                if (before(pv, pc, w, j) && before(w, j, v, c)) { v = w; c = j; }
-            }
+        const Row row = row_at<T>(r, C);
+        const int P = W * G, step = P * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane, ns = (row.nv + step - 1) / step;
+        uint4 q[V];
 #pragma unroll
-            for (int o = 32; o > 0; o >>= 1) {
-                const float w = __shfl_xor(v, o, 64);
-                const int d = __shfl_xor(c, o, 64);
-                if (before(w, d, v, c)) { v = w; c = d; }
+        for (int v = 0; v < V; ++v)
+            if (v < ns) q[v] = load_vector(z, total, row, n0 + v * step, C);
+        int token = -1;
+        float xt = 0.f;
+        if (G == 1 && thread < o.S) {
+            token = tokens[(size_t)r * o.S + thread];
+            if (token >= 0 && token < C) xt = Elem<T>::load(z, (size_t)r * C + token);
+        }
+        float group[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < ns) {
+                float x[N];
+                unpack(q[v], x);
+#pragma unroll
+                for (int e = 0; e < N; ++e) group[e & 3] = fmaxf(group[e & 3], x[e]);
             }
-            if ((tid & 63) == 0) { lds[tid >> 6] = v; lds_c[tid >> 6] = c; }
+        const float lane_most = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
+        float m = wave64(lane_most, Max()), t = 0.f;
+        if (o.K > 0) {
+            const float least = wave64(lane_most, Min());
+            // W wavefronts: K scores reach the least of thresholds that K / W of each one's reach, and the largest of those that K of one's do
+            t = wave_threshold(group, least, m, (o.K + W - 1) / W);
+            if (MULTI) {
+                const float own = wave_threshold(group, least, t, o.K);
+                if (lane == 0) { red[1][wave] = t; red[2][wave] = own; }
+            }
+        }
+        if (MULTI) {
+            if (lane == 0) red[0][wave] = m;
+            if (threadIdx.x == 0) { count = 0; exact = 0; }
             __syncthreads();
-            for (int w = 0; w < THREADS / 64; ++w)
-                if (before(lds[w], lds_c[w], v, c)) { v = lds[w]; c = lds_c[w]; }
+            float all = INFINITY, own = -INFINITY;
+            for (int w = 0; w < W; ++w) {
+                m = fmaxf(m, red[0][w]);
+                all = fminf(all, red[1][w]);
+                own = fmaxf(own, red[2][w]);
+            }
+            if (o.K > 0) t = fmaxf(all, own);
+        }
+        const float m0 = m == -INFINITY ? 0.f : m;
+        float s = 0.f, u = 0.f;
+        int n = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < ns) {
+                float x[N], most = -INFINITY;
+                unpack(q[v], x);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float d = x[e] - m0, p = __builtin_amdgcn_exp2f(d * kscale);
+                    s += p;
+                    u += p * fmaxf(d, -1000.f);  // 0 * -inf is no share of the entropy
+                    most = fmaxf(most, x[e]);
+                }
+                if (o.K > 0 && __any(most >= t)) {
+                    const int c0 = (n0 + v * step) * N - row.head;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const bool take = x[e] >= t && (unsigned)(c0 + e) < (unsigned)C;
+                        const unsigned long long b = __ballot(take);
+                        if (b == 0) continue;
+                        int at = n;
+                        if (MULTI) {
+                            if (lane == 0) at = atomicAdd(&count, __popcll(b));
+                            at = __builtin_amdgcn_readfirstlane(at);
+                        }
+                        n = at + __popcll(b);
+                        at += below(b);
+                        if (take && at < CAP && (!MULTI || at < (int)blockDim.x)) list[at] = ranked(x[e], c0 + e);
+                    }
+                }
+            }
+        s = wave64(s, Sum());
+        u = wave64(u, Sum());
+        if (MULTI) {
             __syncthreads();
-            pv = v;
-            pc = c;
-            if (tid == 0) {
-                top_ids[(size_t)r * K + k] = c;
-                top_logprob[(size_t)r * K + k] = (v - q.m) - logs;
-            }
-        }
-    }
-}
-
-// A gradient's element: overwritten, or added to what is there and rounded once
-template <typename G>
-__device__ __forceinline__ void put(G* dz, size_t i, float v, int accumulate)
-{
-    Elem<G>::store(dz, i, accumulate ? Elem<G>::load(dz, i) + v : v);
-}
-
-template <typename T, typename G>
-__global__ __launch_bounds__(THREADS) void token_bwd_k(const T* __restrict__ z, const float* __restrict__ stats, const int* __restrict__ tokens,
-                                                       const float* __restrict__ dlogprob, const float* __restrict__ dentropy,
-                                                       const int* __restrict__ top_ids, const float* __restrict__ dtop, const int* __restrict__ in_len,
-                                                       G* __restrict__ dz, unsigned rows, unsigned Tp, int C, int S, int K, int accumulate)
-{
-    __shared__ int id[2 * MAX_ENTRIES];
-    __shared__ float g[2 * MAX_ENTRIES];
-    for (unsigned r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T* x = z + (size_t)r * C;
-        G* y = dz + (size_t)r * C;
-        const int tid = threadIdx.x;
-        const float4 q = reinterpret_cast<const float4*>(stats)[r];
-        if (frame_of(in_len, r, Tp) != LIVE || !(fabsf(q.y) < INFINITY)) {
-            if (!accumulate)
-                for (int c = tid; c < C; c += THREADS) Elem<G>::store(y, c, 0.f);
-            continue;
-        }
-        if (tid < S + K) {
-            const int c = tid < S ? tokens[(size_t)r * S + tid] : top_ids[(size_t)r * K + tid - S];
-            const bool there = c >= 0 && c < C;
-            id[tid] = there ? c : -1;
-            g[tid] = there ? tid < S ? dlogprob[(size_t)r * S + tid] : dtop[(size_t)r * K + tid - S] : 0.f;
-        }
-        __syncthreads();
-        float sum = 0.f;
-        for (int j = 0; j < S + K; ++j) sum += g[j];
-        const float h = dentropy ? dentropy[r] : 0.f;
-        for (int c = tid; c < C; c += THREADS) {
-            const float lp = fmaxf((Elem<T>::load(x, c) - q.x) - q.y, -1000.f);
-            float v = -expf(lp) * (sum + h * (lp + q.z));
-            for (int j = 0; j < S + K; ++j) v += id[j] == c ? g[j] : 0.f;
-            put(y, c, v, accumulate);
-        }
-        __syncthreads();
-    }
-}
-
-template <typename T, typename G>
-__global__ __launch_bounds__(THREADS) void distill_k(const T* __restrict__ z, const int* __restrict__ t_ids, const float* __restrict__ t_scores,
-                                                     const int* __restrict__ in_len, const float* __restrict__ weight, float* __restrict__ frame_loss,
-                                                     G* __restrict__ dz, unsigned rows, unsigned Tp, int C, int K, float tau, float inv_tau,
-                                                     float grad_scale, int accumulate)
-{
-    __shared__ float lds[THREADS / 64];
-    __shared__ int id[MAX_ENTRIES];
-    __shared__ float q[MAX_ENTRIES];
-    for (unsigned r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T* x = z + (size_t)r * C;
-        G* y = dz + (size_t)r * C;
-        const int tid = threadIdx.x;
-        const Frame f = frame_of(in_len, r, Tp);
-        float loss = f == BAD ? NAN : 0.f, w = f != LIVE ? 0.f : weight ? weight[r] : 1.f, inv_s = 0.f;
-        RowStats st{0.f, 0.f, 0.f, false};
-        if (w != 0.f) {
-            st = row_stats(x, C, inv_tau, lds);
-            inv_s = 1.f / st.s;
-            const float logs = st.s > 0.f ? logf(st.s) : 0.f;
-            int c = -1;
-            float t = -INFINITY;
-            if (tid < K) {
-                c = t_ids[(size_t)r * K + tid];
-                t = c == -1 ? -INFINITY : t_scores[(size_t)r * K + tid];
-            }
-            const bool odd = (c != -1 && (c < 0 || c >= C)) || !(t < INFINITY);
-            const bool bad = block_reduce(odd ? 1.f : 0.f, larger, lds) != 0.f;
-            const float tm = block_reduce(t, larger, lds);
-            const bool none = tm == -INFINITY;
-            const float d = none ? -INFINITY : (t - tm) * inv_tau, e = none ? 0.f : expf(d), sum = block_reduce(e, add, lds);
-            const bool there = e > 0.f && !odd;
-            float kl = 0.f;
-            if (there) kl = e / sum * ((d - logf(sum)) - ((Elem<T>::load(x, c) - st.m) * inv_tau - logs));
-            kl = block_reduce(kl, add, lds);
-            if (tid < K) {
-                id[tid] = there ? c : -1;
-                q[tid] = there ? e / sum : 0.f;
-            }
-            loss = bad || !st.ok ? NAN : none ? 0.f : w * (tau * tau) * kl;
-            if (none || !(fabsf(loss) < INFINITY)) w = 0.f;
+            if (lane == 0) { red[0][wave] = s; red[1][wave] = u; }
+            n = count;
             __syncthreads();
+            s = u = 0.f;
+            for (int w = 0; w < W; ++w) { s += red[0][w]; u += red[1][w]; }
         }
-        if (tid == 0) frame_loss[r] = loss;
-        if (!dz) continue;
-        if (w == 0.f) {
-            if (!accumulate)
-                for (int c = tid; c < C; c += THREADS) Elem<G>::store(y, c, 0.f);
+        if (o.K > 0 && s == s) {
+            const int room = MULTI ? (int)blockDim.x : CAP;
+            if (n > room) {
+                list[wave * 64 * MULTI + lane] = 0;
+                exchange<MULTI>();
+                n = exact_largest<T, V>(q, ns, step, n0, row, C, o.K, list + wave * 64 * MULTI);
+                if (MULTI) {
+                    if (lane == 0) atomicAdd(&exact, n);
+                    n = room;
+                }
+            }
+        }
+        exchange<MULTI>();
+        if (MULTI && G > 1) {
+            const size_t at = (size_t)r * G + g;
+            if (threadIdx.x == 0) parts.sums[at] = make_float4(m, s, u, 0.f);
+            if (s == s) {
+                if (thread < o.K && thread >= (exact ? exact : n)) parts.best[at * o.K + thread] = 0;
+                if (o.K > 0) rank_list<MULTI>(list, n, o.K, thread, [&](int k, ranked_t a) { if (a) parts.best[at * o.K + k] = a; });
+            }
+        } else if (!(s == s)) {
+            write_absent(o, r, BAD, thread, MULTI ? blockDim.x : 64);
         } else {
-            const float scale = w * grad_scale * tau;
-            for (int c = tid; c < C; c += THREADS) {
-                float v = expf((Elem<T>::load(x, c) - st.m) * inv_tau) * inv_s;
-                for (int j = 0; j < K; ++j) v -= id[j] == c ? q[j] : 0.f;
-                put(y, c, scale * v, accumulate);
+            const Dist d = dist_of(m0, s, u);
+            if (thread == 0) write_dist(o, r, d, s > 0.f);
+            if (thread < o.S) o.logprob[(size_t)r * o.S + thread] = token == -1 ? 0.f : token < 0 || token >= C ? NAN : (xt - d.m) - d.logs;
+            if (o.K > 0)
+                rank_list<MULTI>(list, n, o.K, thread, [&](int k, ranked_t a) {
+                    o.top_ids[(size_t)r * o.K + k] = class_of(a);
+                    o.top_logprob[(size_t)r * o.K + k] = (score_of(a) - d.m) - d.logs;
+                });
+        }
+        exchange<MULTI>();
+    }
+}
+
+// The rows that G workgroups left in parts, a workgroup each.  Of the G sorted lists, entries below the largest K-th of a list or below the
+// smallest ceil(K / G)-th are not among the K best; about 1.5 K pass.
+template <typename T>
+__global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z, const int* __restrict__ tokens, const int* __restrict__ in_len,
+                                                        TokenOut o, Parts parts, unsigned rows, unsigned Tp, int C, int G)
+{
+    __shared__ ranked_t list[MAX_GROUPS * MAX_ENTRIES];
+    __shared__ int count;
+    for (unsigned r = blockIdx.x; r < rows; r += gridDim.x) {
+        const int tid = threadIdx.x;
+        const Frame f = frame_of(in_len, r, Tp);
+        float m = -INFINITY, s = 0.f, u = 0.f;
+        if (f == LIVE) {
+            for (int g = 0; g < G; ++g) m = fmaxf(m, parts.sums[(size_t)r * G + g].x);
+            for (int g = 0; g < G; ++g) {
+                const float4 p = parts.sums[(size_t)r * G + g];
+                if (p.y == 0.f) continue;
+                const float d = p.x - m, scale = expf(d);
+                s += p.y * scale;
+                u += (p.z + (p.y > 0.f ? p.y * fmaxf(d, -1000.f) : 0.f)) * scale;
+            }
+        }
+        if (f != LIVE || !(s == s)) {
+            write_absent(o, r, f == LIVE ? BAD : f, tid, THREADS);
+            continue;
+        }
+        const Dist d = dist_of(m == -INFINITY ? 0.f : m, s, u);
+        if (tid == 0) write_dist(o, r, d, s > 0.f);
+        if (tid < o.S) {
+            const int c = tokens[(size_t)r * o.S + tid];
+            o.logprob[(size_t)r * o.S + tid] = c == -1 ? 0.f : c < 0 || c >= C ? NAN : (Elem<T>::load(z, (size_t)r * C + c) - d.m) - d.logs;
+        }
+        if (o.K == 0) continue;
+        const ranked_t* const best = parts.best + (size_t)r * G * o.K;
+        ranked_t least = ~0ull, most = 0;
+        const int need = (o.K + G - 1) / G;
+        for (int g = 0; g < G; ++g) {
+            const ranked_t a = best[g * o.K + need - 1], b = best[g * o.K + o.K - 1];
+            least = a < least ? a : least;
+            most = b > most ? b : most;
+        }
+        if (least < most) least = most;
+        if (tid == 0) count = 0;
+        __syncthreads();
+        for (int i = tid; i < G * o.K; i += THREADS) {
+            const ranked_t a = best[i];
+            if (a >= least && a != 0) list[atomicAdd(&count, 1)] = a;
+        }
+        __syncthreads();
+        const int n = count;
+        for (int i = tid; i < n; i += THREADS) {
+            const ranked_t a = list[i];
+            int before = 0;
+            for (int j = 0; j < n; ++j) before += list[j] > a;
+            if (before < o.K) {
+                o.top_ids[(size_t)r * o.K + before] = class_of(a);
+                o.top_logprob[(size_t)r * o.K + before] = (score_of(a) - d.m) - d.logs;
             }
         }
         __syncthreads();
+    }
+}
+
+// Rows of up to 16 * NV classes, sixteen lanes each.  The K best are taken one after the other: largest score, then lowest class.
+template <typename T, int NV>
+__global__ __launch_bounds__(THREADS) void token_narrow_k(const T* __restrict__ z, const int* __restrict__ tokens, const int* __restrict__ in_len,
+                                                          TokenOut o, unsigned rows, unsigned Tp, int C)
+{
+    const int l = threadIdx.x & 15;
+    const unsigned stride = gridDim.x * 16;
+    for (unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4); r < rows; r += stride) {
+        const Frame f = frame_of(in_len, r, Tp);
+        if (f != LIVE) {
+            write_absent(o, r, f, l, 16);
+            continue;
+        }
+        const T* const x = z + (size_t)r * C;
+        float v[NV], m = -INFINITY, s = 0.f, u = 0.f;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+            v[q] = l + 16 * q < C ? Elem<T>::load(x, l + 16 * q) : -INFINITY;
+            m = fmaxf(m, v[q]);
+        }
+        m = row16(m, Max());
+        const float m0 = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+            const float d = v[q] - m0, p = __builtin_amdgcn_exp2f(d * LOG2E);
+            s += p;
+            u += p * fmaxf(d, -1000.f);
+        }
+        s = row16(s, Sum());
+        u = row16(u, Sum());
+        if (!(s == s)) {
+            write_absent(o, r, BAD, l, 16);
+            continue;
+        }
+        const Dist d = dist_of(m0, s, u);
+        if (l == 0) write_dist(o, r, d, s > 0.f);
+        for (int j = l; j < o.S; j += 16) {
+            const int c = tokens[(size_t)r * o.S + j];
+            o.logprob[(size_t)r * o.S + j] = c == -1 ? 0.f : c < 0 || c >= C ? NAN : (Elem<T>::load(x, c) - d.m) - d.logs;
+        }
+        unsigned left = 0;  // this lane's classes that are not taken yet
+#pragma unroll
+        for (int q = 0; q < NV; ++q) left |= l + 16 * q < C ? 1u << q : 0u;
+        float score = 0.f;
+        int id = 0;
+        for (int k = 0; k < o.K; ++k) {
+            float w = -INFINITY;
+            int c = MAX_CLASSES;
+#pragma unroll
+            for (int q = NV - 1; q >= 0; --q)
+                if ((left >> q & 1) && v[q] >= w) { w = v[q]; c = l + 16 * q; }
+            const float best = row16(w, Max());
+            // the lowest class at it (whole numbers below 2^24 are exact as floats)
+            const int taken = (int)row16(w == best ? (float)c : (float)MAX_CLASSES, Min());
+            if (c == taken) left &= ~(1u << (c >> 4));
+            if (l == (k & 15)) { score = best; id = taken; }
+            if ((k & 15) == 15 || k == o.K - 1) {
+                const int at = (k & ~15) + l;
+                if (at <= k) {
+                    o.top_ids[(size_t)r * o.K + at] = id;
+                    o.top_logprob[(size_t)r * o.K + at] = (score - d.m) - d.logs;
+                }
+            }
+        }
+    }
+}
+
+// ---- gradients: p_c times a number of the row, corrected in a few columns --------------------------------------
+// Adds or overwrites elements c0 .. c0 + N of a row whose vectors lie on the tensor's grid
+template <typename G, int N>
+__device__ __forceinline__ void put(G* __restrict__ dz, size_t i, int c0, int C, float (&v)[N], int accumulate)
+{
+    constexpr int PER = LANE_VALUES<G> < N ? LANE_VALUES<G> : N, STORES = N / PER;
+    if (c0 >= 0 && c0 + N <= C && PER == LANE_VALUES<G>) {
+#pragma unroll
+        for (int j = 0; j < STORES; ++j) {
+            uint4* const at = reinterpret_cast<uint4*>(dz + i + j * PER);
+            float w[PER];
+            if (accumulate) unpack(*at, w);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) w[e] = accumulate ? w[e] + v[j * PER + e] : v[j * PER + e];
+            *at = pack(w);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if ((unsigned)(c0 + e) < (unsigned)C) Elem<G>::store(dz, i + e, accumulate ? Elem<G>::load(dz, i + e) + v[e] : v[e]);
+}
+
+// Up to 64 * R columns of a row that get something of their own, an entry a lane: its column (-1: none), what is added there, and the slot of the
+// wavefront (counted in vectors of 64 lanes of the row) that it is in
+template <int R>
+struct Columns {
+    int id[R], slot[R];
+    float add[R];
+    template <int N>
+    __device__ __forceinline__ void place(const Row& row)
+    {
+#pragma unroll
+        for (int j = 0; j < R; ++j) slot[j] = id[j] < 0 ? -1 : (id[j] + row.head) / (64 * N);
+    }
+    // adds the entries of this slot to the lane's values, in the order of the entries
+    template <int N>
+    __device__ __forceinline__ void apply(int at, int c0, float (&x)[N]) const
+    {
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            unsigned long long b = __ballot(slot[j] == at);
+            while (b) {
+                const int l = __ffsll((unsigned long long)b) - 1;
+                b &= b - 1;
+                const int c = __builtin_amdgcn_readlane(id[j], l) - c0;
+                const float a = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(add[j]), l));
+#pragma unroll
+                for (int e = 0; e < N; ++e) x[e] += c == e ? a : 0.f;
+            }
+        }
+    }
+};
+
+template <typename T, typename G, int V>
+__global__ __launch_bounds__(THREADS) void token_bwd_rows_k(const T* __restrict__ z, const float* __restrict__ stats, const int* __restrict__ tokens,
+                                                            const float* __restrict__ dlogprob, const float* __restrict__ dentropy,
+                                                            const int* __restrict__ top_ids, const float* __restrict__ dtop,
+                                                            const int* __restrict__ in_len, G* __restrict__ dz, unsigned rows, unsigned Tp, int C, int S,
+                                                            int K, int P, int accumulate)
+{
+    constexpr int N = LANE_VALUES<T>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const size_t total = (size_t)rows * C;
+    const unsigned tasks = rows * P;
+    for (unsigned task = blockIdx.x * 4 + wave; task < tasks; task += gridDim.x * 4) {
+        const unsigned r = task / P;
+        const int p = task - r * P;
+        const Row row = row_at<T>(r, C);
+        const int slots = (row.nv + 63) / 64, first = p * V;
+        if (first >= slots) continue;
+        const int ns = slots - first < V ? slots - first : V;
+        const float4 q = reinterpret_cast<const float4*>(stats)[r];
+        const bool live = frame_of(in_len, r, Tp) == LIVE && fabsf(q.y) < INFINITY;
+        if (!live && accumulate) continue;
+        uint4 data[V];
+        if (live)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v < ns) data[v] = load_vector(z, total, row, (first + v) * 64 + lane, C);
+        Columns<2> cols{{-1, -1}};
+        float sum = 0.f, h = 0.f;
+        if (live) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int i = lane + 64 * j;
+                int c = -1;
+                float a = 0.f;
+                if (i < S) { c = tokens[(size_t)r * S + i]; a = dlogprob[(size_t)r * S + i]; }
+                else if (i < S + K) { c = top_ids[(size_t)r * K + i - S]; a = dtop[(size_t)r * K + i - S]; }
+                const bool there = c >= 0 && c < C;
+                cols.id[j] = there ? c : -1;
+                cols.add[j] = there ? a : 0.f;
+                if (64 * j < S + K) sum += wave64(cols.add[j], Sum());
+            }
+            h = dentropy ? dentropy[r] : 0.f;
+        }
+        cols.template place<N>(row);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < ns) {
+                const int n = (first + v) * 64 + lane, c0 = n * N - row.head;
+                float x[N];
+                if (live) {
+                    unpack(data[v], x);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float lp = fmaxf((x[e] - q.x) - q.y, -1000.f);
+                        x[e] = -__builtin_amdgcn_exp2f(lp * LOG2E) * (sum + h * (lp + q.z));
+                    }
+                    cols.apply(first + v, c0, x);
+                } else
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[e] = 0.f;
+                if (n < row.nv) put(dz, row.first + (size_t)n * N, c0, C, x, accumulate);
+            }
+    }
+}
+
+template <typename T, typename G, int NV>
+__global__ __launch_bounds__(THREADS) void token_bwd_narrow_k(const T* __restrict__ z, const float* __restrict__ stats, const int* __restrict__ tokens,
+                                                              const float* __restrict__ dlogprob, const float* __restrict__ dentropy,
+                                                              const int* __restrict__ top_ids, const float* __restrict__ dtop,
+                                                              const int* __restrict__ in_len, G* __restrict__ dz, unsigned rows, unsigned Tp, int C, int S,
+                                                              int K, int accumulate)
+{
+    const int l = threadIdx.x & 15;
+    const unsigned stride = gridDim.x * 16;
+    for (unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4); r < rows; r += stride) {
+        const size_t i0 = (size_t)r * C;
+        const float4 st = reinterpret_cast<const float4*>(stats)[r];
+        const bool live = frame_of(in_len, r, Tp) == LIVE && fabsf(st.y) < INFINITY;
+        if (!live && accumulate) continue;
+        float direct[NV], sum = 0.f;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) direct[q] = 0.f;
+        if (live)
+            for (int j0 = 0; j0 < S + K; j0 += 16) {
+                const int i = j0 + l;
+                int c = -1;
+                float a = 0.f;
+                if (i < S) { c = tokens[(size_t)r * S + i]; a = dlogprob[(size_t)r * S + i]; }
+                else if (i < S + K) { c = top_ids[(size_t)r * K + i - S]; a = dtop[(size_t)r * K + i - S]; }
+                const int most = S + K - j0 < 16 ? S + K - j0 : 16;
+                for (int j = 0; j < most; ++j) {
+                    const int cj = __shfl(c, j, 16);
+                    const float aj = __shfl(a, j, 16);
+                    if (cj >= 0 && cj < C) sum += aj;
+#pragma unroll
+                    for (int q = 0; q < NV; ++q) direct[q] += cj == l + 16 * q ? aj : 0.f;
+                }
+            }
+        const float h = live && dentropy ? dentropy[r] : 0.f;
+#pragma unroll
+        for (int q = 0; q < NV; ++q)
+            if (l + 16 * q < C) {
+                const size_t i = i0 + l + 16 * q;
+                float v = 0.f;
+                if (live) {
+                    const float lp = fmaxf((Elem<T>::load(z, i) - st.x) - st.y, -1000.f);
+                    v = direct[q] - __builtin_amdgcn_exp2f(lp * LOG2E) * (sum + h * (lp + st.z));
+                }
+                Elem<G>::store(dz, i, accumulate ? Elem<G>::load(dz, i) + v : v);
+            }
+    }
+}
+
+// ---- distillation --------------------------------------------------------------------------------------------
+struct Teacher {
+    const int* ids;
+    const float *scores, *weight;
+    int K;
+    float tau, inv_tau, kscale, grad_scale;  // kscale = log2 e / tau
+};
+
+// Loss of a frame from what its K <= 64 * R entries say, an entry a lane of WIDTH (16 or 64): score t of class c, student score x there; m, s of
+// the student's row at the temperature.  q: the teacher's probability of the lane's entries.  Returns the loss; live: whether there is a gradient.
+template <int R, int WIDTH>
+__device__ __forceinline__ float frame_loss_of(const Teacher& te, const int (&c)[R], const float (&t)[R], const float (&x)[R], float w, float m, float s,
+                                               int C, float (&q)[R], bool& live)
+{
+    auto all = [](float v, auto f) { return WIDTH == 16 ? row16(v, f) : wave64(v, f); };
+    float odd = 0.f, tm = -INFINITY, sum = 0.f, kl = 0.f, d[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        if ((c[j] != -1 && (unsigned)c[j] >= (unsigned)C) || !(t[j] < INFINITY)) odd = 1.f;
+        tm = fmaxf(tm, t[j]);
+    }
+    odd = all(odd, Max());
+    tm = all(tm, Max());
+    const bool none = tm == -INFINITY;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        d[j] = none ? -INFINITY : (t[j] - tm) * te.inv_tau;
+        q[j] = none ? 0.f : expf(d[j]);
+        sum += q[j];
+    }
+    sum = all(sum, Sum());
+    const float logsum = none ? 0.f : logf(sum), logs = s > 0.f ? logf(s) : 0.f, inv = none ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        q[j] *= inv;
+        if (q[j] > 0.f) kl += q[j] * ((d[j] - logsum) - ((x[j] - m) * te.inv_tau - logs));
+    }
+    kl = all(kl, Sum());
+    const float loss = odd != 0.f || !(s == s) ? NAN : none ? 0.f : w * (te.tau * te.tau) * kl;
+    live = !none && fabsf(loss) < INFINITY;
+    return loss;
+}
+
+// sums: (m or -inf, s, ., .) of every row's G workgroups where a row is too long for the registers of one, or rows are few; else NULL
+template <typename T, typename D, int V, bool MULTI>
+__global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void distill_rows_k(const T* __restrict__ z, Teacher te, const int* __restrict__ in_len,
+                                                                                      const float4* __restrict__ sums, float* __restrict__ frame_loss,
+                                                                                      D* __restrict__ dz, unsigned rows, unsigned Tp, int C, int G,
+                                                                                      int accumulate)
+{
+    constexpr int N = LANE_VALUES<T>;
+    constexpr int ROWS = MULTI ? 1 : 4;
+    __shared__ float red[2][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = MULTI ? blockDim.x >> 6 : 1;
+    const size_t total = (size_t)rows * C;
+    const unsigned tasks = rows * G, stride = gridDim.x * ROWS;
+    for (unsigned task = blockIdx.x * ROWS + (MULTI ? 0 : wave); task < tasks; task += stride) {
+        const unsigned r = task / G;
+        const int g = task - r * G;
+        const bool first = g == 0 && (MULTI ? threadIdx.x : lane) == 0;
+        const Frame f = frame_of(in_len, r, Tp);
+        const Row row = row_at<T>(r, C);
+        const int P = W * G, step = P * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane, ns = (row.nv + step - 1) / step;
+        const float w = f != LIVE ? 0.f : te.weight ? te.weight[r] : 1.f;
+        float loss = f == BAD ? NAN : 0.f, m = 0.f, scale = 0.f;
+        bool live = false;
+        uint4 data[V];
+        Columns<1> cols{{-1}};
+        if (w != 0.f) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v < ns) data[v] = load_vector(z, total, row, n0 + v * step, C);
+            int c[1] = {-1};
+            float t[1] = {-INFINITY}, x[1] = {0.f}, q[1];
+            if (lane < te.K) {
+                c[0] = te.ids[(size_t)r * te.K + lane];
+                if (c[0] != -1) t[0] = te.scores[(size_t)r * te.K + lane];
+                if ((unsigned)c[0] < (unsigned)C) x[0] = Elem<T>::load(z, (size_t)r * C + c[0]);
+            }
+            float s = 0.f;
+            m = -INFINITY;
+            if (MULTI && sums) {
+                for (int i = 0; i < G; ++i) m = fmaxf(m, sums[(size_t)r * G + i].x);
+                for (int i = 0; i < G; ++i) {
+                    const float4 a = sums[(size_t)r * G + i];
+                    if (a.y != 0.f) s += a.y * expf((a.x - m) * te.inv_tau);
+                }
+                m = m == -INFINITY ? 0.f : m;
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (v < ns) {
+                        float y[N];
+                        unpack(data[v], y);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) m = fmaxf(m, y[e]);
+                    }
+                m = wave64(m, Max());
+                if (MULTI) {
+                    if (lane == 0) red[0][wave] = m;
+                    __syncthreads();
+                    for (int i = 0; i < W; ++i) m = fmaxf(m, red[0][i]);
+                }
+                m = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (v < ns) {
+                        float y[N];
+                        unpack(data[v], y);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((y[e] - m) * te.kscale);
+                    }
+                s = wave64(s, Sum());
+                if (MULTI) {
+                    if (lane == 0) red[1][wave] = s;
+                    __syncthreads();
+                    s = 0.f;
+                    for (int i = 0; i < W; ++i) s += red[1][i];
+                }
+            }
+            loss = frame_loss_of<1, 64>(te, c, t, x, w, m, s, C, q, live);
+            const float ws = w * te.grad_scale * te.tau;
+            scale = ws / s;
+            cols.id[0] = q[0] > 0.f ? c[0] : -1;
+            cols.add[0] = -q[0] * ws;
+        }
+        if (first) frame_loss[r] = loss;
+        if (!dz || (!live && accumulate)) continue;
+        if (!live) cols.id[0] = -1;
+        cols.template place<N>(row);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < ns) {
+                const int n = n0 + v * step, c0 = n * N - row.head;
+                float x[N];
+                if (live) {
+                    unpack(data[v], x);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[e] = __builtin_amdgcn_exp2f((x[e] - m) * te.kscale) * scale;
+                    cols.apply(n >> 6, c0, x);
+                } else
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[e] = 0.f;
+                if (n < row.nv) put(dz, row.first + (size_t)n * N, c0, C, x, accumulate);
+            }
+    }
+}
+
+template <typename T, typename D, int NV, int R>
+__global__ __launch_bounds__(THREADS) void distill_narrow_k(const T* __restrict__ z, Teacher te, const int* __restrict__ in_len,
+                                                            float* __restrict__ frame_loss, D* __restrict__ dz, unsigned rows, unsigned Tp, int C,
+                                                            int accumulate)
+{
+    const int l = threadIdx.x & 15;
+    const unsigned stride = gridDim.x * 16;
+    for (unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4); r < rows; r += stride) {
+        const size_t i0 = (size_t)r * C;
+        const Frame f = frame_of(in_len, r, Tp);
+        const float w = f != LIVE ? 0.f : te.weight ? te.weight[r] : 1.f;
+        float loss = f == BAD ? NAN : 0.f, g[NV];
+        bool live = false;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) g[j] = 0.f;
+        if (w != 0.f) {
+            float m = -INFINITY, s = 0.f, t[R], x[R], q[R];
+            int c[R];
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                c[j] = -1;
+                t[j] = -INFINITY;
+                x[j] = 0.f;
+                if (l + 16 * j < te.K) {
+                    c[j] = te.ids[(size_t)r * te.K + l + 16 * j];
+                    if (c[j] != -1) t[j] = te.scores[(size_t)r * te.K + l + 16 * j];
+                    if ((unsigned)c[j] < (unsigned)C) x[j] = Elem<T>::load(z, i0 + c[j]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                g[j] = l + 16 * j < C ? Elem<T>::load(z, i0 + l + 16 * j) : -INFINITY;
+                m = fmaxf(m, g[j]);
+            }
+            m = row16(m, Max());
+            m = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                g[j] = __builtin_amdgcn_exp2f((g[j] - m) * te.kscale);
+                s += g[j];
+            }
+            s = row16(s, Sum());
+            loss = frame_loss_of<R, 16>(te, c, t, x, w, m, s, C, q, live);
+            const float ws = w * te.grad_scale * te.tau, scale = ws / s;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) g[j] *= scale;
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                for (int i = 0; i < 16 && i + 16 * k < te.K; ++i) {
+                    const int ci = __shfl(c[k], i, 16);
+                    const float a = __shfl(q[k], i, 16) * ws;
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) g[j] -= ci == l + 16 * j ? a : 0.f;
+                }
+        }
+        if (l == 0) frame_loss[r] = loss;
+        if (!dz || (!live && accumulate)) continue;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (l + 16 * j < C) {
+                const size_t i = i0 + l + 16 * j;
+                const float v = live ? g[j] : 0.f;
+                Elem<D>::store(dz, i, accumulate ? Elem<D>::load(dz, i) + v : v);
+            }
     }
 }
 
@@ -253,18 +970,136 @@ __global__ __launch_bounds__(THREADS) void utterance_loss_k(const float* __restr
 
 bool shape_ok(int B, int Tp, int C, int S, int K)
 {
-    return B > 0 && Tp > 0 && (long long)B * Tp <= 2147483647LL && C > 0 && C <= MAX_CLASSES && S >= 0 && S <= MAX_ENTRIES && K >= 0 &&
+    // a tensor of at most 2^40 scores: rows times workgroups (or wavefronts) a row stay below 2^32
+    return B > 0 && Tp > 0 && (long long)B * Tp <= 2147483647LL && (long long)B * Tp <= (1LL << 40) / (C > 0 ? C : 1) && C > 0 && C <= MAX_CLASSES && S >= 0 && S <= MAX_ENTRIES && K >= 0 &&
            K <= MAX_ENTRIES && K <= C;
 }
 bool grad_dtype_ok(int z_dtype, int dz_dtype) { return valid_dtype(dz_dtype) && (dz_dtype == W2L_F32 || z_dtype == W2L_BF16); }
-unsigned grid_of(unsigned rows) { return rows < (1u << 20) ? rows : 1u << 20; }
+
+// How the rows are dealt out: sixteen lanes a row (W = 0), or W wavefronts of each of G workgroups, V slots of registers.
+struct Plan {
+    int W, G, V;
+};
+Plan plan_of(long long rows, int C, int dtype)
+{
+    if (C <= 64) return {0, 1, C <= 32 ? 2 : 4};
+    const int N = dtype == W2L_BF16 ? 8 : 4, slots = (C + 2 * (N - 1) + 64 * N - 1) / (64 * N);  // wherever in a vector the row begins
+    constexpr int MOST = 16;            // slots of a wavefront: 64 registers
+    long long P = (slots + MOST - 1) / MOST;
+    while (rows * P < 2048 && P * 2 <= slots && P * 2 <= 8 * MAX_GROUPS) P *= 2;  // two wavefronts a SIMD
+    const int W = P <= 8 ? (int)P : 8, G = (int)((P + W - 1) / W), per = (slots + W * G - 1) / (W * G);
+    return {W, G, per <= 2 ? 2 : per <= 8 ? 8 : 16};
+}
+unsigned grid_of(long long groups) { return (unsigned)(groups < (1 << 20) ? groups : 1 << 20); }
+size_t sums_bytes(long long rows, const Plan& p) { return p.G > 1 ? round_up((size_t)rows * p.G * sizeof(float4), 256) : 0; }
+bool workspace_ok(const void* ws, size_t have, size_t need)
+{
+    return need == 0 || (ws && have >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0);
+}
+
+template <typename T, int V>
+void launch_rows(const Plan& p, hipStream_t st, const void* z, const int* tokens, const int* in_len, const TokenOut& o, const Parts& parts,
+                 unsigned rows, unsigned Tp, int C, float kscale)
+{
+    if (p.W > 1 || p.G > 1)
+        hipLaunchKernelGGL((token_rows_k<T, V, true>), dim3(grid_of((long long)rows * p.G)), dim3(64 * p.W), 0, st, (const T*)z, tokens, in_len, o,
+                           parts, rows, Tp, C, p.G, kscale);
+    else
+        hipLaunchKernelGGL((token_rows_k<T, V, false>), dim3(grid_of(((long long)rows + 3) / 4)), dim3(256), 0, st, (const T*)z, tokens, in_len, o,
+                           parts, rows, Tp, C, 1, kscale);
+}
+template <typename T>
+int launch_tokens(const Plan& p, hipStream_t st, const void* z, const int* tokens, const int* in_len, const TokenOut& o, void* ws, unsigned rows,
+                  unsigned Tp, int C, float kscale, bool join)
+{
+    const Parts parts{(float4*)ws, (ranked_t*)((char*)ws + sums_bytes(rows, p))};
+    if (p.W == 0) {
+        const dim3 g(grid_of(((long long)rows + 15) / 16)), b(THREADS);
+        if (p.V == 2) hipLaunchKernelGGL((token_narrow_k<T, 2>), g, b, 0, st, (const T*)z, tokens, in_len, o, rows, Tp, C);
+        else hipLaunchKernelGGL((token_narrow_k<T, 4>), g, b, 0, st, (const T*)z, tokens, in_len, o, rows, Tp, C);
+    } else if (p.V == 2)
+        launch_rows<T, 2>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale);
+    else if (p.V == 8)
+        launch_rows<T, 8>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale);
+    else
+        launch_rows<T, 16>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale);
+    if (int rc = launch_status()) return rc;
+    if (p.G == 1 || !join) return W2L_OK;
+    hipLaunchKernelGGL(token_join_k<T>, dim3(grid_of(rows)), dim3(THREADS), 0, st, (const T*)z, tokens, in_len, o, parts, rows, Tp, C, p.G);
+    return launch_status();
+}
+
+template <typename T, typename D>
+void launch_bwd(hipStream_t st, const void* z, const float* stats, const int* tokens, const float* dlogprob, const float* dentropy, const int* top_ids,
+                const float* dtop, const int* in_len, void* dz, unsigned rows, unsigned Tp, int C, int S, int K, int accumulate)
+{
+    constexpr int V = 4, N = 16 / sizeof(T);
+    if (C <= 64) {
+        const dim3 g(grid_of(((long long)rows + 15) / 16)), b(THREADS);
+        if (C <= 32)
+            hipLaunchKernelGGL((token_bwd_narrow_k<T, D, 2>), g, b, 0, st, (const T*)z, stats, tokens, dlogprob, dentropy, top_ids, dtop, in_len, (D*)dz,
+                               rows, Tp, C, S, K, accumulate);
+        else
+            hipLaunchKernelGGL((token_bwd_narrow_k<T, D, 4>), g, b, 0, st, (const T*)z, stats, tokens, dlogprob, dentropy, top_ids, dtop, in_len, (D*)dz,
+                               rows, Tp, C, S, K, accumulate);
+        return;
+    }
+    const int slots = (C + 2 * (N - 1) + 64 * N - 1) / (64 * N), P = (slots + V - 1) / V;
+    hipLaunchKernelGGL((token_bwd_rows_k<T, D, V>), dim3(grid_of(((long long)rows * P + 3) / 4)), dim3(THREADS), 0, st, (const T*)z, stats, tokens,
+                       dlogprob, dentropy, top_ids, dtop, in_len, (D*)dz, rows, Tp, C, S, K, P, accumulate);
+}
+
+template <typename T, typename D, int V>
+void launch_distill_rows(const Plan& p, hipStream_t st, const void* z, const Teacher& te, const int* in_len, const float4* sums, float* frame_loss,
+                         void* dz, unsigned rows, unsigned Tp, int C, int accumulate)
+{
+    if (p.W > 1 || p.G > 1)
+        hipLaunchKernelGGL((distill_rows_k<T, D, V, true>), dim3(grid_of((long long)rows * p.G)), dim3(64 * p.W), 0, st, (const T*)z, te, in_len, sums,
+                           frame_loss, (D*)dz, rows, Tp, C, p.G, accumulate);
+    else
+        hipLaunchKernelGGL((distill_rows_k<T, D, V, false>), dim3(grid_of(((long long)rows + 3) / 4)), dim3(256), 0, st, (const T*)z, te, in_len, sums,
+                           frame_loss, (D*)dz, rows, Tp, C, 1, accumulate);
+}
+template <typename T, typename D>
+int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& te, const int* in_len, float* frame_loss, void* dz, void* ws,
+                   unsigned rows, unsigned Tp, int C, int accumulate)
+{
+    if (p.W == 0) {
+        const dim3 g(grid_of(((long long)rows + 15) / 16)), b(THREADS);
+#define W2L_NARROW(NV_, R_) \
+    hipLaunchKernelGGL((distill_narrow_k<T, D, NV_, R_>), g, b, 0, st, (const T*)z, te, in_len, frame_loss, (D*)dz, rows, Tp, C, accumulate)
+        if (C <= 32 && te.K <= 16) W2L_NARROW(2, 1);
+        else if (C <= 32) W2L_NARROW(2, 4);
+        else if (te.K <= 16) W2L_NARROW(4, 1);
+        else W2L_NARROW(4, 4);
+#undef W2L_NARROW
+        return launch_status();
+    }
+    const float4* sums = nullptr;
+    if (p.G > 1) {
+        const TokenOut none{nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0};
+        if (int rc = launch_tokens<T>(p, st, z, nullptr, in_len, none, ws, rows, Tp, C, te.kscale, false)) return rc;
+        sums = (const float4*)ws;
+    }
+    if (p.V == 2) launch_distill_rows<T, D, 2>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate);
+    else if (p.V == 8) launch_distill_rows<T, D, 8>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate);
+    else launch_distill_rows<T, D, 16>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate);
+    return launch_status();
+}
 
 }  // namespace
 
-extern "C" size_t w2l_token_logprob_workspace_bytes(int, int, int, int, int) { return 0; }
+extern "C" size_t w2l_token_logprob_workspace_bytes(int B, int Tp, int C, int K, int z_dtype)
+{
+    if (!shape_ok(B, Tp, C, 0, K) || !valid_dtype(z_dtype)) return 0;
+    const long long rows = (long long)B * Tp;
+    const Plan p = plan_of(rows, C, z_dtype);
+    return p.G > 1 ? sums_bytes(rows, p) + (size_t)rows * p.G * K * sizeof(ranked_t) : 0;
+}
 
 extern "C" int w2l_token_logprob_fwd(const void* z, const int* tokens, const int* in_len, float* logprob, float* entropy, int* top_ids,
-                                     float* top_logprob, float* stats, int B, int Tp, int C, int S, int K, int z_dtype, void*, size_t, void* stream)
+                                     float* top_logprob, float* stats, int B, int Tp, int C, int S, int K, int z_dtype, void* workspace,
+                                     size_t ws_bytes, void* stream)
 {
     if (!z || (S > 0 && (!tokens || !logprob)) || (K > 0 && (!top_ids || !top_logprob))) return W2L_ERR_NULL;
     if (!shape_ok(B, Tp, C, S, K)) return W2L_ERR_SHAPE;
@@ -272,15 +1107,12 @@ extern "C" int w2l_token_logprob_fwd(const void* z, const int* tokens, const int
     if (!aligned16(z) || !aligned16(tokens) || !aligned16(in_len) || !aligned16(logprob) || !aligned16(entropy) || !aligned16(top_ids) ||
         !aligned16(top_logprob) || !aligned16(stats))
         return W2L_ERR_ALIGN;
+    if (!workspace_ok(workspace, ws_bytes, w2l_token_logprob_workspace_bytes(B, Tp, C, K, z_dtype))) return W2L_ERR_WORKSPACE;
     const unsigned rows = (unsigned)B * (unsigned)Tp;
-    const dim3 g(grid_of(rows)), b(THREADS);
-    if (z_dtype == W2L_BF16)
-        hipLaunchKernelGGL(token_fwd_k<bf16_t>, g, b, 0, (hipStream_t)stream, (const bf16_t*)z, tokens, in_len, logprob, entropy, top_ids,
-                           top_logprob, stats, rows, (unsigned)Tp, C, S, K);
-    else
-        hipLaunchKernelGGL(token_fwd_k<float>, g, b, 0, (hipStream_t)stream, (const float*)z, tokens, in_len, logprob, entropy, top_ids, top_logprob,
-                           stats, rows, (unsigned)Tp, C, S, K);
-    return launch_status();
+    const Plan p = plan_of(rows, C, z_dtype);
+    const TokenOut o{logprob, entropy, top_ids, top_logprob, stats, S, K};
+    return z_dtype == W2L_BF16 ? launch_tokens<bf16_t>(p, (hipStream_t)stream, z, tokens, in_len, o, workspace, rows, (unsigned)Tp, C, LOG2E, true)
+                               : launch_tokens<float>(p, (hipStream_t)stream, z, tokens, in_len, o, workspace, rows, (unsigned)Tp, C, LOG2E, true);
 }
 
 extern "C" int w2l_token_logprob_bwd(const void* z, const float* stats, const int* tokens, const float* dlogprob, const float* dentropy,
@@ -294,10 +1126,8 @@ extern "C" int w2l_token_logprob_bwd(const void* z, const float* stats, const in
         !aligned16(dtop) || !aligned16(in_len) || !aligned16(dz))
         return W2L_ERR_ALIGN;
     const unsigned rows = (unsigned)B * (unsigned)Tp;
-    const dim3 g(grid_of(rows)), b(THREADS);
-#define W2L_BWD(T_, G_)                                                                                                                      \
-    hipLaunchKernelGGL((token_bwd_k<T_, G_>), g, b, 0, (hipStream_t)stream, (const T_*)z, stats, tokens, dlogprob, dentropy, top_ids, dtop, \
-                       in_len, (G_*)dz, rows, (unsigned)Tp, C, S, K, accumulate)
+#define W2L_BWD(T_, G_)                                                                                                                        \
+    launch_bwd<T_, G_>((hipStream_t)stream, z, stats, tokens, dlogprob, dentropy, top_ids, dtop, in_len, dz, rows, (unsigned)Tp, C, S, K, accumulate)
     if (z_dtype == W2L_F32) W2L_BWD(float, float);
     else if (dz_dtype == W2L_F32) W2L_BWD(bf16_t, float);
     else W2L_BWD(bf16_t, bf16_t);
@@ -305,11 +1135,15 @@ extern "C" int w2l_token_logprob_bwd(const void* z, const float* stats, const in
     return launch_status();
 }
 
-extern "C" size_t w2l_distill_workspace_bytes(int, int, int, int, int) { return 0; }
+extern "C" size_t w2l_distill_workspace_bytes(int B, int Tp, int C, int K, int z_dtype)
+{
+    if (!shape_ok(B, Tp, C, 0, K) || !valid_dtype(z_dtype)) return 0;
+    return sums_bytes((long long)B * Tp, plan_of((long long)B * Tp, C, z_dtype));
+}
 
 extern "C" int w2l_distill_fwd_bwd(const void* z, const int* t_ids, const float* t_scores, const int* in_len, const float* weight,
                                    float* frame_loss, float* loss, void* dz, int B, int Tp, int C, int K, float temperature, float grad_scale,
-                                   int z_dtype, int dz_dtype, int accumulate, void*, size_t, void* stream)
+                                   int z_dtype, int dz_dtype, int accumulate, void* workspace, size_t ws_bytes, void* stream)
 {
     if (!z || !t_ids || !t_scores || !frame_loss) return W2L_ERR_NULL;
     if (!shape_ok(B, Tp, C, 0, K) || K < 1 || !(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature) || !isfinite(grad_scale))
@@ -318,18 +1152,19 @@ extern "C" int w2l_distill_fwd_bwd(const void* z, const int* t_ids, const float*
     if (!aligned16(z) || !aligned16(t_ids) || !aligned16(t_scores) || !aligned16(in_len) || !aligned16(weight) || !aligned16(frame_loss) ||
         !aligned16(loss) || !aligned16(dz))
         return W2L_ERR_ALIGN;
+    if (!workspace_ok(workspace, ws_bytes, w2l_distill_workspace_bytes(B, Tp, C, K, z_dtype))) return W2L_ERR_WORKSPACE;
     const unsigned rows = (unsigned)B * (unsigned)Tp;
-    const dim3 g(grid_of(rows)), b(THREADS);
-#define W2L_DISTILL(T_, G_)                                                                                                                     \
-    hipLaunchKernelGGL((distill_k<T_, G_>), g, b, 0, (hipStream_t)stream, (const T_*)z, t_ids, t_scores, in_len, weight, frame_loss, (G_*)dz, \
-                       rows, (unsigned)Tp, C, K, temperature, 1.f / temperature, grad_scale, accumulate)
+    const Plan p = plan_of(rows, C, z_dtype);
+    const Teacher te{t_ids, t_scores, weight, K, temperature, 1.f / temperature, (float)(1.4426950408889634 / temperature), grad_scale};
+    int rc;
+#define W2L_DISTILL(T_, G_) rc = launch_distill<T_, G_>(p, (hipStream_t)stream, z, te, in_len, frame_loss, dz, workspace, rows, (unsigned)Tp, C, accumulate)
     if (z_dtype == W2L_F32) W2L_DISTILL(float, float);
     else if (dz_dtype == W2L_F32) W2L_DISTILL(bf16_t, float);
     else W2L_DISTILL(bf16_t, bf16_t);
 #undef W2L_DISTILL
-    if (int rc = launch_status()) return rc;
+    if (rc) return rc;
     if (!loss) return W2L_OK;
-    hipLaunchKernelGGL(utterance_loss_k, dim3(B), b, 0, (hipStream_t)stream, frame_loss, loss, (unsigned)Tp);
+    hipLaunchKernelGGL(utterance_loss_k, dim3(B), dim3(THREADS), 0, (hipStream_t)stream, frame_loss, loss, (unsigned)Tp);
     return launch_status();
 }
 

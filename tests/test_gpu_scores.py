@@ -130,7 +130,9 @@ def check_tokens(got, z, tokens, K, in_len=None, grads=None, dz_dtype="fp32", ac
                 ok = (ids >= 0) & (ids < z.shape[2])
                 b, t = (np.broadcast_to(i[..., None], ids.shape) for i in np.indices(ids.shape[:2]))
                 np.add.at(direct, (b[ok], t[ok], ids[ok]), np.abs(g[ok]))
-        bound = bound + (n + 3) * U * (direct + p * factor) + 2.0 ** -126
+        # a probability below 2^-126, the least normal fp32, may come out as 0 (the exponential's instruction gives no subnormals):
+        # |p - 0| < 2^-126, times the row's factor
+        bound = bound + (n + 3) * U * (direct + p * factor) + 2.0 ** -126 * (1 + factor + h[..., None])
         if accumulate is not None:
             before = accumulate.double().cpu().numpy()
             ref = ref + before
@@ -283,7 +285,8 @@ def check_distill(got, z, ids, sc, tau=1.0, weight=None, in_len=None, gs=1.0, dz
     qerr = np.zeros(z.shape)
     np.add.at(qerr, (b[here], r[here], ids[here]), (q * (90 + 4 * Dt[..., None] + 4 * dt) * U)[here])
     lpf = np.where(np.isfinite(lp), lp, 0)
-    bound = abs(gs) * tau * w[..., None] * (p * (logs[..., None] + (4 * np.abs(lpf) + 12) * U) + qerr + (ids.shape[2] + 4) * U * (size + qs)) + 2.0 ** -126
+    bound = abs(gs) * tau * w[..., None] * (p * (logs[..., None] + (4 * np.abs(lpf) + 12) * U) + qerr + (ids.shape[2] + 4) * U * (size + qs))
+    bound = bound + 2.0 ** -126 * (1 + abs(gs) * tau * w[..., None])         # as above
     if accumulate is not None:
         dz = dz + accumulate.double().cpu().numpy()
         bound = bound + U * np.abs(dz)
