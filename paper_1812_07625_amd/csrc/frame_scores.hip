@@ -71,6 +71,14 @@ __device__ __forceinline__ void exchange()
 // registers: V slots at most a wavefront.  Lanes beyond the row, and elements of a vector that belong to its neighbours, are -inf.
 template <typename T> constexpr int LANE_VALUES = 16 / sizeof(T);
 
+// Registers that the compiler must not remember the unpacked values of: unpacking again costs less than holding them
+template <int V>
+__device__ __forceinline__ void opaque(uint4 (&q)[V])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) asm volatile("" : "+v"(q[v].x), "+v"(q[v].y), "+v"(q[v].z), "+v"(q[v].w));
+}
+
 struct Row {
     size_t first;    // element of the tensor that vector 0 begins with
     int head, nv;
@@ -106,27 +114,63 @@ __device__ __forceinline__ uint4 pack(const float (&x)[8])
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// vector n of the row.  A vector that reaches past the tensor's last element is put together from single loads
+// The row's elements of vector n, -inf in the places of its neighbours'
 template <typename T>
-__device__ __forceinline__ uint4 load_vector(const T* __restrict__ z, size_t total, const Row& row, int n, int C)
+__device__ __forceinline__ uint4 own_elements(uint4 q, const Row& row, int n, int C)
 {
     constexpr int N = LANE_VALUES<T>;
     float x[N];
-    const int c0 = n * N - row.head;
-    if (n >= row.nv) {
+    unpack(q, x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = -INFINITY;
-        return pack(x);
-    }
-    const size_t i = row.first + (size_t)n * N;
-    if (c0 >= 0 && c0 + N <= C) return *reinterpret_cast<const uint4*>(z + i);
-    if (i + N <= total) unpack(*reinterpret_cast<const uint4*>(z + i), x);
-    else
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = i + e < total ? Elem<T>::load(z, i + e) : -INFINITY;
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = (unsigned)(c0 + e) < (unsigned)C ? x[e] : -INFINITY;
+    for (int e = 0; e < N; ++e) x[e] = (unsigned)(n * N - row.head + e) < (unsigned)C ? x[e] : -INFINITY;
     return pack(x);
+}
+// Vectors that lie in the tensor whole are loaded whole; one that reaches past its last element (of the last row alone) is put
+// together from single loads
+template <typename T>
+__device__ __forceinline__ int whole_vectors(size_t total, const Row& row)
+{
+    const size_t whole = (total - row.first) / LANE_VALUES<T>;
+    return whole < (size_t)row.nv ? (int)whole : row.nv;
+}
+template <typename T>
+__device__ __forceinline__ uint4 tail_vector(const T* __restrict__ z, size_t total, const Row& row, int whole)
+{
+    constexpr int N = LANE_VALUES<T>;
+    float x[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const size_t i = row.first + (size_t)whole * N + e;
+        x[e] = i < total ? Elem<T>::load(z, i) : -INFINITY;
+    }
+    return pack(x);
+}
+// This lane's vectors n0, n0 + step, ... of a row of more than 64 elements.  Lanes beyond the row load its last whole vector again: without
+// branches all loads are in flight at once.  (-inf survives pack's rounding, and bf16 values do too.)
+template <typename T, int V>
+__device__ __forceinline__ void load_row(uint4 (&q)[V], const T* __restrict__ z, size_t total, const Row& row, int step, int n0, int C)
+{
+    const int whole = whole_vectors<T>(total, row), last = (row.nv - 1) >> 6;
+    const uint4* const at = reinterpret_cast<const uint4*>(z + row.first);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int n = n0 + v * step;
+        q[v] = at[n < whole ? n : whole - 1];
+    }
+    uint4 tail = make_uint4(0, 0, 0, 0);
+    if (whole < row.nv) tail = tail_vector(z, total, row, whole);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int n = n0 + v * step, slot = n >> 6;
+        if (slot == 0 || slot >= last) q[v] = own_elements<T>(n == whole ? tail : q[v], row, n, C);
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint4 load_vector(const T* __restrict__ z, size_t total, const Row& row, int n, int C)
+{
+    uint4 q[1];
+    load_row(q, z, total, row, 64, n, C);
+    return q[0];
 }
 
 // ---- the K largest of a row --------------------------------------------------------------------------------
@@ -139,6 +183,7 @@ __device__ __forceinline__ unsigned key_of(float x)
 }
 __device__ __forceinline__ float of_key(unsigned k) { return __uint_as_float(k ^ ((unsigned)((int)~k >> 31) | 0x80000000u)); }
 typedef unsigned long long ranked_t;
+constexpr int HELD = 128;
 __device__ __forceinline__ ranked_t ranked(float x, int c) { return (ranked_t)key_of(x) << 32 | ~(unsigned)c; }
 __device__ __forceinline__ int class_of(ranked_t k) { return (int)~(unsigned)k; }
 __device__ __forceinline__ float score_of(ranked_t k) { return of_key((unsigned)(k >> 32)); }
@@ -170,63 +215,47 @@ __device__ __forceinline__ float wave_threshold(const float (&group)[4], float l
 }
 
 // The wavefront's K largest classes, exactly, into list[0 .. K) in any order (fewer, if it holds fewer classes); returns how many.
-// For rows where thresholds leave too many: equal scores, or fewer finite ones than K.  The K-th score is bisected over
-// the registers, and of the scores equal to it the lowest classes are taken.
-template <typename T, int V>
-__device__ int exact_largest(const uint4 (&q)[V], int ns, int step, int n0, const Row& row, int C, int K, ranked_t* list)
+// For rows where thresholds leave too many: equal scores, or fewer finite ones than K.  The K-th entry in the order of scores and
+// classes is bisected.  Every step reads the row's vectors again, so that the registers of the usual path carry nothing for it.
+template <typename T>
+__device__ __forceinline__ int exact_largest(const T* __restrict__ z, size_t total, const Row& row, int ns, int step, int n0, int C, int K, ranked_t* list)
 {
     constexpr int N = LANE_VALUES<T>;
-    float least = INFINITY, most = -INFINITY;
+    auto entries = [&](int v, ranked_t (&a)[N]) {  // 0: not the row's
+        float x[N];
+        unpack(load_vector(z, total, row, n0 + v * step, C), x);
+        const int c0 = (n0 + v * step) * N - row.head;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (v < ns) {
-            float x[N];
-            unpack(q[v], x);
-#pragma unroll
-            for (int e = 0; e < N; ++e) { least = fminf(least, x[e]); most = fmaxf(most, x[e]); }
-        }
-    least = wave64(least, Min());
-    most = wave64(most, Max());
-    unsigned lo = key_of(least), hi = key_of(most) + 1, mid = lo + 1;  // first: are more equal to the least than are wanted?
+        for (int e = 0; e < N; ++e) a[e] = (unsigned)(c0 + e) < (unsigned)C ? ranked(x[e], c0 + e) : 0;
+    };
+    ranked_t lo = ranked(-INFINITY, MAX_CLASSES), hi = ~0ull, mid = ranked(-INFINITY, 0) + 1;  // first: are there K above -inf?
+#pragma unroll 1
     while (hi - lo > 1) {
-        const float t = of_key(mid);
         int n = 0;
+#pragma unroll 1
+        for (int v = 0; v < ns; ++v) {
+            ranked_t a[N];
+            entries(v, a);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v < ns) {
-                float x[N];
-                unpack(q[v], x);
-                const int c0 = (n0 + v * step) * N - row.head;
-#pragma unroll
-                for (int e = 0; e < N; ++e) n += __popcll(__ballot(x[e] >= t && (unsigned)(c0 + e) < (unsigned)C));
-            }
+            for (int e = 0; e < N; ++e) n += __popcll(__ballot(a[e] >= mid));
+        }
         (n >= K ? lo : hi) = mid;
+        if (n == K) break;
         mid = lo + (hi - lo) / 2;
     }
-    const float t = of_key(lo);
     int n = 0;
 #pragma unroll 1
-    for (int equal = 0; equal < 2; ++equal)   // those above the threshold, then those at it, in the order of their classes
+    for (int v = 0; v < ns; ++v) {
+        ranked_t a[N];
+        entries(v, a);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v < ns && n < K) {
-                float x[N];
-                unpack(q[v], x);
-                const int c0 = (n0 + v * step) * N - row.head;
-                int before = n, mine = 0;  // of the slot's takers, those in lower lanes come first, then those before in this one
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const unsigned long long b = __ballot((equal ? x[e] == t : x[e] > t) && (unsigned)(c0 + e) < (unsigned)C);
-                    before += below(b);
-                    n += __popcll(b);
-                }
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if ((equal ? x[e] == t : x[e] > t) && (unsigned)(c0 + e) < (unsigned)C) {
-                        if (before + mine < K) list[before + mine] = ranked(x[e], c0 + e);
-                        ++mine;
-                    }
-            }
+        for (int e = 0; e < N; ++e) {
+            const unsigned long long b = __ballot(a[e] >= lo);
+            const int at = n + below(b);
+            if (a[e] >= lo && at < K) list[at] = a[e];
+            n += __popcll(b);
+        }
+    }
     return n < K ? n : K;
 }
 
@@ -238,12 +267,14 @@ __device__ __forceinline__ void rank_list(const ranked_t* list, int n, int K, in
         if (thread >= n) return;
         const ranked_t a = list[thread];
         int before = 0;
+#pragma unroll 4
         for (int j = 0; j < n; ++j) before += list[j] > a;
         if (before < K) out(before, a);
     } else {
         const bool on = thread < n, on2 = thread + 64 < n;
         const ranked_t a = on ? list[thread] : 0, a2 = on2 ? list[thread + 64] : 0;
         int before = 0, before2 = 0;
+#pragma unroll 4
         for (int j = 0; j < n; ++j) {
             const ranked_t w = list[j];
             before += w > a;
@@ -295,14 +326,16 @@ struct Parts {
 // One row by a wavefront (!MULTI, four rows a workgroup), by a workgroup, or by G workgroups, which leave partial results (PARTS) for
 // token_join_k.  kscale = log2 e / temperature.
 template <typename T, int V, bool MULTI>
-__global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
+__global__ __launch_bounds__(MULTI ? 512 : 256) __attribute__((amdgpu_waves_per_eu(V > 8 ? 4 : V > 4 ? 5 : 7))) void token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
                                                                                     const int* __restrict__ in_len, TokenOut o, Parts parts,
                                                                                     unsigned rows, unsigned Tp, int C, int G, float kscale)
 {
     constexpr int N = LANE_VALUES<T>;
-    constexpr int ROWS = MULTI ? 1 : 4, CAP = MULTI ? 1024 : 128;
+    constexpr int ROWS = MULTI ? 1 : 4, CAP = MULTI ? 512 : 128;
     __shared__ ranked_t lists[ROWS][CAP];
-    __shared__ float red[MULTI ? 4 : 1][16];
+    __shared__ uint4 held[MULTI ? 8 : 4][HELD];  // a wavefront's vectors with a score at the threshold, and their numbers
+    __shared__ int held_n[MULTI ? 8 : 4][HELD];
+    __shared__ float red[MULTI ? 3 : 1][8];
     __shared__ int count, exact;  // entries of the list; where they did not fit, those of all wavefronts' own best
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = MULTI ? blockDim.x >> 6 : 1;
     const size_t total = (size_t)rows * C;
@@ -318,11 +351,9 @@ __global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void token_rows
             continue;
         }
         const Row row = row_at<T>(r, C);
-        const int P = W * G, step = P * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane, ns = (row.nv + step - 1) / step;
+        const int P = W * G, step = P * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane;
         uint4 q[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v < ns) q[v] = load_vector(z, total, row, n0 + v * step, C);
+        load_row(q, z, total, row, step, n0, C);
         int token = -1;
         float xt = 0.f;
         if (G == 1 && thread < o.S) {
@@ -332,14 +363,14 @@ __global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void token_rows
         float group[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (v < ns) {
+            {
                 float x[N];
                 unpack(q[v], x);
 #pragma unroll
                 for (int e = 0; e < N; ++e) group[e & 3] = fmaxf(group[e & 3], x[e]);
             }
         const float lane_most = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
-        float m = wave64(lane_most, Max()), t = 0.f;
+        float m = wave64(lane_most, Max()), t = INFINITY;
         if (o.K > 0) {
             const float least = wave64(lane_most, Min());
             // W wavefronts: K scores reach the least of thresholds that K / W of each one's reach, and the largest of those that K of one's do
@@ -363,10 +394,11 @@ __global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void token_rows
         }
         const float m0 = m == -INFINITY ? 0.f : m;
         float s = 0.f, u = 0.f;
-        int n = 0;
+        int n = 0, hits = 0;
+        opaque(q);
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (v < ns) {
+            {
                 float x[N], most = -INFINITY;
                 unpack(q[v], x);
 #pragma unroll
@@ -376,24 +408,44 @@ __global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void token_rows
                     u += p * fmaxf(d, -1000.f);  // 0 * -inf is no share of the entropy
                     most = fmaxf(most, x[e]);
                 }
-                if (o.K > 0 && __any(most >= t)) {
-                    const int c0 = (n0 + v * step) * N - row.head;
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const bool take = x[e] >= t && (unsigned)(c0 + e) < (unsigned)C;
-                        const unsigned long long b = __ballot(take);
-                        if (b == 0) continue;
-                        int at = n;
-                        if (MULTI) {
-                            if (lane == 0) at = atomicAdd(&count, __popcll(b));
-                            at = __builtin_amdgcn_readfirstlane(at);
-                        }
-                        n = at + __popcll(b);
-                        at += below(b);
-                        if (take && at < CAP && (!MULTI || at < (int)blockDim.x)) list[at] = ranked(x[e], c0 + e);
-                    }
+                asm volatile("" : "+v"(s), "+v"(u));  // summed here: left alone, the sums sink below all slots' branches and the values stay in registers
+                const unsigned long long b = __ballot(most >= t);
+                if (b != 0) {
+                    const int at = hits + below(b);
+                    if (most >= t && at < HELD) { held[wave][at] = q[v]; held_n[wave][at] = n0 + v * step; }
+                    hits += __popcll(b);
                 }
             }
+        if (o.K > 0) {
+            exchange<false>();
+            if (hits > HELD) n = CAP + 1;
+#pragma unroll 1
+            for (int base = 0; base < hits && n <= CAP; base += 64) {
+                float x[N];
+                const int i = base + lane;
+                const bool on = i < hits;
+                unpack(held[wave][on ? i : 0], x);
+                const int c0 = held_n[wave][on ? i : 0] * N - row.head;
+                unsigned mine = 0;
+#pragma unroll
+                for (int e = 0; e < N; ++e) mine |= on && x[e] >= t && (unsigned)(c0 + e) < (unsigned)C ? 1u << e : 0u;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const bool take = mine >> e & 1;
+                    const unsigned long long b = __ballot(take);
+                    if (b == 0) continue;
+                    int at = n;
+                    if (MULTI) {
+                        if (lane == 0) at = atomicAdd(&count, __popcll(b));
+                        at = __builtin_amdgcn_readfirstlane(at);
+                    }
+                    n = at + __popcll(b);
+                    at += below(b);
+                    if (take && at < (MULTI ? (int)blockDim.x : CAP)) list[at] = ranked(x[e], c0 + e);
+                }
+            }
+            if (MULTI && hits > HELD && lane == 0) atomicAdd(&count, CAP + 1);
+        }
         s = wave64(s, Sum());
         u = wave64(u, Sum());
         if (MULTI) {
@@ -409,7 +461,7 @@ __global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void token_rows
             if (n > room) {
                 list[wave * 64 * MULTI + lane] = 0;
                 exchange<MULTI>();
-                n = exact_largest<T, V>(q, ns, step, n0, row, C, o.K, list + wave * 64 * MULTI);
+                n = exact_largest(z, total, row, V, step, n0, C, o.K, list + wave * 64 * MULTI);
                 if (MULTI) {
                     if (lane == 0) atomicAdd(&exact, n);
                     n = room;
@@ -641,15 +693,11 @@ __global__ __launch_bounds__(THREADS) void token_bwd_rows_k(const T* __restrict_
         const Row row = row_at<T>(r, C);
         const int slots = (row.nv + 63) / 64, first = p * V;
         if (first >= slots) continue;
-        const int ns = slots - first < V ? slots - first : V;
         const float4 q = reinterpret_cast<const float4*>(stats)[r];
         const bool live = frame_of(in_len, r, Tp) == LIVE && fabsf(q.y) < INFINITY;
         if (!live && accumulate) continue;
         uint4 data[V];
-        if (live)
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v < ns) data[v] = load_vector(z, total, row, (first + v) * 64 + lane, C);
+        if (live) load_row(data, z, total, row, 64, first * 64 + lane, C);
         Columns<2> cols{{-1, -1}};
         float sum = 0.f, h = 0.f;
         if (live) {
@@ -670,7 +718,7 @@ __global__ __launch_bounds__(THREADS) void token_bwd_rows_k(const T* __restrict_
         cols.template place<N>(row);
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (v < ns) {
+            {
                 const int n = (first + v) * 64 + lane, c0 = n * N - row.head;
                 float x[N];
                 if (live) {
@@ -782,14 +830,14 @@ __device__ __forceinline__ float frame_loss_of(const Teacher& te, const int (&c)
 
 // sums: (m or -inf, s, ., .) of every row's G workgroups where a row is too long for the registers of one, or rows are few; else NULL
 template <typename T, typename D, int V, bool MULTI>
-__global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void distill_rows_k(const T* __restrict__ z, Teacher te, const int* __restrict__ in_len,
+__global__ __launch_bounds__(MULTI ? 512 : 256) void distill_rows_k(const T* __restrict__ z, Teacher te, const int* __restrict__ in_len,
                                                                                       const float4* __restrict__ sums, float* __restrict__ frame_loss,
                                                                                       D* __restrict__ dz, unsigned rows, unsigned Tp, int C, int G,
                                                                                       int accumulate)
 {
     constexpr int N = LANE_VALUES<T>;
     constexpr int ROWS = MULTI ? 1 : 4;
-    __shared__ float red[2][16];
+    __shared__ float red[2][8];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = MULTI ? blockDim.x >> 6 : 1;
     const size_t total = (size_t)rows * C;
     const unsigned tasks = rows * G, stride = gridDim.x * ROWS;
@@ -799,16 +847,14 @@ __global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void distill_ro
         const bool first = g == 0 && (MULTI ? threadIdx.x : lane) == 0;
         const Frame f = frame_of(in_len, r, Tp);
         const Row row = row_at<T>(r, C);
-        const int P = W * G, step = P * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane, ns = (row.nv + step - 1) / step;
+        const int P = W * G, step = P * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane;
         const float w = f != LIVE ? 0.f : te.weight ? te.weight[r] : 1.f;
         float loss = f == BAD ? NAN : 0.f, m = 0.f, scale = 0.f;
         bool live = false;
         uint4 data[V];
         Columns<1> cols{{-1}};
         if (w != 0.f) {
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v < ns) data[v] = load_vector(z, total, row, n0 + v * step, C);
+            load_row(data, z, total, row, step, n0, C);
             int c[1] = {-1};
             float t[1] = {-INFINITY}, x[1] = {0.f}, q[1];
             if (lane < te.K) {
@@ -828,7 +874,7 @@ __global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void distill_ro
             } else {
 #pragma unroll
                 for (int v = 0; v < V; ++v)
-                    if (v < ns) {
+                    {
                         float y[N];
                         unpack(data[v], y);
 #pragma unroll
@@ -841,9 +887,10 @@ __global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void distill_ro
                     for (int i = 0; i < W; ++i) m = fmaxf(m, red[0][i]);
                 }
                 m = m == -INFINITY ? 0.f : m;
+                opaque(data);
 #pragma unroll
                 for (int v = 0; v < V; ++v)
-                    if (v < ns) {
+                    {
                         float y[N];
                         unpack(data[v], y);
 #pragma unroll
@@ -867,9 +914,10 @@ __global__ __launch_bounds__(MULTI ? (V > 8 ? 512 : 1024) : 256) void distill_ro
         if (!dz || (!live && accumulate)) continue;
         if (!live) cols.id[0] = -1;
         cols.template place<N>(row);
+        opaque(data);
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (v < ns) {
+            {
                 const int n = n0 + v * step, c0 = n * N - row.head;
                 float x[N];
                 if (live) {
@@ -988,7 +1036,7 @@ Plan plan_of(long long rows, int C, int dtype)
     long long P = (slots + MOST - 1) / MOST;
     while (rows * P < 2048 && P * 2 <= slots && P * 2 <= 8 * MAX_GROUPS) P *= 2;  // two wavefronts a SIMD
     const int W = P <= 8 ? (int)P : 8, G = (int)((P + W - 1) / W), per = (slots + W * G - 1) / (W * G);
-    return {W, G, per <= 2 ? 2 : per <= 8 ? 8 : 16};
+    return {W, G, per <= 2 ? 2 : per <= 4 ? 4 : per <= 8 ? 8 : per <= 12 ? 12 : 16};
 }
 unsigned grid_of(long long groups) { return (unsigned)(groups < (1 << 20) ? groups : 1 << 20); }
 size_t sums_bytes(long long rows, const Plan& p) { return p.G > 1 ? round_up((size_t)rows * p.G * sizeof(float4), 256) : 0; }
@@ -1017,12 +1065,14 @@ int launch_tokens(const Plan& p, hipStream_t st, const void* z, const int* token
         const dim3 g(grid_of(((long long)rows + 15) / 16)), b(THREADS);
         if (p.V == 2) hipLaunchKernelGGL((token_narrow_k<T, 2>), g, b, 0, st, (const T*)z, tokens, in_len, o, rows, Tp, C);
         else hipLaunchKernelGGL((token_narrow_k<T, 4>), g, b, 0, st, (const T*)z, tokens, in_len, o, rows, Tp, C);
-    } else if (p.V == 2)
-        launch_rows<T, 2>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale);
-    else if (p.V == 8)
-        launch_rows<T, 8>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale);
-    else
-        launch_rows<T, 16>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale);
+    } else
+        switch (p.V) {
+            case 2: launch_rows<T, 2>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale); break;
+            case 4: launch_rows<T, 4>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale); break;
+            case 8: launch_rows<T, 8>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale); break;
+            case 12: launch_rows<T, 12>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale); break;
+            default: launch_rows<T, 16>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale);
+        }
     if (int rc = launch_status()) return rc;
     if (p.G == 1 || !join) return W2L_OK;
     hipLaunchKernelGGL(token_join_k<T>, dim3(grid_of(rows)), dim3(THREADS), 0, st, (const T*)z, tokens, in_len, o, parts, rows, Tp, C, p.G);
@@ -1081,9 +1131,13 @@ int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& 
         if (int rc = launch_tokens<T>(p, st, z, nullptr, in_len, none, ws, rows, Tp, C, te.kscale, false)) return rc;
         sums = (const float4*)ws;
     }
-    if (p.V == 2) launch_distill_rows<T, D, 2>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate);
-    else if (p.V == 8) launch_distill_rows<T, D, 8>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate);
-    else launch_distill_rows<T, D, 16>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate);
+    switch (p.V) {
+        case 2: launch_distill_rows<T, D, 2>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate); break;
+        case 4: launch_distill_rows<T, D, 4>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate); break;
+        case 8: launch_distill_rows<T, D, 8>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate); break;
+        case 12: launch_distill_rows<T, D, 12>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate); break;
+        default: launch_distill_rows<T, D, 16>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate);
+    }
     return launch_status();
 }
 
