@@ -13,8 +13,8 @@ using namespace w2l;
 namespace {
 
 constexpr int MAX_CLASSES = 262144, MAX_ENTRIES = 64;
-constexpr int THREADS = 256, MAX_GROUPS = 16;
-constexpr float LOG2E = 1.44269504088896f;
+constexpr int THREADS = 256, MAX_WAVES = 16, MAX_SLOTS = 16, MAX_GROUPS = 8;
+constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
 enum Frame { LIVE = 0, PADDING = 1, BAD = 2 };
 
 __device__ __forceinline__ Frame frame_of(const int* __restrict__ in_len, unsigned r, unsigned Tp)
@@ -183,7 +183,8 @@ __device__ __forceinline__ unsigned key_of(float x)
 }
 __device__ __forceinline__ float of_key(unsigned k) { return __uint_as_float(k ^ ((unsigned)((int)~k >> 31) | 0x80000000u)); }
 typedef unsigned long long ranked_t;
-constexpr int HELD = 128;
+constexpr int HELD = 128, LIST = 128;  // a wavefront's vectors and list entries
+constexpr size_t lds_of(int waves, bool multi) { return waves * (HELD * (sizeof(uint4) + sizeof(int)) + (multi ? 64 : LIST) * sizeof(ranked_t)); }
 __device__ __forceinline__ ranked_t ranked(float x, int c) { return (ranked_t)key_of(x) << 32 | ~(unsigned)c; }
 __device__ __forceinline__ int class_of(ranked_t k) { return (int)~(unsigned)k; }
 __device__ __forceinline__ float score_of(ranked_t k) { return of_key((unsigned)(k >> 32)); }
@@ -193,8 +194,8 @@ __device__ __forceinline__ int below(unsigned long long mask)  // bits of the ma
     return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
 }
 
-// A threshold that at least `need` (<= 64) values of the wavefront reach, and not many more: each lane brings the largest of four
-// groups of its values, and the threshold is bisected (over the order of the bits) until about `need` of these 256 reach it.
+// A threshold that at least `need` (<= 64) values of the wavefront reach, and not many more: each lane brings the largest of up to four
+// groups of its values (-inf: no group), and the threshold is bisected (over the order of the bits) until about `need` of these 256 reach it.
 // least: the smallest of the lanes' largest, which 64 values reach; most: the largest of all.
 __device__ __forceinline__ float wave_threshold(const float (&group)[4], float least, float most, int need)
 {
@@ -323,23 +324,43 @@ struct Parts {
     ranked_t* best;
 };
 
+// The sums of token_rows_k where k m is 2^24 or more, and its rounding no small shift, or m is +inf: from differences of scores
+template <typename T>
+__device__ __forceinline__ void far_sums(const T* __restrict__ z, size_t total, const Row& row, int slots, int step, int n0, int C, float m, float kscale,
+                                         float& s, float& u)
+{
+    s = u = 0.f;
+#pragma unroll 1
+    for (int v = 0; v < slots; ++v) {
+        float x[LANE_VALUES<T>];
+        unpack(load_vector(z, total, row, n0 + v * step, C), x);
+#pragma unroll
+        for (int e = 0; e < LANE_VALUES<T>; ++e) {
+            const float a = (x[e] - m) * kscale, p = __builtin_amdgcn_exp2f(a);
+            s += p;
+            u += p * fmaxf(a, -1000.f);
+        }
+    }
+}
+
 // One row by a wavefront (!MULTI, four rows a workgroup), by a workgroup, or by G workgroups, which leave partial results (PARTS) for
 // token_join_k.  kscale = log2 e / temperature.
 template <typename T, int V, bool MULTI>
-__global__ __launch_bounds__(MULTI ? 512 : 256) __attribute__((amdgpu_waves_per_eu(V > 8 ? 4 : V > 4 ? 5 : 7))) void token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
+__global__ __launch_bounds__(MULTI ? 1024 : 256) __attribute__((amdgpu_waves_per_eu(V > 8 ? 4 : V > 4 ? 5 : 6))) void token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
                                                                                     const int* __restrict__ in_len, TokenOut o, Parts parts,
                                                                                     unsigned rows, unsigned Tp, int C, int G, float kscale)
 {
     constexpr int N = LANE_VALUES<T>;
-    constexpr int ROWS = MULTI ? 1 : 4, CAP = MULTI ? 512 : 128;
-    __shared__ ranked_t lists[ROWS][CAP];
-    __shared__ uint4 held[MULTI ? 8 : 4][HELD];  // a wavefront's vectors with a score at the threshold, and their numbers
-    __shared__ int held_n[MULTI ? 8 : 4][HELD];
-    __shared__ float red[MULTI ? 3 : 1][8];
+    constexpr int ROWS = MULTI ? 1 : 4;
+    extern __shared__ uint4 lds[];
+    __shared__ float red[MULTI ? 3 : 1][16];
     __shared__ int count, exact;  // entries of the list; where they did not fit, those of all wavefronts' own best
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = MULTI ? blockDim.x >> 6 : 1;
+    uint4* const held = lds + wave * HELD;  // the wavefront's vectors with a score at the threshold, and their numbers
+    int* const held_n = reinterpret_cast<int*>(lds + (MULTI ? W : 4) * HELD) + wave * HELD;
+    const int room = MULTI ? W * 64 : LIST;  // of the list: a workgroup's, or each wavefront's
+    ranked_t* const list = reinterpret_cast<ranked_t*>(lds + (MULTI ? W : 4) * (HELD + HELD / 4)) + (MULTI ? 0 : wave * LIST);
     const size_t total = (size_t)rows * C;
-    ranked_t* const list = lists[MULTI ? 0 : wave];
     const int thread = MULTI ? (int)threadIdx.x : lane;
     const unsigned tasks = rows * G, stride = gridDim.x * ROWS;
     for (unsigned task = blockIdx.x * ROWS + (MULTI ? 0 : wave); task < tasks; task += stride) {
@@ -360,15 +381,16 @@ __global__ __launch_bounds__(MULTI ? 512 : 256) __attribute__((amdgpu_waves_per_
             token = tokens[(size_t)r * o.S + thread];
             if (token >= 0 && token < C) xt = Elem<T>::load(z, (size_t)r * C + token);
         }
-        float group[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float most[V], group[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // largest of each vector; of up to four groups of them
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            {
-                float x[N];
-                unpack(q[v], x);
+        for (int v = 0; v < V; ++v) {
+            float x[N];
+            unpack(q[v], x);
+            most[v] = x[0];
 #pragma unroll
-                for (int e = 0; e < N; ++e) group[e & 3] = fmaxf(group[e & 3], x[e]);
-            }
+            for (int e = 1; e < N; ++e) most[v] = fmaxf(most[v], x[e]);
+            group[v * 4 / (V > 4 ? V : 4)] = fmaxf(group[v * 4 / (V > 4 ? V : 4)], most[v]);
+        }
         const float lane_most = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
         float m = wave64(lane_most, Max()), t = INFINITY;
         if (o.K > 0) {
@@ -392,40 +414,45 @@ __global__ __launch_bounds__(MULTI ? 512 : 256) __attribute__((amdgpu_waves_per_
             }
             if (o.K > 0) t = fmaxf(all, own);
         }
-        const float m0 = m == -INFINITY ? 0.f : m;
+        // exp(x - m) as 2^(k x - M), M = k m rounded: what the rounding moves, `shift`, is taken out of the sums at the end
+        const float m0 = m == -INFINITY ? 0.f : m, M = m0 * kscale, shift = __builtin_fmaf(m0, kscale, -M);
         float s = 0.f, u = 0.f;
         int n = 0, hits = 0;
         opaque(q);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            {
-                float x[N], most = -INFINITY;
-                unpack(q[v], x);
+        for (int v = 0; v < V; ++v) {
+            float x[N];
+            unpack(q[v], x);
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float d = x[e] - m0, p = __builtin_amdgcn_exp2f(d * kscale);
-                    s += p;
-                    u += p * fmaxf(d, -1000.f);  // 0 * -inf is no share of the entropy
-                    most = fmaxf(most, x[e]);
-                }
-                asm volatile("" : "+v"(s), "+v"(u));  // summed here: left alone, the sums sink below all slots' branches and the values stay in registers
-                const unsigned long long b = __ballot(most >= t);
-                if (b != 0) {
-                    const int at = hits + below(b);
-                    if (most >= t && at < HELD) { held[wave][at] = q[v]; held_n[wave][at] = n0 + v * step; }
-                    hits += __popcll(b);
-                }
+            for (int e = 0; e < N; ++e) {
+                const float a = __builtin_fmaf(x[e], kscale, -M), p = __builtin_amdgcn_exp2f(a);
+                s += p;
+                u += p * fmaxf(a, -1000.f);  // 0 * -inf is no share of the entropy
             }
+            asm volatile("" : "+v"(s), "+v"(u));  // summed here: left alone, the sums sink below all slots' branches and the values stay in registers
+            const unsigned long long b = __ballot(most[v] >= t);
+            if (b != 0) {
+                const int at = hits + below(b);
+                if (most[v] >= t && at < HELD) { held[at] = q[v]; held_n[at] = n0 + v * step; }
+                hits += __popcll(b);
+            }
+        }
+        if (!(fabsf(M) < 16777216.f)) far_sums(z, total, row, V, step, n0, C, m0, kscale, s, u);
+        else {
+            const float scale = __builtin_amdgcn_exp2f(-shift);
+            u = (u - shift * s) * scale;
+            s *= scale;
+        }
         if (o.K > 0) {
             exchange<false>();
-            if (hits > HELD) n = CAP + 1;
+            if (hits > HELD) n = room + 1;
 #pragma unroll 1
-            for (int base = 0; base < hits && n <= CAP; base += 64) {
+            for (int base = 0; base < hits && n <= room; base += 64) {
                 float x[N];
                 const int i = base + lane;
                 const bool on = i < hits;
-                unpack(held[wave][on ? i : 0], x);
-                const int c0 = held_n[wave][on ? i : 0] * N - row.head;
+                unpack(held[on ? i : 0], x);
+                const int c0 = held_n[on ? i : 0] * N - row.head;
                 unsigned mine = 0;
 #pragma unroll
                 for (int e = 0; e < N; ++e) mine |= on && x[e] >= t && (unsigned)(c0 + e) < (unsigned)C ? 1u << e : 0u;
@@ -441,10 +468,10 @@ __global__ __launch_bounds__(MULTI ? 512 : 256) __attribute__((amdgpu_waves_per_
                     }
                     n = at + __popcll(b);
                     at += below(b);
-                    if (take && at < (MULTI ? (int)blockDim.x : CAP)) list[at] = ranked(x[e], c0 + e);
+                    if (take && at < room) list[at] = ranked(x[e], c0 + e);
                 }
             }
-            if (MULTI && hits > HELD && lane == 0) atomicAdd(&count, CAP + 1);
+            if (MULTI && hits > HELD && lane == 0) atomicAdd(&count, room + 1);
         }
         s = wave64(s, Sum());
         u = wave64(u, Sum());
@@ -456,8 +483,8 @@ __global__ __launch_bounds__(MULTI ? 512 : 256) __attribute__((amdgpu_waves_per_
             s = u = 0.f;
             for (int w = 0; w < W; ++w) { s += red[0][w]; u += red[1][w]; }
         }
+        u *= LN2;
         if (o.K > 0 && s == s) {
-            const int room = MULTI ? (int)blockDim.x : CAP;
             if (n > room) {
                 list[wave * 64 * MULTI + lane] = 0;
                 exchange<MULTI>();
@@ -503,16 +530,14 @@ __global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z,
     for (unsigned r = blockIdx.x; r < rows; r += gridDim.x) {
         const int tid = threadIdx.x;
         const Frame f = frame_of(in_len, r, Tp);
+        const int lane = tid & 63;
         float m = -INFINITY, s = 0.f, u = 0.f;
         if (f == LIVE) {
-            for (int g = 0; g < G; ++g) m = fmaxf(m, parts.sums[(size_t)r * G + g].x);
-            for (int g = 0; g < G; ++g) {
-                const float4 p = parts.sums[(size_t)r * G + g];
-                if (p.y == 0.f) continue;
-                const float d = p.x - m, scale = expf(d);
-                s += p.y * scale;
-                u += (p.z + (p.y > 0.f ? p.y * fmaxf(d, -1000.f) : 0.f)) * scale;
-            }
+            const float4 p = lane < G ? parts.sums[(size_t)r * G + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+            m = wave64(p.x, Max());
+            const float d = p.x - m, scale = expf(d);
+            s = wave64(p.y != 0.f ? p.y * scale : 0.f, Sum());
+            u = wave64(p.y != 0.f ? (p.z + p.y * fmaxf(d, -1000.f)) * scale : 0.f, Sum());
         }
         if (f != LIVE || !(s == s)) {
             write_absent(o, r, f == LIVE ? BAD : f, tid, THREADS);
@@ -526,14 +551,15 @@ __global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z,
         }
         if (o.K == 0) continue;
         const ranked_t* const best = parts.best + (size_t)r * G * o.K;
-        ranked_t least = ~0ull, most = 0;
         const int need = (o.K + G - 1) / G;
-        for (int g = 0; g < G; ++g) {
-            const ranked_t a = best[g * o.K + need - 1], b = best[g * o.K + o.K - 1];
+        ranked_t least = lane < G ? best[lane * o.K + need - 1] : ~0ull, most = lane < G ? best[lane * o.K + o.K - 1] : 0;
+#pragma unroll
+        for (int j = MAX_GROUPS / 2; j > 0; j >>= 1) {
+            const ranked_t a = __shfl_xor(least, j, MAX_GROUPS), b = __shfl_xor(most, j, MAX_GROUPS);
             least = a < least ? a : least;
             most = b > most ? b : most;
         }
-        if (least < most) least = most;
+        least = __shfl(least < most ? most : least, 0, 64);
         if (tid == 0) count = 0;
         __syncthreads();
         for (int i = tid; i < G * o.K; i += THREADS) {
@@ -830,14 +856,14 @@ __device__ __forceinline__ float frame_loss_of(const Teacher& te, const int (&c)
 
 // sums: (m or -inf, s, ., .) of every row's G workgroups where a row is too long for the registers of one, or rows are few; else NULL
 template <typename T, typename D, int V, bool MULTI>
-__global__ __launch_bounds__(MULTI ? 512 : 256) void distill_rows_k(const T* __restrict__ z, Teacher te, const int* __restrict__ in_len,
+__global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __restrict__ z, Teacher te, const int* __restrict__ in_len,
                                                                                       const float4* __restrict__ sums, float* __restrict__ frame_loss,
                                                                                       D* __restrict__ dz, unsigned rows, unsigned Tp, int C, int G,
                                                                                       int accumulate)
 {
     constexpr int N = LANE_VALUES<T>;
     constexpr int ROWS = MULTI ? 1 : 4;
-    __shared__ float red[2][8];
+    __shared__ float red[2][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = MULTI ? blockDim.x >> 6 : 1;
     const size_t total = (size_t)rows * C;
     const unsigned tasks = rows * G, stride = gridDim.x * ROWS;
@@ -1031,11 +1057,10 @@ struct Plan {
 Plan plan_of(long long rows, int C, int dtype)
 {
     if (C <= 64) return {0, 1, C <= 32 ? 2 : 4};
-    const int N = dtype == W2L_BF16 ? 8 : 4, slots = (C + 2 * (N - 1) + 64 * N - 1) / (64 * N);  // wherever in a vector the row begins
-    constexpr int MOST = 16;            // slots of a wavefront: 64 registers
-    long long P = (slots + MOST - 1) / MOST;
-    while (rows * P < 2048 && P * 2 <= slots && P * 2 <= 8 * MAX_GROUPS) P *= 2;  // two wavefronts a SIMD
-    const int W = P <= 8 ? (int)P : 8, G = (int)((P + W - 1) / W), per = (slots + W * G - 1) / (W * G);
+    const int N = dtype == W2L_BF16 ? 8 : 4, most = C % N ? C + 2 * (N - 1) : C, slots = (most + 64 * N - 1) / (64 * N);  // most: wherever in a vector a row begins
+    long long P = (slots + MAX_SLOTS - 1) / MAX_SLOTS;
+    while (rows * P < 2048 && P * 4 <= slots && P * 2 <= MAX_WAVES) P *= 2;  // two wavefronts a SIMD, two slots each
+    const int W = P < MAX_WAVES ? (int)P : MAX_WAVES, G = (int)((P + W - 1) / W), per = (slots + W * G - 1) / (W * G);
     return {W, G, per <= 2 ? 2 : per <= 4 ? 4 : per <= 8 ? 8 : per <= 12 ? 12 : 16};
 }
 unsigned grid_of(long long groups) { return (unsigned)(groups < (1 << 20) ? groups : 1 << 20); }
@@ -1050,10 +1075,10 @@ void launch_rows(const Plan& p, hipStream_t st, const void* z, const int* tokens
                  unsigned rows, unsigned Tp, int C, float kscale)
 {
     if (p.W > 1 || p.G > 1)
-        hipLaunchKernelGGL((token_rows_k<T, V, true>), dim3(grid_of((long long)rows * p.G)), dim3(64 * p.W), 0, st, (const T*)z, tokens, in_len, o,
+        hipLaunchKernelGGL((token_rows_k<T, V, true>), dim3(grid_of((long long)rows * p.G)), dim3(64 * p.W), lds_of(p.W, true), st, (const T*)z, tokens, in_len, o,
                            parts, rows, Tp, C, p.G, kscale);
     else
-        hipLaunchKernelGGL((token_rows_k<T, V, false>), dim3(grid_of(((long long)rows + 3) / 4)), dim3(256), 0, st, (const T*)z, tokens, in_len, o,
+        hipLaunchKernelGGL((token_rows_k<T, V, false>), dim3(grid_of(((long long)rows + 3) / 4)), dim3(256), lds_of(4, false), st, (const T*)z, tokens, in_len, o,
                            parts, rows, Tp, C, 1, kscale);
 }
 template <typename T>
