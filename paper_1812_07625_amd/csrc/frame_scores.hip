@@ -14,6 +14,7 @@ namespace {
 
 constexpr int MAX_CLASSES = 262144, MAX_ENTRIES = 64;
 constexpr int THREADS = 256, MAX_WAVES = 16, MAX_SLOTS = 16, MAX_GROUPS = 8;
+constexpr float FAR = 16777216.f;  // 2^24: k m from here on has roundings that are no small shift
 constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
 enum Frame { LIVE = 0, PADDING = 1, BAD = 2 };
 
@@ -27,30 +28,41 @@ __device__ __forceinline__ Frame frame_of(const int* __restrict__ in_len, unsign
 
 
 // ---- reductions over lanes ----------------------------------------------------------------------------
+// (lanes that receive nothing combine with what changes nothing: then the move becomes an operand of the operation)
+struct Max {
+    static constexpr float none = -INFINITY;
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct Min {
+    static constexpr float none = INFINITY;
+    __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); }
+};
+struct Sum {
+    static constexpr float none = 0.f;
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
 template <int CTRL, int ROWS = 0xf>
-__device__ __forceinline__ float lane_of(float v)
+__device__ __forceinline__ float lane_of(float v, float none)
 {
-    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, ROWS, 0xf, false));
+    if (ROWS == 0xf) return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(v), CTRL, ROWS, 0xf, false));
 }
-struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
-struct Min { __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); } };
-struct Sum { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 // over the sixteen lanes of a DPP row, the same bits in each of them
 template <typename F>
 __device__ __forceinline__ float row16(float v, F f)
 {
-    v = f(v, lane_of<0xB1>(v));   // quad_perm [1,0,3,2]
-    v = f(v, lane_of<0x4E>(v));   // quad_perm [2,3,0,1]
-    v = f(v, lane_of<0x141>(v));  // row_half_mirror
-    return f(v, lane_of<0x140>(v));  // row_mirror
+    v = f(v, lane_of<0xB1>(v, f.none));   // quad_perm [1,0,3,2]
+    v = f(v, lane_of<0x4E>(v, f.none));   // quad_perm [2,3,0,1]
+    v = f(v, lane_of<0x141>(v, f.none));  // row_half_mirror
+    return f(v, lane_of<0x140>(v, f.none));  // row_mirror
 }
 // over the wavefront, uniform
 template <typename F>
 __device__ __forceinline__ float wave64(float v, F f)
 {
     v = row16(v, f);
-    v = f(v, lane_of<0x142, 0xa>(v));  // row_bcast:15 into rows 1 and 3 (lanes that receive nothing hold what nobody reads)
-    v = f(v, lane_of<0x143, 0xc>(v));  // row_bcast:31 into rows 2 and 3
+    v = f(v, lane_of<0x142, 0xa>(v, f.none));  // row_bcast:15 into rows 1 and 3
+    v = f(v, lane_of<0x143, 0xc>(v, f.none));  // row_bcast:31 into rows 2 and 3
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 // LDS written by some lanes of a wavefront (MULTI: a workgroup) and read by others after this
@@ -108,22 +120,43 @@ __device__ __forceinline__ uint4 pack(const float (&x)[4])
 }
 __device__ __forceinline__ uint4 pack(const float (&x)[8])
 {
+    typedef float float2_t __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
     unsigned w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = (unsigned)f32_to_bf16(x[2 * j]) | (unsigned)f32_to_bf16(x[2 * j + 1]) << 16;
+    for (int j = 0; j < 4; ++j) w[j] = __builtin_bit_cast(unsigned, __builtin_convertvector((float2_t){x[2 * j], x[2 * j + 1]}, bf16x2_t));
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Largest of a vector's elements, the instruction itself: fmaxf of loaded values costs one more each, for signalling NaN (rows with
+// NaN are found by their sums, whatever their maximum)
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float largest(const float (&x)[4]) { return max3(max3(x[0], x[1], x[2]), x[3], x[3]); }
+__device__ __forceinline__ float largest(const float (&x)[8])
+{
+    return max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[7]));
 }
 
 // The row's elements of vector n, -inf in the places of its neighbours'
 template <typename T>
 __device__ __forceinline__ uint4 own_elements(uint4 q, const Row& row, int n, int C)
 {
-    constexpr int N = LANE_VALUES<T>;
-    float x[N];
-    unpack(q, x);
+    constexpr int N = LANE_VALUES<T>, PER = N / 4;  // elements of a word
+    const int c0 = n * N - row.head;
+    unsigned w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = (unsigned)(n * N - row.head + e) < (unsigned)C ? x[e] : -INFINITY;
-    return pack(x);
+    for (int j = 0; j < 4; ++j) {
+        unsigned mine = 0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) mine |= (unsigned)(c0 + j * PER + e) < (unsigned)C ? (PER == 1 ? ~0u : 0xffffu << 16 * e) : 0u;
+        w[j] = (w[j] & mine) | ((PER == 1 ? 0xff800000u : 0xff80ff80u) & ~mine);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // Vectors that lie in the tensor whole are loaded whole; one that reaches past its last element (of the last row alone) is put
 // together from single loads
@@ -146,11 +179,11 @@ __device__ __forceinline__ uint4 tail_vector(const T* __restrict__ z, size_t tot
     return pack(x);
 }
 // This lane's vectors n0, n0 + step, ... of a row of more than 64 elements.  Lanes beyond the row load its last whole vector again: without
-// branches all loads are in flight at once.  (-inf survives pack's rounding, and bf16 values do too.)
+// branches all loads are in flight at once.
 template <typename T, int V>
 __device__ __forceinline__ void load_row(uint4 (&q)[V], const T* __restrict__ z, size_t total, const Row& row, int step, int n0, int C)
 {
-    const int whole = whole_vectors<T>(total, row), last = (row.nv - 1) >> 6;
+    const int whole = whole_vectors<T>(total, row), inside = (row.head + C) / (64 * LANE_VALUES<T>);  // inside: slots that end within the row
     const uint4* const at = reinterpret_cast<const uint4*>(z + row.first);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -162,7 +195,7 @@ __device__ __forceinline__ void load_row(uint4 (&q)[V], const T* __restrict__ z,
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int n = n0 + v * step, slot = n >> 6;
-        if (slot == 0 || slot >= last) q[v] = own_elements<T>(n == whole ? tail : q[v], row, n, C);
+        if ((slot == 0 && row.head) || slot >= inside) q[v] = own_elements<T>(n == whole ? tail : q[v], row, n, C);
     }
 }
 template <typename T>
@@ -183,8 +216,11 @@ __device__ __forceinline__ unsigned key_of(float x)
 }
 __device__ __forceinline__ float of_key(unsigned k) { return __uint_as_float(k ^ ((unsigned)((int)~k >> 31) | 0x80000000u)); }
 typedef unsigned long long ranked_t;
-constexpr int HELD = 128, LIST = 128;  // a wavefront's vectors and list entries
-constexpr size_t lds_of(int waves, bool multi) { return waves * (HELD * (sizeof(uint4) + sizeof(int)) + (multi ? 64 : LIST) * sizeof(ranked_t)); }
+constexpr int HELD = 128, LIST = 128;  // a wavefront's vectors and list entries (a list has room for two more)
+constexpr size_t lds_of(int waves, bool multi)
+{
+    return waves * HELD * (sizeof(uint4) + sizeof(int)) + (multi ? waves * 64 + 2 : waves * (LIST + 2)) * sizeof(ranked_t);
+}
 __device__ __forceinline__ ranked_t ranked(float x, int c) { return (ranked_t)key_of(x) << 32 | ~(unsigned)c; }
 __device__ __forceinline__ int class_of(ranked_t k) { return (int)~(unsigned)k; }
 __device__ __forceinline__ float score_of(ranked_t k) { return of_key((unsigned)(k >> 32)); }
@@ -260,29 +296,32 @@ __device__ __forceinline__ int exact_largest(const T* __restrict__ z, size_t tot
     return n < K ? n : K;
 }
 
-// list[0 .. n) of a wavefront (n <= 128) or a workgroup (MULTI: n <= its threads), all different: calls out(rank, entry) for the K first
+// list[0 .. n) of a wavefront (n <= 128) or a workgroup (MULTI: n <= its threads), all different but zeros, and list[n] = 0 (close_list):
+// calls out(rank, entry) for the K first
+__device__ __forceinline__ void close_list(ranked_t* list, int n, int thread)
+{
+    if (thread == 0) list[n] = 0;
+}
 template <bool MULTI, typename F>
 __device__ __forceinline__ void rank_list(const ranked_t* list, int n, int K, int thread, F out)
 {
-    if (MULTI) {
-        if (thread >= n) return;
-        const ranked_t a = list[thread];
-        int before = 0;
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) before += list[j] > a;
-        if (before < K) out(before, a);
-    } else {
-        const bool on = thread < n, on2 = thread + 64 < n;
-        const ranked_t a = on ? list[thread] : 0, a2 = on2 ? list[thread + 64] : 0;
-        int before = 0, before2 = 0;
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) {
-            const ranked_t w = list[j];
-            before += w > a;
-            before2 += w > a2;
+    if (MULTI && (thread & ~63) >= n) return;  // (whole wavefronts)
+    const ranked_t a = thread < n ? list[thread] : 0;
+    int before = 0;
+#pragma unroll 2
+    for (int j = 0; j < n; j += 2) {
+        const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(list + j);
+        before += w.x > a;
+        before += w.y > a;
+    }
+    if (thread < n && before < K) out(before, a);
+    if (!MULTI && n > 64) {  // the entries beyond one a lane: each against all lanes'
+        const ranked_t b = thread + 64 < n ? list[thread + 64] : 0;
+        for (int j = 0; j < n - 64; ++j) {
+            const ranked_t w = list[64 + j];
+            const int k = __popcll(__ballot(a > w)) + __popcll(__ballot(b > w));
+            if (thread == 0 && k < K) out(k, w);
         }
-        if (on && before < K) out(before, a);
-        if (on2 && before2 < K) out(before2, a2);
     }
 }
 
@@ -324,7 +363,7 @@ struct Parts {
     ranked_t* best;
 };
 
-// The sums of token_rows_k where k m is 2^24 or more, and its rounding no small shift, or m is +inf: from differences of scores
+// This lane's sums where k m is FAR, or m is +inf: from differences of scores, read again
 template <typename T>
 __device__ __forceinline__ void far_sums(const T* __restrict__ z, size_t total, const Row& row, int slots, int step, int n0, int C, float m, float kscale,
                                          float& s, float& u)
@@ -359,7 +398,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) __attribute__((amdgpu_waves_per
     uint4* const held = lds + wave * HELD;  // the wavefront's vectors with a score at the threshold, and their numbers
     int* const held_n = reinterpret_cast<int*>(lds + (MULTI ? W : 4) * HELD) + wave * HELD;
     const int room = MULTI ? W * 64 : LIST;  // of the list: a workgroup's, or each wavefront's
-    ranked_t* const list = reinterpret_cast<ranked_t*>(lds + (MULTI ? W : 4) * (HELD + HELD / 4)) + (MULTI ? 0 : wave * LIST);
+    ranked_t* const list = reinterpret_cast<ranked_t*>(lds + (MULTI ? W : 4) * (HELD + HELD / 4)) + (MULTI ? 0 : wave * (LIST + 2));
     const size_t total = (size_t)rows * C;
     const int thread = MULTI ? (int)threadIdx.x : lane;
     const unsigned tasks = rows * G, stride = gridDim.x * ROWS;
@@ -386,9 +425,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) __attribute__((amdgpu_waves_per
         for (int v = 0; v < V; ++v) {
             float x[N];
             unpack(q[v], x);
-            most[v] = x[0];
-#pragma unroll
-            for (int e = 1; e < N; ++e) most[v] = fmaxf(most[v], x[e]);
+            most[v] = largest(x);
             group[v * 4 / (V > 4 ? V : 4)] = fmaxf(group[v * 4 / (V > 4 ? V : 4)], most[v]);
         }
         const float lane_most = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
@@ -437,7 +474,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) __attribute__((amdgpu_waves_per
                 hits += __popcll(b);
             }
         }
-        if (!(fabsf(M) < 16777216.f)) far_sums(z, total, row, V, step, n0, C, m0, kscale, s, u);
+        if (!(fabsf(M) < FAR)) far_sums(z, total, row, V, step, n0, C, m0, kscale, s, u);
         else {
             const float scale = __builtin_amdgcn_exp2f(-shift);
             u = (u - shift * s) * scale;
@@ -495,6 +532,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) __attribute__((amdgpu_waves_per
                 }
             }
         }
+        if (o.K > 0) close_list(list, n, thread);
         exchange<MULTI>();
         if (MULTI && G > 1) {
             const size_t at = (size_t)r * G + g;
@@ -659,9 +697,14 @@ __device__ __forceinline__ void put(G* __restrict__ dz, size_t i, int c0, int C,
         for (int j = 0; j < STORES; ++j) {
             uint4* const at = reinterpret_cast<uint4*>(dz + i + j * PER);
             float w[PER];
-            if (accumulate) unpack(*at, w);
 #pragma unroll
-            for (int e = 0; e < PER; ++e) w[e] = accumulate ? w[e] + v[j * PER + e] : v[j * PER + e];
+            for (int e = 0; e < PER; ++e) w[e] = v[j * PER + e];
+            if (accumulate) {
+                float old[PER];
+                unpack(*at, old);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) w[e] += old[e];
+            }
             *at = pack(w);
         }
         return;
@@ -669,6 +712,18 @@ __device__ __forceinline__ void put(G* __restrict__ dz, size_t i, int c0, int C,
 #pragma unroll
     for (int e = 0; e < N; ++e)
         if ((unsigned)(c0 + e) < (unsigned)C) Elem<G>::store(dz, i + e, accumulate ? Elem<G>::load(dz, i + e) + v[e] : v[e]);
+}
+
+// Zeros in place of a row's gradient
+template <typename T, typename G>
+__device__ __forceinline__ void clear_row(G* __restrict__ dz, const Row& row, int slots, int step, int n0, int C)
+{
+    float zero[LANE_VALUES<T>] = {};
+#pragma unroll 1
+    for (int v = 0; v < slots; ++v) {
+        const int n = n0 + v * step;
+        if (n < row.nv) put(dz, row.first + (size_t)n * LANE_VALUES<T>, n * LANE_VALUES<T> - row.head, C, zero, 0);
+    }
 }
 
 // Up to 64 * R columns of a row that get something of their own, an entry a lane: its column (-1: none), what is added there, and the slot of the
@@ -683,20 +738,22 @@ struct Columns {
 #pragma unroll
         for (int j = 0; j < R; ++j) slot[j] = id[j] < 0 ? -1 : (id[j] + row.head) / (64 * N);
     }
-    // adds the entries of this slot to the lane's values, in the order of the entries
+    // adds the entries of this slot to its lanes' values, in the order of the entries
     template <int N>
-    __device__ __forceinline__ void apply(int at, int c0, float (&x)[N]) const
+    __device__ __forceinline__ void apply(int at, const Row& row, float (&x)[N]) const
     {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             unsigned long long b = __ballot(slot[j] == at);
             while (b) {
                 const int l = __ffsll((unsigned long long)b) - 1;
                 b &= b - 1;
-                const int c = __builtin_amdgcn_readlane(id[j], l) - c0;
-                const float a = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(add[j]), l));
+                const int c = __builtin_amdgcn_readlane(id[j], l) + row.head;
+                const float a = lane == ((c / N) & 63) ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(add[j]), l)) : 0.f;
 #pragma unroll
-                for (int e = 0; e < N; ++e) x[e] += c == e ? a : 0.f;
+                for (int e = 0; e < N; ++e)
+                    if (e == (c & (N - 1))) x[e] += a;  // a uniform choice
             }
         }
     }
@@ -720,46 +777,61 @@ __global__ __launch_bounds__(THREADS) void token_bwd_rows_k(const T* __restrict_
         const int slots = (row.nv + 63) / 64, first = p * V;
         if (first >= slots) continue;
         const float4 q = reinterpret_cast<const float4*>(stats)[r];
-        const bool live = frame_of(in_len, r, Tp) == LIVE && fabsf(q.y) < INFINITY;
-        if (!live && accumulate) continue;
-        uint4 data[V];
-        if (live) load_row(data, z, total, row, 64, first * 64 + lane, C);
-        Columns<2> cols{{-1, -1}};
-        float sum = 0.f, h = 0.f;
-        if (live) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int i = lane + 64 * j;
-                int c = -1;
-                float a = 0.f;
-                if (i < S) { c = tokens[(size_t)r * S + i]; a = dlogprob[(size_t)r * S + i]; }
-                else if (i < S + K) { c = top_ids[(size_t)r * K + i - S]; a = dtop[(size_t)r * K + i - S]; }
-                const bool there = c >= 0 && c < C;
-                cols.id[j] = there ? c : -1;
-                cols.add[j] = there ? a : 0.f;
-                if (64 * j < S + K) sum += wave64(cols.add[j], Sum());
-            }
-            h = dentropy ? dentropy[r] : 0.f;
+        if (frame_of(in_len, r, Tp) != LIVE || !(fabsf(q.y) < INFINITY)) {
+            if (!accumulate) clear_row<T>(dz, row, V, 64, first * 64 + lane, C);
+            continue;
         }
+        uint4 data[V];
+        load_row(data, z, total, row, 64, first * 64 + lane, C);
+        Columns<2> cols;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int i = lane + 64 * j;
+            int c = -1;
+            float a = 0.f;
+            if (i < S) { c = tokens[(size_t)r * S + i]; a = dlogprob[(size_t)r * S + i]; }
+            else if (i < S + K) { c = top_ids[(size_t)r * K + i - S]; a = dtop[(size_t)r * K + i - S]; }
+            const bool there = c >= 0 && c < C;
+            cols.id[j] = there ? c : -1;
+            cols.add[j] = there ? a : 0.f;
+            if (64 * j < S + K) sum += wave64(cols.add[j], Sum());
+        }
+        const float h = dentropy ? dentropy[r] : 0.f;
         cols.template place<N>(row);
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            {
-                const int n = (first + v) * 64 + lane, c0 = n * N - row.head;
+        const float M = q.x * LOG2E;
+        if (!(fabsf(M) < FAR)) {
+#pragma unroll 1
+            for (int v = 0; v < V; ++v) {  // from differences
+                const int n = (first + v) * 64 + lane;
                 float x[N];
-                if (live) {
-                    unpack(data[v], x);
+                unpack(load_vector(z, total, row, n, C), x);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const float lp = fmaxf((x[e] - q.x) - q.y, -1000.f);
-                        x[e] = -__builtin_amdgcn_exp2f(lp * LOG2E) * (sum + h * (lp + q.z));
-                    }
-                    cols.apply(first + v, c0, x);
-                } else
-#pragma unroll
-                    for (int e = 0; e < N; ++e) x[e] = 0.f;
-                if (n < row.nv) put(dz, row.first + (size_t)n * N, c0, C, x, accumulate);
+                for (int e = 0; e < N; ++e) {
+                    const float lp = fmaxf((x[e] - q.x) - q.y, -1000.f);
+                    x[e] = -__builtin_amdgcn_exp2f(lp * LOG2E) * (sum + h * (lp + q.z));
+                }
+                cols.apply(first + v, row, x);
+                if (n < row.nv) put(dz, row.first + (size_t)n * N, n * N - row.head, C, x, accumulate);
             }
+            continue;
+        }
+        // with a = k x - M: lp = ln 2 (a - shift) - log s, and -p (G + h (lp + H)) = 2^a (A + B a)
+        const float shift = __builtin_fmaf(q.x, LOG2E, -M), inv = -__builtin_amdgcn_exp2f(-shift) * expf(-q.y);
+        const float A = inv * (sum + h * ((q.z - q.y) - LN2 * shift)), B = inv * h * LN2;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int n = (first + v) * 64 + lane;
+            float x[N];
+            unpack(data[v], x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float a = __builtin_fmaf(x[e], LOG2E, -M);
+                x[e] = __builtin_amdgcn_exp2f(a) * __builtin_fmaf(B, fmaxf(a, -1000.f), A);
+            }
+            cols.apply(first + v, row, x);
+            if (n < row.nv) put(dz, row.first + (size_t)n * N, n * N - row.head, C, x, accumulate);
+        }
     }
 }
 
@@ -875,87 +947,108 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
         const Row row = row_at<T>(r, C);
         const int P = W * G, step = P * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane;
         const float w = f != LIVE ? 0.f : te.weight ? te.weight[r] : 1.f;
-        float loss = f == BAD ? NAN : 0.f, m = 0.f, scale = 0.f;
-        bool live = false;
+        if (w == 0.f) {
+            if (first) frame_loss[r] = f == BAD ? NAN : 0.f;
+            if (dz && !accumulate) clear_row<T>(dz, row, V, step, n0, C);
+            continue;
+        }
         uint4 data[V];
-        Columns<1> cols{{-1}};
-        if (w != 0.f) {
-            load_row(data, z, total, row, step, n0, C);
-            int c[1] = {-1};
-            float t[1] = {-INFINITY}, x[1] = {0.f}, q[1];
-            if (lane < te.K) {
-                c[0] = te.ids[(size_t)r * te.K + lane];
-                if (c[0] != -1) t[0] = te.scores[(size_t)r * te.K + lane];
-                if ((unsigned)c[0] < (unsigned)C) x[0] = Elem<T>::load(z, (size_t)r * C + c[0]);
+        load_row(data, z, total, row, step, n0, C);
+        int c[1] = {-1};
+        float t[1] = {-INFINITY}, x[1] = {0.f}, q[1];
+        if (lane < te.K) {
+            c[0] = te.ids[(size_t)r * te.K + lane];
+            if (c[0] != -1) t[0] = te.scores[(size_t)r * te.K + lane];
+            if ((unsigned)c[0] < (unsigned)C) x[0] = Elem<T>::load(z, (size_t)r * C + c[0]);
+        }
+        float m = -INFINITY, s = 0.f;
+        if (MULTI && sums) {
+            for (int i = 0; i < G; ++i) m = fmaxf(m, sums[(size_t)r * G + i].x);
+            for (int i = 0; i < G; ++i) {
+                const float4 a = sums[(size_t)r * G + i];
+                if (a.y != 0.f) s += a.y * expf((a.x - m) * te.inv_tau);
             }
-            float s = 0.f;
-            m = -INFINITY;
-            if (MULTI && sums) {
-                for (int i = 0; i < G; ++i) m = fmaxf(m, sums[(size_t)r * G + i].x);
-                for (int i = 0; i < G; ++i) {
-                    const float4 a = sums[(size_t)r * G + i];
-                    if (a.y != 0.f) s += a.y * expf((a.x - m) * te.inv_tau);
-                }
-                m = m == -INFINITY ? 0.f : m;
+            m = m == -INFINITY ? 0.f : m;
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float y[N];
+                unpack(data[v], y);
+                m = fmaxf(m, largest(y));
+            }
+            m = wave64(m, Max());
+            if (MULTI) {
+                if (lane == 0) red[0][wave] = m;
+                __syncthreads();
+                for (int i = 0; i < W; ++i) m = fmaxf(m, red[0][i]);
+            }
+            m = m == -INFINITY ? 0.f : m;
+            opaque(data);
+            const float M = m * te.kscale;
+            if (!(fabsf(M) < FAR)) {
+                float unused;
+                far_sums(z, total, row, V, step, n0, C, m, te.kscale, s, unused);
             } else {
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    {
-                        float y[N];
-                        unpack(data[v], y);
+                for (int v = 0; v < V; ++v) {
+                    float y[N];
+                    unpack(data[v], y);
 #pragma unroll
-                        for (int e = 0; e < N; ++e) m = fmaxf(m, y[e]);
-                    }
-                m = wave64(m, Max());
-                if (MULTI) {
-                    if (lane == 0) red[0][wave] = m;
-                    __syncthreads();
-                    for (int i = 0; i < W; ++i) m = fmaxf(m, red[0][i]);
+                    for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(y[e], te.kscale, -M));
                 }
-                m = m == -INFINITY ? 0.f : m;
-                opaque(data);
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-                    {
-                        float y[N];
-                        unpack(data[v], y);
-#pragma unroll
-                        for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((y[e] - m) * te.kscale);
-                    }
-                s = wave64(s, Sum());
-                if (MULTI) {
-                    if (lane == 0) red[1][wave] = s;
-                    __syncthreads();
-                    s = 0.f;
-                    for (int i = 0; i < W; ++i) s += red[1][i];
-                }
+                s *= __builtin_amdgcn_exp2f(-__builtin_fmaf(m, te.kscale, -M));
             }
-            loss = frame_loss_of<1, 64>(te, c, t, x, w, m, s, C, q, live);
-            const float ws = w * te.grad_scale * te.tau;
-            scale = ws / s;
-            cols.id[0] = q[0] > 0.f ? c[0] : -1;
-            cols.add[0] = -q[0] * ws;
+            s = wave64(s, Sum());
+            if (MULTI) {
+                if (lane == 0) red[1][wave] = s;
+                __syncthreads();
+                s = 0.f;
+                for (int i = 0; i < W; ++i) s += red[1][i];
+            }
         }
+        bool live;
+        const float loss = frame_loss_of<1, 64>(te, c, t, x, w, m, s, C, q, live);
         if (first) frame_loss[r] = loss;
-        if (!dz || (!live && accumulate)) continue;
-        if (!live) cols.id[0] = -1;
+        if (!dz) continue;
+        if (!live) {
+            if (!accumulate) clear_row<T>(dz, row, V, step, n0, C);
+            continue;
+        }
+        const float ws = w * te.grad_scale * te.tau, M0 = m * te.kscale;
+        Columns<1> cols{{q[0] > 0.f ? c[0] : -1}, {0}, {-q[0] * ws}};
         cols.template place<N>(row);
-        opaque(data);
+        if (!(fabsf(M0) < FAR)) {
+#pragma unroll 1
+            for (int v = 0; v < V; ++v) {  // from differences
+                const int n = n0 + v * step;
+                float y[N];
+                unpack(load_vector(z, total, row, n, C), y);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            {
-                const int n = n0 + v * step, c0 = n * N - row.head;
-                float x[N];
-                if (live) {
-                    unpack(data[v], x);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) x[e] = __builtin_amdgcn_exp2f((x[e] - m) * te.kscale) * scale;
-                    cols.apply(n >> 6, c0, x);
-                } else
-#pragma unroll
-                    for (int e = 0; e < N; ++e) x[e] = 0.f;
-                if (n < row.nv) put(dz, row.first + (size_t)n * N, c0, C, x, accumulate);
+                for (int e = 0; e < N; ++e) y[e] = __builtin_amdgcn_exp2f((y[e] - m) * te.kscale) * (ws / s);
+                cols.apply(n >> 6, row, y);
+                if (n < row.nv) put(dz, row.first + (size_t)n * N, n * N - row.head, C, y, accumulate);
             }
+            continue;
+        }
+        opaque(data);
+        // p_c ws = 2^(k x - M) f.  Where f >= 0 and the gradient is stored as bf16, f goes into M: its logarithm and their sum are good to 2^-18, of a
+        // result that is rounded by 2^-9.
+        const float f0 = ws / s * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, te.kscale, -M0));
+        const bool folded = sizeof(D) == 2 && f0 >= 0.f;
+        const float M = folded ? M0 - __builtin_amdgcn_logf(f0) : M0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int n = n0 + v * step;
+            float y[N];
+            unpack(data[v], y);
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[e], te.kscale, -M));
+            if (!folded)
+#pragma unroll
+                for (int e = 0; e < N; ++e) y[e] *= f0;
+            cols.apply(n >> 6, row, y);
+            if (n < row.nv) put(dz, row.first + (size_t)n * N, n * N - row.head, C, y, accumulate);
+        }
     }
 }
 
@@ -1031,7 +1124,13 @@ __global__ __launch_bounds__(THREADS) void utterance_loss_k(const float* __restr
 {
     __shared__ double lds[THREADS / 64];
     double s = 0.;
-    for (unsigned t = threadIdx.x; t < Tp; t += THREADS) s += frame_loss[(size_t)blockIdx.x * Tp + t];
+    for (unsigned t = threadIdx.x; t < Tp; t += 4 * THREADS) {
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = t + j * THREADS < Tp ? frame_loss[(size_t)blockIdx.x * Tp + t + j * THREADS] : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s += v[j];
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
