@@ -242,42 +242,67 @@ def w2l_logsoftmax_bwd(lp, dlp, dz, stream=None):
     return dz
 
 
-def _frames(t, shape, dtype, z, name):
-    """Device pointer of an operand that has to be `shape` of `dtype` beside the scores z (None stays None)."""
+# The stream that torch has current on a device, as the handle itself (torch.cuda.current_stream makes an object for it: 2 us of a call
+# whose kernel may take 3)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_F32, _I32 = torch.float32, torch.int32
+
+
+def _frames(t, shape, dtype, dev, name):
+    """Device pointer of an operand that has to be `shape` of `dtype` on device `dev` (None stays None)."""
     if t is None:
         return None
-    if t.dtype != dtype:
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
-    if t.device != z.device:
-        raise ValueError("%s is on %s, the scores are on %s" % (name, t.device, z.device))
-    return _p(t)
+    if t.get_device() != dev:
+        raise ValueError("%s is on %s, the scores are on cuda:%d" % (name, t.device, dev))
+    raise ValueError("%s must be contiguous" % name)
 
 
 def _scores(z):
+    """Pointer, shape, type code and device index of scores z[B,T,C]."""
     if z.dim() != 3:
         raise ValueError("scores must be [B, T, C], not %s" % (tuple(z.shape),))
     if not z.is_cuda:
         raise ValueError("scores must be on a GPU")
-    return tuple(z.shape)
+    B, T, Cc = z.shape
+    return _p(z), B, T, Cc, _dt(z), z.get_device()
 
 
-def _grad_of(dz, z):
-    if dz is not None and dz.dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError("unsupported tensor dtype %s" % dz.dtype)
-    return _frames(dz, tuple(z.shape), dz.dtype, z, "dz") if dz is not None else None
+def _last(t, name):
+    """Entries of a frame of an operand [B,T,n]; None: 0."""
+    if t is None:
+        return 0
+    if t.dim() != 3:
+        raise ValueError("%s must be [B, T, n], not %s" % (name, tuple(t.shape)))
+    return t.shape[2]
 
 
-def _on_device(z, stream, workspace, call):
-    """call(workspace pointer, its bytes, stream) with the device of z current; its current stream unless one is given."""
-    if workspace is not None and workspace.device != z.device:
-        raise ValueError("workspace is on %s, the scores are on %s" % (workspace.device, z.device))
-    wp, wn = _ws(workspace)
-    if z.device.index == torch.cuda.current_device():
-        return call(wp, wn, _stream(stream))
-    with torch.cuda.device(z.device):
-        return call(wp, wn, _stream(stream))
+def _call(fn, where, dev, args, stream):
+    """fn(*args, stream) with device `dev` current, on its current stream unless one is given."""
+    if stream is None:
+        st = _current_stream(dev)
+    else:
+        st = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+    if torch.cuda.current_device() == dev:
+        rc = fn(*args, st)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, st)
+    if rc != 0:
+        raise W2LError(rc, where)
+
+
+def _scratch(workspace, dev):
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != dev:
+        raise ValueError("workspace is on %s, the scores are on cuda:%d" % (workspace.device, dev))
+    return _p(workspace), workspace.numel() * workspace.element_size()
 
 
 def w2l_token_logprob_workspace_bytes(B, Tp, Cc, K, dtype) -> int:
@@ -288,38 +313,33 @@ def w2l_token_logprob_fwd(z, tokens=None, logprob=None, entropy=None, top_ids=No
                           workspace=None, stream=None):
     """Scores z[B,T,C] -> log-probabilities of tokens[B,T,S], entropy[B,T], the K best classes (top_ids, top_logprob [B,T,K])
     and what the backward call reads (stats [B,T,4]); outputs that are None are not wanted."""
-    B, T, Cc = _scores(z)
-    S = 0 if tokens is None else tokens.shape[-1]
-    K = 0 if top_ids is None else top_ids.shape[-1]
-    f, n = torch.float32, torch.int32
-    ptr = (_p(z), _frames(tokens, (B, T, S), n, z, "tokens"), _frames(in_len, (B,), n, z, "in_len"),
-           _frames(logprob, (B, T, S), f, z, "logprob"), _frames(entropy, (B, T), f, z, "entropy"),
-           _frames(top_ids, (B, T, K), n, z, "top_ids"), _frames(top_logprob, (B, T, K), f, z, "top_logprob"),
-           _frames(stats, (B, T, 4), f, z, "stats"))
-    dt = _dt(z)
-    _check(_on_device(z, stream, workspace, lambda wp, wn, st: raw.w2l_token_logprob_fwd(*ptr, B, T, Cc, S, K, dt, wp, wn, st)),
-           "w2l_token_logprob_fwd")
+    pz, B, T, Cc, dt, dev = _scores(z)
+    S, K = _last(tokens, "tokens"), _last(top_ids, "top_ids")
+    wp, wn = _scratch(workspace, dev)
+    _call(raw.w2l_token_logprob_fwd, "w2l_token_logprob_fwd", dev,
+          (pz, _frames(tokens, (B, T, S), _I32, dev, "tokens"), _frames(in_len, (B,), _I32, dev, "in_len"),
+           _frames(logprob, (B, T, S), _F32, dev, "logprob"), _frames(entropy, (B, T), _F32, dev, "entropy"),
+           _frames(top_ids, (B, T, K), _I32, dev, "top_ids"), _frames(top_logprob, (B, T, K), _F32, dev, "top_logprob"),
+           _frames(stats, (B, T, 4), _F32, dev, "stats"), B, T, Cc, S, K, dt, wp, wn), stream)
     return logprob, entropy, top_ids, top_logprob, stats
 
 
 def w2l_token_logprob_bwd(z, stats, dz, tokens=None, dlogprob=None, dentropy=None, top_ids=None, dtop=None, in_len=None,
                           accumulate=False, stream=None):
     """dz[B,T,C] (accumulate: added to it) from the gradients of the forward call's outputs; those that are None are 0."""
-    B, T, Cc = _scores(z)
+    pz, B, T, Cc, dt, dev = _scores(z)
     if dlogprob is None:
         tokens = None
     if dtop is None:
         top_ids = None
-    S = 0 if tokens is None else tokens.shape[-1]
-    K = 0 if top_ids is None else top_ids.shape[-1]
-    f, n = torch.float32, torch.int32
-    ptr = (_p(z), _frames(stats, (B, T, 4), f, z, "stats"), _frames(tokens, (B, T, S), n, z, "tokens"),
-           _frames(dlogprob, (B, T, S), f, z, "dlogprob"), _frames(dentropy, (B, T), f, z, "dentropy"),
-           _frames(top_ids, (B, T, K), n, z, "top_ids"), _frames(dtop, (B, T, K), f, z, "dtop"),
-           _frames(in_len, (B,), n, z, "in_len"), _grad_of(dz, z))
-    dt, gt = _dt(z), _dt(dz)
-    _check(_on_device(z, stream, None, lambda wp, wn, st: raw.w2l_token_logprob_bwd(*ptr, B, T, Cc, S, K, dt, gt, int(bool(accumulate)), st)),
-           "w2l_token_logprob_bwd")
+    S, K = _last(tokens, "tokens"), _last(top_ids, "top_ids")
+    gt = _dt(dz)
+    _call(raw.w2l_token_logprob_bwd, "w2l_token_logprob_bwd", dev,
+          (pz, _frames(stats, (B, T, 4), _F32, dev, "stats"), _frames(tokens, (B, T, S), _I32, dev, "tokens"),
+           _frames(dlogprob, (B, T, S), _F32, dev, "dlogprob"), _frames(dentropy, (B, T), _F32, dev, "dentropy"),
+           _frames(top_ids, (B, T, K), _I32, dev, "top_ids"), _frames(dtop, (B, T, K), _F32, dev, "dtop"),
+           _frames(in_len, (B,), _I32, dev, "in_len"), _frames(dz, (B, T, Cc), dz.dtype, dev, "dz"), B, T, Cc, S, K, dt, gt,
+           1 if accumulate else 0), stream)
     return dz
 
 
@@ -330,18 +350,16 @@ def w2l_distill_workspace_bytes(B, Tp, Cc, K, dtype) -> int:
 def w2l_distill_fwd_bwd(z, t_ids, t_scores, frame_loss, loss=None, dz=None, in_len=None, weight=None, temperature=1.0,
                         grad_scale=1.0, accumulate=False, workspace=None, stream=None):
     """Loss of a student's scores z[B,T,C] against a teacher's best classes (t_ids, t_scores [B,T,K]) and its gradient dz."""
-    B, T, Cc = _scores(z)
-    K = t_ids.shape[-1]
-    f, n = torch.float32, torch.int32
-    ptr = (_p(z), _frames(t_ids, (B, T, K), n, z, "t_ids"), _frames(t_scores, (B, T, K), f, z, "t_scores"),
-           _frames(in_len, (B,), n, z, "in_len"), _frames(weight, (B, T), f, z, "weight"),
-           _frames(frame_loss, (B, T), f, z, "frame_loss"), _frames(loss, (B,), f, z, "loss"), _grad_of(dz, z))
-    dt = _dt(z)
+    pz, B, T, Cc, dt, dev = _scores(z)
+    K = _last(t_ids, "t_ids")
     gt = dt if dz is None else _dt(dz)
-    _check(_on_device(z, stream, workspace,
-                      lambda wp, wn, st: raw.w2l_distill_fwd_bwd(*ptr, B, T, Cc, K, float(temperature), float(grad_scale), dt, gt,
-                                                                 int(bool(accumulate)), wp, wn, st)),
-           "w2l_distill_fwd_bwd")
+    wp, wn = _scratch(workspace, dev)
+    _call(raw.w2l_distill_fwd_bwd, "w2l_distill_fwd_bwd", dev,
+          (pz, _frames(t_ids, (B, T, K), _I32, dev, "t_ids"), _frames(t_scores, (B, T, K), _F32, dev, "t_scores"),
+           _frames(in_len, (B,), _I32, dev, "in_len"), _frames(weight, (B, T), _F32, dev, "weight"),
+           _frames(frame_loss, (B, T), _F32, dev, "frame_loss"), _frames(loss, (B,), _F32, dev, "loss"),
+           None if dz is None else _frames(dz, (B, T, Cc), dz.dtype, dev, "dz"), B, T, Cc, K, temperature, grad_scale, dt, gt,
+           1 if accumulate else 0, wp, wn), stream)
     return frame_loss, loss, dz
 
 

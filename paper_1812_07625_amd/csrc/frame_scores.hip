@@ -8,12 +8,15 @@
 
 #include <math.h>
 
+#include <initializer_list>
+#include <type_traits>
+
 using namespace w2l;
 
 namespace {
 
 constexpr int MAX_CLASSES = 262144, MAX_ENTRIES = 64;
-constexpr int THREADS = 256, MAX_WAVES = 16, MAX_SLOTS = 16, MAX_GROUPS = 8;
+constexpr int THREADS = 256, MAX_WAVES = 16, MAX_SLOTS = 16, MAX_GROUPS = 16;
 constexpr float FAR = 16777216.f;  // 2^24: k m from here on has roundings that are no small shift
 constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
 enum Frame { LIVE = 0, PADDING = 1, BAD = 2 };
@@ -65,6 +68,7 @@ __device__ __forceinline__ float wave64(float v, F f)
     v = f(v, lane_of<0x143, 0xc>(v, f.none));  // row_bcast:31 into rows 2 and 3
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
+__device__ __forceinline__ float uniform(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
 // LDS written by some lanes of a wavefront (MULTI: a workgroup) and read by others after this
 template <bool MULTI>
 __device__ __forceinline__ void exchange()
@@ -230,25 +234,34 @@ __device__ __forceinline__ int below(unsigned long long mask)  // bits of the ma
     return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
 }
 
-// A threshold that at least `need` (<= 64) values of the wavefront reach, and not many more: each lane brings the largest of up to four
-// groups of its values (-inf: no group), and the threshold is bisected (over the order of the bits) until about `need` of these 256 reach it.
-// least: the smallest of the lanes' largest, which 64 values reach; most: the largest of all.
-__device__ __forceinline__ float wave_threshold(const float (&group)[4], float least, float most, int need)
+// Thresholds that at least need[j] (<= 64) values of the wavefront reach, and not many more: each lane brings the largest of up to four
+// groups of its values (-inf: no group), and a threshold is bisected (over the order of the bits) until about need[j] of these 256 reach
+// it.  least: the smallest of the lanes' largest, which 64 values reach; most: the largest of all.  Two thresholds are sought side by
+// side: a step is a chain of dependent instructions, of which a wavefront alone leaves most cycles empty.
+template <int J>
+__device__ __forceinline__ void wave_thresholds(const float (&group)[4], float least, float most, const int (&need)[J], float (&t)[J])
 {
-    unsigned lo = key_of(least), hi = key_of(most) + 1;
-    while (hi - lo > 1) {
-        const unsigned mid = lo + (hi - lo) / 2;
-        const float t = of_key(mid);
-        int n = 0;
+    unsigned lo[J], hi[J];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) n += __popcll(__ballot(group[j] >= t));
-        if (n >= need) {
-            lo = mid;
-            if (n <= need + 4) break;
-        } else
-            hi = mid;
+    for (int j = 0; j < J; ++j) { lo[j] = key_of(least); hi[j] = key_of(most) + 1; }
+    bool open = hi[0] - lo[0] > 1;
+    while (open) {
+        open = false;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const unsigned mid = lo[j] + (hi[j] - lo[j]) / 2;  // (lo itself once they are neighbours: nothing changes)
+            const float x = of_key(mid);
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += __popcll(__ballot(group[i] >= x));
+            if (n >= need[j]) lo[j] = mid;
+            else hi[j] = mid;
+            if (n >= need[j] && n <= need[j] + 4) hi[j] = mid + 1;  // near enough
+            open |= hi[j] - lo[j] > 1;
+        }
     }
-    return of_key(lo);
+#pragma unroll
+    for (int j = 0; j < J; ++j) t[j] = of_key(lo[j]);
 }
 
 // The wavefront's K largest classes, exactly, into list[0 .. K) in any order (fewer, if it holds fewer classes); returns how many.
@@ -385,7 +398,8 @@ __device__ __forceinline__ void far_sums(const T* __restrict__ z, size_t total, 
 // One row by a wavefront (!MULTI, four rows a workgroup), by a workgroup, or by G workgroups, which leave partial results (PARTS) for
 // token_join_k.  kscale = log2 e / temperature.
 template <typename T, int V, bool MULTI>
-__global__ __launch_bounds__(MULTI ? 1024 : 256) __attribute__((amdgpu_waves_per_eu(V > 8 ? 4 : V > 4 ? 5 : 6))) void token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
+__global__ __launch_bounds__(MULTI ? 1024 : 256) __attribute__((amdgpu_waves_per_eu(V > 16 ? 3 : V > 8 ? 4 : V > 4 ? 5 : 6))) void
+token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
                                                                                     const int* __restrict__ in_len, TokenOut o, Parts parts,
                                                                                     unsigned rows, unsigned Tp, int C, int G, float kscale)
 {
@@ -433,23 +447,23 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) __attribute__((amdgpu_waves_per
         if (o.K > 0) {
             const float least = wave64(lane_most, Min());
             // W wavefronts: K scores reach the least of thresholds that K / W of each one's reach, and the largest of those that K of one's do
-            t = wave_threshold(group, least, m, (o.K + W - 1) / W);
             if (MULTI) {
-                const float own = wave_threshold(group, least, t, o.K);
-                if (lane == 0) { red[1][wave] = t; red[2][wave] = own; }
+                float own[2];
+                wave_thresholds<2>(group, least, m, {(o.K + W - 1) / W, o.K}, own);
+                if (lane == 0) { red[1][wave] = own[0]; red[2][wave] = own[1]; }
+            } else {
+                float own[1];
+                wave_thresholds<1>(group, least, m, {o.K}, own);
+                t = own[0];
             }
         }
         if (MULTI) {
             if (lane == 0) red[0][wave] = m;
             if (threadIdx.x == 0) { count = 0; exact = 0; }
             __syncthreads();
-            float all = INFINITY, own = -INFINITY;
-            for (int w = 0; w < W; ++w) {
-                m = fmaxf(m, red[0][w]);
-                all = fminf(all, red[1][w]);
-                own = fmaxf(own, red[2][w]);
-            }
-            if (o.K > 0) t = fmaxf(all, own);
+            const int w = lane & 15;
+            m = uniform(row16(w < W ? red[0][w] : -INFINITY, Max()));
+            if (o.K > 0) t = uniform(fmaxf(row16(w < W ? red[1][w] : INFINITY, Min()), row16(w < W ? red[2][w] : -INFINITY, Max())));
         }
         // exp(x - m) as 2^(k x - M), M = k m rounded: what the rounding moves, `shift`, is taken out of the sums at the end
         const float m0 = m == -INFINITY ? 0.f : m, M = m0 * kscale, shift = __builtin_fmaf(m0, kscale, -M);
@@ -517,8 +531,9 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) __attribute__((amdgpu_waves_per
             if (lane == 0) { red[0][wave] = s; red[1][wave] = u; }
             n = count;
             __syncthreads();
-            s = u = 0.f;
-            for (int w = 0; w < W; ++w) { s += red[0][w]; u += red[1][w]; }
+            const int w = lane & 15;
+            s = uniform(row16(w < W ? red[0][w] : 0.f, Sum()));
+            u = uniform(row16(w < W ? red[1][w] : 0.f, Sum()));
         }
         u *= LN2;
         if (o.K > 0 && s == s) {
@@ -926,10 +941,11 @@ __device__ __forceinline__ float frame_loss_of(const Teacher& te, const int (&c)
     return loss;
 }
 
-// sums: (m or -inf, s, ., .) of every row's G workgroups where a row is too long for the registers of one, or rows are few; else NULL
+// G > 1, where a row is too long for the registers of a workgroup, or rows are few: sums has (m or -inf, s, ., .) of each of the `parts` that
+// token_rows_k read it in; else it is NULL
 template <typename T, typename D, int V, bool MULTI>
 __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __restrict__ z, Teacher te, const int* __restrict__ in_len,
-                                                                                      const float4* __restrict__ sums, float* __restrict__ frame_loss,
+                                                                                      const float4* __restrict__ sums, int parts, float* __restrict__ frame_loss,
                                                                                       D* __restrict__ dz, unsigned rows, unsigned Tp, int C, int G,
                                                                                       int accumulate)
 {
@@ -963,11 +979,9 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
         }
         float m = -INFINITY, s = 0.f;
         if (MULTI && sums) {
-            for (int i = 0; i < G; ++i) m = fmaxf(m, sums[(size_t)r * G + i].x);
-            for (int i = 0; i < G; ++i) {
-                const float4 a = sums[(size_t)r * G + i];
-                if (a.y != 0.f) s += a.y * expf((a.x - m) * te.inv_tau);
-            }
+            const float4 a = lane < parts ? sums[(size_t)r * parts + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+            m = wave64(a.x, Max());
+            s = wave64(a.y != 0.f ? a.y * expf((a.x - m) * te.inv_tau) : 0.f, Sum());
             m = m == -INFINITY ? 0.f : m;
         } else {
 #pragma unroll
@@ -980,7 +994,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
             if (MULTI) {
                 if (lane == 0) red[0][wave] = m;
                 __syncthreads();
-                for (int i = 0; i < W; ++i) m = fmaxf(m, red[0][i]);
+                m = uniform(row16((lane & 15) < W ? red[0][lane & 15] : -INFINITY, Max()));
             }
             m = m == -INFINITY ? 0.f : m;
             opaque(data);
@@ -1002,8 +1016,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
             if (MULTI) {
                 if (lane == 0) red[1][wave] = s;
                 __syncthreads();
-                s = 0.f;
-                for (int i = 0; i < W; ++i) s += red[1][i];
+                s = uniform(row16((lane & 15) < W ? red[1][lane & 15] : 0.f, Sum()));
             }
         }
         bool live;
@@ -1149,18 +1162,55 @@ bool shape_ok(int B, int Tp, int C, int S, int K)
 }
 bool grad_dtype_ok(int z_dtype, int dz_dtype) { return valid_dtype(dz_dtype) && (dz_dtype == W2L_F32 || z_dtype == W2L_BF16); }
 
-// How the rows are dealt out: sixteen lanes a row (W = 0), or W wavefronts of each of G workgroups, V slots of registers.
+// How the rows are dealt out: sixteen lanes a row of up to 64 classes (W = 0), or W wavefronts of each of G workgroups, V slots of
+// registers each.
 struct Plan {
     int W, G, V;
 };
-Plan plan_of(long long rows, int C, int dtype)
+int tight(int per, std::initializer_list<int> sizes)
+{
+    for (int v : sizes)
+        if (per <= v) return v;
+    return 0;
+}
+int slots_of(int C, int dtype)
+{
+    const int N = dtype == W2L_BF16 ? 8 : 4, most = C % N ? C + 2 * (N - 1) : C;  // wherever in a vector a row begins
+    return (most + 64 * N - 1) / (64 * N);
+}
+// Log-probabilities, entropy, best classes.  What a row costs beside its values -- a threshold, a list, ranks: 700 instructions -- it costs every
+// wavefront, so a row has few: one up to 24 slots (3000 rows of 20 slots: 22 us; two wavefronts 28, five 38; one row: 9 us either way),
+// four to a workgroup beyond.  Workgroups of four that join beat one of up to sixteen that waits at its barriers (400 rows of 137
+// slots: 28 us against 33; one row: 14 against 15), and one row in more of them gains little (256 slots: 13.8 us in 8, 14.9 in 4).
+Plan plan_tokens(int C, int dtype)
 {
     if (C <= 64) return {0, 1, C <= 32 ? 2 : 4};
-    const int N = dtype == W2L_BF16 ? 8 : 4, most = C % N ? C + 2 * (N - 1) : C, slots = (most + 64 * N - 1) / (64 * N);  // most: wherever in a vector a row begins
-    long long P = (slots + MAX_SLOTS - 1) / MAX_SLOTS;
-    while (rows * P < 2048 && P * 4 <= slots && P * 2 <= MAX_WAVES) P *= 2;  // two wavefronts a SIMD, two slots each
-    const int W = P < MAX_WAVES ? (int)P : MAX_WAVES, G = (int)((P + W - 1) / W), per = (slots + W * G - 1) / (W * G);
-    return {W, G, per <= 2 ? 2 : per <= 4 ? 4 : per <= 8 ? 8 : per <= 12 ? 12 : 16};
+    const int slots = slots_of(C, dtype);
+    if (slots <= 24) return {1, 1, tight(slots, {2, 4, 6, 8, 10, 12, 14, 16, 20, 24})};
+    const int P = (slots + 15) / 16, W = P <= 4 ? P : slots <= 512 ? 4 : 8, G = (P + W - 1) / W;
+    return {W, G, tight((slots + W * G - 1) / (W * G), {10, 12, 14, 16})};
+}
+// Distillation.  The values are most of the work, and the gradient is written: a row has wavefronts enough to fill the chip (one row of 20
+// slots: 8 us in five, 9.4 in three; 3000: 38 us in one, 43 in five).  More workgroups a row read it twice, so only few rows or rows beyond
+// the registers of sixteen wavefronts have them (one row of 137 slots: 12 us against 17 in one workgroup; 400: 45 against 40).
+Plan plan_distill(long long rows, int C, int dtype)
+{
+    if (C <= 64) return {0, 1, C <= 32 ? 2 : 4};
+    const int slots = slots_of(C, dtype);
+    if (slots <= 2 || (slots <= 24 && rows >= 2048)) return {1, 1, tight(slots, {2, 4, 6, 8, 10, 12, 14, 16, 20, 24})};
+    int W, G = 1;
+    if (slots <= 64) {
+        W = (slots + 7) / 8;
+        while (rows * W < 2048 && W * 4 <= slots && W * 2 <= MAX_WAVES) W *= 2;
+        if (W < 2) W = 2;
+    } else if (slots <= MAX_WAVES * MAX_SLOTS && rows >= 128)
+        W = (slots + 15) / 16;
+    else {
+        W = 8;
+        G = (slots + 31) / 32;
+        if (G > MAX_GROUPS) G = MAX_GROUPS;
+    }
+    return {W, G, tight((slots + W * G - 1) / (W * G), {2, 4, 8, 12, 16})};
 }
 unsigned grid_of(long long groups) { return (unsigned)(groups < (1 << 20) ? groups : 1 << 20); }
 size_t sums_bytes(long long rows, const Plan& p) { return p.G > 1 ? round_up((size_t)rows * p.G * sizeof(float4), 256) : 0; }
@@ -1169,16 +1219,25 @@ bool workspace_ok(const void* ws, size_t have, size_t need)
     return need == 0 || (ws && have >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0);
 }
 
-template <typename T, int V>
-void launch_rows(const Plan& p, hipStream_t st, const void* z, const int* tokens, const int* in_len, const TokenOut& o, const Parts& parts,
+// f(std::integral_constant<int, V>) for the V of a plan, one of Vs; false if it is none of them
+template <int... Vs, typename F>
+bool with_slots(int V, F f)
+{
+    return ((V == Vs && (f(std::integral_constant<int, Vs>()), true)) || ...);
+}
+template <typename T>
+bool launch_rows(const Plan& p, hipStream_t st, const void* z, const int* tokens, const int* in_len, const TokenOut& o, const Parts& parts,
                  unsigned rows, unsigned Tp, int C, float kscale)
 {
-    if (p.W > 1 || p.G > 1)
-        hipLaunchKernelGGL((token_rows_k<T, V, true>), dim3(grid_of((long long)rows * p.G)), dim3(64 * p.W), lds_of(p.W, true), st, (const T*)z, tokens, in_len, o,
-                           parts, rows, Tp, C, p.G, kscale);
-    else
-        hipLaunchKernelGGL((token_rows_k<T, V, false>), dim3(grid_of(((long long)rows + 3) / 4)), dim3(256), lds_of(4, false), st, (const T*)z, tokens, in_len, o,
-                           parts, rows, Tp, C, 1, kscale);
+    if (p.W > 1)
+        return with_slots<10, 12, 14, 16>(p.V, [&](auto v) {
+            hipLaunchKernelGGL((token_rows_k<T, decltype(v)::value, true>), dim3(grid_of((long long)rows * p.G)), dim3(64 * p.W), lds_of(p.W, true), st,
+                               (const T*)z, tokens, in_len, o, parts, rows, Tp, C, p.G, kscale);
+        });
+    return with_slots<2, 4, 6, 8, 10, 12, 14, 16, 20, 24>(p.V, [&](auto v) {
+            hipLaunchKernelGGL((token_rows_k<T, decltype(v)::value, false>), dim3(grid_of(((long long)rows + 3) / 4)), dim3(256), lds_of(4, false), st,
+                               (const T*)z, tokens, in_len, o, parts, rows, Tp, C, 1, kscale);
+    });
 }
 template <typename T>
 int launch_tokens(const Plan& p, hipStream_t st, const void* z, const int* tokens, const int* in_len, const TokenOut& o, void* ws, unsigned rows,
@@ -1189,16 +1248,10 @@ int launch_tokens(const Plan& p, hipStream_t st, const void* z, const int* token
         const dim3 g(grid_of(((long long)rows + 15) / 16)), b(THREADS);
         if (p.V == 2) hipLaunchKernelGGL((token_narrow_k<T, 2>), g, b, 0, st, (const T*)z, tokens, in_len, o, rows, Tp, C);
         else hipLaunchKernelGGL((token_narrow_k<T, 4>), g, b, 0, st, (const T*)z, tokens, in_len, o, rows, Tp, C);
-    } else
-        switch (p.V) {
-            case 2: launch_rows<T, 2>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale); break;
-            case 4: launch_rows<T, 4>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale); break;
-            case 8: launch_rows<T, 8>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale); break;
-            case 12: launch_rows<T, 12>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale); break;
-            default: launch_rows<T, 16>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale);
-        }
+    } else if (!launch_rows<T>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale))
+        return W2L_ERR_SHAPE;
     if (int rc = launch_status()) return rc;
-    if (p.G == 1 || !join) return W2L_OK;
+    if (p.G == 1 || !join) return W2L_OK;  // (the partial sums of a distillation are not joined)
     hipLaunchKernelGGL(token_join_k<T>, dim3(grid_of(rows)), dim3(THREADS), 0, st, (const T*)z, tokens, in_len, o, parts, rows, Tp, C, p.G);
     return launch_status();
 }
@@ -1223,17 +1276,6 @@ void launch_bwd(hipStream_t st, const void* z, const float* stats, const int* to
                        dlogprob, dentropy, top_ids, dtop, in_len, (D*)dz, rows, Tp, C, S, K, P, accumulate);
 }
 
-template <typename T, typename D, int V>
-void launch_distill_rows(const Plan& p, hipStream_t st, const void* z, const Teacher& te, const int* in_len, const float4* sums, float* frame_loss,
-                         void* dz, unsigned rows, unsigned Tp, int C, int accumulate)
-{
-    if (p.W > 1 || p.G > 1)
-        hipLaunchKernelGGL((distill_rows_k<T, D, V, true>), dim3(grid_of((long long)rows * p.G)), dim3(64 * p.W), 0, st, (const T*)z, te, in_len, sums,
-                           frame_loss, (D*)dz, rows, Tp, C, p.G, accumulate);
-    else
-        hipLaunchKernelGGL((distill_rows_k<T, D, V, false>), dim3(grid_of(((long long)rows + 3) / 4)), dim3(256), 0, st, (const T*)z, te, in_len, sums,
-                           frame_loss, (D*)dz, rows, Tp, C, 1, accumulate);
-}
 template <typename T, typename D>
 int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& te, const int* in_len, float* frame_loss, void* dz, void* ws,
                    unsigned rows, unsigned Tp, int C, int accumulate)
@@ -1250,18 +1292,26 @@ int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& 
         return launch_status();
     }
     const float4* sums = nullptr;
+    int parts = 1;
     if (p.G > 1) {
         const TokenOut none{nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0};
-        if (int rc = launch_tokens<T>(p, st, z, nullptr, in_len, none, ws, rows, Tp, C, te.kscale, false)) return rc;
+        const Plan first = plan_tokens(C, sizeof(T) == 2 ? W2L_BF16 : W2L_F32);  // (G > 1 as well: more than 64 slots)
+        parts = first.G;
+        if (int rc = launch_tokens<T>(first, st, z, nullptr, in_len, none, ws, rows, Tp, C, te.kscale, false)) return rc;
         sums = (const float4*)ws;
     }
-    switch (p.V) {
-        case 2: launch_distill_rows<T, D, 2>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate); break;
-        case 4: launch_distill_rows<T, D, 4>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate); break;
-        case 8: launch_distill_rows<T, D, 8>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate); break;
-        case 12: launch_distill_rows<T, D, 12>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate); break;
-        default: launch_distill_rows<T, D, 16>(p, st, z, te, in_len, sums, frame_loss, dz, rows, Tp, C, accumulate);
-    }
+    bool known;
+    if (p.W > 1)
+        known = with_slots<2, 4, 8, 12, 16>(p.V, [&](auto v) {
+            hipLaunchKernelGGL((distill_rows_k<T, D, decltype(v)::value, true>), dim3(grid_of((long long)rows * p.G)), dim3(64 * p.W), 0, st, (const T*)z, te,
+                               in_len, sums, parts, frame_loss, (D*)dz, rows, Tp, C, p.G, accumulate);
+        });
+    else
+        known = with_slots<2, 4, 6, 8, 10, 12, 14, 16, 20, 24>(p.V, [&](auto v) {
+            hipLaunchKernelGGL((distill_rows_k<T, D, decltype(v)::value, false>), dim3(grid_of(((long long)rows + 3) / 4)), dim3(256), 0, st, (const T*)z, te,
+                               in_len, sums, 1, frame_loss, (D*)dz, rows, Tp, C, 1, accumulate);
+        });
+    if (!known) return W2L_ERR_SHAPE;
     return launch_status();
 }
 
@@ -1271,7 +1321,7 @@ extern "C" size_t w2l_token_logprob_workspace_bytes(int B, int Tp, int C, int K,
 {
     if (!shape_ok(B, Tp, C, 0, K) || !valid_dtype(z_dtype)) return 0;
     const long long rows = (long long)B * Tp;
-    const Plan p = plan_of(rows, C, z_dtype);
+    const Plan p = plan_tokens(C, z_dtype);
     return p.G > 1 ? sums_bytes(rows, p) + (size_t)rows * p.G * K * sizeof(ranked_t) : 0;
 }
 
@@ -1287,7 +1337,7 @@ extern "C" int w2l_token_logprob_fwd(const void* z, const int* tokens, const int
         return W2L_ERR_ALIGN;
     if (!workspace_ok(workspace, ws_bytes, w2l_token_logprob_workspace_bytes(B, Tp, C, K, z_dtype))) return W2L_ERR_WORKSPACE;
     const unsigned rows = (unsigned)B * (unsigned)Tp;
-    const Plan p = plan_of(rows, C, z_dtype);
+    const Plan p = plan_tokens(C, z_dtype);
     const TokenOut o{logprob, entropy, top_ids, top_logprob, stats, S, K};
     return z_dtype == W2L_BF16 ? launch_tokens<bf16_t>(p, (hipStream_t)stream, z, tokens, in_len, o, workspace, rows, (unsigned)Tp, C, LOG2E, true)
                                : launch_tokens<float>(p, (hipStream_t)stream, z, tokens, in_len, o, workspace, rows, (unsigned)Tp, C, LOG2E, true);
@@ -1316,7 +1366,8 @@ extern "C" int w2l_token_logprob_bwd(const void* z, const float* stats, const in
 extern "C" size_t w2l_distill_workspace_bytes(int B, int Tp, int C, int K, int z_dtype)
 {
     if (!shape_ok(B, Tp, C, 0, K) || !valid_dtype(z_dtype)) return 0;
-    return sums_bytes((long long)B * Tp, plan_of((long long)B * Tp, C, z_dtype));
+    const long long rows = (long long)B * Tp;
+    return plan_distill(rows, C, z_dtype).G > 1 ? sums_bytes(rows, plan_tokens(C, z_dtype)) : 0;
 }
 
 extern "C" int w2l_distill_fwd_bwd(const void* z, const int* t_ids, const float* t_scores, const int* in_len, const float* weight,
@@ -1332,7 +1383,7 @@ extern "C" int w2l_distill_fwd_bwd(const void* z, const int* t_ids, const float*
         return W2L_ERR_ALIGN;
     if (!workspace_ok(workspace, ws_bytes, w2l_distill_workspace_bytes(B, Tp, C, K, z_dtype))) return W2L_ERR_WORKSPACE;
     const unsigned rows = (unsigned)B * (unsigned)Tp;
-    const Plan p = plan_of(rows, C, z_dtype);
+    const Plan p = plan_distill(rows, C, z_dtype);
     const Teacher te{t_ids, t_scores, weight, K, temperature, 1.f / temperature, (float)(1.4426950408889634 / temperature), grad_scale};
     int rc;
 #define W2L_DISTILL(T_, G_) rc = launch_distill<T_, G_>(p, (hipStream_t)stream, z, te, in_len, frame_loss, dz, workspace, rows, (unsigned)Tp, C, accumulate)
