@@ -16,19 +16,29 @@ using namespace w2l;
 namespace {
 
 constexpr int MAX_CLASSES = 262144, MAX_ENTRIES = 64;
-constexpr int THREADS = 256, MAX_WAVES = 16, MAX_SLOTS = 16, MAX_GROUPS = 16;
+constexpr int THREADS = 256, MAX_WAVES = 16, MAX_SLOTS = 16, MAX_GROUPS = 16, NARROW = 256;
 constexpr float FAR = 16777216.f;  // 2^24: k m from here on has roundings that are no small shift
 constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
 enum Frame { LIVE = 0, PADDING = 1, BAD = 2 };
 
-__device__ __forceinline__ Frame frame_of(const int* __restrict__ in_len, unsigned r, unsigned Tp)
+// Rows of utterances of Tp frames: r / Tp for r < 2^31 as a product, a fifth of the division's instructions
+struct Frames {
+    const int* in_len;
+    unsigned rows, Tp, mul, shift;
+};
+Frames frames_of(const int* in_len, int B, int Tp)
 {
-    if (!in_len) return LIVE;
-    const unsigned b = r / Tp;
-    const int n = in_len[b];
-    return n < 0 || n > (int)Tp ? BAD : (int)(r - b * Tp) < n ? LIVE : PADDING;
+    unsigned bits = 0;
+    while ((1ull << bits) < (unsigned)Tp) ++bits;  // 2^bits >= Tp: mul = 2^(31 + bits) / Tp rounded up is exact for 31 bits, and fits 32
+    return {in_len, (unsigned)B * (unsigned)Tp, (unsigned)Tp, (unsigned)(((1ull << (31 + bits)) + Tp - 1) / (unsigned)Tp), bits};
 }
-
+__device__ __forceinline__ Frame frame_of(const Frames& fr, unsigned r)
+{
+    if (!fr.in_len) return LIVE;
+    const unsigned b = (unsigned)((unsigned long long)r * fr.mul >> 31 >> fr.shift);
+    const int n = fr.in_len[b];
+    return n < 0 || n > (int)fr.Tp ? BAD : (int)(r - b * fr.Tp) < n ? LIVE : PADDING;
+}
 
 // ---- reductions over lanes ----------------------------------------------------------------------------
 // (lanes that receive nothing combine with what changes nothing: then the move becomes an operand of the operation)
@@ -195,7 +205,10 @@ __device__ __forceinline__ void load_row(uint4 (&q)[V], const T* __restrict__ z,
         q[v] = *reinterpret_cast<const uint4*>(at + (unsigned)(n < whole ? n : whole - 1) * 16u);
     }
     uint4 tail = make_uint4(0, 0, 0, 0);
-    if (whole < row.nv) tail = tail_vector(z, total, row, whole);
+    if (whole < row.nv) {
+        tail = tail_vector(z, total, row, whole);
+        asm volatile("" : "+v"(tail.x), "+v"(tail.y), "+v"(tail.z), "+v"(tail.w));  // waited for here, not wherever its registers are used again
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int n = n0 + v * step, slot = n >> 6;
@@ -321,7 +334,7 @@ __device__ __forceinline__ void rank_list(const ranked_t* list, int n, int K, in
     if (MULTI && (thread & ~63) >= n) return;  // (whole wavefronts)
     const ranked_t a = thread < n ? list[thread] : 0;
     int before = 0;
-#pragma unroll 2
+#pragma unroll 4
     for (int j = 0; j < n; j += 2) {
         const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(list + j);
         before += w.x > a;
@@ -331,7 +344,7 @@ __device__ __forceinline__ void rank_list(const ranked_t* list, int n, int K, in
     if (!MULTI && n > 64) {  // the entries beyond one a lane: each against all lanes'
         const ranked_t b = thread + 64 < n ? list[thread + 64] : 0;
         for (int j = 0; j < n - 64; ++j) {
-            const ranked_t w = list[64 + j];
+            const ranked_t w = (ranked_t)(unsigned)__builtin_amdgcn_readlane((int)(b >> 32), j) << 32 | (unsigned)__builtin_amdgcn_readlane((int)b, j);
             const int k = __popcll(__ballot(a > w)) + __popcll(__ballot(b > w));
             if (thread == 0 && k < K) out(k, w);
         }
@@ -398,11 +411,12 @@ __device__ __forceinline__ void far_sums(const T* __restrict__ z, size_t total, 
 // One row by a wavefront (!MULTI, four rows a workgroup), by a workgroup, or by G workgroups, which leave partial results (PARTS) for
 // token_join_k.  kscale = log2 e / temperature.
 template <typename T, int V, bool MULTI>
-__global__ __launch_bounds__(MULTI ? 512 : 256) __attribute__((amdgpu_waves_per_eu(V > 16 ? 2 : V > 8 ? 3 : 4))) void
+__global__ __launch_bounds__(MULTI ? 512 : 256) __attribute__((amdgpu_waves_per_eu(V > 20 ? 2 : V > 12 ? 3 : V > 8 ? 4 : V > 4 ? 5 : 6))) void
 token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
-                                                                                    const int* __restrict__ in_len, TokenOut o, Parts parts,
-                                                                                    unsigned rows, unsigned Tp, int C, int G, float kscale)
+                                                                                    Frames fr, TokenOut o, Parts parts,
+                                                                                    int C, int groups, float kscale)
 {
+    const int G = MULTI ? groups : 1;
     constexpr int N = LANE_VALUES<T>;
     constexpr int ROWS = MULTI ? 1 : 4;
     extern __shared__ uint4 lds[];
@@ -413,19 +427,19 @@ token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
     int* const held_n = reinterpret_cast<int*>(lds + (MULTI ? W : 4) * HELD) + wave * HELD;
     const int room = MULTI ? W * 64 : LIST;  // of the list: a workgroup's, or each wavefront's
     ranked_t* const list = reinterpret_cast<ranked_t*>(lds + (MULTI ? W : 4) * (HELD + HELD / 4)) + (MULTI ? 0 : wave * (LIST + 2));
-    const size_t total = (size_t)rows * C;
+    const size_t total = (size_t)fr.rows * C;
     const int thread = MULTI ? (int)threadIdx.x : lane;
-    const unsigned tasks = rows * G, stride = gridDim.x * ROWS;
+    const unsigned tasks = fr.rows * G, stride = gridDim.x * ROWS;
     for (unsigned task = blockIdx.x * ROWS + (MULTI ? 0 : wave); task < tasks; task += stride) {
         const unsigned r = task / G;
         const int g = task - r * G;
-        const Frame f = frame_of(in_len, r, Tp);
+        const Frame f = frame_of(fr, r);
         if (f != LIVE) {
             if (G == 1) write_absent(o, r, f, thread, MULTI ? blockDim.x : 64);
             continue;
         }
         const Row row = row_at<T>(r, C);
-        const int P = W * G, step = P * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane;
+        const int step = W * G * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane;
         uint4 q[V];
         load_row(q, z, total, row, step, n0, C);
         int token = -1;
@@ -440,7 +454,10 @@ token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
             float x[N];
             unpack(q[v], x);
             most[v] = largest(x);
-            group[v * 4 / (V > 4 ? V : 4)] = fmaxf(group[v * 4 / (V > 4 ? V : 4)], most[v]);
+            if (V > 2) group[v * 4 / (V > 4 ? V : 4)] = fmaxf(group[v * 4 / (V > 4 ? V : 4)], most[v]);
+            else  // one or two vectors: by element
+#pragma unroll
+                for (int e = 0; e < N; ++e) group[e & 3] = fmaxf(group[e & 3], x[e]);
         }
         const float lane_most = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
         float m = wave64(lane_most, Max()), t = INFINITY;
@@ -452,8 +469,8 @@ token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
                 wave_thresholds<2>(group, least, m, {(o.K + W - 1) / W, o.K}, own);
                 if (lane == 0) { red[1][wave] = own[0]; red[2][wave] = own[1]; }
             } else {
-                float own[1];
-                wave_thresholds<1>(group, least, m, {o.K}, own);
+                float own[1] = {-INFINITY};  // a row of few more classes than are wanted is ranked whole
+                if (C > LIST || o.K < C / 4) wave_thresholds<1>(group, least, m, {o.K}, own);
                 t = own[0];
             }
         }
@@ -575,14 +592,14 @@ token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
 // The rows that G workgroups left in parts, a workgroup each.  Of the G sorted lists, entries below the largest K-th of a list or below the
 // smallest ceil(K / G)-th are not among the K best; about 1.5 K pass.
 template <typename T>
-__global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z, const int* __restrict__ tokens, const int* __restrict__ in_len,
-                                                        TokenOut o, Parts parts, unsigned rows, unsigned Tp, int C, int G)
+__global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z, const int* __restrict__ tokens, Frames fr,
+                                                        TokenOut o, Parts parts, int C, int G)
 {
     __shared__ ranked_t list[MAX_GROUPS * MAX_ENTRIES];
     __shared__ int count;
-    for (unsigned r = blockIdx.x; r < rows; r += gridDim.x) {
+    for (unsigned r = blockIdx.x; r < fr.rows; r += gridDim.x) {
         const int tid = threadIdx.x;
-        const Frame f = frame_of(in_len, r, Tp);
+        const Frame f = frame_of(fr, r);
         const int lane = tid & 63;
         float m = -INFINITY, s = 0.f, u = 0.f;
         if (f == LIVE) {
@@ -636,13 +653,13 @@ __global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z,
 
 // Rows of up to 16 * NV classes, sixteen lanes each.  The K best are taken one after the other: largest score, then lowest class.
 template <typename T, int NV>
-__global__ __launch_bounds__(THREADS) void token_narrow_k(const T* __restrict__ z, const int* __restrict__ tokens, const int* __restrict__ in_len,
-                                                          TokenOut o, unsigned rows, unsigned Tp, int C)
+__global__ __launch_bounds__(THREADS) void token_narrow_k(const T* __restrict__ z, const int* __restrict__ tokens, Frames fr,
+                                                          TokenOut o, int C)
 {
     const int l = threadIdx.x & 15;
     const unsigned stride = gridDim.x * 16;
-    for (unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4); r < rows; r += stride) {
-        const Frame f = frame_of(in_len, r, Tp);
+    for (unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4); r < fr.rows; r += stride) {
+        const Frame f = frame_of(fr, r);
         if (f != LIVE) {
             write_absent(o, r, f, l, 16);
             continue;
@@ -783,13 +800,13 @@ template <typename T, typename G, int V>
 __global__ __launch_bounds__(THREADS) void token_bwd_rows_k(const T* __restrict__ z, const float* __restrict__ stats, const int* __restrict__ tokens,
                                                             const float* __restrict__ dlogprob, const float* __restrict__ dentropy,
                                                             const int* __restrict__ top_ids, const float* __restrict__ dtop,
-                                                            const int* __restrict__ in_len, G* __restrict__ dz, unsigned rows, unsigned Tp, int C, int S,
+                                                            Frames fr, G* __restrict__ dz, int C, int S,
                                                             int K, int P, int how)
 {
     constexpr int N = LANE_VALUES<T>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const size_t total = (size_t)rows * C;
-    const unsigned tasks = rows * P;
+    const size_t total = (size_t)fr.rows * C;
+    const unsigned tasks = fr.rows * P;
     for (unsigned task = blockIdx.x * 4 + wave; task < tasks; task += gridDim.x * 4) {
         const unsigned r = task / P;
         const int p = task - r * P;
@@ -797,7 +814,7 @@ __global__ __launch_bounds__(THREADS) void token_bwd_rows_k(const T* __restrict_
         const int slots = (row.nv + 63) / 64, first = p * V;
         if (first >= slots) continue;
         const float4 q = reinterpret_cast<const float4*>(stats)[r];
-        if (frame_of(in_len, r, Tp) != LIVE || !(fabsf(q.y) < INFINITY)) {
+        if (frame_of(fr, r) != LIVE || !(fabsf(q.y) < INFINITY)) {
             if (!(how & ADD)) clear_row<T>(dz, row, V, 64, first * 64 + lane, C, how);
             continue;
         }
@@ -859,15 +876,15 @@ template <typename T, typename G, int NV>
 __global__ __launch_bounds__(THREADS) void token_bwd_narrow_k(const T* __restrict__ z, const float* __restrict__ stats, const int* __restrict__ tokens,
                                                               const float* __restrict__ dlogprob, const float* __restrict__ dentropy,
                                                               const int* __restrict__ top_ids, const float* __restrict__ dtop,
-                                                              const int* __restrict__ in_len, G* __restrict__ dz, unsigned rows, unsigned Tp, int C, int S,
+                                                              Frames fr, G* __restrict__ dz, int C, int S,
                                                               int K, int accumulate)
 {
     const int l = threadIdx.x & 15;
     const unsigned stride = gridDim.x * 16;
-    for (unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4); r < rows; r += stride) {
+    for (unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4); r < fr.rows; r += stride) {
         const size_t i0 = (size_t)r * C;
         const float4 st = reinterpret_cast<const float4*>(stats)[r];
-        const bool live = frame_of(in_len, r, Tp) == LIVE && fabsf(st.y) < INFINITY;
+        const bool live = frame_of(fr, r) == LIVE && fabsf(st.y) < INFINITY;
         if (!live && accumulate) continue;
         float direct[NV], sum = 0.f;
 #pragma unroll
@@ -949,22 +966,23 @@ __device__ __forceinline__ float frame_loss_of(const Teacher& te, const int (&c)
 // G > 1, where a row is too long for the registers of a workgroup, or rows are few: sums has (m or -inf, s, ., .) of each of the `parts` that
 // token_rows_k read it in; else it is NULL
 template <typename T, typename D, int V, bool MULTI>
-__global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __restrict__ z, Teacher te, const int* __restrict__ in_len,
+__global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __restrict__ z, Teacher te, Frames fr,
                                                                                       const float4* __restrict__ sums, int parts, float* __restrict__ frame_loss,
-                                                                                      D* __restrict__ dz, unsigned rows, unsigned Tp, int C, int G,
+                                                                                      D* __restrict__ dz, int C, int groups,
                                                                                       int how)
 {
+    const int G = MULTI ? groups : 1;
     constexpr int N = LANE_VALUES<T>;
     constexpr int ROWS = MULTI ? 1 : 4;
     __shared__ float red[2][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = MULTI ? blockDim.x >> 6 : 1;
-    const size_t total = (size_t)rows * C;
-    const unsigned tasks = rows * G, stride = gridDim.x * ROWS;
+    const size_t total = (size_t)fr.rows * C;
+    const unsigned tasks = fr.rows * G, stride = gridDim.x * ROWS;
     for (unsigned task = blockIdx.x * ROWS + (MULTI ? 0 : wave); task < tasks; task += stride) {
         const unsigned r = task / G;
         const int g = task - r * G;
         const bool first = g == 0 && (MULTI ? threadIdx.x : lane) == 0;
-        const Frame f = frame_of(in_len, r, Tp);
+        const Frame f = frame_of(fr, r);
         const Row row = row_at<T>(r, C);
         const int P = W * G, step = P * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane;
         const float w = f != LIVE ? 0.f : te.weight ? te.weight[r] : 1.f;
@@ -1071,15 +1089,15 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
 }
 
 template <typename T, typename D, int NV, int R>
-__global__ __launch_bounds__(THREADS) void distill_narrow_k(const T* __restrict__ z, Teacher te, const int* __restrict__ in_len,
-                                                            float* __restrict__ frame_loss, D* __restrict__ dz, unsigned rows, unsigned Tp, int C,
+__global__ __launch_bounds__(THREADS) void distill_narrow_k(const T* __restrict__ z, Teacher te, Frames fr,
+                                                            float* __restrict__ frame_loss, D* __restrict__ dz, int C,
                                                             int accumulate)
 {
     const int l = threadIdx.x & 15;
     const unsigned stride = gridDim.x * 16;
-    for (unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4); r < rows; r += stride) {
+    for (unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4); r < fr.rows; r += stride) {
         const size_t i0 = (size_t)r * C;
-        const Frame f = frame_of(in_len, r, Tp);
+        const Frame f = frame_of(fr, r);
         const float w = f != LIVE ? 0.f : te.weight ? te.weight[r] : 1.f;
         float loss = f == BAD ? NAN : 0.f, g[NV];
         bool live = false;
@@ -1178,6 +1196,8 @@ int tight(int per, std::initializer_list<int> sizes)
         if (per <= v) return v;
     return 0;
 }
+// values of a lane where sixteen lanes hold a row; 0: the row has a wavefront or more
+int narrow_of(int C) { return C <= NARROW ? tight((C + 15) / 16, {2, 4, 8, 16}) : 0; }
 int slots_of(int C, int dtype)
 {
     const int N = dtype == W2L_BF16 ? 8 : 4, most = C % N ? C + 2 * (N - 1) : C;  // wherever in a vector a row begins
@@ -1187,9 +1207,10 @@ int slots_of(int C, int dtype)
 // wavefront, so a row has few: one up to 24 slots (3000 rows of 20 slots: 22 us; two wavefronts 28, five 38; one row: 9 us either way),
 // four to a workgroup beyond.  Workgroups of four that join beat one of up to sixteen that waits at its barriers (400 rows of 137
 // slots: 28 us against 33; one row: 14 against 15), and one row in more of them gains little (256 slots: 13.8 us in 8, 14.9 in 4).
-Plan plan_tokens(int C, int dtype)
+Plan plan_tokens(int C, int K, int dtype)
 {
-    if (C <= 64) return {0, 1, C <= 32 ? 2 : 4};
+    if (C <= 64 || K <= 24)  // (the narrow kernel takes a round for each: 24000 rows of 200: 25 us at K = 16, 78 at 64, where a wavefront a row takes 48)
+        if (const int nv = narrow_of(C)) return {0, 1, nv};
     const int slots = slots_of(C, dtype);
     if (slots <= 24) return {1, 1, tight(slots, {2, 4, 6, 8, 10, 12, 14, 16, 20, 24})};
     const int P = (slots + 15) / 16, W = P <= 4 ? P : slots <= 512 ? 4 : 8, G = (P + W - 1) / W;
@@ -1200,7 +1221,7 @@ Plan plan_tokens(int C, int dtype)
 // the registers of sixteen wavefronts have them (one row of 137 slots: 12 us against 17 in one workgroup; 400: 45 against 40).
 Plan plan_distill(long long rows, int C, int dtype)
 {
-    if (C <= 64) return {0, 1, C <= 32 ? 2 : 4};
+    if (const int nv = narrow_of(C)) return {0, 1, nv};
     const int slots = slots_of(C, dtype);
     if (slots <= 2 || (slots <= 24 && rows >= 2048)) return {1, 1, tight(slots, {2, 4, 6, 8, 10, 12, 14, 16, 20, 24})};
     int W, G = 1;
@@ -1236,90 +1257,88 @@ bool with_slots(int V, F f)
     return ((V == Vs && (f(std::integral_constant<int, Vs>()), true)) || ...);
 }
 template <typename T>
-bool launch_rows(const Plan& p, hipStream_t st, const void* z, const int* tokens, const int* in_len, const TokenOut& o, const Parts& parts,
-                 unsigned rows, unsigned Tp, int C, float kscale)
+bool launch_rows(const Plan& p, hipStream_t st, const void* z, const int* tokens, const Frames& fr, const TokenOut& o, const Parts& parts,
+                 int C, float kscale)
 {
     if (p.W > 1)
         return with_slots<10, 12, 14, 16>(p.V, [&](auto v) {
-            hipLaunchKernelGGL((token_rows_k<T, decltype(v)::value, true>), dim3(grid_of((long long)rows * p.G)), dim3(64 * p.W), lds_of(p.W, true), st,
-                               (const T*)z, tokens, in_len, o, parts, rows, Tp, C, p.G, kscale);
+            hipLaunchKernelGGL((token_rows_k<T, decltype(v)::value, true>), dim3(grid_of((long long)fr.rows * p.G)), dim3(64 * p.W), lds_of(p.W, true), st,
+                               (const T*)z, tokens, fr, o, parts, C, p.G, kscale);
         });
     return with_slots<2, 4, 6, 8, 10, 12, 14, 16, 20, 24>(p.V, [&](auto v) {
-            hipLaunchKernelGGL((token_rows_k<T, decltype(v)::value, false>), dim3(grid_of(((long long)rows + 3) / 4)), dim3(256), lds_of(4, false), st,
-                               (const T*)z, tokens, in_len, o, parts, rows, Tp, C, 1, kscale);
+            hipLaunchKernelGGL((token_rows_k<T, decltype(v)::value, false>), dim3(grid_of(((long long)fr.rows + 3) / 4)), dim3(256), lds_of(4, false), st,
+                               (const T*)z, tokens, fr, o, parts, C, 1, kscale);
     });
 }
 template <typename T>
-int launch_tokens(const Plan& p, hipStream_t st, const void* z, const int* tokens, const int* in_len, const TokenOut& o, void* ws, unsigned rows,
-                  unsigned Tp, int C, float kscale, bool join)
+int launch_tokens(const Plan& p, hipStream_t st, const void* z, const int* tokens, const Frames& fr, const TokenOut& o, void* ws, int C, float kscale, bool join)
 {
-    const Parts parts{(float4*)ws, (ranked_t*)((char*)ws + sums_bytes(rows, p))};
+    const Parts parts{(float4*)ws, (ranked_t*)((char*)ws + sums_bytes(fr.rows, p))};
     if (p.W == 0) {
-        const dim3 g(grid_of(((long long)rows + 15) / 16)), b(THREADS);
-        if (p.V == 2) hipLaunchKernelGGL((token_narrow_k<T, 2>), g, b, 0, st, (const T*)z, tokens, in_len, o, rows, Tp, C);
-        else hipLaunchKernelGGL((token_narrow_k<T, 4>), g, b, 0, st, (const T*)z, tokens, in_len, o, rows, Tp, C);
-    } else if (!launch_rows<T>(p, st, z, tokens, in_len, o, parts, rows, Tp, C, kscale))
+        const dim3 g(grid_of(((long long)fr.rows + 15) / 16)), b(THREADS);
+        if (!with_slots<2, 4, 8, 16>(p.V, [&](auto v) {
+                hipLaunchKernelGGL((token_narrow_k<T, decltype(v)::value>), g, b, 0, st, (const T*)z, tokens, fr, o, C);
+            }))
+            return W2L_ERR_SHAPE;
+    } else if (!launch_rows<T>(p, st, z, tokens, fr, o, parts, C, kscale))
         return W2L_ERR_SHAPE;
     if (int rc = launch_status()) return rc;
     if (p.G == 1 || !join) return W2L_OK;  // (the partial sums of a distillation are not joined)
-    hipLaunchKernelGGL(token_join_k<T>, dim3(grid_of(rows)), dim3(THREADS), 0, st, (const T*)z, tokens, in_len, o, parts, rows, Tp, C, p.G);
+    hipLaunchKernelGGL(token_join_k<T>, dim3(grid_of(fr.rows)), dim3(THREADS), 0, st, (const T*)z, tokens, fr, o, parts, C, p.G);
     return launch_status();
 }
 
 template <typename T, typename D>
 void launch_bwd(hipStream_t st, const void* z, const float* stats, const int* tokens, const float* dlogprob, const float* dentropy, const int* top_ids,
-                const float* dtop, const int* in_len, void* dz, unsigned rows, unsigned Tp, int C, int S, int K, int accumulate)
+                const float* dtop, const Frames& fr, void* dz, int C, int S, int K, int accumulate)
 {
     constexpr int V = 4, N = 16 / sizeof(T);
-    if (C <= 64) {
-        const dim3 g(grid_of(((long long)rows + 15) / 16)), b(THREADS);
-        if (C <= 32)
-            hipLaunchKernelGGL((token_bwd_narrow_k<T, D, 2>), g, b, 0, st, (const T*)z, stats, tokens, dlogprob, dentropy, top_ids, dtop, in_len, (D*)dz,
-                               rows, Tp, C, S, K, accumulate);
-        else
-            hipLaunchKernelGGL((token_bwd_narrow_k<T, D, 4>), g, b, 0, st, (const T*)z, stats, tokens, dlogprob, dentropy, top_ids, dtop, in_len, (D*)dz,
-                               rows, Tp, C, S, K, accumulate);
+    if (const int nv = narrow_of(C)) {
+        with_slots<2, 4, 8, 16>(nv, [&](auto v) {
+            hipLaunchKernelGGL((token_bwd_narrow_k<T, D, decltype(v)::value>), dim3(grid_of(((long long)fr.rows + 15) / 16)), dim3(THREADS), 0, st,
+                               (const T*)z, stats, tokens, dlogprob, dentropy, top_ids, dtop, fr, (D*)dz, C, S, K, accumulate);
+        });
         return;
     }
     const int slots = (C + 2 * (N - 1) + 64 * N - 1) / (64 * N), P = (slots + V - 1) / V;
-    hipLaunchKernelGGL((token_bwd_rows_k<T, D, V>), dim3(grid_of(((long long)rows * P + 3) / 4)), dim3(THREADS), 0, st, (const T*)z, stats, tokens,
-                       dlogprob, dentropy, top_ids, dtop, in_len, (D*)dz, rows, Tp, C, S, K, P, how_of<D>(rows, C, accumulate));
+    hipLaunchKernelGGL((token_bwd_rows_k<T, D, V>), dim3(grid_of(((long long)fr.rows * P + 3) / 4)), dim3(THREADS), 0, st, (const T*)z, stats, tokens,
+                       dlogprob, dentropy, top_ids, dtop, fr, (D*)dz, C, S, K, P, how_of<D>(fr.rows, C, accumulate));
 }
 
 template <typename T, typename D>
-int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& te, const int* in_len, float* frame_loss, void* dz, void* ws,
-                   unsigned rows, unsigned Tp, int C, int accumulate)
+int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& te, const Frames& fr, float* frame_loss, void* dz, void* ws,
+                   int C, int accumulate)
 {
     if (p.W == 0) {
-        const dim3 g(grid_of(((long long)rows + 15) / 16)), b(THREADS);
-#define W2L_NARROW(NV_, R_) \
-    hipLaunchKernelGGL((distill_narrow_k<T, D, NV_, R_>), g, b, 0, st, (const T*)z, te, in_len, frame_loss, (D*)dz, rows, Tp, C, accumulate)
-        if (C <= 32 && te.K <= 16) W2L_NARROW(2, 1);
-        else if (C <= 32) W2L_NARROW(2, 4);
-        else if (te.K <= 16) W2L_NARROW(4, 1);
-        else W2L_NARROW(4, 4);
-#undef W2L_NARROW
+        const dim3 g(grid_of(((long long)fr.rows + 15) / 16)), b(THREADS);
+        if (!with_slots<2, 4, 8, 16>(p.V, [&](auto v) {
+                if (te.K <= 16)
+                    hipLaunchKernelGGL((distill_narrow_k<T, D, decltype(v)::value, 1>), g, b, 0, st, (const T*)z, te, fr, frame_loss, (D*)dz, C, accumulate);
+                else
+                    hipLaunchKernelGGL((distill_narrow_k<T, D, decltype(v)::value, 4>), g, b, 0, st, (const T*)z, te, fr, frame_loss, (D*)dz, C, accumulate);
+            }))
+            return W2L_ERR_SHAPE;
         return launch_status();
     }
     const float4* sums = nullptr;
     int parts = 1;
     if (p.G > 1) {
         const TokenOut none{nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0};
-        const Plan first = plan_tokens(C, sizeof(T) == 2 ? W2L_BF16 : W2L_F32);  // (G > 1 as well: more than 64 slots)
+        const Plan first = plan_tokens(C, 0, sizeof(T) == 2 ? W2L_BF16 : W2L_F32);  // (G > 1 as well: more than 64 slots)
         parts = first.G;
-        if (int rc = launch_tokens<T>(first, st, z, nullptr, in_len, none, ws, rows, Tp, C, te.kscale, false)) return rc;
+        if (int rc = launch_tokens<T>(first, st, z, nullptr, fr, none, ws, C, te.kscale, false)) return rc;
         sums = (const float4*)ws;
     }
     bool known;
     if (p.W > 1)
         known = with_slots<2, 4, 8, 12, 16>(p.V, [&](auto v) {
-            hipLaunchKernelGGL((distill_rows_k<T, D, decltype(v)::value, true>), dim3(grid_of((long long)rows * p.G)), dim3(64 * p.W), 0, st, (const T*)z, te,
-                               in_len, sums, parts, frame_loss, (D*)dz, rows, Tp, C, p.G, how_of<D>(rows, C, accumulate));
+            hipLaunchKernelGGL((distill_rows_k<T, D, decltype(v)::value, true>), dim3(grid_of((long long)fr.rows * p.G)), dim3(64 * p.W), 0, st, (const T*)z, te,
+                               fr, sums, parts, frame_loss, (D*)dz, C, p.G, how_of<D>(fr.rows, C, accumulate));
         });
     else
         known = with_slots<2, 4, 6, 8, 10, 12, 14, 16, 20, 24>(p.V, [&](auto v) {
-            hipLaunchKernelGGL((distill_rows_k<T, D, decltype(v)::value, false>), dim3(grid_of(((long long)rows + 3) / 4)), dim3(256), 0, st, (const T*)z, te,
-                               in_len, sums, 1, frame_loss, (D*)dz, rows, Tp, C, 1, how_of<D>(rows, C, accumulate));
+            hipLaunchKernelGGL((distill_rows_k<T, D, decltype(v)::value, false>), dim3(grid_of(((long long)fr.rows + 3) / 4)), dim3(256), 0, st, (const T*)z, te,
+                               fr, sums, 1, frame_loss, (D*)dz, C, 1, how_of<D>(fr.rows, C, accumulate));
         });
     if (!known) return W2L_ERR_SHAPE;
     return launch_status();
@@ -1331,7 +1350,7 @@ extern "C" size_t w2l_token_logprob_workspace_bytes(int B, int Tp, int C, int K,
 {
     if (!shape_ok(B, Tp, C, 0, K) || !valid_dtype(z_dtype)) return 0;
     const long long rows = (long long)B * Tp;
-    const Plan p = plan_tokens(C, z_dtype);
+    const Plan p = plan_tokens(C, K, z_dtype);
     return p.G > 1 ? sums_bytes(rows, p) + (size_t)rows * p.G * K * sizeof(ranked_t) : 0;
 }
 
@@ -1346,11 +1365,11 @@ extern "C" int w2l_token_logprob_fwd(const void* z, const int* tokens, const int
         !aligned16(top_logprob) || !aligned16(stats))
         return W2L_ERR_ALIGN;
     if (!workspace_ok(workspace, ws_bytes, w2l_token_logprob_workspace_bytes(B, Tp, C, K, z_dtype))) return W2L_ERR_WORKSPACE;
-    const unsigned rows = (unsigned)B * (unsigned)Tp;
-    const Plan p = plan_tokens(C, z_dtype);
+    const Frames fr = frames_of(in_len, B, Tp);
+    const Plan p = plan_tokens(C, K, z_dtype);
     const TokenOut o{logprob, entropy, top_ids, top_logprob, stats, S, K};
-    return z_dtype == W2L_BF16 ? launch_tokens<bf16_t>(p, (hipStream_t)stream, z, tokens, in_len, o, workspace, rows, (unsigned)Tp, C, LOG2E, true)
-                               : launch_tokens<float>(p, (hipStream_t)stream, z, tokens, in_len, o, workspace, rows, (unsigned)Tp, C, LOG2E, true);
+    return z_dtype == W2L_BF16 ? launch_tokens<bf16_t>(p, (hipStream_t)stream, z, tokens, fr, o, workspace, C, LOG2E, true)
+                               : launch_tokens<float>(p, (hipStream_t)stream, z, tokens, fr, o, workspace, C, LOG2E, true);
 }
 
 extern "C" int w2l_token_logprob_bwd(const void* z, const float* stats, const int* tokens, const float* dlogprob, const float* dentropy,
@@ -1363,9 +1382,9 @@ extern "C" int w2l_token_logprob_bwd(const void* z, const float* stats, const in
     if (!aligned16(z) || !aligned16(stats) || !aligned16(tokens) || !aligned16(dlogprob) || !aligned16(dentropy) || !aligned16(top_ids) ||
         !aligned16(dtop) || !aligned16(in_len) || !aligned16(dz))
         return W2L_ERR_ALIGN;
-    const unsigned rows = (unsigned)B * (unsigned)Tp;
+    const Frames fr = frames_of(in_len, B, Tp);
 #define W2L_BWD(T_, G_)                                                                                                                        \
-    launch_bwd<T_, G_>((hipStream_t)stream, z, stats, tokens, dlogprob, dentropy, top_ids, dtop, in_len, dz, rows, (unsigned)Tp, C, S, K, accumulate)
+    launch_bwd<T_, G_>((hipStream_t)stream, z, stats, tokens, dlogprob, dentropy, top_ids, dtop, fr, dz, C, S, K, accumulate)
     if (z_dtype == W2L_F32) W2L_BWD(float, float);
     else if (dz_dtype == W2L_F32) W2L_BWD(bf16_t, float);
     else W2L_BWD(bf16_t, bf16_t);
@@ -1377,7 +1396,7 @@ extern "C" size_t w2l_distill_workspace_bytes(int B, int Tp, int C, int K, int z
 {
     if (!shape_ok(B, Tp, C, 0, K) || !valid_dtype(z_dtype)) return 0;
     const long long rows = (long long)B * Tp;
-    return plan_distill(rows, C, z_dtype).G > 1 ? sums_bytes(rows, plan_tokens(C, z_dtype)) : 0;
+    return plan_distill(rows, C, z_dtype).G > 1 ? sums_bytes(rows, plan_tokens(C, 0, z_dtype)) : 0;
 }
 
 extern "C" int w2l_distill_fwd_bwd(const void* z, const int* t_ids, const float* t_scores, const int* in_len, const float* weight,
@@ -1392,11 +1411,11 @@ extern "C" int w2l_distill_fwd_bwd(const void* z, const int* t_ids, const float*
         !aligned16(loss) || !aligned16(dz))
         return W2L_ERR_ALIGN;
     if (!workspace_ok(workspace, ws_bytes, w2l_distill_workspace_bytes(B, Tp, C, K, z_dtype))) return W2L_ERR_WORKSPACE;
-    const unsigned rows = (unsigned)B * (unsigned)Tp;
-    const Plan p = plan_distill(rows, C, z_dtype);
+    const Frames fr = frames_of(in_len, B, Tp);
+    const Plan p = plan_distill(fr.rows, C, z_dtype);
     const Teacher te{t_ids, t_scores, weight, K, temperature, 1.f / temperature, (float)(1.4426950408889634 / temperature), grad_scale};
     int rc;
-#define W2L_DISTILL(T_, G_) rc = launch_distill<T_, G_>(p, (hipStream_t)stream, z, te, in_len, frame_loss, dz, workspace, rows, (unsigned)Tp, C, accumulate)
+#define W2L_DISTILL(T_, G_) rc = launch_distill<T_, G_>(p, (hipStream_t)stream, z, te, fr, frame_loss, dz, workspace, C, accumulate)
     if (z_dtype == W2L_F32) W2L_DISTILL(float, float);
     else if (dz_dtype == W2L_F32) W2L_DISTILL(bf16_t, float);
     else W2L_DISTILL(bf16_t, bf16_t);
