@@ -203,6 +203,11 @@ int w2l_distill_fwd_bwd(const void *z, const int *t_ids, const float *t_scores, 
                         float *frame_loss, float *loss, void *dz, int B, int Tp, int C, int K, float temperature,
                         float grad_scale, int z_dtype, int dz_dtype, int accumulate,
                         void *workspace, size_t ws_bytes, void *stream);
+/* Host-only queries: how the two calls above deal out a row -- wavefronts of each of `groups` workgroups that take it, `slots`
+ * vectors of 16 bytes a lane (wavefronts 0: sixteen lanes a row, `slots` values each).  For tests and tuning; launch
+ * nothing.  Errors as the calls themselves. */
+int w2l_token_logprob_launch_config(int B, int Tp, int C, int K, int z_dtype, int *wavefronts, int *groups, int *slots);
+int w2l_distill_launch_config(int B, int Tp, int C, int K, int z_dtype, int *wavefronts, int *groups, int *slots);
 /* HOST pointers: ids [B,Tp,n] (tokens or t_ids), in_len [B] or NULL.  Returns W2L_ERR_TARGET for an in_len outside [0,Tp] or, in
  * a frame t < in_len[b], an id other than -1 outside [0,C). */
 int w2l_frame_ids_check_host(const int *ids, const int *in_len, int B, int Tp, int C, int n);

@@ -25,7 +25,8 @@ __all__ = [
     "w2l_ctc_check_targets_host", "w2l_ctc_launch_config", "w2l_asg_launch_config", "w2l_asg_workspace_bytes", "w2l_asg_fwd_bwd", "w2l_asg_check_targets_host",
     "w2l_logmel_num_frames", "w2l_logmel_fwd",
     "w2l_token_logprob_workspace_bytes", "w2l_token_logprob_fwd", "w2l_token_logprob_bwd",
-    "w2l_distill_workspace_bytes", "w2l_distill_fwd_bwd", "w2l_frame_ids_check_host",
+    "w2l_token_logprob_launch_config", "w2l_distill_workspace_bytes", "w2l_distill_fwd_bwd", "w2l_distill_launch_config",
+    "w2l_frame_ids_check_host",
     "w2l_train_step_workspace_bytes", "w2l_train_step", "w2l_train_step_asg_workspace_bytes", "w2l_train_step_asg",
     "w2l_train_step_launch_config", "w2l_train_step_layer_config", "w2l_sgd_momentum_step",
     "w2l_probe_mfma", "raw",
@@ -75,6 +76,8 @@ def _load():
         "w2l_token_logprob_bwd": (i, [vp] * 9 + [i] * 8 + [vp]),
         "w2l_distill_workspace_bytes": (sz, [i] * 5),
         "w2l_distill_fwd_bwd": (i, [vp] * 8 + [i] * 4 + [f, f] + [i] * 3 + [vp, sz, vp]),
+        "w2l_token_logprob_launch_config": (i, [i] * 5 + [C.POINTER(C.c_int)] * 3),
+        "w2l_distill_launch_config": (i, [i] * 5 + [C.POINTER(C.c_int)] * 3),
         "w2l_frame_ids_check_host": (i, [vp, vp] + [i] * 4),
         "w2l_ctc_workspace_bytes": (sz, [i] * 4),
         "w2l_ctc_fwd_bwd": (i, [vp, i, vp, vp, vp, vp, vp, i, i, i, i, i, f, vp, sz, vp]),
@@ -361,6 +364,20 @@ def w2l_distill_fwd_bwd(z, t_ids, t_scores, frame_loss, loss=None, dz=None, in_l
            None if dz is None else _frames(dz, (B, T, Cc), dz.dtype, dev, "dz"), B, T, Cc, K, temperature, grad_scale, dt, gt,
            1 if accumulate else 0, wp, wn), stream)
     return frame_loss, loss, dz
+
+
+def w2l_token_logprob_launch_config(B, Tp, Cc, K, dtype):
+    """(wavefronts, workgroups, slots) that w2l_token_logprob_fwd gives a row; host only."""
+    out = [C.c_int() for _ in range(3)]
+    _check(raw.w2l_token_logprob_launch_config(B, Tp, Cc, K, dtype, *[C.byref(o) for o in out]), "w2l_token_logprob_launch_config")
+    return tuple(o.value for o in out)
+
+
+def w2l_distill_launch_config(B, Tp, Cc, K, dtype):
+    """(wavefronts, workgroups, slots) that w2l_distill_fwd_bwd gives a row; host only."""
+    out = [C.c_int() for _ in range(3)]
+    _check(raw.w2l_distill_launch_config(B, Tp, Cc, K, dtype, *[C.byref(o) for o in out]), "w2l_distill_launch_config")
+    return tuple(o.value for o in out)
 
 
 def w2l_frame_ids_check_host(ids, in_len, Cc) -> int:

@@ -16,7 +16,7 @@ using namespace w2l;
 namespace {
 
 constexpr int MAX_CLASSES = 262144, MAX_ENTRIES = 64;
-constexpr int THREADS = 256, MAX_WAVES = 16, MAX_SLOTS = 16, MAX_GROUPS = 16, NARROW = 256;
+constexpr int THREADS = 256, MAX_WAVES = 16, MAX_SLOTS = 16, MAX_GROUPS = 16, NARROW = 256, FEW_ROWS = 64;
 constexpr float FAR = 16777216.f;  // 2^24: k m from here on has roundings that are no small shift
 constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
 enum Frame { LIVE = 0, PADDING = 1, BAD = 2 };
@@ -595,34 +595,41 @@ template <typename T>
 __global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z, const int* __restrict__ tokens, Frames fr,
                                                         TokenOut o, Parts parts, int C, int G)
 {
-    __shared__ ranked_t list[MAX_GROUPS * MAX_ENTRIES];
+    __shared__ __attribute__((aligned(16))) ranked_t list[MAX_GROUPS * MAX_ENTRIES + 2];
     __shared__ int count;
+    constexpr int MINE = MAX_GROUPS * MAX_ENTRIES / THREADS;
     for (unsigned r = blockIdx.x; r < fr.rows; r += gridDim.x) {
-        const int tid = threadIdx.x;
+        const int tid = threadIdx.x, lane = tid & 63, need = (o.K + G - 1) / G;
         const Frame f = frame_of(fr, r);
-        const int lane = tid & 63;
-        float m = -INFINITY, s = 0.f, u = 0.f;
-        if (f == LIVE) {
-            const float4 p = lane < G ? parts.sums[(size_t)r * G + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-            m = wave64(p.x, Max());
-            const float d = p.x - m, scale = expf(d);
-            s = wave64(p.y != 0.f ? p.y * scale : 0.f, Sum());
-            u = wave64(p.y != 0.f ? (p.z + p.y * fmaxf(d, -1000.f)) * scale : 0.f, Sum());
+        if (f != LIVE) {
+            write_absent(o, r, f, tid, THREADS);
+            continue;
         }
-        if (f != LIVE || !(s == s)) {
-            write_absent(o, r, f == LIVE ? BAD : f, tid, THREADS);
+        // everything that is read, at once: a few rows are a chain of round trips to memory.  (A row of NaN left no lists: what is read there is not used.)
+        const float4 p = lane < G ? parts.sums[(size_t)r * G + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        const ranked_t* const best = parts.best + (size_t)r * G * o.K;
+        ranked_t least = ~0ull, most = 0, mine[MINE] = {};
+        if (o.K > 0 && lane < G) { least = best[lane * o.K + need - 1]; most = best[lane * o.K + o.K - 1]; }
+#pragma unroll
+        for (int j = 0; j < MINE; ++j)
+            if (tid + j * THREADS < G * o.K) mine[j] = best[tid + j * THREADS];
+        int token = -1;
+        float xt = 0.f;
+        if (tid < o.S) {
+            token = tokens[(size_t)r * o.S + tid];
+            if (token >= 0 && token < C) xt = Elem<T>::load(z, (size_t)r * C + token);
+        }
+        const float m = wave64(p.x, Max()), apart = p.x - m, scale = expf(apart);
+        const float s = wave64(p.y != 0.f ? p.y * scale : 0.f, Sum());
+        const float u = wave64(p.y != 0.f ? (p.z + p.y * fmaxf(apart, -1000.f)) * scale : 0.f, Sum());
+        if (!(s == s)) {
+            write_absent(o, r, BAD, tid, THREADS);
             continue;
         }
         const Dist d = dist_of(m == -INFINITY ? 0.f : m, s, u);
         if (tid == 0) write_dist(o, r, d, s > 0.f);
-        if (tid < o.S) {
-            const int c = tokens[(size_t)r * o.S + tid];
-            o.logprob[(size_t)r * o.S + tid] = c == -1 ? 0.f : c < 0 || c >= C ? NAN : (Elem<T>::load(z, (size_t)r * C + c) - d.m) - d.logs;
-        }
+        if (tid < o.S) o.logprob[(size_t)r * o.S + tid] = token == -1 ? 0.f : token < 0 || token >= C ? NAN : (xt - d.m) - d.logs;
         if (o.K == 0) continue;
-        const ranked_t* const best = parts.best + (size_t)r * G * o.K;
-        const int need = (o.K + G - 1) / G;
-        ranked_t least = lane < G ? best[lane * o.K + need - 1] : ~0ull, most = lane < G ? best[lane * o.K + o.K - 1] : 0;
 #pragma unroll
         for (int j = MAX_GROUPS / 2; j > 0; j >>= 1) {
             const ranked_t a = __shfl_xor(least, j, MAX_GROUPS), b = __shfl_xor(most, j, MAX_GROUPS);
@@ -632,16 +639,22 @@ __global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z,
         least = __shfl(least < most ? most : least, 0, 64);
         if (tid == 0) count = 0;
         __syncthreads();
-        for (int i = tid; i < G * o.K; i += THREADS) {
-            const ranked_t a = best[i];
-            if (a >= least && a != 0) list[atomicAdd(&count, 1)] = a;
-        }
+#pragma unroll
+        for (int j = 0; j < MINE; ++j)
+            if (mine[j] >= least && mine[j] != 0) list[atomicAdd(&count, 1)] = mine[j];
         __syncthreads();
         const int n = count;
+        close_list(list, n, tid);
+        __syncthreads();
         for (int i = tid; i < n; i += THREADS) {
             const ranked_t a = list[i];
             int before = 0;
-            for (int j = 0; j < n; ++j) before += list[j] > a;
+#pragma unroll 4
+            for (int j = 0; j < n; j += 2) {
+                const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(list + j);
+                before += w.x > a;
+                before += w.y > a;
+            }
             if (before < o.K) {
                 o.top_ids[(size_t)r * o.K + before] = class_of(a);
                 o.top_logprob[(size_t)r * o.K + before] = (score_of(a) - d.m) - d.logs;
@@ -1088,18 +1101,20 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
     }
 }
 
+// Rows of up to 16 * NV classes, sixteen lanes each.  loss (nullable): one workgroup has all rows, FEW_ROWS at most, and adds the utterances' losses up as well.
 template <typename T, typename D, int NV, int R>
-__global__ __launch_bounds__(THREADS) void distill_narrow_k(const T* __restrict__ z, Teacher te, Frames fr,
-                                                            float* __restrict__ frame_loss, D* __restrict__ dz, int C,
+__global__ __launch_bounds__(1024) void distill_narrow_k(const T* __restrict__ z, Teacher te, Frames fr,
+                                                            float* __restrict__ frame_loss, float* __restrict__ loss, D* __restrict__ dz, int C,
                                                             int accumulate)
 {
+    __shared__ float few[FEW_ROWS];
     const int l = threadIdx.x & 15;
-    const unsigned stride = gridDim.x * 16;
-    for (unsigned r = blockIdx.x * 16 + (threadIdx.x >> 4); r < fr.rows; r += stride) {
+    const unsigned per = blockDim.x / 16, stride = gridDim.x * per;
+    for (unsigned r = blockIdx.x * per + (threadIdx.x >> 4); r < fr.rows; r += stride) {
         const size_t i0 = (size_t)r * C;
         const Frame f = frame_of(fr, r);
         const float w = f != LIVE ? 0.f : te.weight ? te.weight[r] : 1.f;
-        float loss = f == BAD ? NAN : 0.f, g[NV];
+        float here = f == BAD ? NAN : 0.f, g[NV];
         bool live = false;
 #pragma unroll
         for (int j = 0; j < NV; ++j) g[j] = 0.f;
@@ -1130,7 +1145,7 @@ __global__ __launch_bounds__(THREADS) void distill_narrow_k(const T* __restrict_
                 s += g[j];
             }
             s = row16(s, Sum());
-            loss = frame_loss_of<R, 16>(te, c, t, x, w, m, s, C, q, live);
+            here = frame_loss_of<R, 16>(te, c, t, x, w, m, s, C, q, live);
             const float ws = w * te.grad_scale * te.tau, scale = ws / s;
 #pragma unroll
             for (int j = 0; j < NV; ++j) g[j] *= scale;
@@ -1143,7 +1158,8 @@ __global__ __launch_bounds__(THREADS) void distill_narrow_k(const T* __restrict_
                     for (int j = 0; j < NV; ++j) g[j] -= ci == l + 16 * j ? a : 0.f;
                 }
         }
-        if (l == 0) frame_loss[r] = loss;
+        if (l == 0) frame_loss[r] = here;
+        if (l == 0 && loss) few[r] = here;
         if (!dz || (!live && accumulate)) continue;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
@@ -1152,6 +1168,13 @@ __global__ __launch_bounds__(THREADS) void distill_narrow_k(const T* __restrict_
                 const float v = live ? g[j] : 0.f;
                 Elem<D>::store(dz, i, accumulate ? Elem<D>::load(dz, i) + v : v);
             }
+    }
+    if (!loss) return;
+    __syncthreads();
+    for (unsigned b = threadIdx.x; b < fr.rows / fr.Tp; b += blockDim.x) {
+        double sum = 0.;
+        for (unsigned t = 0; t < fr.Tp; ++t) sum += few[b * fr.Tp + t];
+        loss[b] = (float)sum;
     }
 }
 
@@ -1305,20 +1328,32 @@ void launch_bwd(hipStream_t st, const void* z, const float* stats, const int* to
                        dlogprob, dentropy, top_ids, dtop, fr, (D*)dz, C, S, K, P, how_of<D>(fr.rows, C, accumulate));
 }
 
+// the status of the launch before it, and the utterances' losses if they are wanted
+int launch_losses(hipStream_t st, const Frames& fr, const float* frame_loss, float* loss)
+{
+    const int rc = launch_status();
+    if (rc || !loss) return rc;
+    hipLaunchKernelGGL(utterance_loss_k, dim3(fr.rows / fr.Tp), dim3(THREADS), 0, st, frame_loss, loss, fr.Tp);
+    return launch_status();
+}
 template <typename T, typename D>
-int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& te, const Frames& fr, float* frame_loss, void* dz, void* ws,
+int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& te, const Frames& fr, float* frame_loss, float* loss, void* dz, void* ws,
                    int C, int accumulate)
 {
     if (p.W == 0) {
-        const dim3 g(grid_of(((long long)fr.rows + 15) / 16)), b(THREADS);
+        const bool whole = fr.rows <= FEW_ROWS;  // then a launch less
+        const dim3 g(whole ? 1 : grid_of(((long long)fr.rows + 15) / 16)), b(whole ? 1024 : THREADS);
+        float* const sums = whole ? loss : nullptr;
         if (!with_slots<2, 4, 8, 16>(p.V, [&](auto v) {
                 if (te.K <= 16)
-                    hipLaunchKernelGGL((distill_narrow_k<T, D, decltype(v)::value, 1>), g, b, 0, st, (const T*)z, te, fr, frame_loss, (D*)dz, C, accumulate);
+                    hipLaunchKernelGGL((distill_narrow_k<T, D, decltype(v)::value, 1>), g, b, 0, st, (const T*)z, te, fr, frame_loss, sums, (D*)dz, C,
+                                       accumulate);
                 else
-                    hipLaunchKernelGGL((distill_narrow_k<T, D, decltype(v)::value, 4>), g, b, 0, st, (const T*)z, te, fr, frame_loss, (D*)dz, C, accumulate);
+                    hipLaunchKernelGGL((distill_narrow_k<T, D, decltype(v)::value, 4>), g, b, 0, st, (const T*)z, te, fr, frame_loss, sums, (D*)dz, C,
+                                       accumulate);
             }))
             return W2L_ERR_SHAPE;
-        return launch_status();
+        return whole ? launch_status() : launch_losses(st, fr, frame_loss, loss);
     }
     const float4* sums = nullptr;
     int parts = 1;
@@ -1341,7 +1376,7 @@ int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& 
                                fr, sums, 1, frame_loss, (D*)dz, C, 1, how_of<D>(fr.rows, C, accumulate));
         });
     if (!known) return W2L_ERR_SHAPE;
-    return launch_status();
+    return launch_losses(st, fr, frame_loss, loss);
 }
 
 }  // namespace
@@ -1415,15 +1450,36 @@ extern "C" int w2l_distill_fwd_bwd(const void* z, const int* t_ids, const float*
     const Plan p = plan_distill(fr.rows, C, z_dtype);
     const Teacher te{t_ids, t_scores, weight, K, temperature, 1.f / temperature, (float)(1.4426950408889634 / temperature), grad_scale};
     int rc;
-#define W2L_DISTILL(T_, G_) rc = launch_distill<T_, G_>(p, (hipStream_t)stream, z, te, fr, frame_loss, dz, workspace, C, accumulate)
+#define W2L_DISTILL(T_, G_) rc = launch_distill<T_, G_>(p, (hipStream_t)stream, z, te, fr, frame_loss, loss, dz, workspace, C, accumulate)
     if (z_dtype == W2L_F32) W2L_DISTILL(float, float);
     else if (dz_dtype == W2L_F32) W2L_DISTILL(bf16_t, float);
     else W2L_DISTILL(bf16_t, bf16_t);
 #undef W2L_DISTILL
-    if (rc) return rc;
-    if (!loss) return W2L_OK;
-    hipLaunchKernelGGL(utterance_loss_k, dim3(B), dim3(THREADS), 0, (hipStream_t)stream, frame_loss, loss, (unsigned)Tp);
-    return launch_status();
+    return rc;
+}
+
+extern "C" int w2l_token_logprob_launch_config(int B, int Tp, int C, int K, int z_dtype, int* wavefronts, int* groups, int* slots)
+{
+    if (!wavefronts || !groups || !slots) return W2L_ERR_NULL;
+    if (!shape_ok(B, Tp, C, 0, K)) return W2L_ERR_SHAPE;
+    if (!valid_dtype(z_dtype)) return W2L_ERR_DTYPE;
+    const Plan p = plan_tokens(C, K, z_dtype);
+    *wavefronts = p.W;
+    *groups = p.G;
+    *slots = p.V;
+    return W2L_OK;
+}
+
+extern "C" int w2l_distill_launch_config(int B, int Tp, int C, int K, int z_dtype, int* wavefronts, int* groups, int* slots)
+{
+    if (!wavefronts || !groups || !slots) return W2L_ERR_NULL;
+    if (!shape_ok(B, Tp, C, 0, K) || K < 1) return W2L_ERR_SHAPE;
+    if (!valid_dtype(z_dtype)) return W2L_ERR_DTYPE;
+    const Plan p = plan_distill((long long)B * Tp, C, z_dtype);
+    *wavefronts = p.W;
+    *groups = p.G;
+    *slots = p.V;
+    return W2L_OK;
 }
 
 extern "C" int w2l_frame_ids_check_host(const int* ids, const int* in_len, int B, int Tp, int C, int n)

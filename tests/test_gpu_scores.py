@@ -14,6 +14,7 @@ import torch
 
 import oracle
 from gpu_util import DEV, empty, to_dev, to_host
+from score_cases import CASES, distill_cases
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -174,6 +175,16 @@ def test_tokens(P, size):
     check_tokens(run_tokens(P, z, none, 0, None, dtype, (None, grads[1], None)), z, none, 0, None, (None, grads[1], None))
 
 
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "C%d-K%d-%s" % c)
+def test_tokens_in_every_form(P, case):
+    C, K, dtype = case
+    size = (2, 3, C, K, 2, dtype)
+    z, tokens, in_len, grads = token_case(*size, seed=7)
+    z[:, 1] = rounded(np.sort(z[:, 1], -1)[..., ::-1], dtype)        # classes by their scores, as inventories sorted by frequency are
+    dz_dtype = dtype
+    check_tokens(run_tokens(P, z, tokens, K, in_len, dtype, grads, dz_dtype), z, tokens, K, in_len, grads, dz_dtype)
+
+
 def hard_rows(C, dtype):
     """Rows where a statistic or the order can go wrong, as the type holds them."""
     rng = np.random.default_rng(C)
@@ -183,6 +194,7 @@ def hard_rows(C, dtype):
           np.where(np.arange(C) < C // 2, -big, rng.standard_normal(C)), np.where(np.arange(C) == 0, big, -big)]
     r += [np.arange(C) * 1.0, -np.arange(C) * 1.0, np.sort(rng.standard_normal(C)), -np.sort(rng.standard_normal(C))]
     r += [rng.integers(0, 3, C) * 1.0, rng.integers(-1, 1, C) * 1e-3 + 2e4, np.where(rng.random(C) < 0.5, 0.0, -0.0)]
+    r += [1.2e7 + rng.integers(0, 4, C), -3e8 + 65536. * rng.integers(0, 3, C)]       # differences that k x - M would not keep
     r += [rng.standard_normal(C) * 1e-30, rng.standard_normal(C) * 300, np.where(np.arange(C) // 64 == (C - 1) // 64, 5.0, rng.standard_normal(C))]
     for at in (0, C // 2, C - 1):
         for v in (np.nan, np.inf):
@@ -320,6 +332,23 @@ def test_distill(P, size):
     check_distill(check, z, ids, sc, tau)
 
 
+def _distill_case_ids():
+    import paper_1812_07625_amd as Pm
+    return distill_cases(Pm)
+
+
+@pytest.mark.parametrize("case", _distill_case_ids(), ids=lambda c: "rows%d-C%d-K%d-%s" % c)
+def test_distill_in_every_form(P, case):
+    rows, C, K, dtype = case
+    live = min(rows, 20)
+    z, ids, sc, w, _ = distill_case(1, live, C, K, dtype, 11)
+    pad = lambda a, v: np.concatenate([a, np.full((1, rows - live) + a.shape[2:], v, a.dtype)], 1)    # what is behind the utterance is not read
+    w = np.where(np.arange(live) % 7 == 3, -w, w)
+    z, ids, sc, w = pad(z, np.nan), pad(ids, -7), pad(sc, np.nan), pad(w, np.nan)
+    for gs in (0.5, -2.0):
+        check_distill(run_distill(P, z, ids, sc, 2.0, w, [live], gs, dtype, dtype), z, ids, sc, 2.0, w, [live], gs, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("C,K", HARD)
 def test_distill_of_hard_rows(P, C, K, dtype):
@@ -363,6 +392,85 @@ def test_distill_gradient_is_added(P, C, dz_dtype):
     held = torch.randn((2, 5, C), device=DEV, generator=torch.Generator(DEV).manual_seed(5)).to(torch.bfloat16 if dz_dtype == "bf16" else torch.float32)
     got = run_distill(P, z, ids, sc, 2.0, w, in_len, 1.0, "bf16", dz_dtype, held)
     check_distill(got, z, ids, sc, 2.0, w, in_len, 1.0, dz_dtype, held)
+
+
+@pytest.mark.parametrize("B,T", [(1, 1), (64, 1), (1, 64), (5, 12), (1, 65), (9, 8)])
+def test_distill_losses_of_few_frames(P, B, T):
+    """Up to 64 frames of a short row are one workgroup's, utterance losses included."""
+    z, ids, sc, w, in_len = distill_case(B, T, 29, 8, "fp32", 5)
+    check_distill(run_distill(P, z, ids, sc, 2.0, w, in_len), z, ids, sc, 2.0, w, in_len)
+
+
+@pytest.mark.parametrize("C,T,dtype", [(40001, 230, "fp32"), (9000, 2100, "bf16")])
+def test_large_gradients(P, C, T, dtype):
+    """Gradients of more than 32 MB, which are stored past the caches: written, added, and zeros behind the utterance."""
+    live = 12
+    z, tokens, _, grads = token_case(1, live, C, 4, 1, dtype, 9)
+    pad = lambda a, v: np.concatenate([a, np.full((1, T - live) + a.shape[2:], v, a.dtype)], 1)
+    z, tokens, grads = pad(z, np.nan), pad(tokens, -1), tuple(pad(g, 0.) for g in grads)
+    ids, sc = pad(np.argsort(-z[:, :live], -1)[..., :5], -1), pad(-np.sort(-z[:, :live], -1)[..., :5], 0.)
+    held = torch.full((1, T, C), 0.5, device=DEV).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    for acc in (None, held):
+        check_tokens(run_tokens(P, z, tokens, 4, [live], dtype, grads, dtype, acc), z, tokens, 4, [live], grads, dtype, acc)
+        check_distill(run_distill(P, z, ids, sc, 1.0, None, [live], 1.0, dtype, dtype, acc), z, ids, sc, 1.0, None, [live], 1.0, dtype, acc)
+
+
+def test_offsets_beyond_32_bits(P):
+    """Frames at the end of a tensor of more than 2^31 scores give what they give alone."""
+    C, B, K = 70000, 31000, 5
+    g = torch.Generator(DEV).manual_seed(3)
+    z = torch.empty((B, 1, C), dtype=torch.bfloat16, device=DEV)
+    assert z.numel() > 2 ** 31
+    z[-2:] = torch.randn((2, 1, C), generator=g, device=DEV)
+    il = torch.zeros(B, dtype=torch.int32, device=DEV)
+    il[-2:] = 1
+    tok = torch.randint(0, C, (B, 1, 1), generator=g, device=DEV, dtype=torch.int32)
+    gl, gh = torch.ones((B, 1, 1), device=DEV), torch.ones((B, 1), device=DEV)
+
+    def run(z, tok, gl, gh, il):
+        n = z.shape[0]
+        o = dict(lp=empty((n, 1, 1)), H=empty((n, 1)), ids=torch.zeros((n, 1, K), dtype=torch.int32, device=DEV), top=empty((n, 1, K)), st=empty((n, 1, 4)))
+        P.w2l_token_logprob_fwd(z, tok, o["lp"], o["H"], o["ids"], o["top"], o["st"], in_len=il,
+                                workspace=P.workspace(P.w2l_token_logprob_workspace_bytes(n, 1, C, K, P.W2L_BF16)))
+        dz = torch.zeros_like(z)
+        P.w2l_token_logprob_bwd(z, o["st"], dz, tok, gl, gh, in_len=il, accumulate=True)
+        o["dz"] = dz[-2:].clone()
+        dz.zero_()
+        o["fl"] = empty((n, 1))
+        P.w2l_distill_fwd_bwd(z, o["ids"], o["top"], o["fl"], None, dz, in_len=il, temperature=2.0, accumulate=True,
+                              workspace=P.workspace(P.w2l_distill_workspace_bytes(n, 1, C, K, P.W2L_BF16)))
+        o["dk"] = dz[-2:].clone()
+        torch.cuda.synchronize()
+        return {k: v[-2:].clone() for k, v in o.items()}
+
+    far = run(z, tok, gl, gh, il)
+    near = run(z[-2:].clone(), tok[-2:].clone(), gl[-2:].clone(), gh[-2:].clone(), il[-2:].clone())
+    for k in near:
+        if k in ("dk", "fl"):       # by other numbers of workgroups a row: other roundings of the sums
+            assert torch.allclose(far[k].float(), near[k].float(), rtol=2 ** -7, atol=1e-6), k
+        else:
+            assert torch.equal(far[k], near[k]), k
+
+
+def test_same_results_twice_and_on_two_streams(P):
+    """Bit-reproducible, whatever runs beside: two streams with workspaces of their own."""
+    C, K, T = 50001, 64, 40
+    zd = torch.randn((1, T, C), device=DEV, generator=torch.Generator(DEV).manual_seed(1)).bfloat16()
+    def call():
+        o = [torch.zeros((1, T, K), dtype=torch.int32, device=DEV), empty((1, T, K)), empty((1, T)), empty((1, T)), empty((1, T, C))]
+        P.w2l_token_logprob_fwd(zd, entropy=o[2], top_ids=o[0], top_logprob=o[1], workspace=P.workspace(P.w2l_token_logprob_workspace_bytes(1, T, C, K, 1)))
+        P.w2l_distill_fwd_bwd(zd, o[0], o[1], o[3], None, o[4], workspace=P.workspace(P.w2l_distill_workspace_bytes(1, T, C, K, 1)))
+        return o
+    first = call()
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    out = []
+    for st in (a, b, a, b):
+        with torch.cuda.stream(st):
+            out.append(call())
+    torch.cuda.synchronize()
+    for o in out:
+        assert all(torch.equal(x, y) for x, y in zip(first, o))
 
 
 # ------------------------------------------------------------------------------------ together

@@ -61,6 +61,17 @@ def test_distillation_call():
         assert distill(**{k: A + 4}) == -4, k
 
 
+def test_workspace():
+    big = dict(C=100000, K=9)
+    need = P.w2l_token_logprob_workspace_bytes(2, 3, 100000, 9, 0)
+    assert need > 0
+    assert fwd(ws=N, n=0, **big) == -5 and fwd(n=need - 1, **big) == -5 and fwd(ws=WS + 16, n=need, **big) == -5
+    need = P.w2l_distill_workspace_bytes(2, 3, 100000, 9, 0)
+    assert need > 0
+    assert distill(ws=N, n=0, **big) == -5 and distill(n=need - 1, **big) == -5 and distill(ws=WS + 16, n=need, **big) == -5
+    assert fwd(C=262144, B=8192, T=600) == -2 and bwd(C=262144, B=8192, T=600) == -2 and distill(C=262144, B=8192, T=600) == -2   # over 2^40 scores
+
+
 def test_host_check_of_ids():
     ids = np.array([[[0, 4], [-1, 3]], [[2, 2], [7, -9]]], np.int32)      # [2,2,2]; the last frame is out of range
     assert P.w2l_frame_ids_check_host(ids, [2, 1], 5) == 0
