@@ -173,7 +173,7 @@ int w2l_token_logprob_fwd(const void *z, const int *tokens, const int *in_len, f
  * (gradient with respect to top_logprob), all fp32.  With G = sum_j dlogprob_j + sum_k dtop_k over the entries that are there:
  *   dz_c = -p_c (G + dentropy (lp_c + entropy)) + sum_{j: tokens_j = c} dlogprob_j + sum_{k: top_ids_k = c} dtop_k
  * z, tokens, in_len as for the forward call, stats and top_ids as it wrote them; dz: [B,Tp,C], dz_dtype W2L_F32, or
- * W2L_BF16 where z is bf16.  accumulate = 0 overwrites dz, 1 adds to it (the sum is rounded once).  tokens and dlogprob are NULL
+ * W2L_BF16 where z is bf16.  accumulate = 0 overwrites dz, 1 adds to it (the sum is rounded once); it does not overlap z.  tokens and dlogprob are NULL
  * if S = 0; top_ids and dtop if K = 0.  The gradient of a frame that is not there (t >= in_len[b], bad in_len) or has no
  * distribution (NaN, +inf, nothing but -inf) is 0, of entries that are not (token or top_ids outside [0,C)) as well.  No workspace. */
 int w2l_token_logprob_bwd(const void *z, const float *stats, const int *tokens, const float *dlogprob,
@@ -190,10 +190,10 @@ int w2l_token_logprob_bwd(const void *z, const float *stats, const int *tokens, 
  *   dz[b,t,c]       = grad_scale * d(sum_b loss_b)/d z = grad_scale * weight[b,t] * tau * (p_c - sum_{k: id_k = c} q_k)
  * z: [B,Tp,C] (z_dtype);  t_ids [B,Tp,K] int32, t_scores [B,Tp,K] fp32;  in_len [B] int32 (0..Tp) or NULL: all
  * frames;  weight [B,Tp] fp32 or NULL: 1;  frame_loss [B,Tp] and loss [B] fp32 (loss nullable);  dz [B,Tp,C] or NULL
- * (losses alone), dz_dtype W2L_F32, or W2L_BF16 where z is bf16.  accumulate = 0 overwrites dz, 1 adds to it, rounding
+ * (losses alone), dz_dtype W2L_F32, or W2L_BF16 where z is bf16, not overlapping z.  accumulate = 0 overwrites dz, 1 adds to it, rounding
  * the sum once (to the gradient that w2l_ctc_fwd_bwd left there, say).
  * An id of -1 or a score of -inf is an entry that is not there; the same id in two entries counts twice.  Frames t >=
- * in_len[b] and frames of weight 0 are not read, and like frames with no entry they have loss 0 and zero gradient.
+ * in_len[b] and frames of weight 0, whatever they hold, and frames with no entry have loss 0 and zero gradient.
  * A class of probability zero (z = -inf) that the teacher gives weight to: frame_loss +inf.  NaN or +inf in the frame's
  * z or t_scores, an id other than -1 outside [0,C), an in_len outside its range: frame_loss NaN (the whole utterance in the last
  * case).  A frame whose loss is no finite fp32 number has zero gradient.

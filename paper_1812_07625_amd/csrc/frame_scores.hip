@@ -3,7 +3,9 @@
 // All three are one softmax statistic of the row -- m = max x, s = sum exp(x - m), u = sum exp(x - m)(x - m), from which
 // lp_c = (x_c - m) - log s and H = log s - u / s -- and a few of its columns; the gradients are p_c times a number of the row,
 // corrected in those columns.  Log-probabilities are formed from x - m, never from x - (m + log s): a row of large
-// scores keeps the bits of its differences.
+// scores keeps the bits of its differences.  Scores are widened to fp32, all sums are fp32; a gradient is rounded once, where it is stored.
+// What bounds them is memory, and close behind it the instructions: a copy moves 5.0 TB/s here (reading alone 5.9), and the vector units
+// take 551 G instructions of 64 lanes a second (an exponential counts twice), which leaves a bf16 score about fourteen of them.
 #include "common.h"
 
 #include <math.h>
@@ -93,8 +95,8 @@ __device__ __forceinline__ void exchange()
 // ---- rows in registers ---------------------------------------------------------------------------------
 // A row lies in 16-byte vectors on the grid of the whole tensor (rows of odd length begin inside one): nv of them, `head`
 // elements before the row's first.  They are dealt out in slots of 64, a vector a lane, in turn over the row's wavefronts
-// (those of a workgroup, and of several workgroups where there are few rows), so that the row is read once, with whole loads, and stays in
-// registers: V slots at most a wavefront.  Lanes beyond the row, and elements of a vector that belong to its neighbours, are -inf.
+// (one, those of a workgroup, or those of several), so that the row is read once, with whole loads, and stays in
+// registers: V slots a wavefront.  Lanes beyond the row, and elements of a vector that belong to its neighbours, are -inf.
 template <typename T> constexpr int LANE_VALUES = 16 / sizeof(T);
 
 // Registers that the compiler must not remember the unpacked values of: unpacking again costs less than holding them
@@ -408,13 +410,17 @@ __device__ __forceinline__ void far_sums(const T* __restrict__ z, size_t total, 
     }
 }
 
-// One row by a wavefront (!MULTI, four rows a workgroup), by a workgroup, or by G workgroups, which leave partial results (PARTS) for
-// token_join_k.  kscale = log2 e / temperature.
+// One row by a wavefront (!MULTI, four rows a workgroup), by a workgroup, or by G workgroups, which leave partial results (parts) for
+// token_join_k.  kscale = log2 e / temperature.  The row is read once.  The first pass over its registers finds the maximum and a threshold that
+// the K best reach, the second the sums; vectors with a score at the threshold go to LDS on the way, their scores to a list, and
+// each entry's rank is the number of entries before it.
+// 24000 rows of 4096 fp32 (393 MB): 68 us = 5.8 TB/s without best classes, 77 with 16, 95 with 64 (1200 instructions a row, 370 of them for its
+// values; the units 60 % busy).  5000 of 9997 bf16, K = 16: 30 us = 3.3 TB/s: 20 us of instructions beside 20 of memory.
+// Loading the next row while this one's ranks are taken gained nothing (92 -> 106 us at 4096, K = 64: the loads' queue is full as it is), nor did
+// one pass with a running maximum (93 us); fewer wavefronts a SIMD, as long as nothing spills, lose nothing.
 template <typename T, int V, bool MULTI>
 __global__ __launch_bounds__(MULTI ? 512 : 256) __attribute__((amdgpu_waves_per_eu(V > 20 ? 2 : V > 12 ? 3 : V > 8 ? 4 : V > 4 ? 5 : 6))) void
-token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
-                                                                                    Frames fr, TokenOut o, Parts parts,
-                                                                                    int C, int groups, float kscale)
+token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens, Frames fr, TokenOut o, Parts parts, int C, int groups, float kscale)
 {
     const int G = MULTI ? groups : 1;
     constexpr int N = LANE_VALUES<T>;
@@ -590,10 +596,10 @@ token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens,
 }
 
 // The rows that G workgroups left in parts, a workgroup each.  Of the G sorted lists, entries below the largest K-th of a list or below the
-// smallest ceil(K / G)-th are not among the K best; about 1.5 K pass.
+// smallest ceil(K / G)-th are not among the K best; about 1.5 K pass.  4 rows, G = 4, K = 40: 4.4 us, latency.
 template <typename T>
-__global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z, const int* __restrict__ tokens, Frames fr,
-                                                        TokenOut o, Parts parts, int C, int G)
+__global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z, const int* __restrict__ tokens, Frames fr, TokenOut o, Parts parts,
+                                                        int C, int G)
 {
     __shared__ __attribute__((aligned(16))) ranked_t list[MAX_GROUPS * MAX_ENTRIES + 2];
     __shared__ int count;
@@ -665,6 +671,7 @@ __global__ __launch_bounds__(THREADS) void token_join_k(const T* __restrict__ z,
 }
 
 // Rows of up to 16 * NV classes, sixteen lanes each.  The K best are taken one after the other: largest score, then lowest class.
+// 24000 rows of 29: 4.1 us without best classes, 7.6 with 8 (each a round of some 25 instructions for four rows); of 200: 7, 12 with 4, 26 with 16.
 template <typename T, int NV>
 __global__ __launch_bounds__(THREADS) void token_narrow_k(const T* __restrict__ z, const int* __restrict__ tokens, Frames fr,
                                                           TokenOut o, int C)
@@ -809,12 +816,13 @@ struct Columns {
     }
 };
 
+// V slots of a row a wavefront, nothing between wavefronts.  2700 rows of 10001 bf16: 22 us = 4.9 TB/s of reading and writing; 350 of 65536
+// fp32: 30 us = 6.1 TB/s.
 template <typename T, typename G, int V>
 __global__ __launch_bounds__(THREADS) void token_bwd_rows_k(const T* __restrict__ z, const float* __restrict__ stats, const int* __restrict__ tokens,
                                                             const float* __restrict__ dlogprob, const float* __restrict__ dentropy,
-                                                            const int* __restrict__ top_ids, const float* __restrict__ dtop,
-                                                            Frames fr, G* __restrict__ dz, int C, int S,
-                                                            int K, int P, int how)
+                                                            const int* __restrict__ top_ids, const float* __restrict__ dtop, Frames fr, G* __restrict__ dz, int C,
+                                                            int S, int K, int P, int how)
 {
     constexpr int N = LANE_VALUES<T>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -888,9 +896,8 @@ __global__ __launch_bounds__(THREADS) void token_bwd_rows_k(const T* __restrict_
 template <typename T, typename G, int NV>
 __global__ __launch_bounds__(THREADS) void token_bwd_narrow_k(const T* __restrict__ z, const float* __restrict__ stats, const int* __restrict__ tokens,
                                                               const float* __restrict__ dlogprob, const float* __restrict__ dentropy,
-                                                              const int* __restrict__ top_ids, const float* __restrict__ dtop,
-                                                              Frames fr, G* __restrict__ dz, int C, int S,
-                                                              int K, int accumulate)
+                                                              const int* __restrict__ top_ids, const float* __restrict__ dtop, Frames fr, G* __restrict__ dz, int C,
+                                                              int S, int K, int accumulate)
 {
     const int l = threadIdx.x & 15;
     const unsigned stride = gridDim.x * 16;
@@ -977,12 +984,13 @@ __device__ __forceinline__ float frame_loss_of(const Teacher& te, const int (&c)
 }
 
 // G > 1, where a row is too long for the registers of a workgroup, or rows are few: sums has (m or -inf, s, ., .) of each of the `parts` that
-// token_rows_k read it in; else it is NULL
+// token_rows_k read it in; else it is NULL.  The row is read once (G > 1: twice), its gradient made from the registers.
+// 5400 rows of 4096 bf16: 25 us = 3.5 TB/s of reading and writing, all of them in flight at once, so that loads and stores do not overlap; 2900 of
+// 32000 bf16, K = 64: 85 us = 4.4 TB/s.
 template <typename T, typename D, int V, bool MULTI>
 __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __restrict__ z, Teacher te, Frames fr,
-                                                                                      const float4* __restrict__ sums, int parts, float* __restrict__ frame_loss,
-                                                                                      D* __restrict__ dz, int C, int groups,
-                                                                                      int how)
+                                                                         const float4* __restrict__ sums, int parts, float* __restrict__ frame_loss,
+                                                                         D* __restrict__ dz, int C, int groups, int how)
 {
     const int G = MULTI ? groups : 1;
     constexpr int N = LANE_VALUES<T>;
@@ -1178,7 +1186,7 @@ __global__ __launch_bounds__(1024) void distill_narrow_k(const T* __restrict__ z
     }
 }
 
-// loss[b] = sum of the utterance's frames, in double and in a fixed order
+// loss[b] = sum of the utterance's frames, in double and in a fixed order.  8 utterances of 750: 4 us, a launch and a round trip to memory
 __global__ __launch_bounds__(THREADS) void utterance_loss_k(const float* __restrict__ frame_loss, float* __restrict__ loss, unsigned Tp)
 {
     __shared__ double lds[THREADS / 64];
@@ -1208,7 +1216,7 @@ bool shape_ok(int B, int Tp, int C, int S, int K)
 }
 bool grad_dtype_ok(int z_dtype, int dz_dtype) { return valid_dtype(dz_dtype) && (dz_dtype == W2L_F32 || z_dtype == W2L_BF16); }
 
-// How the rows are dealt out: sixteen lanes a row of up to 64 classes (W = 0), or W wavefronts of each of G workgroups, V slots of
+// How the rows are dealt out: sixteen lanes a row of up to 256 classes (W = 0), or W wavefronts of each of G workgroups, V slots of
 // registers each.
 struct Plan {
     int W, G, V;
@@ -1232,7 +1240,7 @@ int slots_of(int C, int dtype)
 // slots: 28 us against 33; one row: 14 against 15), and one row in more of them gains little (256 slots: 13.8 us in 8, 14.9 in 4).
 Plan plan_tokens(int C, int K, int dtype)
 {
-    if (C <= 64 || K <= 24)  // (the narrow kernel takes a round for each: 24000 rows of 200: 25 us at K = 16, 78 at 64, where a wavefront a row takes 48)
+    if (C <= 64 || K <= 24)  // (the narrow kernel takes a round for each: 24000 rows of 200: 26 us at K = 16, 78 at 64, where a wavefront a row takes 35)
         if (const int nv = narrow_of(C)) return {0, 1, nv};
     const int slots = slots_of(C, dtype);
     if (slots <= 24) return {1, 1, tight(slots, {2, 4, 6, 8, 10, 12, 14, 16, 20, 24})};
@@ -1289,8 +1297,8 @@ bool launch_rows(const Plan& p, hipStream_t st, const void* z, const int* tokens
                                (const T*)z, tokens, fr, o, parts, C, p.G, kscale);
         });
     return with_slots<2, 4, 6, 8, 10, 12, 14, 16, 20, 24>(p.V, [&](auto v) {
-            hipLaunchKernelGGL((token_rows_k<T, decltype(v)::value, false>), dim3(grid_of(((long long)fr.rows + 3) / 4)), dim3(256), lds_of(4, false), st,
-                               (const T*)z, tokens, fr, o, parts, C, 1, kscale);
+        hipLaunchKernelGGL((token_rows_k<T, decltype(v)::value, false>), dim3(grid_of(((long long)fr.rows + 3) / 4)), dim3(256), lds_of(4, false), st,
+                           (const T*)z, tokens, fr, o, parts, C, 1, kscale);
     });
 }
 template <typename T>
