@@ -570,7 +570,7 @@ token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens, Frames fr,
                 }
             }
         }
-        if (o.K > 0) close_list(list, n, thread);
+        if (o.K > 0 && s == s) close_list(list, n, thread);  // (n <= room: a row of NaN or +inf may have counted past it)
         exchange<MULTI>();
         if (MULTI && G > 1) {
             const size_t at = (size_t)r * G + g;

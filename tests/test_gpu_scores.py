@@ -221,6 +221,25 @@ def test_tokens_of_hard_rows(P, C, K, dtype):
     check_tokens(run_tokens(P, z, tokens, K, None, dtype, (gl, gh, gt)), z, tokens, K, None, (gl, gh, gt))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("C", [300, 512, 1000, 9001, 60001])
+def test_rows_without_a_distribution_beside_full_lists(P, C, dtype):
+    """Rows of equal scores and one NaN or +inf, which leave more candidates than a list holds, between rows whose candidates nearly fill
+    theirs: the second kind's classes and log-probabilities are as they would be alone."""
+    rng = np.random.default_rng(C)
+    rows = []
+    for k in range(24):
+        x = np.full(C, 1.0)
+        if k % 2 == 0:
+            x[rng.integers(0, C)] = (np.nan, np.inf)[k // 2 % 2]
+        else:
+            x[rng.permutation(C)[120 + k // 4:]] = -1.0 - rng.random(C - 120 - k // 4)     # 120 to 125 equal scores, the largest
+        rows.append(x)
+    z = rounded(np.stack(rows)[None], dtype)
+    tokens = rng.integers(0, C, (1, 24, 2))
+    check_tokens(run_tokens(P, z, tokens, 64, None, dtype), z, tokens, 64)
+
+
 def test_tokens_that_are_not_there_and_lengths(P):
     C, K = 37, 5
     rng = np.random.default_rng(8)
