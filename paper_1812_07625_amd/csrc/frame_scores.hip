@@ -975,10 +975,11 @@ __device__ __forceinline__ float frame_loss_of(const Teacher& te, const int (&c)
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         q[j] *= inv;
-        if (q[j] > 0.f) kl += q[j] * ((d[j] - logsum) - ((x[j] - m) * te.inv_tau - logs));
+        // tau (log q - log p): differences of scores are not divided by a small tau, and tau^2 is not formed
+        if (q[j] > 0.f) kl += q[j] * (((t[j] - tm) - te.tau * logsum) - ((x[j] - m) - te.tau * logs));
     }
     kl = all(kl, Sum());
-    const float loss = odd != 0.f || !(s == s) ? NAN : none ? 0.f : w * (te.tau * te.tau) * kl;
+    const float loss = odd != 0.f || !(s == s) ? NAN : none ? 0.f : w * te.tau * kl;
     live = !none && fabsf(loss) < INFINITY;
     return loss;
 }
@@ -1447,7 +1448,7 @@ extern "C" int w2l_distill_fwd_bwd(const void* z, const int* t_ids, const float*
                                    int z_dtype, int dz_dtype, int accumulate, void* workspace, size_t ws_bytes, void* stream)
 {
     if (!z || !t_ids || !t_scores || !frame_loss) return W2L_ERR_NULL;
-    if (!shape_ok(B, Tp, C, 0, K) || K < 1 || !(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature) || !isfinite(grad_scale))
+    if (!shape_ok(B, Tp, C, 0, K) || K < 1 || !(temperature > 0.f) || !isnormal(temperature) || !isnormal(1.f / temperature) || !isfinite(grad_scale))
         return W2L_ERR_SHAPE;
     if (!valid_dtype(z_dtype) || !grad_dtype_ok(z_dtype, dz_dtype)) return W2L_ERR_DTYPE;
     if (!aligned16(z) || !aligned16(t_ids) || !aligned16(t_scores) || !aligned16(in_len) || !aligned16(weight) || !aligned16(frame_loss) ||

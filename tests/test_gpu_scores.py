@@ -351,6 +351,20 @@ def test_distill(P, size):
     check_distill(check, z, ids, sc, tau)
 
 
+@pytest.mark.parametrize("tau", [2.0 ** -126, 1e-30, 1e-12, 1e-3, 1e3, 1e12, 1e25])
+@pytest.mark.parametrize("C", [29, 1000, 20000])
+def test_distill_at_the_ends_of_the_temperature(P, C, tau):
+    """Scores of the temperature's size, so that the distributions are ordinary ones; at the smallest, differences of many temperatures, one class
+    with all the weight.  Weights that keep losses and gradients within fp32's normal numbers."""
+    z, ids, sc, w, in_len = distill_case(2, 3, C, 5, "fp32")
+    tau = float(np.float32(tau))
+    size = tau if tau > 1e-6 else 2.0 ** -20
+    z, sc = (np.asarray(a * size, np.float32).astype(np.float64) for a in (z, sc))
+    w = w / tau if not 1e-6 < tau < 1e10 else w
+    w = w.astype(np.float32).astype(np.float64)
+    check_distill(run_distill(P, z, ids, sc, tau, w, in_len), z, ids, sc, tau, w, in_len)
+
+
 def _distill_case_ids():
     import paper_1812_07625_amd as Pm
     return distill_cases(Pm)

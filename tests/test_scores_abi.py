@@ -52,7 +52,7 @@ def test_distillation_call():
     for kw in (dict(z=N), dict(ids=N), dict(sc=N), dict(frame=N)):
         assert distill(**kw) == -1, kw
     assert distill(K=0) == -2
-    for tau in (0.0, -1.0, float("nan"), float("inf"), 1e-45):
+    for tau in (0.0, -1.0, float("nan"), float("inf"), 1e-45, 3e-39, 1e38, 3e38):
         assert distill(tau=tau) == -2, tau
     for gs in (float("nan"), float("inf")):
         assert distill(gs=gs) == -2
