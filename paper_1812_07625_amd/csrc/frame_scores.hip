@@ -1188,24 +1188,27 @@ __global__ __launch_bounds__(1024) void distill_narrow_k(const T* __restrict__ z
 }
 
 // loss[b] = sum of the utterance's frames, in double and in a fixed order.  8 utterances of 750: 4 us, a launch and a round trip to memory
-__global__ __launch_bounds__(THREADS) void utterance_loss_k(const float* __restrict__ frame_loss, float* __restrict__ loss, unsigned Tp)
+__global__ __launch_bounds__(THREADS) void utterance_loss_k(const float* __restrict__ frame_loss, float* __restrict__ loss, unsigned utterances, unsigned Tp)
 {
     __shared__ double lds[THREADS / 64];
-    double s = 0.;
-    for (unsigned t = threadIdx.x; t < Tp; t += 4 * THREADS) {
-        float v[4];
+    for (unsigned b = blockIdx.x; b < utterances; b += gridDim.x) {
+        double s = 0.;
+        for (unsigned t = threadIdx.x; t < Tp; t += 4 * THREADS) {
+            float v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = t + j * THREADS < Tp ? frame_loss[(size_t)blockIdx.x * Tp + t + j * THREADS] : 0.f;
+            for (int j = 0; j < 4; ++j) v[j] = t + j * THREADS < Tp ? frame_loss[(size_t)b * Tp + t + j * THREADS] : 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s += v[j];
-    }
+            for (int j = 0; j < 4; ++j) s += v[j];
+        }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < THREADS / 64; ++w) s += lds[w];
-        loss[blockIdx.x] = (float)s;
+        for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < THREADS / 64; ++w) s += lds[w];
+            loss[b] = (float)s;
+        }
+        __syncthreads();
     }
 }
 
@@ -1342,7 +1345,7 @@ int launch_losses(hipStream_t st, const Frames& fr, const float* frame_loss, flo
 {
     const int rc = launch_status();
     if (rc || !loss) return rc;
-    hipLaunchKernelGGL(utterance_loss_k, dim3(fr.rows / fr.Tp), dim3(THREADS), 0, st, frame_loss, loss, fr.Tp);
+    hipLaunchKernelGGL(utterance_loss_k, dim3(grid_of(fr.rows / fr.Tp)), dim3(THREADS), 0, st, frame_loss, loss, fr.rows / fr.Tp, fr.Tp);
     return launch_status();
 }
 template <typename T, typename D>

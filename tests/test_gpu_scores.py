@@ -365,6 +365,22 @@ def test_distill_at_the_ends_of_the_temperature(P, C, tau):
     check_distill(run_distill(P, z, ids, sc, tau, w, in_len), z, ids, sc, tau, w, in_len)
 
 
+def test_distill_of_more_utterances_than_a_launch_has_workgroups(P):
+    """2^24 + 5 utterances of one frame of two classes, one of them the teacher's: the frame's loss is -log p of it, the utterance's is the frame's."""
+    B = 2 ** 24 + 5
+    z = torch.randn((B, 1, 2), device=DEV, generator=torch.Generator(DEV).manual_seed(4))
+    ids = torch.ones((B, 1, 1), dtype=torch.int32, device=DEV)
+    frame, loss, dz = empty((B, 1)), empty((B,)), torch.empty_like(z)
+    P.w2l_distill_fwd_bwd(z, ids, torch.zeros((B, 1, 1), device=DEV), frame, loss, dz)
+    torch.cuda.synchronize()
+    assert torch.equal(frame[:, 0], loss)
+    d = (z[:, 0, 0] - z[:, 0, 1]).double()
+    # |d| < 12: d and the loss are rounded once each (12 U), exp(d) by (2 |d| + 6) U of itself (at most 8 U), log s and p follow it (10 U)
+    assert float((loss - torch.nn.functional.softplus(d)).abs().max()) <= 64 * U
+    assert float((dz[:, 0, 0] - torch.sigmoid(d)).abs().max()) <= 64 * U
+    assert float((dz[:, 0, 1] + torch.sigmoid(d)).abs().max()) <= 64 * U
+
+
 def _distill_case_ids():
     import paper_1812_07625_amd as Pm
     return distill_cases(Pm)
