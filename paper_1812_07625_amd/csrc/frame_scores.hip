@@ -1089,10 +1089,10 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
             continue;
         }
         opaque(data);
-        // p_c ws = 2^(k x - M) f.  Where f >= 0 and the gradient is stored as bf16, f goes into M: its logarithm and their sum are good to 2^-18, of a
-        // result that is rounded by 2^-9.
+        // p_c ws = 2^(k x - M) f.  Where f >= 0 and the gradient is stored as bf16, f goes into M: their sum is off by at most 2^-15 below 1024, of
+        // a result that is rounded by 2^-9.
         const float f0 = ws / s * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, te.kscale, -M0));
-        const bool folded = sizeof(D) == 2 && f0 >= 0.f;
+        const bool folded = sizeof(D) == 2 && f0 >= 0.f && fabsf(M0) < 1024.f;
         const float M = folded ? M0 - __builtin_amdgcn_logf(f0) : M0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {

@@ -381,6 +381,28 @@ def test_distill_of_more_utterances_than_a_launch_has_workgroups(P):
     assert float((dz[:, 0, 1] + torch.sigmoid(d)).abs().max()) <= 64 * U
 
 
+@pytest.mark.parametrize("C", [200, 1000, 20000, 140001])
+def test_large_scores(P, C):
+    """Rows of one large score, of either sign, and of two neighbouring ones, up to the largest whose products with log2 e fp32 still separates, and
+    beyond: what the rounding of such a product moves must not reach a result."""
+    rng = np.random.default_rng(C)
+    rows = []
+    for k in range(8, 27):
+        for sign in (1.0, -1.0):
+            x = np.full(C, sign * 2.0 ** k * (1 + 0.78125 * rng.random()))
+            x[rng.random(C) < 0.5] -= min(2.0 ** (k - 8), 8.0)
+            rows.append(x)
+    z = rounded(np.stack(rows)[None], "bf16")
+    T = z.shape[1]
+    ids = rng.integers(0, C, (1, T, 4))
+    sc = rng.standard_normal((1, T, 4)).astype(np.float32).astype(np.float64)
+    for dz_dtype in ("bf16", "fp32"):
+        for gs, tau in ((0.7, 1.0), (-1.5, 2.5)):
+            check_distill(run_distill(P, z, ids, sc, tau, None, None, gs, "bf16", dz_dtype), z, ids, sc, tau, None, None, gs, dz_dtype)
+        grads = tuple(rng.standard_normal(s).astype(np.float32).astype(np.float64) for s in ((1, T, 4), (1, T), (1, T, 3)))
+        check_tokens(run_tokens(P, z, ids, 3, None, "bf16", grads, dz_dtype), z, ids, 3, None, grads, dz_dtype)
+
+
 def _distill_case_ids():
     import paper_1812_07625_amd as Pm
     return distill_cases(Pm)
