@@ -417,7 +417,8 @@ __device__ __forceinline__ void far_sums(const T* __restrict__ z, size_t total, 
 // 24000 rows of 4096 fp32 (393 MB): 68 us = 5.8 TB/s without best classes, 77 with 16, 95 with 64 (1200 instructions a row, 370 of them for its
 // values; the units 60 % busy).  5000 of 9997 bf16, K = 16: 30 us = 3.3 TB/s: 20 us of instructions beside 20 of memory.
 // Loading the next row while this one's ranks are taken gained nothing (92 -> 106 us at 4096, K = 64: the loads' queue is full as it is), nor did
-// one pass with a running maximum (93 us); fewer wavefronts a SIMD, as long as nothing spills, lose nothing.
+// one pass with a running maximum (93 us), the clamp left out of slots that hold no -inf (a branch a slot: 33 -> 35 us at 9997), the sums as
+// products of the matrix pipe (33 -> 40); fewer wavefronts a SIMD, as long as nothing spills, lose nothing.
 template <typename T, int V, bool MULTI>
 __global__ __launch_bounds__(MULTI ? 512 : 256) __attribute__((amdgpu_waves_per_eu(V > 20 ? 2 : V > 12 ? 3 : V > 8 ? 4 : V > 4 ? 5 : 6))) void
 token_rows_k(const T* __restrict__ z, const int* __restrict__ tokens, Frames fr, TokenOut o, Parts parts, int C, int groups, float kscale)
