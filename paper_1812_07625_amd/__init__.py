@@ -24,7 +24,10 @@ def __getattr__(name):
         raise AttributeError(name)
     if name in ("build", "binding"):
         return importlib.import_module("." + name, __name__)
-    return getattr(_load_binding(), name)
+    value = getattr(_load_binding(), name)
+    if callable(value):
+        globals()[name] = value  # found without this call from now on
+    return value
 
 
 def __dir__():

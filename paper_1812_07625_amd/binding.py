@@ -245,44 +245,51 @@ def w2l_logsoftmax_bwd(lp, dlp, dz, stream=None):
     return dz
 
 
-# The stream that torch has current on a device, as the handle itself (torch.cuda.current_stream makes an object for it: 2 us of a call
-# whose kernel may take 3)
+# The stream that torch has current on a device, and the current device, as the handle and the number themselves: torch.cuda's own calls make
+# objects and check for initialisation, 2.5 us of a call whose kernel may take 3.  For the same reason a call's operands are checked in one loop.
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _F32, _I32 = torch.float32, torch.int32
 
 
-def _frames(t, shape, dtype, dev, name):
-    """Device pointer of an operand that has to be `shape` of `dtype` on device `dev` (None stays None)."""
-    if t is None:
-        return None
-    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
-        return t.data_ptr()
-    if t.dtype is not dtype:
-        raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
-    if t.shape != shape:
-        raise ValueError("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
-    if t.get_device() != dev:
-        raise ValueError("%s is on %s, the scores are on cuda:%d" % (name, t.device, dev))
-    raise ValueError("%s must be contiguous" % name)
+def _pointers(dev, operands):
+    """Device pointers of operands (name, tensor, shape, dtype), which have to be of that shape and type and on device `dev` (None stays None)."""
+    out = []
+    for name, t, shape, dtype in operands:
+        if t is None:
+            out.append(None)
+        elif t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+            out.append(t.data_ptr())
+        elif t.dtype is not dtype:
+            raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+        elif t.shape != shape:
+            raise ValueError("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
+        elif t.get_device() != dev:
+            raise ValueError("%s is on %s, the scores are on cuda:%d" % (name, t.device, dev))
+        else:
+            raise ValueError("%s must be contiguous" % name)
+    return out
 
 
 def _scores(z):
-    """Pointer, shape, type code and device index of scores z[B,T,C]."""
-    if z.dim() != 3:
-        raise ValueError("scores must be [B, T, C], not %s" % (tuple(z.shape),))
-    if not z.is_cuda:
+    """Shape, type code and device index of scores z[B,T,C]."""
+    shape = z.shape
+    if len(shape) != 3:
+        raise ValueError("scores must be [B, T, C], not %s" % (tuple(shape),))
+    dev = z.get_device()
+    if dev < 0:
         raise ValueError("scores must be on a GPU")
-    B, T, Cc = z.shape
-    return _p(z), B, T, Cc, _dt(z), z.get_device()
+    return shape, _dt(z), dev
 
 
 def _last(t, name):
     """Entries of a frame of an operand [B,T,n]; None: 0."""
     if t is None:
         return 0
-    if t.dim() != 3:
-        raise ValueError("%s must be [B, T, n], not %s" % (name, tuple(t.shape)))
-    return t.shape[2]
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError("%s must be [B, T, n], not %s" % (name, tuple(shape)))
+    return shape[2]
 
 
 def _call(fn, where, dev, args, stream):
@@ -291,7 +298,7 @@ def _call(fn, where, dev, args, stream):
         st = _current_stream(dev)
     else:
         st = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
-    if torch.cuda.current_device() == dev:
+    if _current_device() == dev:
         rc = fn(*args, st)
     else:
         with torch.cuda.device(dev):
@@ -305,7 +312,7 @@ def _scratch(workspace, dev):
         return None, 0
     if workspace.get_device() != dev:
         raise ValueError("workspace is on %s, the scores are on cuda:%d" % (workspace.device, dev))
-    return _p(workspace), workspace.numel() * workspace.element_size()
+    return _p(workspace), workspace.nbytes
 
 
 def w2l_token_logprob_workspace_bytes(B, Tp, Cc, K, dtype) -> int:
@@ -316,33 +323,31 @@ def w2l_token_logprob_fwd(z, tokens=None, logprob=None, entropy=None, top_ids=No
                           workspace=None, stream=None):
     """Scores z[B,T,C] -> log-probabilities of tokens[B,T,S], entropy[B,T], the K best classes (top_ids, top_logprob [B,T,K])
     and what the backward call reads (stats [B,T,4]); outputs that are None are not wanted."""
-    pz, B, T, Cc, dt, dev = _scores(z)
+    shape, dt, dev = _scores(z)
+    B, T, Cc = shape
     S, K = _last(tokens, "tokens"), _last(top_ids, "top_ids")
-    wp, wn = _scratch(workspace, dev)
-    _call(raw.w2l_token_logprob_fwd, "w2l_token_logprob_fwd", dev,
-          (pz, _frames(tokens, (B, T, S), _I32, dev, "tokens"), _frames(in_len, (B,), _I32, dev, "in_len"),
-           _frames(logprob, (B, T, S), _F32, dev, "logprob"), _frames(entropy, (B, T), _F32, dev, "entropy"),
-           _frames(top_ids, (B, T, K), _I32, dev, "top_ids"), _frames(top_logprob, (B, T, K), _F32, dev, "top_logprob"),
-           _frames(stats, (B, T, 4), _F32, dev, "stats"), B, T, Cc, S, K, dt, wp, wn), stream)
+    ptr = _pointers(dev, (("scores", z, shape, z.dtype), ("tokens", tokens, (B, T, S), _I32), ("in_len", in_len, (B,), _I32),
+                          ("logprob", logprob, (B, T, S), _F32), ("entropy", entropy, (B, T), _F32), ("top_ids", top_ids, (B, T, K), _I32),
+                          ("top_logprob", top_logprob, (B, T, K), _F32), ("stats", stats, (B, T, 4), _F32)))
+    _call(raw.w2l_token_logprob_fwd, "w2l_token_logprob_fwd", dev, (*ptr, B, T, Cc, S, K, dt, *_scratch(workspace, dev)), stream)
     return logprob, entropy, top_ids, top_logprob, stats
 
 
 def w2l_token_logprob_bwd(z, stats, dz, tokens=None, dlogprob=None, dentropy=None, top_ids=None, dtop=None, in_len=None,
                           accumulate=False, stream=None):
     """dz[B,T,C] (accumulate: added to it) from the gradients of the forward call's outputs; those that are None are 0."""
-    pz, B, T, Cc, dt, dev = _scores(z)
+    shape, dt, dev = _scores(z)
+    B, T, Cc = shape
     if dlogprob is None:
         tokens = None
     if dtop is None:
         top_ids = None
     S, K = _last(tokens, "tokens"), _last(top_ids, "top_ids")
     gt = _dt(dz)
-    _call(raw.w2l_token_logprob_bwd, "w2l_token_logprob_bwd", dev,
-          (pz, _frames(stats, (B, T, 4), _F32, dev, "stats"), _frames(tokens, (B, T, S), _I32, dev, "tokens"),
-           _frames(dlogprob, (B, T, S), _F32, dev, "dlogprob"), _frames(dentropy, (B, T), _F32, dev, "dentropy"),
-           _frames(top_ids, (B, T, K), _I32, dev, "top_ids"), _frames(dtop, (B, T, K), _F32, dev, "dtop"),
-           _frames(in_len, (B,), _I32, dev, "in_len"), _frames(dz, (B, T, Cc), dz.dtype, dev, "dz"), B, T, Cc, S, K, dt, gt,
-           1 if accumulate else 0), stream)
+    ptr = _pointers(dev, (("scores", z, shape, z.dtype), ("stats", stats, (B, T, 4), _F32), ("tokens", tokens, (B, T, S), _I32),
+                          ("dlogprob", dlogprob, (B, T, S), _F32), ("dentropy", dentropy, (B, T), _F32), ("top_ids", top_ids, (B, T, K), _I32),
+                          ("dtop", dtop, (B, T, K), _F32), ("in_len", in_len, (B,), _I32), ("dz", dz, shape, dz.dtype)))
+    _call(raw.w2l_token_logprob_bwd, "w2l_token_logprob_bwd", dev, (*ptr, B, T, Cc, S, K, dt, gt, 1 if accumulate else 0), stream)
     return dz
 
 
@@ -353,16 +358,15 @@ def w2l_distill_workspace_bytes(B, Tp, Cc, K, dtype) -> int:
 def w2l_distill_fwd_bwd(z, t_ids, t_scores, frame_loss, loss=None, dz=None, in_len=None, weight=None, temperature=1.0,
                         grad_scale=1.0, accumulate=False, workspace=None, stream=None):
     """Loss of a student's scores z[B,T,C] against a teacher's best classes (t_ids, t_scores [B,T,K]) and its gradient dz."""
-    pz, B, T, Cc, dt, dev = _scores(z)
+    shape, dt, dev = _scores(z)
+    B, T, Cc = shape
     K = _last(t_ids, "t_ids")
-    gt = dt if dz is None else _dt(dz)
-    wp, wn = _scratch(workspace, dev)
+    gt, gtype = (dt, None) if dz is None else (_dt(dz), dz.dtype)
+    ptr = _pointers(dev, (("scores", z, shape, z.dtype), ("t_ids", t_ids, (B, T, K), _I32), ("t_scores", t_scores, (B, T, K), _F32),
+                          ("in_len", in_len, (B,), _I32), ("weight", weight, (B, T), _F32), ("frame_loss", frame_loss, (B, T), _F32),
+                          ("loss", loss, (B,), _F32), ("dz", dz, shape, gtype)))
     _call(raw.w2l_distill_fwd_bwd, "w2l_distill_fwd_bwd", dev,
-          (pz, _frames(t_ids, (B, T, K), _I32, dev, "t_ids"), _frames(t_scores, (B, T, K), _F32, dev, "t_scores"),
-           _frames(in_len, (B,), _I32, dev, "in_len"), _frames(weight, (B, T), _F32, dev, "weight"),
-           _frames(frame_loss, (B, T), _F32, dev, "frame_loss"), _frames(loss, (B,), _F32, dev, "loss"),
-           None if dz is None else _frames(dz, (B, T, Cc), dz.dtype, dev, "dz"), B, T, Cc, K, temperature, grad_scale, dt, gt,
-           1 if accumulate else 0, wp, wn), stream)
+          (*ptr, B, T, Cc, K, temperature, grad_scale, dt, gt, 1 if accumulate else 0, *_scratch(workspace, dev)), stream)
     return frame_loss, loss, dz
 
 
