@@ -325,7 +325,8 @@ __device__ __forceinline__ int exact_largest(const T* __restrict__ z, size_t tot
 }
 
 // list[0 .. n) of a wavefront (n <= 128) or a workgroup (MULTI: n <= its threads), all different but zeros, and list[n] = 0 (close_list):
-// calls out(rank, entry) for the K first
+// calls out(rank, entry) for the K first.  (A wavefront's entries beyond 64 are ranked in the same pass, two a lane: 24000 rows of 4096, K = 64: 96 -> 89 us
+// against one after the other by all lanes.  Counting by the scores alone, the classes only where two are equal, was no faster.)
 __device__ __forceinline__ void close_list(ranked_t* list, int n, int thread)
 {
     if (thread == 0) list[n] = 0;
@@ -334,23 +335,27 @@ template <bool MULTI, typename F>
 __device__ __forceinline__ void rank_list(const ranked_t* list, int n, int K, int thread, F out)
 {
     if (MULTI && (thread & ~63) >= n) return;  // (whole wavefronts)
-    const ranked_t a = thread < n ? list[thread] : 0;
-    int before = 0;
+    const bool two = !MULTI && n > 64;  // two entries a lane
+    const ranked_t a = thread < n ? list[thread] : 0, b = two && thread + 64 < n ? list[thread + 64] : 0;
+    int before = 0, before_b = 0;
+    if (two)
 #pragma unroll 4
-    for (int j = 0; j < n; j += 2) {
-        const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(list + j);
-        before += w.x > a;
-        before += w.y > a;
-    }
-    if (thread < n && before < K) out(before, a);
-    if (!MULTI && n > 64) {  // the entries beyond one a lane: each against all lanes'
-        const ranked_t b = thread + 64 < n ? list[thread + 64] : 0;
-        for (int j = 0; j < n - 64; ++j) {
-            const ranked_t w = (ranked_t)(unsigned)__builtin_amdgcn_readlane((int)(b >> 32), j) << 32 | (unsigned)__builtin_amdgcn_readlane((int)b, j);
-            const int k = __popcll(__ballot(a > w)) + __popcll(__ballot(b > w));
-            if (thread == 0 && k < K) out(k, w);
+        for (int j = 0; j < n; j += 2) {
+            const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(list + j);
+            before += w.x > a;
+            before_b += w.x > b;
+            before += w.y > a;
+            before_b += w.y > b;
         }
-    }
+    else
+#pragma unroll 4
+        for (int j = 0; j < n; j += 2) {
+            const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(list + j);
+            before += w.x > a;
+            before += w.y > a;
+        }
+    if (thread < n && before < K) out(before, a);
+    if (two && thread + 64 < n && before_b < K) out(before_b, b);
 }
 
 // ---- log-probabilities, entropy, best classes --------------------------------------------------------
@@ -414,8 +419,8 @@ __device__ __forceinline__ void far_sums(const T* __restrict__ z, size_t total, 
 // token_join_k.  kscale = log2 e / temperature.  The row is read once.  The first pass over its registers finds the maximum and a threshold that
 // the K best reach, the second the sums; vectors with a score at the threshold go to LDS on the way, their scores to a list, and
 // each entry's rank is the number of entries before it.
-// 24000 rows of 4096 fp32 (393 MB): 68 us = 5.8 TB/s without best classes, 77 with 16, 95 with 64 (1200 instructions a row, 370 of them for its
-// values; the units 60 % busy).  5000 of 9997 bf16, K = 16: 30 us = 3.3 TB/s: 20 us of instructions beside 20 of memory.
+// 24000 rows of 4096 fp32 (393 MB): 68 us = 5.8 TB/s without best classes, 77 with 16, 82 with 48, 88 with 64 (beyond 64 candidates
+// a lane has two).  5000 of 9997 bf16, K = 16: 30 us = 3.3 TB/s: 20 us of instructions beside 20 of memory.
 // Loading the next row while this one's ranks are taken gained nothing (92 -> 106 us at 4096, K = 64: the loads' queue is full as it is), nor did
 // one pass with a running maximum (93 us), the clamp left out of slots that hold no -inf (a branch a slot: 33 -> 35 us at 9997), the sums as
 // products of the matrix pipe (33 -> 40); fewer wavefronts a SIMD, as long as nothing spills, lose nothing.
