@@ -789,17 +789,19 @@ __device__ __forceinline__ void clear_row(G* __restrict__ dz, const Row& row, in
     }
 }
 
-// Up to 64 * R columns of a row that get something of their own, an entry a lane: its column (-1: none), what is added there, and the slot of the
-// wavefront (counted in vectors of 64 lanes of the row) that it is in
-template <int R>
+// Columns of a row that get something of their own, an entry a lane: its column (-1: none) and the slot of the wavefront (counted in vectors of
+// 64 lanes of the row) that it is in
+template <int N>
+__device__ __forceinline__ int slot_of(int id, const Row& row) { return id < 0 ? -1 : (id + row.head) / (64 * N); }
+// Up to 128 columns, and what is added there
 struct Columns {
-    int id[R], slot[R];
-    float add[R];
+    int id[2], slot[2];
+    float add[2];
     template <int N>
     __device__ __forceinline__ void place(const Row& row)
     {
 #pragma unroll
-        for (int j = 0; j < R; ++j) slot[j] = id[j] < 0 ? -1 : (id[j] + row.head) / (64 * N);
+        for (int j = 0; j < 2; ++j) slot[j] = slot_of<N>(id[j], row);
     }
     // adds the entries of this slot to its lanes' values, in the order of the entries
     template <int N>
@@ -807,7 +809,7 @@ struct Columns {
     {
         const int lane = threadIdx.x & 63;
 #pragma unroll
-        for (int j = 0; j < R; ++j) {
+        for (int j = 0; j < 2; ++j) {
             unsigned long long b = __ballot(slot[j] == at);
             while (b) {
                 const int l = __ffsll((unsigned long long)b) - 1;
@@ -818,6 +820,29 @@ struct Columns {
                 for (int e = 0; e < N; ++e)
                     if (e == (c & (N - 1))) x[e] += a;  // a uniform choice
             }
+        }
+    }
+};
+// Up to 64 columns whose values are replaced: `value`, less the `also` of every further entry of the same column
+struct Replaced {
+    int id, slot;
+    float value, also;
+    template <int N>
+    __device__ __forceinline__ void apply(int at, const Row& row, float (&x)[N]) const
+    {
+        const int lane = threadIdx.x & 63;
+        unsigned long long b = __ballot(slot == at);
+        while (b) {
+            const int l = __ffsll((unsigned long long)b) - 1, column = __builtin_amdgcn_readlane(id, l), c = column + row.head;
+            float a = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(value), l));
+            unsigned long long same = __ballot(id == column);
+            b &= ~same;
+            for (same &= same - 1; same; same &= same - 1)  // (its lowest lane is l)
+                a -= __int_as_float(__builtin_amdgcn_readlane(__float_as_int(also), __ffsll((unsigned long long)same) - 1));
+            const bool mine = lane == ((c / N) & 63);
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (e == (c & (N - 1))) x[e] = mine ? a : x[e];  // a uniform choice
         }
     }
 };
@@ -847,7 +872,7 @@ __global__ __launch_bounds__(THREADS) void token_bwd_rows_k(const T* __restrict_
         }
         uint4 data[V];
         load_row(data, z, total, row, 64, first * 64 + lane, C);
-        Columns<2> cols;
+        Columns cols;
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -1078,28 +1103,34 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
             if (!(how & ADD)) clear_row<T>(dz, row, V, step, n0, C, how);
             continue;
         }
+        // ws (p_c - q_c): at the teacher's columns p and q may be close, so their difference is formed from fp32 values, whatever the rest of the
+        // row is made from
         const float ws = w * te.grad_scale * te.tau, M0 = m * te.kscale;
-        Columns<1> cols{{q[0] > 0.f ? c[0] : -1}, {0}, {-q[0] * ws}};
-        cols.template place<N>(row);
-        if (!(fabsf(M0) < FAR)) {
+        const bool far = !(fabsf(M0) < FAR);
+        const float f0 = far ? ws / s : ws / s * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, te.kscale, -M0));
+        const float px = __builtin_amdgcn_exp2f(far ? (x[0] - m) * te.kscale : __builtin_fmaf(x[0], te.kscale, -M0)) * f0;
+        const int id = q[0] > 0.f ? c[0] : -1;
+        const Replaced cols{id, slot_of<N>(id, row), px - q[0] * ws, q[0] * ws};
+        if (far) {
 #pragma unroll 1
             for (int v = 0; v < V; ++v) {  // from differences
                 const int n = n0 + v * step;
                 float y[N];
                 unpack(load_vector(z, total, row, n, C), y);
 #pragma unroll
-                for (int e = 0; e < N; ++e) y[e] = __builtin_amdgcn_exp2f((y[e] - m) * te.kscale) * (ws / s);
+                for (int e = 0; e < N; ++e) y[e] = __builtin_amdgcn_exp2f((y[e] - m) * te.kscale) * f0;
                 cols.apply(n >> 6, row, y);
                 if (n < row.nv) put(dz, row.first + (size_t)n * N, n * N - row.head, C, y, how);
             }
             continue;
         }
         opaque(data);
-        // p_c ws = 2^(k x - M) f.  Where f >= 0 and the gradient is stored as bf16, f goes into M: their sum is off by at most 2^-15 below 1024, of
-        // a result that is rounded by 2^-9.
-        const float f0 = ws / s * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, te.kscale, -M0));
-        const bool folded = sizeof(D) == 2 && f0 >= 0.f && fabsf(M0) < 1024.f;
-        const float M = folded ? M0 - __builtin_amdgcn_logf(f0) : M0;
+        // p_c ws = 2^(k x - M) f.  Where f > 0 and the gradient is stored as bf16, f goes into M.  Below 128 the sum is rounded by 2^-18 and the
+        // logarithm is off by 2^-17 at most, so that p_c ws is by less than 2^-17 of itself: where that is the result (the columns above are not
+        // made this way), bf16 rounds it by up to 2^-8.
+        const float folded_M = M0 - __builtin_amdgcn_logf(f0);
+        const bool folded = sizeof(D) == 2 && fabsf(folded_M) < 128.f;  // (f <= 0: NaN or an infinity)
+        const float M = folded ? folded_M : M0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int n = n0 + v * step;
