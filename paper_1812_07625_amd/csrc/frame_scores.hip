@@ -979,6 +979,9 @@ struct Teacher {
     float tau, inv_tau, kscale, grad_scale;  // kscale = log2 e / tau
 };
 
+// (x - m) k, k < 2^127: of halves, which fp32 holds where a difference of 6e38 and a temperature of 1e38 are no infinity
+__device__ __forceinline__ float difference(float x, float m, float k) { return __builtin_fmaf(x, 0.5f, -0.5f * m) * (2.f * k); }
+
 // Loss of a frame from what its K <= 64 * R entries say, an entry a lane of WIDTH (16 or 64): score t of class c, student score x there; m, s of
 // the student's row at the temperature.  q: the teacher's probability of the lane's entries.  Returns the loss; live: whether there is a gradient.
 template <int R, int WIDTH>
@@ -997,20 +1000,23 @@ __device__ __forceinline__ float frame_loss_of(const Teacher& te, const int (&c)
     const bool none = tm == -INFINITY;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-        d[j] = none ? -INFINITY : (t[j] - tm) * te.inv_tau;
+        d[j] = none ? -INFINITY : difference(t[j], tm, te.inv_tau);
         q[j] = none ? 0.f : expf(d[j]);
         sum += q[j];
     }
     sum = all(sum, Sum());
-    const float logsum = none ? 0.f : logf(sum), logs = s > 0.f ? logf(s) : 0.f, inv = none ? 0.f : 1.f / sum;
+    const float inv = none ? 0.f : 1.f / sum;
+    // tau sum q (log q - log p) = sum q ((t - tm) - (x - m)) + tau log(s / sum): differences of scores are not divided by a small tau, and tau^2 is
+    // not formed.  A quarter of them, which fp32 holds whatever the scores, and the rest in 64 bits: at a large tau each logarithm's
+    // product with it may be beyond fp32 where the loss is not.
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         q[j] *= inv;
-        // tau (log q - log p): differences of scores are not divided by a small tau, and tau^2 is not formed
-        if (q[j] > 0.f) kl += q[j] * (((t[j] - tm) - te.tau * logsum) - ((x[j] - m) - te.tau * logs));
+        if (q[j] > 0.f) kl += q[j] * (__builtin_fmaf(t[j], 0.25f, -0.25f * tm) - __builtin_fmaf(x[j], 0.25f, -0.25f * m));
     }
     kl = all(kl, Sum());
-    const float loss = odd != 0.f || !(s == s) ? NAN : none ? 0.f : w * te.tau * kl;
+    const double apart = 4. * kl + (double)te.tau * (s > 0.f ? logf(s * inv) : 0.f);
+    const float loss = odd != 0.f || !(s == s) ? NAN : none ? 0.f : (float)(w * te.tau * apart);
     live = !none && fabsf(loss) < INFINITY;
     return loss;
 }
@@ -1057,7 +1063,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
         if (MULTI && sums) {
             const float4 a = lane < parts ? sums[(size_t)r * parts + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
             m = wave64(a.x, Max());
-            s = wave64(a.y != 0.f ? a.y * expf((a.x - m) * te.inv_tau) : 0.f, Sum());
+            s = wave64(a.y != 0.f ? a.y * expf(difference(a.x, m, te.inv_tau)) : 0.f, Sum());
             m = m == -INFINITY ? 0.f : m;
         } else {
 #pragma unroll
@@ -1187,7 +1193,7 @@ __global__ __launch_bounds__(1024) void distill_narrow_k(const T* __restrict__ z
             m = m == -INFINITY ? 0.f : m;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                g[j] = __builtin_amdgcn_exp2f((g[j] - m) * te.kscale);
+                g[j] = __builtin_amdgcn_exp2f(difference(g[j], m, te.kscale));
                 s += g[j];
             }
             s = row16(s, Sum());

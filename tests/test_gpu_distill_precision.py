@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 import oracle
-from test_gpu_scores import U, close, rounded, run_distill
+from test_gpu_scores import U, check_distill, close, distill_case, rounded, run_distill
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,33 @@ def test_gradient_where_student_and_teacher_agree(P, C, T, centre, repeat):
             if dz_dtype == "bf16":
                 bound = bound * 1.01 + 2.0 ** -8 * np.abs(ref)
             close(got, ref, bound, "dz " + dz_dtype)
+
+
+@pytest.mark.parametrize("K", [1, 30, 60, 64])
+@pytest.mark.parametrize("C", [200, 1000, 4096, 20000, 70000])
+def test_loss_at_the_largest_temperatures(P, C, K):
+    """p and q are even and the loss is weight tau^2 log(C / K), which fp32 holds where tau log C, tau log K or both are beyond it."""
+    z, ids, sc, _, _ = distill_case(2, 3, C, K, "fp32", 5)
+    for tau in (2.0 ** 124, 2.0 ** 125, 2.0 ** 126):
+        w = np.full((2, 3), 2.0 ** -126)
+        check_distill(run_distill(P, z, ids, sc, tau, w), z, ids, sc, tau, w)
+
+
+@pytest.mark.parametrize("C", [29, 300, 20000, 70000])
+def test_scores_whose_difference_is_beyond_fp32(P, C):
+    """Losses that fp32 holds, of scores that are up to 6e38 apart."""
+    rng = np.random.default_rng(C)
+    z, ids, sc, _, _ = distill_case(2, 3, C, 5, "fp32", 6)
+    z = np.where(rng.random(z.shape) < 0.5, 2e38, -3e38) + 1e37 * z
+    z[..., 0] = 3e38
+    z[1, :, 1] = -3e38
+    z = np.clip(z, -3.4e38, 3.4e38).astype(np.float32).astype(np.float64)
+    ids[0, 0], ids[1] = 0, 1
+    sc[1] = np.where(rng.random(sc[1].shape) < 0.5, 3e38, -3e38)
+    sc[1, :, 0] = 3e38
+    sc = sc.astype(np.float32).astype(np.float64)
+    for tau, w in ((2.0 ** -10, 2.0 ** -4), (2.0 ** 10, 2.0 ** -14), (2.0 ** 100, 2.0 ** -104), (2.0 ** 126, 2.0 ** -126)):
+        w = np.full((2, 3), w)
+        got = run_distill(P, z, ids, sc, tau, w)
+        check_distill(got, z, ids, sc, tau, w)
+        assert tau > 2.0 ** 120 or (np.all(np.isfinite(got[0])) and np.all(got[0][1] > 0))
