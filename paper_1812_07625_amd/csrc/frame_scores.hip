@@ -1111,7 +1111,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
         }
         // ws (p_c - q_c): at the teacher's columns p and q may be close, so their difference is formed from fp32 values, whatever the rest of the
         // row is made from
-        const float ws = w * te.grad_scale * te.tau, M0 = m * te.kscale;
+        const float ws = (float)((double)w * te.grad_scale * te.tau), M0 = m * te.kscale;  // (a product of two of them may be beyond fp32)
         const bool far = !(fabsf(M0) < FAR);
         const float f0 = far ? ws / s : ws / s * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, te.kscale, -M0));
         const float px = __builtin_amdgcn_exp2f(far ? (x[0] - m) * te.kscale : __builtin_fmaf(x[0], te.kscale, -M0)) * f0;
@@ -1198,7 +1198,7 @@ __global__ __launch_bounds__(1024) void distill_narrow_k(const T* __restrict__ z
             }
             s = row16(s, Sum());
             here = frame_loss_of<R, 16>(te, c, t, x, w, m, s, C, q, live);
-            const float ws = w * te.grad_scale * te.tau, scale = ws / s;
+            const float ws = (float)((double)w * te.grad_scale * te.tau), scale = ws / s;
 #pragma unroll
             for (int j = 0; j < NV; ++j) g[j] *= scale;
 #pragma unroll

@@ -85,3 +85,17 @@ def test_scores_whose_difference_is_beyond_fp32(P, C):
         got = run_distill(P, z, ids, sc, tau, w)
         check_distill(got, z, ids, sc, tau, w)
         assert tau > 2.0 ** 120 or (np.all(np.isfinite(got[0])) and np.all(got[0][1] > 0))
+
+
+@pytest.mark.parametrize("C", [29, 300, 6000, 40001])
+def test_factors_whose_product_alone_is_in_range(P, C):
+    """weight, grad_scale and temperature, of which two have a product beyond fp32 or below its normal numbers, and all three do not."""
+    z, ids, sc, w, in_len = distill_case(2, 5, C, 6, "fp32", 12)
+    for tau, weight, gs in ((1e-30, 1e30, 1e30), (1e30, 1e-30, 1e-30), (1e25, 1e-25, 1e25), (1e-25, 1e10, 1e30), (2.0 ** -126, 2.0 ** 100, 2.0 ** 27)):
+        tau, weight, gs = (float(np.float32(v)) for v in (tau, weight, gs))
+        size = np.float32(tau if tau > 1 else 2.0 ** -20)
+        zt, st = ((a * size).astype(np.float32).astype(np.float64) for a in (z, sc))
+        wt = (w * weight).astype(np.float32).astype(np.float64)
+        got = run_distill(P, zt, ids, st, tau, wt, in_len, gs)
+        check_distill(got, zt, ids, st, tau, wt, in_len, gs)
+        assert np.all(np.isfinite(got[2])) and np.abs(got[2]).max() > 0
