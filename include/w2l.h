@@ -197,7 +197,9 @@ int w2l_token_logprob_bwd(const void *z, const float *stats, const int *tokens, 
  * A class of probability zero (z = -inf) that the teacher gives weight to: frame_loss +inf.  NaN or +inf in the frame's
  * z or t_scores, an id other than -1 outside [0,C), an in_len outside its range: frame_loss NaN (the whole utterance in the last
  * case).  A frame whose loss is no finite fp32 number has zero gradient.
- * 2^-126 <= temperature <= 2^126, grad_scale finite.  Limits and workspace as above; 1 <= K. */
+ * Accuracy: fp32 leaves a loss some 2^-20 (tau^2 + the loss) up to a temperature of 4, and beyond where it is above tau^2 / 4; smaller losses there, and
+ * their gradients, are good to some 2^-18 of themselves where a frame's entries are of different classes.
+ * 2^-126 <= temperature <= 2^126, grad_scale and weight * grad_scale * temperature finite.  Limits and workspace as above; 1 <= K. */
 size_t w2l_distill_workspace_bytes(int B, int Tp, int C, int K, int z_dtype);
 int w2l_distill_fwd_bwd(const void *z, const int *t_ids, const float *t_scores, const int *in_len, const float *weight,
                         float *frame_loss, float *loss, void *dz, int B, int Tp, int C, int K, float temperature,

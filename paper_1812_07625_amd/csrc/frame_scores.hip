@@ -978,15 +978,20 @@ struct Teacher {
     int K;
     float tau, inv_tau, kscale, grad_scale;  // kscale = log2 e / tau
 };
+__device__ __forceinline__ float weight_of(const Teacher& te, unsigned r) { return te.weight ? te.weight[r] : 1.f; }
 
 // (x - m) k, k < 2^127: of halves, which fp32 holds where a difference of 6e38 and a temperature of 1e38 are no infinity
 __device__ __forceinline__ float difference(float x, float m, float k) { return __builtin_fmaf(x, 0.5f, -0.5f * m) * (2.f * k); }
 
 // Loss of a frame from what its K <= 64 * R entries say, an entry a lane of WIDTH (16 or 64): score t of class c, student score x there; m, s of
 // the student's row at the temperature.  q: the teacher's probability of the lane's entries.  Returns the loss; live: whether there is a gradient.
+// The loss is off by a few tau^2 2^-24 log C.  At tau = 4 that is 4e-6 of a loss of 0.5; beyond (WARM) ordinary scores, whose loss does not grow with
+// tau, would have 2e-4 at tau = 20 and all of it at 1000 (made the other way: 2e-7 at any tau).  near: a loss below tau^2 / 4 there, which distill_near_k makes, with the row's gradient.
+constexpr float WARM = 4.f;
+constexpr unsigned NEAR = 0x7fc00001u;  // what it finds in place of the loss: a NaN that no operation gives
 template <int R, int WIDTH>
 __device__ __forceinline__ float frame_loss_of(const Teacher& te, const int (&c)[R], const float (&t)[R], const float (&x)[R], float w, float m, float s,
-                                               int C, float (&q)[R], bool& live)
+                                               int C, float (&q)[R], bool& near, bool& live)
 {
     auto all = [](float v, auto f) { return WIDTH == 16 ? row16(v, f) : wave64(v, f); };
     float odd = 0.f, tm = -INFINITY, sum = 0.f, kl = 0.f, d[R];
@@ -1016,9 +1021,11 @@ __device__ __forceinline__ float frame_loss_of(const Teacher& te, const int (&c)
     }
     kl = all(kl, Sum());
     const double apart = 4. * kl + (double)te.tau * (s > 0.f ? logf(s * inv) : 0.f);
-    const float loss = odd != 0.f || !(s == s) ? NAN : none ? 0.f : (float)(w * te.tau * apart);
+    const bool defined = odd == 0.f && s == s;
+    near = te.tau > WARM && defined && !none && fabs(apart) < 0.25 * te.tau;
+    const float loss = !defined ? NAN : none ? 0.f : (float)((double)w * te.tau * apart);
     live = !none && fabsf(loss) < INFINITY;
-    return loss;
+    return near ? __uint_as_float(NEAR) : loss;
 }
 
 // G > 1, where a row is too long for the registers of a workgroup, or rows are few: sums has (m or -inf, s, ., .) of each of the `parts` that
@@ -1044,7 +1051,7 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
         const Frame f = frame_of(fr, r);
         const Row row = row_at<T>(r, C);
         const int P = W * G, step = P * 64, n0 = (g * W + (MULTI ? wave : 0)) * 64 + lane;
-        const float w = f != LIVE ? 0.f : te.weight ? te.weight[r] : 1.f;
+        const float w = f != LIVE ? 0.f : weight_of(te, r);
         if (w == 0.f) {
             if (first) frame_loss[r] = f == BAD ? NAN : 0.f;
             if (dz && !(how & ADD)) clear_row<T>(dz, row, V, step, n0, C, how);
@@ -1101,10 +1108,10 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
                 s = uniform(row16((lane & 15) < W ? red[1][lane & 15] : 0.f, Sum()));
             }
         }
-        bool live;
-        const float loss = frame_loss_of<1, 64>(te, c, t, x, w, m, s, C, q, live);
+        bool near, live;
+        const float loss = frame_loss_of<1, 64>(te, c, t, x, w, m, s, C, q, near, live);
         if (first) frame_loss[r] = loss;
-        if (!dz) continue;
+        if (!dz || near) continue;
         if (!live) {
             if (!(how & ADD)) clear_row<T>(dz, row, V, step, n0, C, how);
             continue;
@@ -1165,9 +1172,9 @@ __global__ __launch_bounds__(1024) void distill_narrow_k(const T* __restrict__ z
     for (unsigned r = blockIdx.x * per + (threadIdx.x >> 4); r < fr.rows; r += stride) {
         const size_t i0 = (size_t)r * C;
         const Frame f = frame_of(fr, r);
-        const float w = f != LIVE ? 0.f : te.weight ? te.weight[r] : 1.f;
+        const float w = f != LIVE ? 0.f : weight_of(te, r);
         float here = f == BAD ? NAN : 0.f, g[NV];
-        bool live = false;
+        bool near = false, live = false;
 #pragma unroll
         for (int j = 0; j < NV; ++j) g[j] = 0.f;
         if (w != 0.f) {
@@ -1197,7 +1204,7 @@ __global__ __launch_bounds__(1024) void distill_narrow_k(const T* __restrict__ z
                 s += g[j];
             }
             s = row16(s, Sum());
-            here = frame_loss_of<R, 16>(te, c, t, x, w, m, s, C, q, live);
+            here = frame_loss_of<R, 16>(te, c, t, x, w, m, s, C, q, near, live);
             const float ws = (float)((double)w * te.grad_scale * te.tau), scale = ws / s;
 #pragma unroll
             for (int j = 0; j < NV; ++j) g[j] *= scale;
@@ -1212,7 +1219,7 @@ __global__ __launch_bounds__(1024) void distill_narrow_k(const T* __restrict__ z
         }
         if (l == 0) frame_loss[r] = here;
         if (l == 0 && loss) few[r] = here;
-        if (!dz || (!live && accumulate)) continue;
+        if (!dz || near || (!live && accumulate)) continue;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (l + 16 * j < C) {
@@ -1227,6 +1234,101 @@ __global__ __launch_bounds__(1024) void distill_narrow_k(const T* __restrict__ z
         double sum = 0.;
         for (unsigned t = 0; t < fr.Tp; ++t) sum += few[b * fr.Tp + t];
         loss[b] = (float)sum;
+    }
+}
+
+__device__ __forceinline__ double sum64(double v)  // over the wavefront, the same bits in each lane
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// Loss and gradient of the frames that are NEAR, from quantities that vanish with the loss.  With d = (x - m) - (t - tm) of the entries,
+// y = (d - sum q d) / tau, f(y) = e^y - 1 - y, I = sum e^((x - m) / tau) of the entries, O that of all other classes, less what classes named again
+// count twice:
+//   log p - log q = y - L     L = sum q (log q - log p) = log(1 + sum q f(y)) + log(1 + O / I)     p - q = q (e^(y - L) - 1)
+// so that for different classes nothing cancels, whatever tau is.  (m: the largest score of an entry: below tau^2 / 4 the others' mass is no more than I's.)
+// W wavefronts a row; NARROW: rows that may be shorter than a wavefront's vectors, by element.  What bounds it is the loops over entries, one after the
+// other: beside the 17 us of 24000 rows of 29 with K = 29 it takes 45 where all are NEAR (6000 of 4096 bf16, K = 64: 86 beside 47; 3000 of 32000: 62
+// beside 109), and 3 to 4 where none is.
+template <typename T, typename D, bool NARROW, int W>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void distill_near_k(const T* __restrict__ z, Teacher te, Frames fr, float* __restrict__ frame_loss,
+                                                                        D* __restrict__ dz, int C, int how)
+{
+    constexpr int N = NARROW ? 1 : LANE_VALUES<T>, ROWS = W == 1 ? 4 : 1;
+    __shared__ float red[16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w0 = W == 1 ? 0 : wave;
+    const size_t total = (size_t)fr.rows * C;
+    for (unsigned r = blockIdx.x * ROWS + (W == 1 ? wave : 0); r < fr.rows; r += gridDim.x * ROWS) {
+        if (reinterpret_cast<const unsigned*>(frame_loss)[r] != NEAR) continue;
+        const Row row = NARROW ? Row{(size_t)r * C, 0, C} : row_at<T>(r, C);
+        auto scores = [&](int at, float (&x)[N]) {  // of slot `at`
+            if constexpr (NARROW) x[0] = at * 64 + lane < C ? Elem<T>::load(z, row.first + at * 64 + lane) : -INFINITY;
+            else unpack(load_vector(z, total, row, at * 64 + lane, C), x);
+        };
+        int c = -1;
+        float t = -INFINITY, x = 0.f;
+        if (lane < te.K) {
+            c = te.ids[(size_t)r * te.K + lane];
+            if (c != -1) { t = te.scores[(size_t)r * te.K + lane]; x = Elem<T>::load(z, (size_t)r * C + c); }
+        }
+        const float tm = wave64(t, Max()), raw = expf(difference(t, tm, te.inv_tau)), q = raw * (1.f / wave64(raw, Sum()));
+        const bool on = q > 0.f && x > -INFINITY;  // (the second only where q is next to nothing: the loss would be no finite number)
+        const int id = on ? c : -1;
+        const float m = wave64(on ? x : -INFINITY, Max()), e = on ? __builtin_amdgcn_exp2f(difference(x, m, te.kscale)) : 0.f;
+        const double d = on ? ((double)x - m) - ((double)t - tm) : 0., y = (d - sum64(q * d) / sum64(q)) * te.inv_tau;
+        const float yf = (float)y;
+        double f = 0.;
+        if (fabsf(yf) < 0.5f)  // the power series; what it leaves out is below 2^-24 of it
+            f = q * (y * y) * (0.5f + yf * (1.f / 6 + yf * (1.f / 24 + yf * (1.f / 120 + yf * (1.f / 720 + yf * (1.f / 5040 + yf * (1.f / 40320)))))));
+        else if (on)  // (e^60 and more of a q of 2^-87 and less: their product is of ordinary size)
+            f = yf < 60.f ? q * (expf(yf) - 1.f - yf) : expf(logf(q) + yf);
+        f = sum64(f);
+        bool again = false;
+        for (int i = 0; i < te.K; ++i) again |= on && i < lane && __builtin_amdgcn_readlane(id, i) == id;
+        const float I = wave64(e, Sum()), twice = wave64(again ? e : 0.f, Sum());
+        const Replaced others{id, slot_of<N>(id, row), -INFINITY, 0.f};
+        float rest = 0.f;
+#pragma unroll 2
+        for (int at = w0; at * 64 < row.nv; at += W) {
+            float v[N];
+            scores(at, v);
+            others.apply(at, row, v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) rest += __builtin_amdgcn_exp2f(difference(v[k], m, te.kscale));
+        }
+        rest = wave64(rest, Sum());
+        if (W > 1) {
+            if (lane == 0) red[wave] = rest;
+            __syncthreads();
+            rest = uniform(row16((lane & 15) < W ? red[lane & 15] : 0.f, Sum()));
+            __syncthreads();
+        }
+        rest -= twice;
+        auto log_1p = [](double v) { return fabs(v) < 0x1p-24 ? v : (double)log1pf((float)v); };
+        const double L = log_1p(f) + log_1p(rest / I), v = y - L, factor = (double)weight_of(te, r) * te.grad_scale * te.tau;
+        const float loss = (float)((double)weight_of(te, r) * te.tau * (te.tau * L));
+        if (w0 == 0 && lane == 0) frame_loss[r] = loss;  // (all wavefronts of the row have read it)
+        if (!dz) continue;
+        const bool live = fabsf(loss) < INFINITY;
+        if (!live && (how & ADD)) continue;
+        const float ws = live ? (float)factor : 0.f, f0 = ws / (I + rest);
+        const double apart = q * (fabs(v) < 0x1p-10 ? v * (1. + 0.5 * v) : (double)expm1f((float)v));
+        const Replaced cols{id, slot_of<N>(id, row), live ? (float)(factor * apart) : 0.f, q * ws};
+#pragma unroll 2
+        for (int at = w0; at * 64 < row.nv; at += W) {
+            float v[N];
+            scores(at, v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = __builtin_amdgcn_exp2f(difference(v[k], m, te.kscale)) * f0;
+            cols.apply(at, row, v);
+            const int n = at * 64 + lane;
+            if constexpr (NARROW) {
+                if (n < C) Elem<D>::store(dz, row.first + n, how & ADD ? Elem<D>::load(dz, row.first + n) + v[0] : v[0]);
+            } else if (n < row.nv)
+                put(dz, row.first + (size_t)n * N, n * N - row.head, C, v, how);
+        }
     }
 }
 
@@ -1383,10 +1485,21 @@ void launch_bwd(hipStream_t st, const void* z, const float* stats, const int* to
                        dlogprob, dentropy, top_ids, dtop, fr, (D*)dz, C, S, K, P, how_of<D>(fr.rows, C, accumulate));
 }
 
-// the status of the launch before it, and the utterances' losses if they are wanted
-int launch_losses(hipStream_t st, const Frames& fr, const float* frame_loss, float* loss)
+// the status of the launch before it, the frames that it left, and the utterances' losses if they are wanted
+template <typename T, typename D>
+int launch_rest(hipStream_t st, const void* z, const Teacher& te, const Frames& fr, float* frame_loss, float* loss, void* dz, int C, int accumulate)
 {
-    const int rc = launch_status();
+    int rc = launch_status();
+    if (!rc && te.tau > WARM) {
+        const int how = how_of<D>(fr.rows, C, accumulate);
+        if (C <= NARROW)
+            hipLaunchKernelGGL((distill_near_k<T, D, true, 1>), dim3(grid_of(((long long)fr.rows + 3) / 4)), dim3(256), 0, st, (const T*)z, te, fr, frame_loss, (D*)dz, C, how);
+        else if (C <= 32768)
+            hipLaunchKernelGGL((distill_near_k<T, D, false, 4>), dim3(grid_of(fr.rows)), dim3(256), 0, st, (const T*)z, te, fr, frame_loss, (D*)dz, C, how);
+        else
+            hipLaunchKernelGGL((distill_near_k<T, D, false, 16>), dim3(grid_of(fr.rows)), dim3(1024), 0, st, (const T*)z, te, fr, frame_loss, (D*)dz, C, how);
+        rc = launch_status();
+    }
     if (rc || !loss) return rc;
     hipLaunchKernelGGL(utterance_loss_k, dim3(grid_of(fr.rows / fr.Tp)), dim3(THREADS), 0, st, frame_loss, loss, fr.rows / fr.Tp, fr.Tp);
     return launch_status();
@@ -1396,7 +1509,7 @@ int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& 
                    int C, int accumulate)
 {
     if (p.W == 0) {
-        const bool whole = fr.rows <= FEW_ROWS;  // then a launch less
+        const bool whole = fr.rows <= FEW_ROWS && !(te.tau > WARM);  // then a launch less
         const dim3 g(whole ? 1 : grid_of(((long long)fr.rows + 15) / 16)), b(whole ? 1024 : THREADS);
         float* const sums = whole ? loss : nullptr;
         if (!with_slots<2, 4, 8, 16>(p.V, [&](auto v) {
@@ -1408,7 +1521,7 @@ int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& 
                                        accumulate);
             }))
             return W2L_ERR_SHAPE;
-        return whole ? launch_status() : launch_losses(st, fr, frame_loss, loss);
+        return whole ? launch_status() : launch_rest<T, D>(st, z, te, fr, frame_loss, loss, dz, C, accumulate);
     }
     const float4* sums = nullptr;
     int parts = 1;
@@ -1431,7 +1544,7 @@ int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& 
                                fr, sums, 1, frame_loss, (D*)dz, C, 1, how_of<D>(fr.rows, C, accumulate));
         });
     if (!known) return W2L_ERR_SHAPE;
-    return launch_losses(st, fr, frame_loss, loss);
+    return launch_rest<T, D>(st, z, te, fr, frame_loss, loss, dz, C, accumulate);
 }
 
 }  // namespace
