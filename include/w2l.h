@@ -47,7 +47,8 @@ typedef enum {
     W2L_ERR_ALIGN = -4,     /* a pointer is not 16-byte aligned */
     W2L_ERR_WORKSPACE = -5, /* workspace NULL, misaligned or too small */
     W2L_ERR_TARGET = -6,    /* (host validation helper) bad label or length */
-    W2L_ERR_LAUNCH = -7     /* HIP reported an error; see w2l_last_hip_error() */
+    W2L_ERR_LAUNCH = -7,    /* HIP reported an error; see w2l_last_hip_error() */
+    W2L_ERR_OVERLAP = -8    /* (calls that say so) an output overlaps an input */
 } w2l_status;
 
 typedef enum { W2L_F32 = 0, W2L_BF16 = 1 } w2l_dtype;
@@ -163,6 +164,7 @@ int w2l_logsoftmax_bwd(const float *lp, const float *dlp, float *dz, long long r
  * entropy 0 and log-probabilities -inf.  A frame that holds NaN or +inf has no distribution: all its outputs are NaN,
  * its top_ids -1; so have all frames of an utterance whose in_len is outside its range.  A token other than -1
  * outside [0,C) gives NaN.  (w2l_frame_ids_check_host() validates host copies.)
+ * No output, nor the workspace, may overlap an input (W2L_ERR_OVERLAP, here and in the two calls below).
  * Limits: C <= 262144, S <= 64, K <= 64, K <= C, B * Tp < 2^31, B * Tp * C <= 2^40.  Workspace: 256-byte aligned, the queried bytes (0: NULL will do).
  * Results do not depend on the batch a frame is in, apart from the rounding of fp32 sums, and are bit-reproducible. */
 size_t w2l_token_logprob_workspace_bytes(int B, int Tp, int C, int K, int z_dtype);
@@ -173,7 +175,7 @@ int w2l_token_logprob_fwd(const void *z, const int *tokens, const int *in_len, f
  * (gradient with respect to top_logprob), all fp32.  With G = sum_j dlogprob_j + sum_k dtop_k over the entries that are there:
  *   dz_c = -p_c (G + dentropy (lp_c + entropy)) + sum_{j: tokens_j = c} dlogprob_j + sum_{k: top_ids_k = c} dtop_k
  * z, tokens, in_len as for the forward call, stats and top_ids as it wrote them; dz: [B,Tp,C], dz_dtype W2L_F32, or
- * W2L_BF16 where z is bf16.  accumulate = 0 overwrites dz, 1 adds to it (the sum is rounded once); it does not overlap z.  tokens and dlogprob are NULL
+ * W2L_BF16 where z is bf16.  accumulate = 0 overwrites dz, 1 adds to it (the sum is rounded once).  tokens and dlogprob are NULL
  * if S = 0; top_ids and dtop if K = 0.  The gradient of a frame that is not there (t >= in_len[b], bad in_len) or has no
  * distribution (NaN, +inf, nothing but -inf) is 0, of entries that are not (token or top_ids outside [0,C)) as well.  No workspace. */
 int w2l_token_logprob_bwd(const void *z, const float *stats, const int *tokens, const float *dlogprob,
@@ -190,7 +192,7 @@ int w2l_token_logprob_bwd(const void *z, const float *stats, const int *tokens, 
  *   dz[b,t,c]       = grad_scale * d(sum_b loss_b)/d z = grad_scale * weight[b,t] * tau * (p_c - sum_{k: id_k = c} q_k)
  * z: [B,Tp,C] (z_dtype);  t_ids [B,Tp,K] int32, t_scores [B,Tp,K] fp32;  in_len [B] int32 (0..Tp) or NULL: all
  * frames;  weight [B,Tp] fp32 or NULL: 1;  frame_loss [B,Tp] and loss [B] fp32 (loss nullable);  dz [B,Tp,C] or NULL
- * (losses alone), dz_dtype W2L_F32, or W2L_BF16 where z is bf16, not overlapping z.  accumulate = 0 overwrites dz, 1 adds to it, rounding
+ * (losses alone), dz_dtype W2L_F32, or W2L_BF16 where z is bf16.  accumulate = 0 overwrites dz, 1 adds to it, rounding
  * the sum once (to the gradient that w2l_ctc_fwd_bwd left there, say).
  * An id of -1 or a score of -inf is an entry that is not there; the same id in two entries counts twice.  Frames t >=
  * in_len[b] and frames of weight 0, whatever they hold, and frames with no entry have loss 0 and zero gradient.

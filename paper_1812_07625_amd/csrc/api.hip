@@ -25,6 +25,7 @@ extern "C" const char* w2l_status_str(int s)
         case W2L_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
         case W2L_ERR_TARGET: return "bad target label or length";
         case W2L_ERR_LAUNCH: return "HIP launch failed";
+        case W2L_ERR_OVERLAP: return "output overlaps an input";
         default: return "unknown status";
     }
 }

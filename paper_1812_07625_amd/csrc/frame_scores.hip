@@ -1430,6 +1430,22 @@ bool workspace_ok(const void* ws, size_t have, size_t need)
     return need == 0 || (ws && have >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0);
 }
 
+// Operands of a call (NULL: not there), of which no output may lie on an input: vectors hold elements of neighbouring rows, and some paths read a
+// row again after others have been written
+struct Span {
+    const void* p;
+    size_t bytes;
+};
+bool apart(std::initializer_list<Span> in, std::initializer_list<Span> out)
+{
+    for (const Span& o : out)
+        for (const Span& i : in) {
+            const uintptr_t a = reinterpret_cast<uintptr_t>(o.p), b = reinterpret_cast<uintptr_t>(i.p);
+            if (o.p && i.p && o.bytes && i.bytes && a < b + i.bytes && b < a + o.bytes) return false;
+        }
+    return true;
+}
+
 // f(std::integral_constant<int, V>) for the V of a plan, one of Vs; false if it is none of them
 template <int... Vs, typename F>
 bool with_slots(int V, F f)
@@ -1567,7 +1583,11 @@ extern "C" int w2l_token_logprob_fwd(const void* z, const int* tokens, const int
     if (!aligned16(z) || !aligned16(tokens) || !aligned16(in_len) || !aligned16(logprob) || !aligned16(entropy) || !aligned16(top_ids) ||
         !aligned16(top_logprob) || !aligned16(stats))
         return W2L_ERR_ALIGN;
-    if (!workspace_ok(workspace, ws_bytes, w2l_token_logprob_workspace_bytes(B, Tp, C, K, z_dtype))) return W2L_ERR_WORKSPACE;
+    const size_t rows = (size_t)B * Tp, need = w2l_token_logprob_workspace_bytes(B, Tp, C, K, z_dtype);
+    if (!workspace_ok(workspace, ws_bytes, need)) return W2L_ERR_WORKSPACE;
+    if (!apart({{z, rows * C * dtype_size(z_dtype)}, {tokens, rows * S * 4}, {in_len, (size_t)B * 4}},
+               {{logprob, rows * S * 4}, {entropy, rows * 4}, {top_ids, rows * K * 4}, {top_logprob, rows * K * 4}, {stats, rows * 16}, {workspace, need}}))
+        return W2L_ERR_OVERLAP;
     const Frames fr = frames_of(in_len, B, Tp);
     const Plan p = plan_tokens(C, K, z_dtype);
     const TokenOut o{logprob, entropy, top_ids, top_logprob, stats, S, K};
@@ -1585,6 +1605,11 @@ extern "C" int w2l_token_logprob_bwd(const void* z, const float* stats, const in
     if (!aligned16(z) || !aligned16(stats) || !aligned16(tokens) || !aligned16(dlogprob) || !aligned16(dentropy) || !aligned16(top_ids) ||
         !aligned16(dtop) || !aligned16(in_len) || !aligned16(dz))
         return W2L_ERR_ALIGN;
+    const size_t rows = (size_t)B * Tp;
+    if (!apart({{z, rows * C * dtype_size(z_dtype)}, {stats, rows * 16}, {tokens, rows * S * 4}, {dlogprob, rows * S * 4}, {dentropy, rows * 4},
+                {top_ids, rows * K * 4}, {dtop, rows * K * 4}, {in_len, (size_t)B * 4}},
+               {{dz, rows * C * dtype_size(dz_dtype)}}))
+        return W2L_ERR_OVERLAP;
     const Frames fr = frames_of(in_len, B, Tp);
 #define W2L_BWD(T_, G_)                                                                                                                        \
     launch_bwd<T_, G_>((hipStream_t)stream, z, stats, tokens, dlogprob, dentropy, top_ids, dtop, fr, dz, C, S, K, accumulate)
@@ -1613,7 +1638,11 @@ extern "C" int w2l_distill_fwd_bwd(const void* z, const int* t_ids, const float*
     if (!aligned16(z) || !aligned16(t_ids) || !aligned16(t_scores) || !aligned16(in_len) || !aligned16(weight) || !aligned16(frame_loss) ||
         !aligned16(loss) || !aligned16(dz))
         return W2L_ERR_ALIGN;
-    if (!workspace_ok(workspace, ws_bytes, w2l_distill_workspace_bytes(B, Tp, C, K, z_dtype))) return W2L_ERR_WORKSPACE;
+    const size_t rows = (size_t)B * Tp, need = w2l_distill_workspace_bytes(B, Tp, C, K, z_dtype);
+    if (!workspace_ok(workspace, ws_bytes, need)) return W2L_ERR_WORKSPACE;
+    if (!apart({{z, rows * C * dtype_size(z_dtype)}, {t_ids, rows * K * 4}, {t_scores, rows * K * 4}, {in_len, (size_t)B * 4}, {weight, rows * 4}},
+               {{frame_loss, rows * 4}, {loss, (size_t)B * 4}, {dz, rows * C * dtype_size(dz_dtype)}, {workspace, need}}))
+        return W2L_ERR_OVERLAP;
     const Frames fr = frames_of(in_len, B, Tp);
     const Plan p = plan_distill(fr.rows, C, z_dtype);
     const Teacher te{t_ids, t_scores, weight, K, temperature, 1.f / temperature, (float)(1.4426950408889634 / temperature), grad_scale};
