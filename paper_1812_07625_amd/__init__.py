@@ -28,8 +28,8 @@ class _Binding(types.ModuleType):
 
 def _forget(name):
     for n in list(_found) if name.startswith("__") else [name]:  # (__spec__ and the like: the binding is loaded again)
-        if n in _found and globals().get(n) is _found.pop(n):
-            del globals()[n]
+        if n in _found and globals().get(n) is _found[n]:  # (not what a program has put in its place here)
+            del globals()[n], _found[n]
 
 
 def _load_binding():
