@@ -112,14 +112,14 @@ def exact_frame(x, ids, t, tau):
     with localcontext() as ctx:
         ctx.prec = 130
         D, tau = Decimal, Decimal(float(tau))
-        held = np.nonzero(x > -np.inf)[0]
-        on = [(int(c), D(float(v))) for c, v in zip(ids, t) if c >= 0 and v > -np.inf]
-        e = {int(c): (D(float(x[c])) / tau).exp() for c in held}
+        xs = {int(c): D(float(x[c])) - D(float(x.max())) for c in np.nonzero(x > -np.inf)[0]}
+        on = [(int(c), D(float(v)) - D(float(t.max()))) for c, v in zip(ids, t) if c >= 0 and v > -np.inf]
+        e = {c: (v / tau).exp() for c, v in xs.items()}
         S = sum(e.values())
         w = [(v / tau).exp() for _, v in on]
         Q = sum(w)
         q = [v / Q for v in w]
-        d = [D(float(x[c])) - v for c, v in on]
+        d = [xs[c] - v for c, v in on]
         mean = sum(a * b for a, b in zip(q, d))
         entries = (sum(e[c] for c, _ in on) / Q).ln() - mean / tau
         I = sum(e[c] for c, _ in on)
@@ -241,6 +241,29 @@ def test_high_temperatures_beside_other_frames(P, C, K, T, dz_dtype):
     for b, r in ((0, 0), (1, 3), (1, 4)):
         loss, dz = exact_frame(z[b, r], ids[b, r], sc[b, r], tau)[:2]
         assert 0 < loss < 1 and abs(got[0][b, r] - w[b, r] * loss) <= 2.0 ** -14 * loss
+
+
+@pytest.mark.parametrize("offset", [2.0 ** 12, -2.0 ** 20, 2.0 ** 30])
+@pytest.mark.parametrize("C,K", [(29, 29), (300, 64), (40001, 64)])
+def test_large_scores_at_high_temperatures(P, C, K, offset):
+    """Ordinary differences of large scores, whose exponents fp32 has to take from differences; weights that are NaN, one of them of any bits."""
+    rng = np.random.default_rng(C)
+    n = min(C, K)
+    z = np.full((1, 6, C), -np.inf)
+    z[..., :n] = offset + np.round(rng.standard_normal((1, 6, n)) * 64) / 32
+    z = rounded(z, "fp32")
+    ids = np.broadcast_to(np.arange(n), (1, 6, n)).copy()
+    sc = (z[..., :n] - offset + rng.standard_normal((1, 6, n))).astype(np.float32).astype(np.float64)
+    w = np.ones((1, 6), np.float32)
+    w[0, 4:] = np.array([0x7fc00001, 0xffc00001], np.uint32).view(np.float32)
+    for tau in (5.0, 100.0):
+        frame, _, dz = run_distill(P, z, ids, sc, tau, w)
+        for r in range(4):
+            loss, grad, p, q, y, terms, Lt, mean_y = exact_frame(z[0, r], ids[0, r], sc[0, r], tau)
+            assert loss < tau * tau / 4
+            close(frame[0, r], loss, 257 * U * terms, "frame_loss")
+            close(dz[0, r], grad, 49 * U * np.abs(grad) + q * (80 * U * mean_y + 4 * U * y + 256 * U * Lt), "dz")
+        assert np.all(np.isnan(frame[0, 4:])) and not dz[0, 4:].any()
 
 
 @pytest.mark.parametrize("C,K,T", [(29, 29, 40), (3000, 64, 40), (40001, 64, 3)])
