@@ -194,6 +194,8 @@ int w2l_token_logprob_bwd(const void *z, const float *stats, const int *tokens, 
  * frames;  weight [B,Tp] fp32 or NULL: 1;  frame_loss [B,Tp] and loss [B] fp32 (loss nullable);  dz [B,Tp,C] or NULL
  * (losses alone), dz_dtype W2L_F32, or W2L_BF16 where z is bf16.  accumulate = 0 overwrites dz, 1 adds to it, rounding
  * the sum once (to the gradient that w2l_ctc_fwd_bwd left there, say).
+ * A call of its own: w2l_train_step has no such term and does not hand out the gradient at the logits, so a program that distils calls the layers'
+ * passes itself, this and (if it trains on transcriptions as well) w2l_ctc_fwd_bwd between them.
  * An id of -1 or a score of -inf is an entry that is not there; the same id in two entries counts twice.  Frames t >=
  * in_len[b] and frames of weight 0, whatever they hold, and frames with no entry have loss 0 and zero gradient.
  * A class of probability zero (z = -inf) that the teacher gives weight to: frame_loss +inf.  NaN or +inf in the frame's

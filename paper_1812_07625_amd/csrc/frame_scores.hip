@@ -280,7 +280,9 @@ __device__ __forceinline__ void wave_thresholds(const float (&group)[4], float l
 }
 
 // The wavefront's K largest classes, exactly, into list[0 .. K) in any order (fewer, if it holds fewer classes); returns how many.
-// For rows where thresholds leave too many: equal scores, or fewer finite ones than K.  The K-th entry in the order of scores and
+// For rows where thresholds leave too many: equal scores, fewer finite ones than K, or best classes that are neighbours and so few groups' largest, as in
+// inventories ordered by frequency.  That costs: with scores -ln(class) + N(0,1) all rows come here at K = 64, and 24000 of 4096 fp32 take 1340 us where
+// independent scores take 88 (K = 32: 80 and 76), 6000 of 9997 bf16 1470 where they take 39 (K = 32: 164 and 33, K = 16: 32 and 31).  The K-th entry in the order of scores and
 // classes is bisected.  Every step reads the row's vectors again, so that the registers of the usual path carry nothing for it.
 template <typename T>
 __device__ __forceinline__ int exact_largest(const T* __restrict__ z, size_t total, const Row& row, int ns, int step, int n0, int C, int K, ranked_t* list)
@@ -1160,7 +1162,9 @@ __global__ __launch_bounds__(MULTI ? 1024 : 256) void distill_rows_k(const T* __
     }
 }
 
-// Rows of up to 16 * NV classes, sixteen lanes each.  loss (nullable): one workgroup has all rows, FEW_ROWS at most, and adds the utterances' losses up as well.
+// Rows of up to 16 * NV classes, sixteen lanes each.  loss (nullable): one workgroup has all rows, FEW_ROWS at most, and adds the utterances' losses up as well:
+// 64 rows of 29 with K = 8 in 4.6 us (65 rows, two launches: 4.8), 16 in 3.2.  Rows of many classes and entries lose by it, 64 of 64 with K = 64 11.7 (10.2),
+// 64 of 256 with K = 64 24 (17.5).
 template <typename T, typename D, int NV, int R>
 __global__ __launch_bounds__(1024) void distill_narrow_k(const T* __restrict__ z, Teacher te, Frames fr,
                                                             float* __restrict__ frame_loss, float* __restrict__ loss, D* __restrict__ dz, int C,
@@ -1250,8 +1254,8 @@ __device__ __forceinline__ double sum64(double v)  // over the wavefront, the sa
 //   log p - log q = y - L     L = sum q (log q - log p) = log(1 + sum q f(y)) + log(1 + O / I)     p - q = q (e^(y - L) - 1)
 // so that for different classes nothing cancels, whatever tau is.  (m: the largest score of an entry: below tau^2 / 4 the others' mass is no more than I's.)
 // W wavefronts a row; NARROW: rows that may be shorter than a wavefront's vectors, by element.  What bounds it is the loops over entries, one after the
-// other: beside the 17 us of 24000 rows of 29 with K = 29 it takes 45 where all are NEAR (6000 of 4096 bf16, K = 64: 86 beside 47; 3000 of 32000: 62
-// beside 109), and 3 to 4 where none is.
+// other: where all rows are NEAR, 50 us for 24000 of 29 with K = 29 beside 9 of the first kernel, 123 for 6000 of 4096 bf16 with K = 64 beside 13; where none
+// is, 3 to 4.
 template <typename T, typename D, bool NARROW, int W>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void distill_near_k(const T* __restrict__ z, Teacher te, Frames fr, float* __restrict__ frame_loss,
                                                                         D* __restrict__ dz, int C, int how)
@@ -1271,7 +1275,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void distill_near_k(const T*
         float t = -INFINITY, x = 0.f;
         if (lane < te.K) {
             c = te.ids[(size_t)r * te.K + lane];
-            if (c != -1) { t = te.scores[(size_t)r * te.K + lane]; x = Elem<T>::load(z, (size_t)r * C + c); }
+            if (c != -1) t = te.scores[(size_t)r * te.K + lane];
+            if ((unsigned)c < (unsigned)C) x = Elem<T>::load(z, (size_t)r * C + c);
         }
         const float tm = wave64(t, Max()), raw = expf(difference(t, tm, te.inv_tau)), q = raw * (1.f / wave64(raw, Sum()));
         const bool on = q > 0.f && x > -INFINITY;  // (the second only where q is next to nothing: the loss would be no finite number)
