@@ -139,6 +139,34 @@ int w2l_glu_fwd(const void *y, void *h, long long rows, int Cout, int dtype, voi
 int w2l_glu_bwd(const void *y, const void *dh, void *dy, long long rows, int Cout, int dtype,
                 void *stream);
 
+/* ---- group norm with an activation (between a convolution and the next, in deep networks) -------------
+ * The channels of x [B,T,C] form G groups of C/G neighbours.  With len = in_len[b], over the len * C/G values of group g of
+ * utterance b: mean[b,g], var the mean squared deviation, rstd[b,g] = 1 / sqrt(var + eps), and with
+ *   xhat = (x - mean) rstd,  u = gamma[c] xhat + beta[c]
+ *   y = u (W2L_ACT_NONE), max(u, 0) (_RELU), u sigmoid(u) (_SILU): [B,T,C]
+ *   y = u[:C/2] sigmoid(u[C/2:]) (_GLU, value half and gate half as in w2l_glu_fwd): [B,T,C/2]
+ * G = 1 normalises an utterance as a whole, G = C every channel over time.  x, y share `dtype`; gamma, beta [C] fp32 or NULL (1, 0);
+ * mean, rstd [B,G] fp32; in_len [B] int32 (0..T) or NULL: all frames.  The arithmetic is fp32, y is rounded once.
+ * Frames t >= in_len[b] are not read, whatever they hold; y is 0 there.  An utterance of no frames has mean = rstd = 0.  An in_len
+ * outside its range: y, mean and rstd of that utterance are NaN.  NaN or an infinity in a live frame makes its group NaN.
+ * Limits: C <= 8192, T <= 2^24, B <= 65534, B * T < 2^31, B * T * C <= 2^40; C divisible by G (and by 2 with GLU); eps > 0.  Workspace: the queried
+ * bytes (one query for both calls), 256-byte aligned.  No output nor the workspace may overlap an input or another output (W2L_ERR_OVERLAP).
+ * Results are bit-reproducible and do not depend on the other utterances of the batch beyond the rounding of fp32 sums. */
+typedef enum { W2L_ACT_NONE = 0, W2L_ACT_RELU = 1, W2L_ACT_SILU = 2, W2L_ACT_GLU = 3 } w2l_act;
+size_t w2l_groupnorm_workspace_bytes(int B, int T, int C, int G, int act, int dtype);
+int w2l_groupnorm_fwd(const void *x, const float *gamma, const float *beta, const int *in_len, void *y, float *mean,
+                      float *rstd, int B, int T, int C, int G, float eps, int act, int dtype,
+                      void *workspace, size_t ws_bytes, void *stream);
+/* Gradients, given dy of the shape and type of y, and mean and rstd as the forward call wrote them.  With du = dy dy/du and
+ * m1, m2 the means of gamma du and gamma du xhat over the group's live values:
+ *   dx = rstd (gamma du - m1 - xhat m2)                          [B,T,C], `dtype`, 0 in frames t >= in_len[b]
+ *   dgamma[c] = sum_{b,t} du xhat,   dbeta[c] = sum_{b,t} du     [C] fp32, nullable; accumulate = 1 adds to them
+ * The derivative of max(u, 0) at 0 is 0.  Frames t >= in_len[b] of x and dy are not read.  An utterance with an in_len outside its range has dx 0 and no
+ * part in dgamma and dbeta. */
+int w2l_groupnorm_bwd(const void *x, const void *dy, const float *mean, const float *rstd, const float *gamma,
+                      const float *beta, const int *in_len, void *dx, float *dgamma, float *dbeta, int B, int T, int C,
+                      int G, int act, int dtype, int accumulate, void *workspace, size_t ws_bytes, void *stream);
+
 /* ---- per-frame log-softmax (normalised scores for the criterion, Sec. 2.3) ---------
  *   fwd:  lp[r,c] = z[r,c] - max_c z[r,:] - log sum_c exp(z[r,c] - max_c z[r,:])
  *   bwd:  dz[r,c] = dlp[r,c] - exp(lp[r,c]) * sum_c dlp[r,:]
@@ -209,7 +237,7 @@ int w2l_distill_fwd_bwd(const void *z, const int *t_ids, const float *t_scores, 
                         float *frame_loss, float *loss, void *dz, int B, int Tp, int C, int K, float temperature,
                         float grad_scale, int z_dtype, int dz_dtype, int accumulate,
                         void *workspace, size_t ws_bytes, void *stream);
-/* Host-only queries: how the two calls above deal out a row -- wavefronts of each of `groups` workgroups that take it, `slots`
+/* Host-only queries: how w2l_token_logprob_fwd and w2l_distill_fwd_bwd deal out a row -- wavefronts of each of `groups` workgroups that take it, `slots`
  * vectors of 16 bytes a lane (wavefronts 0: sixteen lanes a row, `slots` values each).  For tests and tuning; launch
  * nothing.  Errors as the calls themselves. */
 int w2l_token_logprob_launch_config(int B, int Tp, int C, int K, int z_dtype, int *wavefronts, int *groups, int *slots);
@@ -217,6 +245,31 @@ int w2l_distill_launch_config(int B, int Tp, int C, int K, int z_dtype, int *wav
 /* HOST pointers: ids [B,Tp,n] (tokens or t_ids), in_len [B] or NULL.  Returns W2L_ERR_TARGET for an in_len outside [0,Tp] or, in
  * a frame t < in_len[b], an id other than -1 outside [0,C). */
 int w2l_frame_ids_check_host(const int *ids, const int *in_len, int B, int Tp, int C, int n);
+
+/* ---- clipped policy loss with a KL term ------------------------------------------------------------
+ * A criterion for networks that are rewarded for what they transcribe (for a low error rate, say): labels tokens[b,t] were
+ * sampled frame by frame from an earlier state of the network, which gave them old_logprob[b,t], and the utterance's (or the frame's)
+ * sample was better or worse than others by `advantage`.  With lp the log-probability of the token under the softmax of z[b,t,:], A the advantage,
+ *   r = exp(lp - old_logprob),   e = ref_logprob - lp
+ *   frame_loss[b,t] = weight[b,t] (- min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(e) - e - 1))
+ *   loss[b]         = sum_{t < in_len[b]} frame_loss[b,t]
+ *   f               = weight[b,t] (- r A [the minimum is r A] - kl_coef (exp(e) - 1))        = d frame_loss / d lp
+ *   dz[b,t,c]       = grad_scale * f * ([c = token] - p_c)
+ * exp(e) - e - 1 is never negative, and its mean over samples is the KL divergence from the reference network.
+ * z: [B,Tp,C] (z_dtype);  tokens [B,Tp] int32;  old_logprob, ref_logprob (NULL if kl_coef = 0), weight (NULL: 1) [B,Tp] fp32;  advantage [B] fp32, or
+ * [B,Tp] if advantage_per_frame;  in_len [B] int32 (0..Tp) or NULL: all frames;  frame_loss [B,Tp], loss [B] (nullable), logprob [B,Tp]
+ * (nullable: lp) fp32;  dz [B,Tp,C] or NULL, dz_dtype W2L_F32, or W2L_BF16 where z is bf16;  accumulate = 0 overwrites dz, 1 adds to it, rounding the sum once.
+ * Frames t >= in_len[b], frames of token -1 and frames of weight 0, whatever they hold, have loss, logprob and gradient 0.  An
+ * advantage of 0 leaves the KL term alone.  NaN or +inf in the frame's z, a token other than -1 outside [0,C), an in_len outside its range: loss and
+ * logprob are NaN (of the whole utterance in the last case); nothing but -inf: logprob -inf.  A frame whose loss is no finite fp32 number has zero gradient.
+ * 0 <= clip_low <= 1, clip_high >= 0 (+inf: no bound), kl_coef >= 0 finite, weight * grad_scale * f finite.  Limits and workspace as
+ * w2l_token_logprob_fwd; no output nor the workspace may overlap an input (W2L_ERR_OVERLAP). */
+size_t w2l_policy_workspace_bytes(int B, int Tp, int C, int z_dtype);
+int w2l_policy_fwd_bwd(const void *z, const int *tokens, const float *old_logprob, const float *ref_logprob,
+                       const float *advantage, int advantage_per_frame, const float *weight, const int *in_len,
+                       float *frame_loss, float *loss, float *logprob, void *dz, int B, int Tp, int C, float clip_low,
+                       float clip_high, float kl_coef, float grad_scale, int z_dtype, int dz_dtype, int accumulate,
+                       void *workspace, size_t ws_bytes, void *stream);
 
 /* ---- SGD with momentum (Sec. 4.1: the optimiser of every run in the paper) ---------
  * The paper names the optimiser and does not write the update out; this is the classical
@@ -230,6 +283,44 @@ int w2l_frame_ids_check_host(const int *ids, const int *in_len, int B, int Tp, i
  * aligned.  Arithmetic is fp32.  Returns W2L_ERR_NULL / _SHAPE / _ALIGN like the other calls. */
 int w2l_sgd_momentum_step(float *w, float *v, const float *grad, void *w_lowp, long long n, float lr,
                           float momentum, float weight_decay, void *stream);
+
+/* ---- AdamW over many tensors at once ---------------------------------------------------------------
+ * For every value of every tensor, with t the step (1 at the first) and g the gradient:
+ *   g' = g * (grad_scale * min(1, max_norm / (norm + 1e-6)))      norm = |grad_scale| sqrt(sum over all tensors of g^2)
+ *   m  = m * beta1 + g' * (1 - beta1),    v = v * beta2 + (g' * g') * (1 - beta2)
+ *   w  = w * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *   w_lowp = bf16(w)                       (only if w_lowp != NULL)
+ * max_norm = 0: not clipped.  The norm is formed if max_norm > 0 or grad_norm != NULL (grad_norm [1] fp32 receives it); if it is not finite, the
+ * call changes no tensor.  w fp32; grad fp32 or bf16 (grad_dtype, one for all tensors); moment_bits 32 or 8, one for all:
+ *   32: m and v [n] fp32.
+ *   8:  m and v [n] bytes, m_exp and v_exp [ceil(n / 256)] int8.  Value i is the e4m3 number (OCP, no infinity) of its byte times 2^exp of block i / 256;
+ *       m holds the first moment, v the ROOT of the second.  A block's exponent is the least, and at least -100, with which its largest magnitude
+ *       is at most 448 * 2^exp (0 where all are 0).  Values are rounded up or down at random, in proportion to how near they are, with random bits of
+ *       (seed, t, index of the tensor, index of the value): the same call gives the same bits.  A root above 0 stays above 0.  NaN and
+ *       infinities are kept as NaN.  All bytes and exponents zero: moments of zero.
+ * Arithmetic is fp32 (the moments with each product and sum rounded as written, the norm's sum and the step's constants in 64 bits), w is
+ * off by a few half steps.  lr_dev, step_dev [1] (nullable): fp32 lr and int32 step, read on the device in place of lr and step, so that a captured graph
+ * steps on; a step below 1 there changes nothing.  They, grad_norm and the exponents need natural alignment only.
+ * tensors: HOST array, its pointers DEVICE pointers; n = 0: skipped.  Nothing the call writes may overlap anything else it reads or writes
+ * (W2L_ERR_OVERLAP: a tensor listed twice, say).  Workspace (queried bytes, 256-byte aligned) where the norm, lr_dev or step_dev is asked for; NULL will do
+ * otherwise.  1 <= n_tensors <= W2L_ADAMW_MAX_TENSORS, n <= W2L_ADAMW_MAX_VALUES, step >= 1, lr, weight_decay, max_norm >= 0, 0 <= beta <= 1 - 1e-7,
+ * 1e-37 <= eps, all finite. */
+#define W2L_ADAMW_MAX_TENSORS 65536
+#define W2L_ADAMW_MAX_VALUES (1LL << 36)
+typedef struct {
+    float *w;
+    const void *grad;
+    void *m, *v;
+    signed char *m_exp, *v_exp; /* 8-bit moments only */
+    void *w_lowp;               /* nullable */
+    long long n;
+    double weight_decay;
+} w2l_adamw_tensor;
+size_t w2l_adamw_workspace_bytes(const w2l_adamw_tensor *tensors, int n_tensors);
+int w2l_adamw_step(const w2l_adamw_tensor *tensors, int n_tensors, int grad_dtype, int moment_bits, long long step,
+                   double lr, double beta1, double beta2, double eps, double grad_scale, double max_norm, unsigned seed,
+                   const float *lr_dev, const int *step_dev, float *grad_norm, void *workspace, size_t ws_bytes,
+                   void *stream);
 
 /* ---- CTC criterion (Sec. 2.3, after Graves et al. 2006) ---------------------------
  * For utterance b with T_b = in_len[b] valid frames and target l (L_b = tgt_len[b]

@@ -291,6 +291,93 @@ def distill(z, t_ids, t_scores, tau=1.0, weight=None, in_len=None, grad_scale=1.
     return frame, frame.sum(1), dz
 
 
+# ----------------------------------------------------------------------------- group norm
+def _sigmoid(u):
+    with np.errstate(over="ignore"):
+        return 1.0 / (1.0 + np.exp(-u))
+
+
+def _act(u, act):
+    """(y, dy/du as a function of dy -> du) of an activation: "none", "relu", "silu", "glu"."""
+    if act == "glu":
+        a, s = u[..., :u.shape[-1] // 2], _sigmoid(u[..., u.shape[-1] // 2:])
+        return a * s, lambda dy: np.concatenate((dy * s, dy * a * s * (1 - s)), -1)
+    s = _sigmoid(u)
+    if act == "silu":
+        return u * s, lambda dy: dy * s * (1 + u * (1 - s))
+    return (np.maximum(u, 0), lambda dy: np.where(u > 0, dy, 0.0)) if act == "relu" else (u, lambda dy: dy)
+
+
+def groupnorm(x, G, gamma=None, beta=None, in_len=None, eps=1e-5, act="none", dy=None):
+    """Group norm of x[B,T,C] over the first in_len[b] frames and C/G neighbouring channels, then gamma, beta and the activation.
+    Frames beyond are 0, an utterance without any has mean = rstd = 0, a length out of range makes an utterance NaN.  Returns a dict of
+    y, mean, rstd, hat, u and, given dy, dx, dgamma, dbeta, du (0 and no part of them where the length is out of range)."""
+    x = np.asarray(x, dtype=np.float64)
+    B, T, C = x.shape
+    gamma = np.ones(C) if gamma is None else np.asarray(gamma, dtype=np.float64)
+    beta = np.zeros(C) if beta is None else np.asarray(beta, dtype=np.float64)
+    Cy = C // 2 if act == "glu" else C
+    o = dict(y=np.zeros((B, T, Cy)), mean=np.zeros((B, G)), rstd=np.zeros((B, G)), hat=np.zeros((B, T, C)), u=np.zeros((B, T, C)))
+    if dy is not None:
+        o.update(dx=np.zeros((B, T, C)), dgamma=np.zeros(C), dbeta=np.zeros(C), du=np.zeros((B, T, C)))
+    for b in range(B):
+        n = T if in_len is None else int(in_len[b])
+        if n < 0 or n > T:
+            o["y"][b] = o["mean"][b] = o["rstd"][b] = np.nan
+            continue
+        if n == 0:
+            continue
+        xb = x[b, :n].reshape(n, G, C // G)
+        mean = xb.mean((0, 2))
+        rstd = 1 / np.sqrt(((xb - mean[:, None]) ** 2).mean((0, 2)) + eps)
+        hat = (xb - mean[:, None]) * rstd[:, None]
+        u = gamma * hat.reshape(n, C) + beta
+        y, back = _act(u, act)
+        o["y"][b, :n], o["mean"][b], o["rstd"][b], o["hat"][b, :n], o["u"][b, :n] = y, mean, rstd, hat.reshape(n, C), u
+        if dy is not None:
+            du = back(np.asarray(dy, dtype=np.float64)[b, :n])
+            dh = (gamma * du).reshape(n, G, C // G)
+            dx = (dh - dh.mean((0, 2))[:, None] - hat * (dh * hat).mean((0, 2))[:, None]) * rstd[:, None]
+            o["dx"][b, :n], o["du"][b, :n] = dx.reshape(n, C), du
+            o["dgamma"] += (du * hat.reshape(n, C)).sum(0)
+            o["dbeta"] += du.sum(0)
+    return o
+
+
+# ----------------------------------------------------------------------------- clipped policy loss
+def policy(z, tokens, old, advantage, ref=None, weight=None, in_len=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, grad_scale=1.0):
+    """(frame_loss[B,T], loss[B], logprob[B,T], dz[B,T,C], f[B,T]) of weight * (-min(r A, clip(r) A) + kl_coef (exp(e) - e - 1)), r = exp(lp - old),
+    e = ref - lp, with lp the log-probability of tokens; f: grad_scale times the derivative with respect to lp.  advantage: [B] or [B,T]."""
+    z = np.asarray(z, dtype=np.float64)
+    B, T, C = z.shape
+    tokens = np.asarray(tokens)
+    w = np.ones((B, T)) if weight is None else np.asarray(weight, dtype=np.float64)
+    A = np.broadcast_to(np.asarray(advantage, dtype=np.float64).reshape((B, -1)), (B, T))
+    live, badlen = _frame_kind(in_len, B, T)
+    live = live & (tokens != -1) & (w != 0)
+    lps, odd = _log_probs(z)
+    known = (tokens >= 0) & (tokens < C)
+    lp = np.take_along_axis(lps, np.where(known, tokens, 0)[..., None], 2)[..., 0]
+    lp = np.where(known & ~odd, lp, np.nan)
+    with np.errstate(invalid="ignore", over="ignore"):
+        r = np.exp(lp - np.asarray(old, dtype=np.float64))
+        plain, held = r * A, np.clip(r, 1 - clip_low, 1 + clip_high) * A
+        inside = plain <= held
+        loss = np.where(A == 0, 0.0, -np.where(inside, plain, held))
+        d = np.where((A == 0) | ~inside, 0.0, -plain)
+        if kl_coef:
+            e = np.asarray(ref, dtype=np.float64) - lp
+            loss = loss + kl_coef * np.where(e == np.inf, np.inf, np.expm1(e) - e)
+            d = d - kl_coef * np.expm1(e)
+        loss = np.where(np.isnan(r), np.nan, loss * w)
+        frame = np.where(live, loss, np.where(badlen, np.nan, 0.0))
+        f = np.where(live & (np.abs(loss) <= np.finfo(np.float32).max), d * w * grad_scale, 0.0)
+    dz = -np.exp(lps) * np.where(f == 0, 0, f)[..., None]
+    rows = np.nonzero(f)
+    dz[rows[0], rows[1], tokens[rows]] = (f * -np.expm1(np.where(f == 0, 0.0, lp)))[rows]
+    return frame, frame.sum(1), np.where(live, lp, np.where(badlen, np.nan, 0.0)), dz, f
+
+
 # ----------------------------------------------------------------------------- optimiser
 def sgd_momentum(w, v, g, lr, momentum, weight_decay=0.0):
     """One SGD-with-momentum update (Sec. 4.1; heavy-ball form): returns (w', v') with
@@ -302,6 +389,92 @@ def sgd_momentum(w, v, g, lr, momentum, weight_decay=0.0):
     _load().orc_sgd_momentum(w2.ctypes.data_as(C.POINTER(C.c_double)), v2.ctypes.data_as(C.POINTER(C.c_double)), pg,
                              C.c_longlong(w2.size), C.c_double(lr), C.c_double(momentum), C.c_double(weight_decay))
     return w2.reshape(np.shape(w)), v2.reshape(np.shape(v))
+
+
+def mix32(x):
+    """The finaliser of MurmurHash3 (Appleby 2008) over uint64 arrays of numbers below 2^32."""
+    m = np.uint64(0xFFFFFFFF)
+    x = np.asarray(x, dtype=np.uint64)
+    x = x ^ (x >> np.uint64(16))
+    x = x * np.uint64(0x85EBCA6B) & m
+    x = x ^ (x >> np.uint64(13))
+    x = x * np.uint64(0xC2B2AE35) & m
+    return x ^ (x >> np.uint64(16))
+
+
+E4M3 = np.array([(f if e == 0 else (8 + f) * 2.0 ** (e - 1)) * 2.0 ** -9 for e in range(16) for f in range(8)])  # by code; the last is no number
+
+
+def from_e4m3(codes, exps):
+    """Values of moments in 8 bits (fp64): e4m3 numbers times 2^exponent of their block of 256; code 127 is NaN."""
+    codes = np.asarray(codes)
+    v = np.where(codes & 127 == 127, np.nan, E4M3[codes & 127]) * np.where(codes & 128, -1.0, 1.0)
+    return v * 2.0 ** np.repeat(np.asarray(exps, dtype=np.float64), 256)[:len(codes)]
+
+
+def to_e4m3(x, r, keep=False):
+    """fp32 values rounded at random to e4m3 codes and exponents: with r in [0, 1) a multiple of 2^-16 for each, up where the part of the
+    spacing that is left over and r make a whole.  keep: a value that is no zero does not become one."""
+    x = np.asarray(x, dtype=np.float64)
+    n = len(x)
+    codes, exps = np.zeros(n, dtype=np.uint8), np.zeros((n + 255) // 256, dtype=np.int8)
+    for k in range(len(exps)):
+        s = slice(256 * k, min(n, 256 * k + 256))
+        a = np.abs(x[s])
+        fin = np.isfinite(a)
+        most = a[fin].max() if fin.any() else 0.0
+        if most > 0:
+            E = -100
+            while 448.0 * 2.0 ** E < most:
+                E += 1
+            exps[k] = E
+        u = np.where(fin, a, 0.0) * 2.0 ** -float(exps[k])
+        low = np.searchsorted(E4M3[:127], u, side="right") - 1                       # the largest number that is not above u
+        high = np.minimum(low + 1, 126)
+        gap = np.where(high > low, E4M3[high] - E4M3[low], 1.0)
+        c = np.where((u - E4M3[low]) / gap + r[s] >= 1.0, high, low)
+        near = u < E4M3[8]                                                           # below 2^-6, in units of 2^-9, the sum is one of fp32
+        c = np.where(near, np.floor(np.float32(np.where(near, u, 0) * 512) + np.float32(r[s])).astype(int), c)
+        if keep:
+            c = np.where((u > 0) & (c == 0), 1, c)
+        codes[s] = np.where(fin, c, 127) | np.where(x[s] < 0, 128, 0)
+    return codes, exps
+
+
+def adamw_dither(seed, step, tensor, n):
+    """The 16 random bits of each of a tensor's n values, as multiples of 2^-16 in [0, 1)."""
+    key = mix32(mix32(mix32(np.uint64(seed)) ^ np.uint64(step & 0xFFFFFFFF)) ^ np.uint64(tensor))
+    i = np.arange(n, dtype=np.uint64)
+    h = mix32(((i >> np.uint64(1)) * np.uint64(0x9E3779B1) + key) & np.uint64(0xFFFFFFFF))
+    return np.where(i % np.uint64(2) == 0, h & np.uint64(0xFFFF), h >> np.uint64(16)).astype(np.float64) / 65536.0
+
+
+def adamw_norm(grads, grad_scale=1.0):
+    return abs(grad_scale) * np.sqrt(sum((np.asarray(g, dtype=np.float64) ** 2).sum() for g in grads))
+
+
+def adamw_factor(grads, grad_scale=1.0, max_norm=0.0):
+    """What gradients are multiplied by (fp64)."""
+    norm = adamw_norm(grads, grad_scale)
+    return grad_scale * (min(1.0, max_norm / (norm + 1e-6)) if max_norm > 0 else 1.0)
+
+
+def adamw_moments(g, m, v, factor, beta1, beta2):
+    """The moments in fp32, every product and sum rounded as written (factor, beta and 1 - beta rounded to fp32 first)."""
+    f = np.float32
+    g = np.asarray(g, dtype=f) * f(factor)
+    m = np.asarray(m, dtype=f) * f(beta1) + g * f(1 - beta1)
+    return m, np.asarray(v, dtype=f) * f(beta2) + (g * g) * f(1 - beta2)
+
+
+def adamw(w, g, m, v, factor, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0):
+    """(w, m, v) after one step, fp64."""
+    w, g, m, v = (np.asarray(a, dtype=np.float64) for a in (w, g, m, v))
+    g = g * factor
+    m = m * beta1 + g * (1 - beta1)
+    v = v * beta2 + g * g * (1 - beta2)
+    with np.errstate(invalid="ignore"):
+        return w * (1 - lr * weight_decay) - lr / (1 - beta1 ** step) * m / (np.sqrt(v) / np.sqrt(1 - beta2 ** step) + eps), m, v
 
 
 # ----------------------------------------------------------------------------- CTC

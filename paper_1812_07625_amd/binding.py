@@ -12,6 +12,7 @@ import os
 import torch
 
 W2L_F32, W2L_BF16 = 0, 1
+W2L_ACT_NONE, W2L_ACT_RELU, W2L_ACT_SILU, W2L_ACT_GLU = 0, 1, 2, 3
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # W2L_LIB: another build of the same sources (the sanitizer run of the host-side tests uses this)
 _LIB_PATH = os.environ.get("W2L_LIB") or os.path.join(_HERE, "libw2l.so")
@@ -27,6 +28,9 @@ __all__ = [
     "w2l_token_logprob_workspace_bytes", "w2l_token_logprob_fwd", "w2l_token_logprob_bwd",
     "w2l_token_logprob_launch_config", "w2l_distill_workspace_bytes", "w2l_distill_fwd_bwd", "w2l_distill_launch_config",
     "w2l_frame_ids_check_host",
+    "W2L_ACT_NONE", "W2L_ACT_RELU", "W2L_ACT_SILU", "W2L_ACT_GLU", "w2l_groupnorm_workspace_bytes", "w2l_groupnorm_fwd", "w2l_groupnorm_bwd",
+    "w2l_policy_workspace_bytes", "w2l_policy_fwd_bwd",
+    "w2l_adamw_tensor", "adamw_tensors", "w2l_adamw_workspace_bytes", "w2l_adamw_step",
     "w2l_train_step_workspace_bytes", "w2l_train_step", "w2l_train_step_asg_workspace_bytes", "w2l_train_step_asg",
     "w2l_train_step_launch_config", "w2l_train_step_layer_config", "w2l_sgd_momentum_step",
     "w2l_probe_mfma", "raw",
@@ -42,6 +46,11 @@ class W2LError(RuntimeError):
 
 class w2l_layer(C.Structure):
     _fields_ = [("k", C.c_int), ("stride", C.c_int), ("cin", C.c_int), ("cout", C.c_int), ("glu", C.c_int)]
+
+
+class w2l_adamw_tensor(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("w_lowp", C.c_void_p), ("n", C.c_longlong), ("weight_decay", C.c_double)]
 
 
 def lib_path() -> str:
@@ -79,6 +88,13 @@ def _load():
         "w2l_token_logprob_launch_config": (i, [i] * 5 + [C.POINTER(C.c_int)] * 3),
         "w2l_distill_launch_config": (i, [i] * 5 + [C.POINTER(C.c_int)] * 3),
         "w2l_frame_ids_check_host": (i, [vp, vp] + [i] * 4),
+        "w2l_groupnorm_workspace_bytes": (sz, [i] * 6),
+        "w2l_groupnorm_fwd": (i, [vp] * 7 + [i] * 4 + [f] + [i] * 2 + [vp, sz, vp]),
+        "w2l_groupnorm_bwd": (i, [vp] * 10 + [i] * 7 + [vp, sz, vp]),
+        "w2l_policy_workspace_bytes": (sz, [i] * 4),
+        "w2l_policy_fwd_bwd": (i, [vp] * 5 + [i] + [vp] * 6 + [i] * 3 + [f] * 4 + [i] * 3 + [vp, sz, vp]),
+        "w2l_adamw_workspace_bytes": (sz, [vp, i]),
+        "w2l_adamw_step": (i, [vp, i, i, i, ll] + [C.c_double] * 6 + [C.c_uint] + [vp] * 4 + [sz, vp]),
         "w2l_ctc_workspace_bytes": (sz, [i] * 4),
         "w2l_ctc_fwd_bwd": (i, [vp, i, vp, vp, vp, vp, vp, i, i, i, i, i, f, vp, sz, vp]),
         "w2l_ctc_fwd_bwd_noalloc": (i, [vp, i, vp, vp, vp, vp, vp, i, i, i, i, i, f, vp]),
@@ -252,7 +268,7 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 _F32, _I32 = torch.float32, torch.int32
 
 
-def _pointers(dev, operands):
+def _pointers(dev, operands, where="the scores are"):
     """Device pointers of operands (name, tensor, shape, dtype), which have to be of that shape and type and on device `dev` (None stays None)."""
     out = []
     for name, t, shape, dtype in operands:
@@ -265,7 +281,7 @@ def _pointers(dev, operands):
         elif t.shape != shape:
             raise ValueError("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
         elif t.get_device() != dev:
-            raise ValueError("%s is on %s, the scores are on cuda:%d" % (name, t.device, dev))
+            raise ValueError("%s is on %s, %s on cuda:%d" % (name, t.device, where, dev))
         else:
             raise ValueError("%s must be contiguous" % name)
     return out
@@ -307,11 +323,11 @@ def _call(fn, where, dev, args, stream):
         raise W2LError(rc, where)
 
 
-def _scratch(workspace, dev):
+def _scratch(workspace, dev, where="the scores are"):
     if workspace is None:
         return None, 0
     if workspace.get_device() != dev:
-        raise ValueError("workspace is on %s, the scores are on cuda:%d" % (workspace.device, dev))
+        raise ValueError("workspace is on %s, %s on cuda:%d" % (workspace.device, where, dev))
     return _p(workspace), workspace.nbytes
 
 
@@ -391,6 +407,127 @@ def w2l_frame_ids_check_host(ids, in_len, Cc) -> int:
     il = None if in_len is None else np.ascontiguousarray(in_len, dtype=np.int32)
     B, T, n = t.shape
     return raw.w2l_frame_ids_check_host(t.ctypes.data, None if il is None else il.ctypes.data, B, T, Cc, n)
+
+
+def w2l_policy_workspace_bytes(B, Tp, Cc, dtype) -> int:
+    return raw.w2l_policy_workspace_bytes(B, Tp, Cc, dtype)
+
+
+def w2l_policy_fwd_bwd(z, tokens, old_logprob, advantage, frame_loss, loss=None, dz=None, logprob=None, ref_logprob=None, weight=None, in_len=None,
+                       clip_low=0.2, clip_high=0.2, kl_coef=0.0, grad_scale=1.0, accumulate=False, workspace=None, stream=None):
+    """Clipped policy loss of sampled tokens[B,T] under scores z[B,T,C], with a KL term against ref_logprob, and its gradient dz.
+    advantage: [B] or [B,T]."""
+    shape, dt, dev = _scores(z)
+    B, T, Cc = shape
+    gt, gtype = (dt, None) if dz is None else (_dt(dz), dz.dtype)
+    BT = (B, T)
+    per_frame = advantage.dim() == 2
+    ptr = _pointers(dev, (("scores", z, shape, z.dtype), ("tokens", tokens, BT, _I32), ("old_logprob", old_logprob, BT, _F32),
+                          ("ref_logprob", ref_logprob, BT, _F32), ("advantage", advantage, BT if per_frame else (B,), _F32)))
+    out = _pointers(dev, (("weight", weight, BT, _F32), ("in_len", in_len, (B,), _I32), ("frame_loss", frame_loss, BT, _F32), ("loss", loss, (B,), _F32),
+                          ("logprob", logprob, BT, _F32), ("dz", dz, shape, gtype)))
+    _call(raw.w2l_policy_fwd_bwd, "w2l_policy_fwd_bwd", dev, (*ptr, int(per_frame), *out, B, T, Cc, clip_low, clip_high, kl_coef, grad_scale, dt, gt,
+                                                              1 if accumulate else 0, *_scratch(workspace, dev)), stream)
+    return frame_loss, loss, dz
+
+
+def w2l_groupnorm_workspace_bytes(B, T, Cc, groups, act, dtype) -> int:
+    return raw.w2l_groupnorm_workspace_bytes(B, T, Cc, groups, act, dtype)
+
+
+def _norm_input(x, act):
+    """Shape of x[B,T,C], of the activation's output, type code and device index."""
+    if x.dim() != 3:
+        raise ValueError("x must be [B, T, C], not %s" % (tuple(x.shape),))
+    dev = x.get_device()
+    if dev < 0:
+        raise ValueError("x must be on a GPU")
+    B, T, Cc = x.shape
+    return x.shape, (B, T, Cc // 2 if act == W2L_ACT_GLU else Cc), _dt(x), dev
+
+
+def w2l_groupnorm_fwd(x, y, mean, rstd, gamma=None, beta=None, in_len=None, eps=1e-5, act=W2L_ACT_NONE, workspace=None, stream=None):
+    """y = act(gamma * group norm of x[B,T,C] + beta); mean, rstd [B,G] receive the statistics, and their shape says how many groups there are.
+    y: [B,T,C], with W2L_ACT_GLU [B,T,C/2]."""
+    shape, out, dt, dev = _norm_input(x, act)
+    B, T, Cc = shape
+    G = mean.shape[-1]
+    ptr = _pointers(dev, (("x", x, shape, x.dtype), ("gamma", gamma, (Cc,), _F32), ("beta", beta, (Cc,), _F32), ("in_len", in_len, (B,), _I32),
+                          ("y", y, out, x.dtype), ("mean", mean, (B, G), _F32), ("rstd", rstd, (B, G), _F32)), "x is")
+    _call(raw.w2l_groupnorm_fwd, "w2l_groupnorm_fwd", dev, (*ptr, B, T, Cc, G, eps, act, dt, *_scratch(workspace, dev, "x is")), stream)
+    return y, mean, rstd
+
+
+def w2l_groupnorm_bwd(x, dy, mean, rstd, dx, gamma=None, beta=None, dgamma=None, dbeta=None, in_len=None, act=W2L_ACT_NONE, accumulate=False,
+                      workspace=None, stream=None):
+    """dx[B,T,C], dgamma[C] and dbeta[C] (accumulate: added to these two) of w2l_groupnorm_fwd from dy and the statistics it wrote."""
+    shape, out, dt, dev = _norm_input(x, act)
+    B, T, Cc = shape
+    G = mean.shape[-1]
+    ptr = _pointers(dev, (("x", x, shape, x.dtype), ("dy", dy, out, x.dtype), ("mean", mean, (B, G), _F32), ("rstd", rstd, (B, G), _F32),
+                          ("gamma", gamma, (Cc,), _F32), ("beta", beta, (Cc,), _F32), ("in_len", in_len, (B,), _I32), ("dx", dx, shape, x.dtype),
+                          ("dgamma", dgamma, (Cc,), _F32), ("dbeta", dbeta, (Cc,), _F32)), "x is")
+    _call(raw.w2l_groupnorm_bwd, "w2l_groupnorm_bwd", dev, (*ptr, B, T, Cc, G, act, dt, 1 if accumulate else 0, *_scratch(workspace, dev, "x is")), stream)
+    return dx, dgamma, dbeta
+
+
+class AdamwTensors:
+    """The tensors of an optimiser as w2l_adamw_step takes them; holds them, and their addresses at the time it was made."""
+
+    def __init__(self, rows):
+        rows = list(rows)
+        if not rows:
+            raise ValueError("there are no tensors")
+        first = rows[0]["w"]
+        dev = first.get_device()
+        if dev < 0:
+            raise ValueError("tensors must be on a GPU")
+        gtype, mtype = rows[0]["grad"].dtype, rows[0]["m"].dtype
+        if mtype not in (torch.float32, torch.float8_e4m3fn, torch.uint8):
+            raise TypeError("moments must be float32, or float8_e4m3fn (uint8) with exponents, not %s" % mtype)
+        self.device, self.bits = dev, 32 if mtype == torch.float32 else 8
+        self.grad_dtype, self.array, self.held = _dt(rows[0]["grad"]), (w2l_adamw_tensor * len(rows))(), rows
+        known = {"w", "grad", "m", "v", "m_exp", "v_exp", "w_lowp", "weight_decay"}
+        for i, (a, row) in enumerate(zip(self.array, rows)):
+            if not set(row) <= known:
+                raise ValueError("tensor %d: %s is none of %s" % (i, sorted(set(row) - known), sorted(known)))
+            shape, n = row["w"].shape, row["w"].numel()
+            blocks = ((n + 255) // 256,)
+            exps = [(k, row.get(k), blocks, torch.int8) for k in ("m_exp", "v_exp")]
+            if self.bits == 8 and n and any(t is None for _, t, _, _ in exps):
+                raise ValueError("tensor %d: moments in 8 bits need m_exp and v_exp" % i)
+            ptr = _pointers(dev, [("w", row["w"], shape, _F32), ("grad", row["grad"], shape, gtype), ("m", row["m"], shape, mtype), ("v", row["v"], shape, mtype)]
+                            + (exps if self.bits == 8 else [("m_exp", None, None, None)] * 2) + [("w_lowp", row.get("w_lowp"), shape, torch.bfloat16)],
+                            "tensor 0 is")
+            a.w, a.grad, a.m, a.v, a.m_exp, a.v_exp, a.w_lowp = ptr
+            a.n, a.weight_decay = n, row.get("weight_decay", 0.0)
+
+    def __len__(self):
+        return len(self.array)
+
+
+def adamw_tensors(rows):
+    """What w2l_adamw_step updates: a dict a tensor, of w (fp32), grad (fp32 or bf16), m, v, and optionally w_lowp (bf16) and weight_decay.  m and v are
+    fp32, or float8_e4m3fn (or uint8) with m_exp, v_exp, int8 [ceil(n / 256)].  To be made once: gradients have to stay where they are."""
+    return AdamwTensors(rows)
+
+
+def w2l_adamw_workspace_bytes(tensors) -> int:
+    return raw.w2l_adamw_workspace_bytes(tensors.array, len(tensors.array))
+
+
+def w2l_adamw_step(tensors, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, max_norm=0.0, seed=0, grad_norm=None, lr_dev=None, step_dev=None,
+                   workspace=None, stream=None):
+    """One AdamW step over adamw_tensors(...): see w2l.h.  grad_norm, lr_dev (fp32) and step_dev (int32): tensors of one value on the device."""
+    dev = tensors.device
+    one = []
+    for name, t, dtype in (("lr_dev", lr_dev, _F32), ("step_dev", step_dev, _I32), ("grad_norm", grad_norm, _F32)):
+        if t is not None and t.numel() != 1:
+            raise ValueError("%s must have one value" % name)
+        one.append((name, t, None if t is None else t.shape, dtype))
+    _call(raw.w2l_adamw_step, "w2l_adamw_step", dev, (tensors.array, len(tensors.array), tensors.grad_dtype, tensors.bits, step, lr, beta1, beta2, eps, grad_scale,
+                                                      max_norm, seed & 0xFFFFFFFF, *_pointers(dev, one, "the tensors are"),
+                                                      *_scratch(workspace, dev, "the tensors are")), stream)
 
 
 def w2l_sgd_momentum_step(w, v, grad, w_lowp, lr, momentum, weight_decay=0.0, stream=None):

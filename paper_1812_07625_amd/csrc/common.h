@@ -235,6 +235,10 @@ int asg_fwd_bwd_strided(const float* emissions, const float* trans, const int* t
                         float* loss, float* grad_emissions, float* grad_trans, int B, int Tp, int C, int Lmax, float grad_scale,
                         void* workspace, size_t ws_bytes, void* stream, int len_div);
 
+// Of rows that w2l_token_logprob_fwd would give several workgroups: what each finds of its part, (m or -inf, s, u, 0) with s = sum exp(x - m), into
+// ws [rows][*parts] float4, w2l_token_logprob_workspace_bytes() with K = 0 (frame_scores.hip)
+int frame_row_sums(const void* z, const int* in_len, int B, int Tp, int C, int dtype, void* ws, int* parts, hipStream_t st);
+
 // GLU with an explicit output layout (elementwise.hip).  y (and dh) are dense [B*Tp, Cout]
 // ([B*Tp, Cout/2]); the output is written with the given pitch and halo, halo and slack
 // frames included (as zeros).  live, here and below: as ConvDesc::h_live.

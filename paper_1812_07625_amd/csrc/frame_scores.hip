@@ -1184,6 +1184,16 @@ int launch_distill(const Plan& p, hipStream_t st, const void* z, const Teacher& 
 
 }  // namespace
 
+int w2l::frame_row_sums(const void* z, const int* in_len, int B, int Tp, int C, int dtype, void* ws, int* parts, hipStream_t st)
+{
+    const TokenOut none{nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0};
+    const Plan p = plan_tokens(C, 0, dtype);
+    const Frames fr = frames_of(in_len, B, Tp);
+    *parts = p.G;
+    return dtype == W2L_BF16 ? launch_tokens<bf16_t>(p, st, z, nullptr, fr, none, ws, C, LOG2E, false)
+                             : launch_tokens<float>(p, st, z, nullptr, fr, none, ws, C, LOG2E, false);
+}
+
 extern "C" size_t w2l_token_logprob_workspace_bytes(int B, int Tp, int C, int K, int z_dtype)
 {
     if (!shape_ok(B, Tp, C, 0, K) || !valid_dtype(z_dtype)) return 0;
