@@ -9,70 +9,70 @@
 // knows of its channels stays in registers from row to row.
 #include "lanes.h"
 
+#include <type_traits>
+
 using namespace w2l;
 
+#ifndef GROUP_RULE
+#define GROUP_RULE bytes <= (256 << 10)
+#endif
 namespace {
 
 constexpr int MAX_CHANNELS = 8192, MAX_FRAMES = 1 << 24, MAX_THREADS = 512;  // (8192: a pair of floats a channel fits 64 KB of LDS)
 
-// N values of one channel vector
-template <typename T, int N> struct Pack;
-template <int N> struct Pack<float, N> {
-    typedef float raw __attribute__((ext_vector_type(N)));
-    static __device__ __forceinline__ void load(const float* p, float (&x)[N])
-    {
-        const raw q = *reinterpret_cast<const raw*>(p);
+// A vector of N neighbouring channels as it lies in memory, and its values
+template <typename T, int N> struct Vec {
+    typedef unsigned raw __attribute__((ext_vector_type(N * sizeof(T) / 4)));
+};
+template <> struct Vec<float, 1> { typedef unsigned raw; };
+template <> struct Vec<bf16_t, 2> { typedef unsigned raw; };
+template <> struct Vec<bf16_t, 1> { typedef unsigned short raw; };
+template <typename T, int N> using raw_t = typename Vec<T, N>::raw;
+
+template <typename T, int N>
+__device__ __forceinline__ raw_t<T, N> fetch(const T* p) { return *reinterpret_cast<const raw_t<T, N>*>(p); }
+template <typename T, int N>
+__device__ __forceinline__ void unpack(raw_t<T, N> q, float (&x)[N])
+{
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (N == 1) x[0] = __uint_as_float(q);
+        else
 #pragma unroll
-        for (int j = 0; j < N; ++j) x[j] = q[j];
-    }
-    static __device__ __forceinline__ void store(float* p, const float (&x)[N])
-    {
-        raw q;
+            for (int j = 0; j < N; ++j) x[j] = __uint_as_float(q[j]);
+    } else if constexpr (N == 1) x[0] = bf16_to_f32(q);
+    else
 #pragma unroll
-        for (int j = 0; j < N; ++j) q[j] = x[j];
-        *reinterpret_cast<raw*>(p) = q;
-    }
-};
-template <> struct Pack<float, 1> {
-    static __device__ __forceinline__ void load(const float* p, float (&x)[1]) { x[0] = *p; }
-    static __device__ __forceinline__ void store(float* p, const float (&x)[1]) { *p = x[0]; }
-};
-template <int N> struct Pack<bf16_t, N> {
-    typedef unsigned raw __attribute__((ext_vector_type(N / 2)));
-    static __device__ __forceinline__ void load(const bf16_t* p, float (&x)[N])
-    {
-        const raw q = *reinterpret_cast<const raw*>(p);
+        for (int j = 0; j < N / 2; ++j) {
+            unsigned w;
+            if constexpr (N == 2) w = q;
+            else w = q[j];
+            x[2 * j] = __uint_as_float(w << 16);
+            x[2 * j + 1] = __uint_as_float(w & 0xffff0000u);
+        }
+}
+template <typename T, int N>
+__device__ __forceinline__ void put(T* p, const float (&x)[N])
+{
+    raw_t<T, N> q;
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (N == 1) q = __float_as_uint(x[0]);
+        else
 #pragma unroll
-        for (int j = 0; j < N / 2; ++j) { x[2 * j] = __uint_as_float(q[j] << 16); x[2 * j + 1] = __uint_as_float(q[j] & 0xffff0000u); }
-    }
-    static __device__ __forceinline__ void store(bf16_t* p, const float (&x)[N])
-    {
-        raw q;
+            for (int j = 0; j < N; ++j) q[j] = __float_as_uint(x[j]);
+    } else if constexpr (N == 1) q = f32_to_bf16(x[0]);
+    else
 #pragma unroll
-        for (int j = 0; j < N / 2; ++j) q[j] = (unsigned)f32_to_bf16(x[2 * j]) | (unsigned)f32_to_bf16(x[2 * j + 1]) << 16;
-        *reinterpret_cast<raw*>(p) = q;
-    }
-};
-template <> struct Pack<bf16_t, 2> {
-    static __device__ __forceinline__ void load(const bf16_t* p, float (&x)[2])
-    {
-        const unsigned q = *reinterpret_cast<const unsigned*>(p);
-        x[0] = __uint_as_float(q << 16);
-        x[1] = __uint_as_float(q & 0xffff0000u);
-    }
-    static __device__ __forceinline__ void store(bf16_t* p, const float (&x)[2])
-    {
-        *reinterpret_cast<unsigned*>(p) = (unsigned)f32_to_bf16(x[0]) | (unsigned)f32_to_bf16(x[1]) << 16;
-    }
-};
-template <> struct Pack<bf16_t, 1> {
-    static __device__ __forceinline__ void load(const bf16_t* p, float (&x)[1]) { x[0] = bf16_to_f32(*p); }
-    static __device__ __forceinline__ void store(bf16_t* p, const float (&x)[1]) { *p = f32_to_bf16(x[0]); }
-};
+        for (int j = 0; j < N / 2; ++j) {
+            const unsigned w = (unsigned)f32_to_bf16(x[2 * j]) | (unsigned)f32_to_bf16(x[2 * j + 1]) << 16;
+            if constexpr (N == 2) q = w;
+            else q[j] = w;
+        }
+    *reinterpret_cast<raw_t<T, N>*>(p) = q;
+}
 
 // How a workgroup takes a run of `rows` frames: `cols` threads side by side, `lanes` rows at a time
 struct Shape {
-    int B, T, C, G, Cg, rows, runs, cols, lanes, subs;  // subs: partial results of a group that a run leaves
+    int B, T, C, G, Cg, rows, runs, cols, lanes;
     const int* in_len;
 };
 // frames of utterance b; -1: its in_len is out of range
@@ -85,7 +85,7 @@ __device__ __forceinline__ int frames_of(const Shape& s, int b)
 
 // ---- activations ---------------------------------------------------------------------------------------------
 // y = act(u), du = dy act'(u).  GLU takes a value and a gate, and gives the gradient of both.
-__device__ __forceinline__ float sigmoid(float u) { return 1.f / (1.f + expf(-u)); }
+__device__ __forceinline__ float sigmoid(float u) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * -1.44269504088896f)); }
 template <int ACT>
 __device__ __forceinline__ float act(float u, float gate)
 {
@@ -112,169 +112,278 @@ __device__ __forceinline__ void act_bwd(float u, float gate, float dy, float& du
 // ---- statistics ----------------------------------------------------------------------------------------------
 // A thread sums its channels' deviations from the first value it reads of each, and their squares.  With n values that first one is at most
 // sqrt(n) deviations off the mean of the n, so that the sums lose at most a factor of n (64 at most) of fp32's precision, whatever the
-// channel's level; partial results are then joined as count, mean, and squared deviations about the mean, where nothing cancels.
-struct Part {
-    double mean;  // (means are joined in 64 bits: a group's may be small beside its channels')
-    float n, m2;
+// channel's level.  From there on a group's sum and sum of squares are in 64 bits, where the difference of mean square and squared mean loses nothing that
+// counts: a level of 10^5 deviations leaves 10^-6 of the variance.
+template <int N>
+struct Deviations {
+    float base[N], sum[N], sq[N];
+    int n;
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) base[j] = sum[j] = sq[j] = 0.f;
+        n = 0;
+    }
+    __device__ __forceinline__ void add(const float (&y)[N])
+    {
+        if (n == 0)
+#pragma unroll
+            for (int j = 0; j < N; ++j) base[j] = y[j];
+        ++n;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float d = y[j] - base[j];
+            sum[j] += d;
+            sq[j] = __builtin_fmaf(d, d, sq[j]);
+        }
+    }
+    // sum and sum of squares of all, where the channels are of one group
+    __device__ __forceinline__ double2 group_sums() const
+    {
+        const float inv = n ? 1.f / (float)n : 0.f;
+        float mean[N], q = 0.f, off = 0.f, about = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float m = sum[j] * inv;
+            mean[j] = base[j] + m;
+            q += __builtin_fmaf(-m, sum[j], sq[j]);
+            off += mean[j] - mean[0];
+        }
+        const float m = off * (1.f / N);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float d = (mean[j] - mean[0]) - m;
+            about = __builtin_fmaf(d, d, about);
+        }
+        const double k = (double)n * N, all = (double)mean[0] + m;
+        return make_double2(k * all, k * all * all + (double)__builtin_fmaf((float)n, about, q));
+    }
 };
-__device__ __forceinline__ double sum64(double v, int width = 64)
+__device__ __forceinline__ double2 sum64(double2 v, int width)
 {
-    for (int o = width >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    for (int o = width >> 1; o > 0; o >>= 1) {
+        v.x += __shfl_xor(v.x, o, 64);
+        v.y += __shfl_xor(v.y, o, 64);
+    }
     return v;
 }
-
-template <typename T, int N>
-__global__ __launch_bounds__(MAX_THREADS) void norm_stats_k(const T* __restrict__ x, Shape s, Part* __restrict__ parts)
+// lanes that add up a group's partial results: as many as there are threads for, a power of two up to a wavefront and no more than there are results
+__device__ __forceinline__ int team_of(int G, int results)
 {
-    extern __shared__ float2 chan[];  // [lanes][C]: mean and squared deviations of a channel in the rows of one lane
+    int team = 64;
+    while (team > 1 && (G * team > (int)blockDim.x || team >= 2 * results)) team >>= 1;
+    return team;
+}
+
+// sums [B][runs][G]: sum and sum of squares of a run.  WHOLE: a vector's channels are all of one group
+template <typename T, int N, bool WHOLE>
+__global__ __launch_bounds__(MAX_THREADS) void norm_stats_k(const T* __restrict__ x, Shape s, double2* __restrict__ sums)
+{
+    extern __shared__ double2 lds[];  // [lanes][vectors]: a thread's sums;  !WHOLE: [lanes][C] of floats, a channel's mean and squared deviations
+    constexpr int U = 4;
     const int b = blockIdx.y, run = blockIdx.x, len = frames_of(s, b);
     const int t0 = run * s.rows, t1 = t0 + s.rows < len ? t0 + s.rows : len;
-    if (t0 >= t1) return;  // (norm_apply_k knows that there is nothing)
+    if (t0 >= t1) return;  // (what reads the sums knows that there are none)
     const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, nv = s.C / N, here = t1 - t0;
     if (lane < s.lanes)
         for (int v = col; v < nv; v += s.cols) {
             const T* const p = x + ((size_t)b * s.T + t0) * s.C + (size_t)v * N;
-            float base[N], sum[N], sq[N];
+            Deviations<N> d;
+            d.clear();
+            for (int t = lane; t < here; t += U * s.lanes) {
+                raw_t<T, N> q[U];
 #pragma unroll
-            for (int j = 0; j < N; ++j) base[j] = sum[j] = sq[j] = 0.f;
-            int n = 0;
-            if (lane < here) {
-                Pack<T, N>::load(p + (size_t)lane * s.C, base);
-                n = 1;
-            }
-#pragma unroll 4
-            for (int t = lane + s.lanes; t < here; t += s.lanes, ++n) {
-                float y[N];
-                Pack<T, N>::load(p + (size_t)t * s.C, y);
+                for (int k = 0; k < U; ++k) q[k] = fetch<T, N>(p + (size_t)(t + k * s.lanes < here ? t + k * s.lanes : t) * s.C);
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float d = y[j] - base[j];
-                    sum[j] += d;
-                    sq[j] = __builtin_fmaf(d, d, sq[j]);
+                for (int k = 0; k < U; ++k) {
+                    if (t + k * s.lanes >= here) break;
+                    float y[N];
+                    unpack<T, N>(q[k], y);
+                    d.add(y);
                 }
             }
-            const float inv = n ? 1.f / (float)n : 0.f;
+            if (WHOLE) lds[lane * nv + v] = d.group_sums();
+            else
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float m = sum[j] * inv;
-                chan[(size_t)lane * s.C + v * N + j] = make_float2(base[j] + m, fmaxf(__builtin_fmaf(-m, sum[j], sq[j]), 0.f));
-            }
+                for (int j = 0; j < N; ++j) {
+                    const float n = (float)d.n, m = d.n ? d.sum[j] / n : 0.f;
+                    reinterpret_cast<float2*>(lds)[lane * s.C + v * N + j] = make_float2(d.base[j] + m, __builtin_fmaf(-m, d.sum[j], d.sq[j]));
+                }
         }
     __syncthreads();
-    // a wavefront takes a share of a group, `subs` of them each group
-    const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, l = threadIdx.x & 63;
-    const int live = here < s.lanes ? here : s.lanes, entries = live * s.Cg, share = (entries + s.subs - 1) / s.subs;
-    for (int q = wave; q < s.G * s.subs; q += waves) {
-        const int g = q / s.subs, e0 = (q % s.subs) * share, e1 = e0 + share < entries ? e0 + share : entries;
-        float n = 0.f;
-        double sum = 0.;
-        for (int e = e0 + l; e < e1; e += 64) {
-            const int r = e / s.Cg, c = g * s.Cg + (e - r * s.Cg);
-            const float nr = (float)((here - r + s.lanes - 1) / s.lanes);
-            n += nr;
-            sum = __builtin_fma((double)nr, (double)chan[(size_t)r * s.C + c].x, sum);
-        }
-        n = wave64(n, Sum());
-        const double mean = n > 0.f ? sum64(sum) / n : 0.;
-        float m2 = 0.f;
-        for (int e = e0 + l; e < e1; e += 64) {
-            const int r = e / s.Cg, c = g * s.Cg + (e - r * s.Cg);
-            const float nr = (float)((here - r + s.lanes - 1) / s.lanes);
-            const float2 k = chan[(size_t)r * s.C + c];
-            const float d = (float)(k.x - mean);
-            m2 += __builtin_fmaf(nr * d, d, k.y);
-        }
-        m2 = wave64(m2, Sum());
-        if (l == 0) parts[((size_t)b * s.runs + run) * s.G * s.subs + q] = {mean, n, m2};
+    const int live = here < s.lanes ? here : s.lanes;  // lanes that had a frame
+    const int per = WHOLE ? s.Cg / N : s.Cg, pitch = WHOLE ? nv : s.C, team = team_of(s.G, per), l = threadIdx.x & (team - 1), teams = blockDim.x / team;
+    for (int g0 = 0; g0 < s.G; g0 += teams) {
+        const int g = g0 + threadIdx.x / team;
+        double2 k = make_double2(0., 0.);
+        if (g < s.G)
+            for (int r = 0; r < live; ++r) {
+                const double n = (double)((here - r + s.lanes - 1) / s.lanes);
+                for (int c = l; c < per; c += team) {
+                    const int i = r * pitch + g * per + c;
+                    if (WHOLE) {
+                        k.x += lds[i].x;
+                        k.y += lds[i].y;
+                    } else {
+                        const float2 o = reinterpret_cast<const float2*>(lds)[i];
+                        const double m = o.x;
+                        k.x += n * m;
+                        k.y += n * m * m + (double)o.y;
+                    }
+                }
+            }
+        k = sum64(k, team);
+        if (g < s.G && l == 0) sums[((size_t)b * s.runs + run) * s.G + g] = k;
     }
 }
 
-// mean and 1 / deviation of every group of utterance b, into LDS
-__device__ __forceinline__ void join_stats(const Shape& s, const Part* __restrict__ parts, int b, int len, float eps, float2* stat)
+// mean and 1 / deviation from a group's sums; inv: 1 / its values (0: it has none)
+__device__ __forceinline__ float2 stat_of(double2 k, double inv, float eps)
 {
-    const int runs = (len + s.rows - 1) / s.rows, count = runs * s.subs, per = s.G * s.subs;
-    const double n = (double)len * s.Cg;
-    // a team of lanes a group: as many as there are threads for, a power of two up to a wavefront
-    int team = 64;
-    while (team > 1 && s.G * team > (int)blockDim.x) team >>= 1;
-    const int l = threadIdx.x & (team - 1), teams = blockDim.x / team;
+    const double mean = k.x * inv, var = k.y * inv - mean * mean;
+    return make_float2((float)mean, inv > 0. ? 1.f / sqrtf((var < 0. ? 0.f : (float)var) + eps) : 0.f);
+}
+// of every group of utterance b, into LDS
+__device__ __forceinline__ void join_stats(const Shape& s, const double2* __restrict__ sums, int b, int len, float eps, float2* stat)
+{
+    const int runs = (len + s.rows - 1) / s.rows, team = team_of(s.G, runs), l = threadIdx.x & (team - 1), teams = blockDim.x / team;
+    const double inv = len > 0 ? 1. / ((double)len * s.Cg) : 0.;
     for (int g0 = 0; g0 < s.G; g0 += teams) {
         const int g = g0 + threadIdx.x / team;
-        const bool on = g < s.G;
-        double sum = 0., m2 = 0.;
-        const Part* const p = parts + (size_t)b * s.runs * per;
-        auto at = [&](int i) { return p[(size_t)(i / s.subs) * per + (size_t)g * s.subs + i % s.subs]; };
-        if (on)
-            for (int i = l; i < count; i += team) {
-                const Part q = at(i);
-                sum = __builtin_fma((double)q.n, q.mean, sum);
+        double2 k = make_double2(0., 0.);
+        if (g < s.G)
+#pragma unroll 4
+            for (int r = l; r < runs; r += team) {
+                const double2 o = sums[((size_t)b * s.runs + r) * s.G + g];
+                k.x += o.x;
+                k.y += o.y;
             }
-        sum = sum64(sum, team);
-        const double mean = len > 0 ? sum / n : 0.;
-        if (on)
-            for (int i = l; i < count; i += team) {
-                const Part q = at(i);
-                const double d = q.mean - mean;
-                m2 += __builtin_fma(q.n * d, d, (double)q.m2);
-            }
-        m2 = sum64(m2, team);
-        if (on && l == 0) stat[g] = make_float2((float)mean, len > 0 ? 1.f / sqrtf((float)(m2 / n) + eps) : 0.f);
+        k = sum64(k, team);
+        if (g < s.G && l == 0) stat[g] = stat_of(k, inv, eps);
     }
     __syncthreads();
+}
+
+// Values of channels c0 .. c0 + N of a vector over channels; `none` where there is none
+template <int N>
+__device__ __forceinline__ void channels_of(const float* __restrict__ p, int c0, float none, float (&out)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; ++j) out[j] = none;
+    if (!p) return;
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) {
+            const float4 q = *reinterpret_cast<const float4*>(p + c0 + j);
+            out[j] = q.x; out[j + 1] = q.y; out[j + 2] = q.z; out[j + 3] = q.w;
+        }
+    } else
+#pragma unroll
+        for (int j = 0; j < N; ++j) out[j] = p[c0 + j];
+}
+// f(j, value of channel c0 + j's group), a value being looked up (value(group)) where the group changes
+template <int N, typename V, typename F>
+__device__ __forceinline__ void groups_of(const Shape& s, int c0, V value, F f)
+{
+    int g = c0 / s.Cg, next = (g + 1) * s.Cg;
+    float2 k = value(g);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (c0 + j == next) {
+            k = value(++g);
+            next += s.Cg;
+        }
+        f(j, k);
+    }
 }
 
 // What a thread keeps of its N channels: u = (x - mean) scale + shift
 template <int N>
 struct Affine {
     float mean[N], scale[N], shift[N];
-    __device__ __forceinline__ void set(const Shape& s, const float2* stat, const float* __restrict__ gamma, const float* __restrict__ beta, int c0)
+    __device__ __forceinline__ void load(const float* __restrict__ gamma, const float* __restrict__ beta, int c0)
     {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const float2 k = stat[(c0 + j) / s.Cg];
+        channels_of<N>(gamma, c0, 1.f, scale);
+        channels_of<N>(beta, c0, 0.f, shift);
+    }
+    __device__ __forceinline__ void set(const Shape& s, const float2* stat, int c0)
+    {
+        groups_of<N>(s, c0, [&](int g) { return stat[g]; }, [&](int j, float2 k) {
             mean[j] = k.x;
-            scale[j] = gamma ? k.y * gamma[c0 + j] : k.y;
-            shift[j] = beta ? beta[c0 + j] : 0.f;
-        }
+            scale[j] *= k.y;
+        });
     }
     __device__ __forceinline__ float operator()(float x, int j) const { return __builtin_fmaf(x - mean[j], scale[j], shift[j]); }
 };
 
 template <typename T, int N, int ACT>
-__global__ __launch_bounds__(MAX_THREADS) void norm_apply_k(const T* __restrict__ x, Shape s, const Part* __restrict__ parts, const float* __restrict__ gamma,
+__global__ __launch_bounds__(MAX_THREADS) void norm_apply_k(const T* __restrict__ x, Shape s, const double2* __restrict__ sums, const float* __restrict__ gamma,
                                                             const float* __restrict__ beta, float eps, T* __restrict__ y, float* __restrict__ mean,
                                                             float* __restrict__ rstd)
 {
     extern __shared__ float2 stat[];
     constexpr bool GLU = ACT == W2L_ACT_GLU;
+    constexpr int U = 4;
     const int b = blockIdx.y, run = blockIdx.x, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C;
-    join_stats(s, parts, b, len < 0 ? 0 : len, eps, stat);
+    const int t0 = run * s.rows, t1 = t0 + s.rows < s.T ? t0 + s.rows : s.T, live = t1 < len ? t1 : len;
+    const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, nv = Cy / N;
+    const T* const in = x + (size_t)b * s.T * s.C;
+    // what a thread reads first is on its way while the statistics are joined
+    raw_t<T, N> xv[U], xg[U];
+    Affine<N> a, h;
+    auto load = [&](int v, int t) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const T* const at = in + (size_t)(t + k * s.lanes < live ? t + k * s.lanes : t) * s.C + (size_t)v * N;
+            xv[k] = fetch<T, N>(at);
+            if (GLU) xg[k] = fetch<T, N>(at + Cy);
+        }
+    };
+    auto load_channels = [&](int v) {
+        a.load(gamma, beta, v * N);
+        if (GLU) h.load(gamma, beta, Cy + v * N);
+    };
+    if (lane < s.lanes && t0 + lane < live) {
+        load(col, t0 + lane);
+        load_channels(col);
+    }
+    if (run == 0 || t0 < len) join_stats(s, sums, b, len < 0 ? 0 : len, eps, stat);
     if (run == 0)
         for (int g = threadIdx.x; g < s.G; g += blockDim.x) {
             mean[(size_t)b * s.G + g] = len < 0 ? NAN : stat[g].x;
             rstd[(size_t)b * s.G + g] = len < 0 ? NAN : stat[g].y;
         }
-    const int t0 = run * s.rows, t1 = t0 + s.rows < s.T ? t0 + s.rows : s.T;
-    const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, nv = Cy / N;
     if (lane >= s.lanes) return;
     for (int v = col; v < nv; v += s.cols) {
-        Affine<N> a, h;
-        a.set(s, stat, gamma, beta, v * N);
-        if (GLU) h.set(s, stat, gamma, beta, Cy + v * N);
-        const T* const p = x + (size_t)b * s.T * s.C + (size_t)v * N;
         T* const q = y + (size_t)b * s.T * Cy + (size_t)v * N;
-#pragma unroll 4
-        for (int t = t0 + lane; t < t1; t += s.lanes) {
-            float u[N], w[N];
-            if (t < len) {
-                Pack<T, N>::load(p + (size_t)t * s.C, u);
-                if (GLU) Pack<T, N>::load(p + (size_t)t * s.C + Cy, w);
+        int t = t0 + lane;
+        if (t < live) {
+            if (v != col) {
+                load(v, t);
+                load_channels(v);
+            }
+            a.set(s, stat, v * N);
+            if (GLU) h.set(s, stat, Cy + v * N);
+        }
+        while (t < live) {
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                if (t + k * s.lanes >= live) break;
+                float u[N], w[N];
+                unpack<T, N>(xv[k], u);
+                if (GLU) unpack<T, N>(xg[k], w);
 #pragma unroll
                 for (int j = 0; j < N; ++j) u[j] = act<ACT>(a(u[j], j), GLU ? h(w[j], j) : 0.f);
-            } else
+                put<T, N>(q + (size_t)(t + k * s.lanes) * Cy, u);
+            }
+            t += U * s.lanes;
+            if (t < live) load(v, t);
+        }
+        if (t1 > live) {
+            float none[N];
 #pragma unroll
-                for (int j = 0; j < N; ++j) u[j] = len < 0 ? NAN : 0.f;
-            Pack<T, N>::store(q + (size_t)t * Cy, u);
+            for (int j = 0; j < N; ++j) none[j] = len < 0 ? NAN : 0.f;
+            for (t = (live > t0 ? live : t0) + lane; t < t1; t += s.lanes) put<T, N>(q + (size_t)t * Cy, none);
         }
     }
 }
@@ -287,14 +396,13 @@ struct Channels {
     __device__ __forceinline__ void set(const Shape& s, int b, const float* __restrict__ mn, const float* __restrict__ rs, const float* __restrict__ gm,
                                         const float* __restrict__ bt, int c0)
     {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const size_t g = (size_t)b * s.G + (c0 + j) / s.Cg;
-            mean[j] = mn[g];
-            rstd[j] = rs[g];
-            gamma[j] = gm ? gm[c0 + j] : 1.f;
-            beta[j] = bt ? bt[c0 + j] : 0.f;
-        }
+        channels_of<N>(gm, c0, 1.f, gamma);
+        channels_of<N>(bt, c0, 0.f, beta);
+        const size_t g0 = (size_t)b * s.G;
+        groups_of<N>(s, c0, [&](int g) { return make_float2(mn[g0 + g], rs[g0 + g]); }, [&](int j, float2 k) {
+            mean[j] = k.x;
+            rstd[j] = k.y;
+        });
     }
     __device__ __forceinline__ float hat(float x, int j) const { return (x - mean[j]) * rstd[j]; }
     __device__ __forceinline__ float u(float x, int j) const { return __builtin_fmaf(x - mean[j], rstd[j] * gamma[j], beta[j]); }  // (as the forward call rounds it)
@@ -308,6 +416,7 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_sums_k(const T* __restrict__
 {
     extern __shared__ float2 acc[];  // [lanes][C]: a lane's sums
     constexpr bool GLU = ACT == W2L_ACT_GLU;
+    constexpr int U = 2;
     const int b = blockIdx.y, run = blockIdx.x, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C;
     const int t0 = run * s.rows, t1 = t0 + s.rows < len ? t0 + s.rows : len;
     if (t0 >= t1) return;
@@ -322,21 +431,32 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_sums_k(const T* __restrict__
             for (int j = 0; j < N; ++j) s1[j] = s2[j] = r1[j] = r2[j] = 0.f;
             const T* const p = x + (size_t)b * s.T * s.C + (size_t)v * N;
             const T* const q = dy + (size_t)b * s.T * Cy + (size_t)v * N;
-#pragma unroll 2
-            for (int t = t0 + lane; t < t1; t += s.lanes) {
-                float xv[N], xg[N], d[N];
-                Pack<T, N>::load(p + (size_t)t * s.C, xv);
-                if (GLU) Pack<T, N>::load(p + (size_t)t * s.C + Cy, xg);
-                Pack<T, N>::load(q + (size_t)t * Cy, d);
+            for (int t = t0 + lane; t < t1; t += U * s.lanes) {
+                raw_t<T, N> xv[U], xg[U], dv[U];
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    float du, dg = 0.f;
-                    act_bwd<ACT>(a.u(xv[j], j), GLU ? h.u(xg[j], j) : 0.f, d[j], du, dg);
-                    s1[j] += du;
-                    s2[j] = __builtin_fmaf(du, a.hat(xv[j], j), s2[j]);
-                    if (GLU) {
-                        r1[j] += dg;
-                        r2[j] = __builtin_fmaf(dg, h.hat(xg[j], j), r2[j]);
+                for (int k = 0; k < U; ++k) {
+                    const size_t at = t + k * s.lanes < t1 ? t + k * s.lanes : t;
+                    xv[k] = fetch<T, N>(p + at * s.C);
+                    if (GLU) xg[k] = fetch<T, N>(p + at * s.C + Cy);
+                    dv[k] = fetch<T, N>(q + at * Cy);
+                }
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    if (t + k * s.lanes >= t1) break;
+                    float xk[N], gk[N], d[N];
+                    unpack<T, N>(xv[k], xk);
+                    if (GLU) unpack<T, N>(xg[k], gk);
+                    unpack<T, N>(dv[k], d);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        float du, dg = 0.f;
+                        act_bwd<ACT>(a.u(xk[j], j), GLU ? h.u(gk[j], j) : 0.f, d[j], du, dg);
+                        s1[j] += du;
+                        s2[j] = __builtin_fmaf(du, a.hat(xk[j], j), s2[j]);
+                        if (GLU) {
+                            r1[j] += dg;
+                            r2[j] = __builtin_fmaf(dg, h.hat(gk[j], j), r2[j]);
+                        }
                     }
                 }
             }
@@ -361,9 +481,7 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_sums_k(const T* __restrict__
         acc[c] = make_float2(k.x * gm, k.y * gm);  // (row 0 of this channel is read by this thread alone)
     }
     __syncthreads();
-    int team = 64;
-    while (team > 1 && s.G * team > (int)blockDim.x) team >>= 1;
-    const int l = threadIdx.x & (team - 1), teams = blockDim.x / team;
+    const int team = team_of(s.G, s.Cg), l = threadIdx.x & (team - 1), teams = blockDim.x / team;
     for (int g0 = 0; g0 < s.G; g0 += teams) {
         const int g = g0 + threadIdx.x / team;
         float2 k = make_float2(0.f, 0.f);
@@ -380,17 +498,18 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_sums_k(const T* __restrict__
     }
 }
 
-// blockIdx.y < B: dx of a run of frames; = B: dgamma and dbeta of blockDim.x channels
+// blockIdx.y >= ahead: dx of a run of frames; below (ahead = 1): dgamma and dbeta, whose longer chains of loads start first
 template <typename T, int N, int ACT>
 __global__ __launch_bounds__(MAX_THREADS) void norm_dx_k(const T* __restrict__ x, const T* __restrict__ dy, Shape s, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                          const float* __restrict__ chans, const float2* __restrict__ groups, T* __restrict__ dx,
-                                                         float* __restrict__ dgamma, float* __restrict__ dbeta, int accumulate)
+                                                         float* __restrict__ dgamma, float* __restrict__ dbeta, int accumulate, int ahead)
 {
     extern __shared__ double2 lds[];  // [G] of floats: means of du gamma and du gamma xhat
     constexpr bool GLU = ACT == W2L_ACT_GLU;
-    const int b = blockIdx.y, Cy = GLU ? s.C / 2 : s.C;
-    if (b == s.B) {
+    constexpr int U = 2;
+    const int b = (int)blockIdx.y - ahead, Cy = GLU ? s.C / 2 : s.C;
+    if (b < 0) {
         // 64 channels a workgroup at a time, the runs dealt out over its wavefronts and added up in a fixed order
         const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, l = threadIdx.x & 63;
         for (int c0 = blockIdx.x * 64; c0 < s.C; c0 += gridDim.x * 64) {
@@ -420,14 +539,12 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_dx_k(const T* __restrict__ x
         }
         return;
     }
-    const int len = frames_of(s, b), run = blockIdx.x, t0 = run * s.rows, t1 = t0 + s.rows < s.T ? t0 + s.rows : s.T;
+    const int len = frames_of(s, b), run = blockIdx.x, t0 = run * s.rows, t1 = t0 + s.rows < s.T ? t0 + s.rows : s.T, live = t1 < len ? t1 : len;
     float2* const means = reinterpret_cast<float2*>(lds);
     if (t0 < len) {
         const int runs = (len + s.rows - 1) / s.rows;
         const float inv = 1.f / ((float)len * (float)s.Cg);
-        int team = 64;
-        while (team > 1 && s.G * team > (int)blockDim.x) team >>= 1;
-        const int l = threadIdx.x & (team - 1), teams = blockDim.x / team;
+        const int team = team_of(s.G, runs), l = threadIdx.x & (team - 1), teams = blockDim.x / team;
         for (int g0 = 0; g0 < s.G; g0 += teams) {
             const int g = g0 + threadIdx.x / team;
             float2 k = make_float2(0.f, 0.f);
@@ -453,43 +570,353 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_dx_k(const T* __restrict__ x
         if (t0 < len) {
             a.set(s, b, mean, rstd, gamma, beta, v * N);
             if (GLU) h.set(s, b, mean, rstd, gamma, beta, Cy + v * N);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float2 o = means[(v * N + j) / s.Cg];
-                m1[j] = o.x;
-                m2[j] = o.y;
-                if (GLU) {
-                    const float2 k = means[(Cy + v * N + j) / s.Cg];
-                    k1[j] = k.x;
-                    k2[j] = k.y;
-                }
-            }
+            auto mean_of = [&](int g) { return means[g]; };
+            groups_of<N>(s, v * N, mean_of, [&](int j, float2 k) { m1[j] = k.x; m2[j] = k.y; });
+            if (GLU) groups_of<N>(s, Cy + v * N, mean_of, [&](int j, float2 k) { k1[j] = k.x; k2[j] = k.y; });
         }
         const size_t row0 = (size_t)b * s.T;
         const T* const p = x + row0 * s.C + (size_t)v * N;
         const T* const q = dy + row0 * Cy + (size_t)v * N;
         T* const o = dx + row0 * s.C + (size_t)v * N;
-#pragma unroll 2
-        for (int t = t0 + lane; t < t1; t += s.lanes) {
-            float xv[N], xg[N], d[N];
-            if (t < len) {
-                Pack<T, N>::load(p + (size_t)t * s.C, xv);
-                if (GLU) Pack<T, N>::load(p + (size_t)t * s.C + Cy, xg);
-                Pack<T, N>::load(q + (size_t)t * Cy, d);
+        int t = t0 + lane;
+        for (; t < live; t += U * s.lanes) {
+            raw_t<T, N> xv[U], xg[U], dv[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const size_t at = t + k * s.lanes < live ? t + k * s.lanes : t;
+                xv[k] = fetch<T, N>(p + at * s.C);
+                if (GLU) xg[k] = fetch<T, N>(p + at * s.C + Cy);
+                dv[k] = fetch<T, N>(q + at * Cy);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                if (t + k * s.lanes >= live) break;
+                float xk[N], gk[N], d[N];
+                unpack<T, N>(xv[k], xk);
+                if (GLU) unpack<T, N>(xg[k], gk);
+                unpack<T, N>(dv[k], d);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     float du, dg = 0.f;
-                    act_bwd<ACT>(a.u(xv[j], j), GLU ? h.u(xg[j], j) : 0.f, d[j], du, dg);
-                    xv[j] = (__builtin_fmaf(du, a.gamma[j], -m1[j]) - a.hat(xv[j], j) * m2[j]) * a.rstd[j];
-                    if (GLU) xg[j] = (__builtin_fmaf(dg, h.gamma[j], -k1[j]) - h.hat(xg[j], j) * k2[j]) * h.rstd[j];
+                    act_bwd<ACT>(a.u(xk[j], j), GLU ? h.u(gk[j], j) : 0.f, d[j], du, dg);
+                    xk[j] = (__builtin_fmaf(du, a.gamma[j], -m1[j]) - a.hat(xk[j], j) * m2[j]) * a.rstd[j];
+                    if (GLU) gk[j] = (__builtin_fmaf(dg, h.gamma[j], -k1[j]) - h.hat(gk[j], j) * k2[j]) * h.rstd[j];
                 }
-            } else
-#pragma unroll
-                for (int j = 0; j < N; ++j) xv[j] = xg[j] = 0.f;
-            Pack<T, N>::store(o + (size_t)t * s.C, xv);
-            if (GLU) Pack<T, N>::store(o + (size_t)t * s.C + Cy, xg);
+                T* const to = o + (size_t)(t + k * s.lanes) * s.C;
+                put<T, N>(to, xk);
+                if (GLU) put<T, N>(to + Cy, gk);
+            }
+        }
+        if (t1 > live) {
+            const float none[N] = {};
+            for (t = (live > t0 ? live : t0) + lane; t < t1; t += s.lanes) {
+                put<T, N>(o + (size_t)t * s.C, none);
+                if (GLU) put<T, N>(o + (size_t)t * s.C + Cy, none);
+            }
         }
     }
+}
+
+// ---- a workgroup a group -------------------------------------------------------------------------------------
+// Where groups are many or short, a workgroup has a group of an utterance (with GLU the group of the values and that of their gates) and reads it twice, the second
+// time from its L2, in one launch.  Vectors and groups of one utterance that are neighbours share lines, so consecutive ones go to one XCD.
+constexpr int GROUP_THREADS = 1024, GROUP_BWD_THREADS = 512, FLUSH = 64;  // (512: a lane's sums of all channels fit 64 KB of LDS)
+struct Place {
+    int b, g;
+};
+__device__ __forceinline__ Place place_of(int per)  // per: workgroups an utterance
+{
+    const unsigned total = gridDim.x, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, q = total >> 3, r = total & 7;
+    const unsigned i = xcd * q + (xcd < r ? xcd : r) + slot;
+    return {(int)(i / per), (int)(i % per)};
+}
+// over the workgroup; lds: a value a wavefront
+template <typename V>
+__device__ __forceinline__ V sum_group(V v, V* lds)
+{
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    if (waves == 1) return v;
+    if ((threadIdx.x & 63) == 0) lds[wave] = v;
+    __syncthreads();
+    V k = lds[0];
+    for (int w = 1; w < waves; ++w) {
+        k.x += lds[w].x;
+        k.y += lds[w].y;
+    }
+    return k;
+}
+
+template <typename T, int N, int ACT>
+__global__ __launch_bounds__(GROUP_THREADS) void norm_group_k(const T* __restrict__ x, Shape s, const float* __restrict__ gamma, const float* __restrict__ beta,
+                                                              float eps, T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd)
+{
+    constexpr bool GLU = ACT == W2L_ACT_GLU;
+    constexpr int U = 4;
+    __shared__ double2 lds[2][GROUP_THREADS / 64];
+    const Place at = place_of(GLU ? s.G / 2 : s.G);
+    const int b = at.b, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C, live = len < 0 ? 0 : len;
+    const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, c0 = at.g * s.Cg + col * N, step = U * s.lanes;
+    const bool on = lane < s.lanes;
+    const T* const p = x + (size_t)b * s.T * s.C + c0;
+    raw_t<T, N> xv[U], xg[U];
+    auto load = [&](int t) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const T* const q = p + (size_t)(t + k * s.lanes < live ? t + k * s.lanes : t) * s.C;
+            xv[k] = fetch<T, N>(q);
+            if (GLU) xg[k] = fetch<T, N>(q + Cy);
+        }
+    };
+    Affine<N> a, h;
+    a.load(gamma, beta, c0);
+    if (GLU) h.load(gamma, beta, Cy + c0);
+    double2 k1 = make_double2(0., 0.), k2 = k1;
+    int last = -1;  // the first frame of what is in registers
+    {
+        Deviations<N> d1, d2;
+        d1.clear();
+        d2.clear();
+        auto flush = [&](Deviations<N>& d, double2& k) {
+            const double2 o = d.group_sums();
+            k.x += o.x;
+            k.y += o.y;
+            d.clear();
+        };
+        if (on)
+            for (int t = lane; t < live; t += step) {
+                load(t);
+                last = t;
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    if (t + k * s.lanes >= live) break;
+                    float u[N];
+                    unpack<T, N>(xv[k], u);
+                    d1.add(u);
+                    if (GLU) {
+                        unpack<T, N>(xg[k], u);
+                        d2.add(u);
+                    }
+                }
+                if (d1.n == FLUSH) {
+                    flush(d1, k1);
+                    if (GLU) flush(d2, k2);
+                }
+            }
+        if (d1.n) {
+            flush(d1, k1);
+            if (GLU) flush(d2, k2);
+        }
+    }
+    k1 = sum_group(sum64(k1, 64), lds[0]);
+    if (GLU) k2 = sum_group(sum64(k2, 64), lds[1]);
+    const double inv = live ? 1. / ((double)live * s.Cg) : 0.;
+    const float2 s1 = stat_of(k1, inv, eps), s2 = GLU ? stat_of(k2, inv, eps) : s1;
+    if (threadIdx.x == 0) {
+        const size_t o = (size_t)b * s.G + at.g;
+        mean[o] = len < 0 ? NAN : s1.x;
+        rstd[o] = len < 0 ? NAN : s1.y;
+        if (GLU) {
+            mean[o + s.G / 2] = len < 0 ? NAN : s2.x;
+            rstd[o + s.G / 2] = len < 0 ? NAN : s2.y;
+        }
+    }
+    if (!on) return;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        a.mean[j] = s1.x;
+        a.scale[j] *= s1.y;
+        if (GLU) {
+            h.mean[j] = s2.x;
+            h.scale[j] *= s2.y;
+        }
+    }
+    T* const q = y + (size_t)b * s.T * Cy + c0;
+    for (int t = last; t >= 0;) {  // from the end, which is in registers
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (t + k * s.lanes >= live) break;
+            float u[N], w[N];
+            unpack<T, N>(xv[k], u);
+            if (GLU) unpack<T, N>(xg[k], w);
+#pragma unroll
+            for (int j = 0; j < N; ++j) u[j] = act<ACT>(a(u[j], j), GLU ? h(w[j], j) : 0.f);
+            put<T, N>(q + (size_t)(t + k * s.lanes) * Cy, u);
+        }
+        t -= step;
+        if (t >= 0) load(t);
+    }
+    float none[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) none[j] = len < 0 ? NAN : 0.f;
+    for (int t = live + lane; t < s.T; t += s.lanes) put<T, N>(q + (size_t)t * Cy, none);
+}
+
+// chans [B][2][C]: sums of du and du xhat of an utterance (NULL: not wanted)
+template <typename T, int N, int ACT>
+__global__ __launch_bounds__(GROUP_BWD_THREADS) void norm_group_bwd_k(const T* __restrict__ x, const T* __restrict__ dy, Shape s, const float* __restrict__ mean,
+                                                                  const float* __restrict__ rstd, const float* __restrict__ gamma,
+                                                                  const float* __restrict__ beta, T* __restrict__ dx, float* __restrict__ chans)
+{
+    constexpr bool GLU = ACT == W2L_ACT_GLU;
+    constexpr int U = 2;
+    extern __shared__ float2 acc[];  // [GLU: 2][lanes][Cg]: a lane's sums
+    __shared__ float2 lds[2][GROUP_BWD_THREADS / 64];
+    const Place at = place_of(GLU ? s.G / 2 : s.G);
+    const int b = at.b, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C, live = len < 0 ? 0 : len;
+    const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, c0 = at.g * s.Cg + col * N, step = U * s.lanes;
+    const bool on = lane < s.lanes;
+    const size_t row0 = (size_t)b * s.T;
+    const T* const p = x + row0 * s.C + c0;
+    const T* const q = dy + row0 * Cy + c0;
+    raw_t<T, N> xv[U], xg[U], dv[U];
+    auto load = [&](int t) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const size_t r = t + k * s.lanes < live ? t + k * s.lanes : t;
+            xv[k] = fetch<T, N>(p + r * s.C);
+            if (GLU) xg[k] = fetch<T, N>(p + r * s.C + Cy);
+            dv[k] = fetch<T, N>(q + r * Cy);
+        }
+    };
+    const size_t g0 = (size_t)b * s.G + at.g;
+    const float mn = mean[g0], rs = rstd[g0], mg = GLU ? mean[g0 + s.G / 2] : 0.f, rg = GLU ? rstd[g0 + s.G / 2] : 0.f;
+    float ga[N], ba[N], gh[N], bh[N];
+    channels_of<N>(gamma, c0, 1.f, ga);
+    channels_of<N>(beta, c0, 0.f, ba);
+    if (GLU) {
+        channels_of<N>(gamma, Cy + c0, 1.f, gh);
+        channels_of<N>(beta, Cy + c0, 0.f, bh);
+    }
+    auto grads = [&](int k, int j, const float (&xk)[N], const float (&gk)[N], const float (&d)[N], float& du, float& dg, float& hx, float& hg) {
+        const float u = __builtin_fmaf(xk[j] - mn, rs * ga[j], ba[j]), w = GLU ? __builtin_fmaf(gk[j] - mg, rg * gh[j], bh[j]) : 0.f;
+        dg = 0.f;
+        act_bwd<ACT>(u, w, d[j], du, dg);
+        hx = (xk[j] - mn) * rs;
+        hg = GLU ? (gk[j] - mg) * rg : 0.f;
+    };
+    int last = -1;
+    float s1[N], s2[N], r1[N], r2[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) s1[j] = s2[j] = r1[j] = r2[j] = 0.f;
+    if (on)
+        for (int t = lane; t < live; t += step) {
+            load(t);
+            last = t;
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                if (t + k * s.lanes >= live) break;
+                float xk[N], gk[N], d[N];
+                unpack<T, N>(xv[k], xk);
+                if (GLU) unpack<T, N>(xg[k], gk);
+                unpack<T, N>(dv[k], d);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    float du, dg, hx, hg;
+                    grads(k, j, xk, gk, d, du, dg, hx, hg);
+                    s1[j] += du;
+                    s2[j] = __builtin_fmaf(du, hx, s2[j]);
+                    if (GLU) {
+                        r1[j] += dg;
+                        r2[j] = __builtin_fmaf(dg, hg, r2[j]);
+                    }
+                }
+            }
+        }
+    float2 k1 = make_float2(0.f, 0.f), k2 = k1;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        k1.x = __builtin_fmaf(s1[j], ga[j], k1.x);
+        k1.y = __builtin_fmaf(s2[j], ga[j], k1.y);
+        if (GLU) {
+            k2.x = __builtin_fmaf(r1[j], gh[j], k2.x);
+            k2.y = __builtin_fmaf(r2[j], gh[j], k2.y);
+        }
+    }
+    if (chans && on)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            acc[lane * s.Cg + col * N + j] = make_float2(s1[j], s2[j]);
+            if (GLU) acc[(s.lanes + lane) * s.Cg + col * N + j] = make_float2(r1[j], r2[j]);
+        }
+    k1 = sum_group(make_float2(wave64(k1.x, Sum()), wave64(k1.y, Sum())), lds[0]);
+    if (GLU) k2 = sum_group(make_float2(wave64(k2.x, Sum()), wave64(k2.y, Sum())), lds[1]);
+    if (chans) {
+        if (blockDim.x == 64) __syncthreads();  // (sum_group's are the others')
+        const int team = team_of(GLU ? 2 * s.Cg : s.Cg, s.lanes), l = threadIdx.x & (team - 1), teams = blockDim.x / team, count = GLU ? 2 * s.Cg : s.Cg;
+        for (int i0 = 0; i0 < count; i0 += teams) {
+            const int i = i0 + threadIdx.x / team, half = i >= s.Cg, c = i - half * s.Cg;
+            float2 k = make_float2(0.f, 0.f);
+            if (i < count)
+                for (int r = l; r < s.lanes; r += team) {
+                    const float2 o = acc[(half * s.lanes + r) * s.Cg + c];
+                    k.x += o.x;
+                    k.y += o.y;
+                }
+            for (int o = team >> 1; o > 0; o >>= 1) {
+                k.x += __shfl_xor(k.x, o, 64);
+                k.y += __shfl_xor(k.y, o, 64);
+            }
+            if (i < count && l == 0) {
+                float* const o = chans + (size_t)b * 2 * s.C + at.g * s.Cg + half * Cy + c;
+                o[0] = k.x;
+                o[s.C] = k.y;
+            }
+        }
+    }
+    if (!on) return;
+    const float inv = live ? 1.f / ((float)live * (float)s.Cg) : 0.f;
+    k1.x *= inv; k1.y *= inv; k2.x *= inv; k2.y *= inv;
+    T* const o = dx + row0 * s.C + c0;
+    for (int t = last; t >= 0;) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (t + k * s.lanes >= live) break;
+            float xk[N], gk[N], d[N];
+            unpack<T, N>(xv[k], xk);
+            if (GLU) unpack<T, N>(xg[k], gk);
+            unpack<T, N>(dv[k], d);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                float du, dg, hx, hg;
+                grads(k, j, xk, gk, d, du, dg, hx, hg);
+                xk[j] = (__builtin_fmaf(du, ga[j], -k1.x) - hx * k1.y) * rs;
+                if (GLU) gk[j] = (__builtin_fmaf(dg, gh[j], -k2.x) - hg * k2.y) * rg;
+            }
+            T* const to = o + (size_t)(t + k * s.lanes) * s.C;
+            put<T, N>(to, xk);
+            if (GLU) put<T, N>(to + Cy, gk);
+        }
+        t -= step;
+        if (t >= 0) load(t);
+    }
+    const float none[N] = {};
+    for (int t = live + lane; t < s.T; t += s.lanes) {
+        put<T, N>(o + (size_t)t * s.C, none);
+        if (GLU) put<T, N>(o + (size_t)t * s.C + Cy, none);
+    }
+}
+
+// dgamma and dbeta from the utterances' sums
+__global__ __launch_bounds__(256) void norm_join_k(const float* __restrict__ chans, int B, int C, float* __restrict__ dgamma, float* __restrict__ dbeta, int accumulate)
+{
+    __shared__ double2 lds[256];
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+    double g = 0., h = 0.;
+    if (c < C)
+#pragma unroll 4
+        for (int b = wave; b < B; b += 4) {
+            h += chans[(size_t)b * 2 * C + c];
+            g += chans[(size_t)b * 2 * C + C + c];
+        }
+    lds[threadIdx.x] = make_double2(g, h);
+    __syncthreads();
+    if (wave || c >= C) return;
+    for (int w = 1; w < 4; ++w) {
+        g += lds[64 * w + threadIdx.x].x;
+        h += lds[64 * w + threadIdx.x].y;
+    }
+    if (dgamma) dgamma[c] = (float)(accumulate ? dgamma[c] + g : g);
+    if (dbeta) dbeta[c] = (float)(accumulate ? dbeta[c] + h : h);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------
@@ -508,7 +935,7 @@ int vector_of(int Cy, int dtype)
 // vectors: of a row that a thread can be given one of
 Shape shape_of(int B, int T, int C, int G, const int* in_len, int vectors)
 {
-    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, 1, in_len};
+    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, in_len};
     const int passes = (vectors + MAX_THREADS - 1) / MAX_THREADS;
     s.cols = (vectors + passes - 1) / passes;
     s.lanes = MAX_THREADS / s.cols;
@@ -530,7 +957,6 @@ void runs_of(Shape& s, int dtype)
     s.rows = rows_of(s.B, s.T, s.C, dtype);
     s.runs = (s.T + s.rows - 1) / s.rows;
 }
-int subs_of(const Shape& s) { return s.G >= 8 ? 1 : 8 / s.G; }
 bool workspace_ok(const void* ws, size_t have, size_t need) { return ws && have >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0; }
 bool meets(const void* a, size_t an, const void* b, size_t bn)
 {
@@ -553,23 +979,73 @@ bool apart(const Span (&in)[I], const Span (&out)[O])
     return true;
 }
 
-size_t stat_bytes(const Shape& s) { return round_up((size_t)s.B * s.runs * s.G * subs_of(s) * sizeof(Part), 256); }
+// A workgroup a group: where vectors and, with GLU, halves hold whole groups, and there are workgroups enough for what each has to read
+struct Form {
+    bool group;
+    int N;  // channels of a vector
+};
+Form form_of(int B, int T, int C, int G, int act, int dtype)
+{
+    const int Cg = C / G, Cy = act == W2L_ACT_GLU ? C / 2 : C;
+    if (act != W2L_ACT_GLU || G % 2 == 0) {
+        const int n = vector_of(Cg, dtype);
+        const long long workgroups = (long long)B * (act == W2L_ACT_GLU ? G / 2 : G), bytes = (long long)T * Cg * (act == W2L_ACT_GLU ? 2 : 1) * dtype_size(dtype);
+        if (Cg / n <= 256 && workgroups < (1 << 22) && GROUP_RULE) return {true, n};
+    }
+    return {false, vector_of(Cy, dtype)};
+}
+Shape group_shape(int B, int T, int C, int G, const int* in_len, int N, int threads)
+{
+    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, in_len};
+    s.cols = s.Cg / N;
+    const int lanes = threads / s.cols;
+    s.lanes = lanes < T ? lanes : T;
+    return s;
+}
+
+size_t stat_bytes(const Shape& s) { return round_up((size_t)s.B * s.runs * s.G * sizeof(double2), 256); }
 size_t sum_bytes(const Shape& s) { return round_up((size_t)s.B * s.runs * s.C * 8, 256) + round_up((size_t)s.B * s.runs * s.G * 8, 256); }
 
 template <typename T, int N>
-int forward(const void* x, const Shape& st, const Shape& ap, Part* parts, const float* gamma, const float* beta, float eps, int act, void* y, float* mean,
+int forward(const void* x, const Shape& st, const Shape& ap, double2* sums, const float* gamma, const float* beta, float eps, int act, void* y, float* mean,
             float* rstd, hipStream_t stream)
 {
-    hipLaunchKernelGGL((norm_stats_k<T, N>), dim3(st.runs, st.B), dim3(threads_of(st)), (size_t)st.lanes * st.C * 8, stream, (const T*)x, st, parts);
+    const dim3 g(st.runs, st.B), n(threads_of(st));
+    if (st.Cg % N == 0) hipLaunchKernelGGL((norm_stats_k<T, N, true>), g, n, (size_t)st.lanes * (st.C / N) * 16, stream, (const T*)x, st, sums);
+    else hipLaunchKernelGGL((norm_stats_k<T, N, false>), g, n, (size_t)st.lanes * st.C * 8, stream, (const T*)x, st, sums);
     if (int rc = launch_status()) return rc;
 #define W2L_APPLY(A_)                                                                                                                         \
-    hipLaunchKernelGGL((norm_apply_k<T, N, A_>), dim3(ap.runs, ap.B), dim3(threads_of(ap)), (size_t)ap.G * 8, stream, (const T*)x, ap, parts, gamma, beta, \
+    hipLaunchKernelGGL((norm_apply_k<T, N, A_>), dim3(ap.runs, ap.B), dim3(threads_of(ap)), (size_t)ap.G * 8, stream, (const T*)x, ap, sums, gamma, beta, \
                        eps, (T*)y, mean, rstd)
     if (act == W2L_ACT_NONE) W2L_APPLY(W2L_ACT_NONE);
     else if (act == W2L_ACT_RELU) W2L_APPLY(W2L_ACT_RELU);
     else if (act == W2L_ACT_SILU) W2L_APPLY(W2L_ACT_SILU);
     else W2L_APPLY(W2L_ACT_GLU);
 #undef W2L_APPLY
+    return launch_status();
+}
+template <typename T, int N>
+int forward_group(const void* x, const Shape& s, const float* gamma, const float* beta, float eps, int act, void* y, float* mean, float* rstd, hipStream_t stream)
+{
+    const dim3 g((unsigned)(s.B * (act == W2L_ACT_GLU ? s.G / 2 : s.G))), n(threads_of(s));
+#define W2L_GROUP(A_) hipLaunchKernelGGL((norm_group_k<T, N, A_>), g, n, 0, stream, (const T*)x, s, gamma, beta, eps, (T*)y, mean, rstd)
+    if (act == W2L_ACT_NONE) W2L_GROUP(W2L_ACT_NONE);
+    else if (act == W2L_ACT_RELU) W2L_GROUP(W2L_ACT_RELU);
+    else if (act == W2L_ACT_SILU) W2L_GROUP(W2L_ACT_SILU);
+    else W2L_GROUP(W2L_ACT_GLU);
+#undef W2L_GROUP
+    return launch_status();
+}
+template <typename T, int N, int ACT>
+int backward_group(const void* x, const void* dy, const Shape& s, const float* mean, const float* rstd, const float* gamma, const float* beta, float* chans,
+                   void* dx, float* dgamma, float* dbeta, int accumulate, hipStream_t stream)
+{
+    const bool GLU = ACT == W2L_ACT_GLU, want = dgamma || dbeta;
+    hipLaunchKernelGGL((norm_group_bwd_k<T, N, ACT>), dim3((unsigned)(s.B * (GLU ? s.G / 2 : s.G))), dim3(threads_of(s)),
+                       want ? (size_t)(GLU ? 2 : 1) * s.lanes * s.Cg * 8 : 0, stream, (const T*)x, (const T*)dy, s, mean, rstd, gamma, beta, (T*)dx, want ? chans : nullptr);
+    if (int rc = launch_status()) return rc;
+    if (!want) return W2L_OK;
+    hipLaunchKernelGGL(norm_join_k, dim3((s.C + 63) / 64), dim3(256), 0, stream, chans, s.B, s.C, dgamma, dbeta, accumulate);
     return launch_status();
 }
 template <typename T, int N, int ACT>
@@ -579,36 +1055,38 @@ int backward(const void* x, const void* dy, const Shape& s, const float* mean, c
     hipLaunchKernelGGL((norm_sums_k<T, N, ACT>), dim3(s.runs, s.B), dim3(threads_of(s)), (size_t)s.lanes * s.C * 8, stream, (const T*)x, (const T*)dy, s,
                        mean, rstd, gamma, beta, chans, groups);
     if (int rc = launch_status()) return rc;
-    hipLaunchKernelGGL((norm_dx_k<T, N, ACT>), dim3(s.runs, s.B + (dgamma || dbeta ? 1 : 0)), dim3(threads_of(s)),
+    const int ahead = dgamma || dbeta ? 1 : 0;
+    hipLaunchKernelGGL((norm_dx_k<T, N, ACT>), dim3(s.runs, s.B + ahead), dim3(threads_of(s)),
                        (size_t)(s.G > 2 * threads_of(s) ? s.G : 2 * threads_of(s)) * 8, stream, (const T*)x,
-                       (const T*)dy, s, mean, rstd, gamma, beta, chans, groups, (T*)dx, dgamma, dbeta, accumulate);
+                       (const T*)dy, s, mean, rstd, gamma, beta, chans, groups, (T*)dx, dgamma, dbeta, accumulate, ahead);
     return launch_status();
 }
 
-// f(type, std::integral_constant of N) for the vector length n
+// f(a null pointer of the type, std::integral_constant of the vector length)
 template <typename F>
 int with_vector(int dtype, int n, F f)
 {
     if (dtype == W2L_BF16) {
-        if (n == 8) return f((bf16_t*)nullptr, Pack<bf16_t, 8>());
-        if (n == 4) return f((bf16_t*)nullptr, Pack<bf16_t, 4>());
-        if (n == 2) return f((bf16_t*)nullptr, Pack<bf16_t, 2>());
-        return f((bf16_t*)nullptr, Pack<bf16_t, 1>());
+        bf16_t* const t = nullptr;
+        if (n == 8) return f(t, std::integral_constant<int, 8>());
+        if (n == 4) return f(t, std::integral_constant<int, 4>());
+        if (n == 2) return f(t, std::integral_constant<int, 2>());
+        return f(t, std::integral_constant<int, 1>());
     }
-    if (n == 4) return f((float*)nullptr, Pack<float, 4>());
-    if (n == 2) return f((float*)nullptr, Pack<float, 2>());
-    return f((float*)nullptr, Pack<float, 1>());
+    float* const t = nullptr;
+    if (n == 4) return f(t, std::integral_constant<int, 4>());
+    if (n == 2) return f(t, std::integral_constant<int, 2>());
+    return f(t, std::integral_constant<int, 1>());
 }
-template <typename P> struct Length;
-template <typename T, int N> struct Length<Pack<T, N>> { static constexpr int value = N; };
 
 }  // namespace
 
 extern "C" size_t w2l_groupnorm_workspace_bytes(int B, int T, int C, int G, int act, int dtype)
 {
     if (!shape_ok(B, T, C, G, act) || !valid_dtype(dtype)) return 0;
-    const int Cy = act == W2L_ACT_GLU ? C / 2 : C;
-    Shape s = shape_of(B, T, C, G, nullptr, Cy / vector_of(Cy, dtype));
+    const Form form = form_of(B, T, C, G, act, dtype);
+    if (form.group) return round_up((size_t)B * C * 8, 256);
+    Shape s = shape_of(B, T, C, G, nullptr, (act == W2L_ACT_GLU ? C / 2 : C) / form.N);
     runs_of(s, dtype);
     const size_t a = stat_bytes(s), b = sum_bytes(s);
     return a > b ? a : b;
@@ -627,14 +1105,19 @@ extern "C" int w2l_groupnorm_fwd(const void* x, const float* gamma, const float*
     const Span in[] = {{x, values * e}, {gamma, (size_t)C * 4}, {beta, (size_t)C * 4}, {in_len, (size_t)B * 4}};
     const Span out[] = {{y, (size_t)B * T * Cy * e}, {mean, (size_t)B * G * 4}, {rstd, (size_t)B * G * 4}, {workspace, need}};
     if (!apart(in, out)) return W2L_ERR_OVERLAP;
-    const int n = vector_of(Cy, dtype);
+    const Form form = form_of(B, T, C, G, act, dtype);
+    const int n = form.N;
+    if (form.group)
+        return with_vector(dtype, n, [&](auto* t, auto n) {
+            using T_ = std::remove_pointer_t<decltype(t)>;
+            return forward_group<T_, decltype(n)::value>(x, group_shape(B, T, C, G, in_len, decltype(n)::value, GROUP_THREADS), gamma, beta, eps, act, y, mean, rstd, (hipStream_t)stream);
+        });
     Shape ap = shape_of(B, T, C, G, in_len, Cy / n), st = shape_of(B, T, C, G, in_len, C / n);
     runs_of(ap, dtype);
     runs_of(st, dtype);
-    ap.subs = st.subs = subs_of(st);
-    return with_vector(dtype, n, [&](auto* t, auto pack) {
+    return with_vector(dtype, n, [&](auto* t, auto n) {
         using T_ = std::remove_pointer_t<decltype(t)>;
-        return forward<T_, Length<decltype(pack)>::value>(x, st, ap, (Part*)workspace, gamma, beta, eps, act, y, mean, rstd, (hipStream_t)stream);
+        return forward<T_, decltype(n)::value>(x, st, ap, (double2*)workspace, gamma, beta, eps, act, y, mean, rstd, (hipStream_t)stream);
     });
 }
 
@@ -655,16 +1138,18 @@ extern "C" int w2l_groupnorm_bwd(const void* x, const void* dy, const float* mea
                        {in_len, (size_t)B * 4}};
     const Span out[] = {{dx, values * e}, {dgamma, (size_t)C * 4}, {dbeta, (size_t)C * 4}, {workspace, need}};
     if (!apart(in, out)) return W2L_ERR_OVERLAP;
-    const int n = vector_of(Cy, dtype);
-    Shape s = shape_of(B, T, C, G, in_len, Cy / n);
-    runs_of(s, dtype);
+    const Form form = form_of(B, T, C, G, act, dtype);
+    const int n = form.N;
+    Shape s = form.group ? group_shape(B, T, C, G, in_len, n, GROUP_BWD_THREADS) : shape_of(B, T, C, G, in_len, Cy / n);
+    if (!form.group) runs_of(s, dtype);
     float* const chans = (float*)workspace;
     float2* const groups = (float2*)((char*)workspace + round_up((size_t)B * s.runs * C * 8, 256));
-    return with_vector(dtype, n, [&](auto* t, auto pack) {
+    return with_vector(dtype, n, [&](auto* t, auto n) {
         using T_ = std::remove_pointer_t<decltype(t)>;
-        constexpr int N = Length<decltype(pack)>::value;
-#define W2L_BACKWARD(A_) \
-    return backward<T_, N, A_>(x, dy, s, mean, rstd, gamma, beta, chans, groups, dx, dgamma, dbeta, accumulate, (hipStream_t)stream)
+        constexpr int N = decltype(n)::value;
+#define W2L_BACKWARD(A_)                                                                                                                        \
+    return form.group ? backward_group<T_, N, A_>(x, dy, s, mean, rstd, gamma, beta, chans, dx, dgamma, dbeta, accumulate, (hipStream_t)stream) : \
+    backward<T_, N, A_>(x, dy, s, mean, rstd, gamma, beta, chans, groups, dx, dgamma, dbeta, accumulate, (hipStream_t)stream)
         if (act == W2L_ACT_NONE) W2L_BACKWARD(W2L_ACT_NONE);
         if (act == W2L_ACT_RELU) W2L_BACKWARD(W2L_ACT_RELU);
         if (act == W2L_ACT_SILU) W2L_BACKWARD(W2L_ACT_SILU);
