@@ -166,6 +166,9 @@ int w2l_groupnorm_fwd(const void *x, const float *gamma, const float *beta, cons
 int w2l_groupnorm_bwd(const void *x, const void *dy, const float *mean, const float *rstd, const float *gamma,
                       const float *beta, const int *in_len, void *dx, float *dgamma, float *dbeta, int B, int T, int C,
                       int G, int act, int dtype, int accumulate, void *workspace, size_t ws_bytes, void *stream);
+/* Host-only query: whether the two calls give every group of an utterance a workgroup (1) or deal out runs of frames (0), and how many neighbouring channels a
+ * thread takes at a time.  For tests and tuning; launches nothing.  Errors as the calls themselves. */
+int w2l_groupnorm_launch_config(int B, int T, int C, int G, int act, int dtype, int *group, int *vector);
 
 /* ---- per-frame log-softmax (normalised scores for the criterion, Sec. 2.3) ---------
  *   fwd:  lp[r,c] = z[r,c] - max_c z[r,:] - log sum_c exp(z[r,c] - max_c z[r,:])

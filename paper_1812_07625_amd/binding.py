@@ -28,7 +28,7 @@ __all__ = [
     "w2l_token_logprob_workspace_bytes", "w2l_token_logprob_fwd", "w2l_token_logprob_bwd",
     "w2l_token_logprob_launch_config", "w2l_distill_workspace_bytes", "w2l_distill_fwd_bwd", "w2l_distill_launch_config",
     "w2l_frame_ids_check_host",
-    "W2L_ACT_NONE", "W2L_ACT_RELU", "W2L_ACT_SILU", "W2L_ACT_GLU", "w2l_groupnorm_workspace_bytes", "w2l_groupnorm_fwd", "w2l_groupnorm_bwd",
+    "W2L_ACT_NONE", "W2L_ACT_RELU", "W2L_ACT_SILU", "W2L_ACT_GLU", "w2l_groupnorm_workspace_bytes", "w2l_groupnorm_fwd", "w2l_groupnorm_bwd", "w2l_groupnorm_launch_config",
     "w2l_policy_workspace_bytes", "w2l_policy_fwd_bwd",
     "w2l_adamw_tensor", "adamw_tensors", "w2l_adamw_workspace_bytes", "w2l_adamw_step",
     "w2l_train_step_workspace_bytes", "w2l_train_step", "w2l_train_step_asg_workspace_bytes", "w2l_train_step_asg",
@@ -91,6 +91,7 @@ def _load():
         "w2l_groupnorm_workspace_bytes": (sz, [i] * 6),
         "w2l_groupnorm_fwd": (i, [vp] * 7 + [i] * 4 + [f] + [i] * 2 + [vp, sz, vp]),
         "w2l_groupnorm_bwd": (i, [vp] * 10 + [i] * 7 + [vp, sz, vp]),
+        "w2l_groupnorm_launch_config": (i, [i] * 6 + [C.POINTER(C.c_int)] * 2),
         "w2l_policy_workspace_bytes": (sz, [i] * 4),
         "w2l_policy_fwd_bwd": (i, [vp] * 5 + [i] + [vp] * 6 + [i] * 3 + [f] * 4 + [i] * 3 + [vp, sz, vp]),
         "w2l_adamw_workspace_bytes": (sz, [vp, i]),
@@ -469,6 +470,13 @@ def w2l_groupnorm_bwd(x, dy, mean, rstd, dx, gamma=None, beta=None, dgamma=None,
                           ("dgamma", dgamma, (Cc,), _F32), ("dbeta", dbeta, (Cc,), _F32)), "x is")
     _call(raw.w2l_groupnorm_bwd, "w2l_groupnorm_bwd", dev, (*ptr, B, T, Cc, G, act, dt, 1 if accumulate else 0, *_scratch(workspace, dev, "x is")), stream)
     return dx, dgamma, dbeta
+
+
+def w2l_groupnorm_launch_config(B, T, Cc, groups, act, dtype):
+    """(a workgroup a group, channels of a vector) of w2l_groupnorm_fwd and _bwd; host only."""
+    out = [C.c_int() for _ in range(2)]
+    _check(raw.w2l_groupnorm_launch_config(B, T, Cc, groups, act, dtype, *[C.byref(o) for o in out]), "w2l_groupnorm_launch_config")
+    return tuple(o.value for o in out)
 
 
 class AdamwTensors:

@@ -1,11 +1,12 @@
-// Group norm over [B,T,C], channels last, and the activation behind it: w2l_groupnorm_fwd / _bwd.
-//   forward   norm_stats_k: count, mean and sum of squared deviations of every group in a run of an utterance's frames;
-//             norm_apply_k: joins the runs of an utterance, normalises, applies the activation
-//   backward  norm_sums_k: sums over a run of frames of du and du xhat of every channel, and of both times gamma of every group;
-//             norm_dx_k: joins them and writes dx; workgroups of its own add up dgamma and dbeta
-// Memory bounds all four: a pass moves 2 or 4 bytes a value and takes some ten instructions.  The second pass of either call reads what the first did
-// and finds it in the caches where they hold it.
-// A thread has a vector of N neighbouring channels (16 bytes where rows are whole vectors, less where they are not) in some rows of the run; what it
+// Group norm over [B,T,C], channels last, and the activation behind it: w2l_groupnorm_fwd / _bwd.  Two ways:
+//   runs of frames     norm_stats_k: every group's sum and sum of squares in a run of an utterance's frames;
+//                      norm_apply_k: joins the runs of an utterance, normalises, applies the activation;
+//                      norm_sums_k: sums over a run of du and du xhat of every channel, and of both times gamma of every group;
+//                      norm_dx_k: joins them and writes dx; workgroups of its own add up dgamma and dbeta
+//   a workgroup a group  norm_group_k, norm_group_bwd_k (and norm_join_k for dgamma and dbeta): groups that one workgroup reads twice
+// What bounds them is memory where a batch is large (16x1500x2048 bf16, one group, 20000 live frames: both calls together move 656 MB in 144 us, 4.6 TB/s), and where
+// it is small the launches and a chain of loads, sums over lanes, and stores (3.6 us a launch).  The second reading finds in the caches what they hold.
+// A thread has a vector of N neighbouring channels (16 bytes where groups are whole vectors, less where they are not) in some rows; what it
 // knows of its channels stays in registers from row to row.
 #include "lanes.h"
 
@@ -13,12 +14,9 @@
 
 using namespace w2l;
 
-#ifndef GROUP_RULE
-#define GROUP_RULE bytes <= (256 << 10)
-#endif
 namespace {
 
-constexpr int MAX_CHANNELS = 8192, MAX_FRAMES = 1 << 24, MAX_THREADS = 512;  // (8192: a pair of floats a channel fits 64 KB of LDS)
+constexpr int MAX_CHANNELS = 8192, MAX_FRAMES = 1 << 24, MAX_THREADS = 512, BATCH = 4;  // (8192: a pair of floats a channel fits 64 KB of LDS)
 
 // A vector of N neighbouring channels as it lies in memory, and its values
 template <typename T, int N> struct Vec {
@@ -51,7 +49,7 @@ __device__ __forceinline__ void unpack(raw_t<T, N> q, float (&x)[N])
         }
 }
 template <typename T, int N>
-__device__ __forceinline__ void put(T* p, const float (&x)[N])
+__device__ __forceinline__ void put(T* p, const float (&x)[N], bool past)
 {
     raw_t<T, N> q;
     if constexpr (sizeof(T) == 4) {
@@ -63,18 +61,39 @@ __device__ __forceinline__ void put(T* p, const float (&x)[N])
     else
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) {
-            const unsigned w = (unsigned)f32_to_bf16(x[2 * j]) | (unsigned)f32_to_bf16(x[2 * j + 1]) << 16;
+            typedef float float2_t __attribute__((ext_vector_type(2)));
+            typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+            const unsigned w = __builtin_bit_cast(unsigned, __builtin_convertvector((float2_t){x[2 * j], x[2 * j + 1]}, bf16x2_t));
             if constexpr (N == 2) q = w;
             else q[j] = w;
         }
-    *reinterpret_cast<raw_t<T, N>*>(p) = q;
+    if (past) __builtin_nontemporal_store(q, reinterpret_cast<raw_t<T, N>*>(p));
+    else *reinterpret_cast<raw_t<T, N>*>(p) = q;
 }
 
 // How a workgroup takes a run of `rows` frames: `cols` threads side by side, `lanes` rows at a time
 struct Shape {
     int B, T, C, G, Cg, rows, runs, cols, lanes;
     const int* in_len;
+    float inv_Cg, inv_cols;
+    bool past;  // outputs go past the L2s: they are more than these hold (16x1500x2048 bf16 and its gradient: 150 -> 144 us)
+    // column and row of a thread (a thousand of them at most: see group_of)
+    __device__ __forceinline__ void split(int& col, int& lane) const
+    {
+        lane = (int)(((float)threadIdx.x + 0.5f) * inv_cols);
+        col = (int)threadIdx.x - lane * cols;
+    }
 };
+// Task i's utterance and run of frames.  Runs that are the same of every utterance follow one another, so that those behind short utterances' ends come last and
+// take no place from others; the utterances are rotated from run to run, so that long and short ones are spread over the XCDs.
+struct Task {
+    int b, run;
+};
+__device__ __forceinline__ Task task_of(const Shape& s, unsigned i)
+{
+    const unsigned run = i / (unsigned)s.B, k = i - run * s.B + run % (unsigned)s.B;
+    return {(int)(k < (unsigned)s.B ? k : k - s.B), (int)run};
+}
 // frames of utterance b; -1: its in_len is out of range
 __device__ __forceinline__ int frames_of(const Shape& s, int b)
 {
@@ -175,16 +194,75 @@ __device__ __forceinline__ int team_of(int G, int results)
     return team;
 }
 
-// sums [B][runs][G]: sum and sum of squares of a run.  WHOLE: a vector's channels are all of one group
-template <typename T, int N, bool WHOLE>
+__device__ __forceinline__ float2 sum64(float2 v, int width)
+{
+    for (int o = width >> 1; o > 0; o >>= 1) {
+        v.x += __shfl_xor(v.x, o, 64);
+        v.y += __shfl_xor(v.y, o, 64);
+    }
+    return v;
+}
+// out(g, sum of value(r, c) over r < rows and the group's entries c < per) for every group.  Where groups are fewer than the workgroup's teams, several teams share one
+// (16x1500x2048 bf16 in one group: 34 -> 26 us for norm_stats_k).  lds: a V for every wavefront
+// (only teams of a whole wavefront share a group: fewer lanes are taken where they are enough for it)
+template <typename V, typename F, typename O>
+__device__ __forceinline__ void sum_groups(int G, int rows, int per, V* lds, F value, O out)
+{
+    const int team = team_of(G, per), l = threadIdx.x & (team - 1), teams = blockDim.x / team, mine = threadIdx.x / team;
+    int shares = teams / G;
+    if ((shares - 1) * team >= per) shares = (per + team - 1) / team;
+    if (shares <= 1) {
+        for (int g0 = 0; g0 < G; g0 += teams) {
+            const int g = g0 + mine;
+            V k{};
+            if (g < G)
+                for (int r = 0; r < rows; ++r)
+                    for (int c = l; c < per; c += team) {
+                        const V o = value(g, r, c);
+                        k.x += o.x;
+                        k.y += o.y;
+                    }
+            k = sum64(k, team);
+            if (g < G && l == 0) out(g, k);
+        }
+        return;
+    }
+    const int g = mine % G, share = mine / G;
+    V k{};
+    if (share < shares)
+        for (int r = 0; r < rows; ++r)
+            for (int c = share * team + l; c < per; c += team * shares) {
+                const V o = value(g, r, c);
+                k.x += o.x;
+                k.y += o.y;
+            }
+    k = sum64(k, team);
+    if (l == 0) lds[mine] = k;
+    __syncthreads();
+    if ((int)threadIdx.x < G) {
+        V all = lds[threadIdx.x];
+        for (int i = 1; i < shares; ++i) {
+            all.x += lds[i * G + threadIdx.x].x;
+            all.y += lds[i * G + threadIdx.x].y;
+        }
+        out((int)threadIdx.x, all);
+    }
+}
+
+// sums [B][runs][G]: sum and sum of squares of a run
+template <typename T, int N>
 __global__ __launch_bounds__(MAX_THREADS) void norm_stats_k(const T* __restrict__ x, Shape s, double2* __restrict__ sums)
 {
-    extern __shared__ double2 lds[];  // [lanes][vectors]: a thread's sums;  !WHOLE: [lanes][C] of floats, a channel's mean and squared deviations
-    constexpr int U = 4;
-    const int b = blockIdx.y, run = blockIdx.x, len = frames_of(s, b);
+    extern __shared__ double2 lds[];  // [lanes][vectors]: a thread's sums
+    __shared__ double2 part[MAX_THREADS / 64];
+    constexpr int U = BATCH;
+    const Task task = task_of(s, blockIdx.x);
+    const int b = task.b, run = task.run, len = frames_of(s, b);
     const int t0 = run * s.rows, t1 = t0 + s.rows < len ? t0 + s.rows : len;
     if (t0 >= t1) return;  // (what reads the sums knows that there are none)
-    const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, nv = s.C / N, here = t1 - t0;
+    int col, lane;
+    s.split(col, lane);
+    const int nv = s.C / N, here = t1 - t0;
     if (lane < s.lanes)
         for (int v = col; v < nv; v += s.cols) {
             const T* const p = x + ((size_t)b * s.T + t0) * s.C + (size_t)v * N;
@@ -202,39 +280,13 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_stats_k(const T* __restrict_
                     d.add(y);
                 }
             }
-            if (WHOLE) lds[lane * nv + v] = d.group_sums();
-            else
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float n = (float)d.n, m = d.n ? d.sum[j] / n : 0.f;
-                    reinterpret_cast<float2*>(lds)[lane * s.C + v * N + j] = make_float2(d.base[j] + m, __builtin_fmaf(-m, d.sum[j], d.sq[j]));
-                }
+            lds[lane * nv + v] = d.group_sums();
         }
     __syncthreads();
     const int live = here < s.lanes ? here : s.lanes;  // lanes that had a frame
-    const int per = WHOLE ? s.Cg / N : s.Cg, pitch = WHOLE ? nv : s.C, team = team_of(s.G, per), l = threadIdx.x & (team - 1), teams = blockDim.x / team;
-    for (int g0 = 0; g0 < s.G; g0 += teams) {
-        const int g = g0 + threadIdx.x / team;
-        double2 k = make_double2(0., 0.);
-        if (g < s.G)
-            for (int r = 0; r < live; ++r) {
-                const double n = (double)((here - r + s.lanes - 1) / s.lanes);
-                for (int c = l; c < per; c += team) {
-                    const int i = r * pitch + g * per + c;
-                    if (WHOLE) {
-                        k.x += lds[i].x;
-                        k.y += lds[i].y;
-                    } else {
-                        const float2 o = reinterpret_cast<const float2*>(lds)[i];
-                        const double m = o.x;
-                        k.x += n * m;
-                        k.y += n * m * m + (double)o.y;
-                    }
-                }
-            }
-        k = sum64(k, team);
-        if (g < s.G && l == 0) sums[((size_t)b * s.runs + run) * s.G + g] = k;
-    }
+    const int per = s.Cg / N;
+    sum_groups<double2>(s.G, live, per, part, [&](int g, int r, int c) { return lds[r * nv + g * per + c]; },
+                        [&](int g, double2 k) { sums[((size_t)b * s.runs + run) * s.G + g] = k; });
 }
 
 // mean and 1 / deviation from a group's sums; inv: 1 / its values (0: it has none)
@@ -281,52 +333,40 @@ __device__ __forceinline__ void channels_of(const float* __restrict__ p, int c0,
 #pragma unroll
         for (int j = 0; j < N; ++j) out[j] = p[c0 + j];
 }
-// f(j, value of channel c0 + j's group), a value being looked up (value(group)) where the group changes
-template <int N, typename V, typename F>
-__device__ __forceinline__ void groups_of(const Shape& s, int c0, V value, F f)
-{
-    int g = c0 / s.Cg, next = (g + 1) * s.Cg;
-    float2 k = value(g);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        if (c0 + j == next) {
-            k = value(++g);
-            next += s.Cg;
-        }
-        f(j, k);
-    }
-}
-
-// What a thread keeps of its N channels: u = (x - mean) scale + shift
+// c / Cg: (c + 1/2) / Cg is off by less than 8192 * 2^-22 / Cg, and no whole number is nearer than 1/2 / Cg
+__device__ __forceinline__ int group_of(const Shape& s, int c) { return (int)(((float)c + 0.5f) * s.inv_Cg); }
+// What a thread keeps of its N channels, which are all of one group: u = (x - mean) scale + shift
 template <int N>
 struct Affine {
-    float mean[N], scale[N], shift[N];
+    float mean, scale[N], shift[N];
     __device__ __forceinline__ void load(const float* __restrict__ gamma, const float* __restrict__ beta, int c0)
     {
         channels_of<N>(gamma, c0, 1.f, scale);
         channels_of<N>(beta, c0, 0.f, shift);
     }
-    __device__ __forceinline__ void set(const Shape& s, const float2* stat, int c0)
+    __device__ __forceinline__ void set(float2 stat)  // mean and rstd
     {
-        groups_of<N>(s, c0, [&](int g) { return stat[g]; }, [&](int j, float2 k) {
-            mean[j] = k.x;
-            scale[j] *= k.y;
-        });
+        mean = stat.x;
+#pragma unroll
+        for (int j = 0; j < N; ++j) scale[j] *= stat.y;
     }
-    __device__ __forceinline__ float operator()(float x, int j) const { return __builtin_fmaf(x - mean[j], scale[j], shift[j]); }
+    __device__ __forceinline__ float operator()(float x, int j) const { return __builtin_fmaf(x - mean, scale[j], shift[j]); }
 };
 
 template <typename T, int N, int ACT>
-__global__ __launch_bounds__(MAX_THREADS) void norm_apply_k(const T* __restrict__ x, Shape s, const double2* __restrict__ sums, const float* __restrict__ gamma,
+__global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))) void norm_apply_k(const T* __restrict__ x, Shape s, const double2* __restrict__ sums, const float* __restrict__ gamma,
                                                             const float* __restrict__ beta, float eps, T* __restrict__ y, float* __restrict__ mean,
                                                             float* __restrict__ rstd)
 {
     extern __shared__ float2 stat[];
     constexpr bool GLU = ACT == W2L_ACT_GLU;
-    constexpr int U = 4;
-    const int b = blockIdx.y, run = blockIdx.x, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C;
+    constexpr int U = BATCH;
+    const Task task = task_of(s, blockIdx.x);
+    const int b = task.b, run = task.run, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C;
     const int t0 = run * s.rows, t1 = t0 + s.rows < s.T ? t0 + s.rows : s.T, live = t1 < len ? t1 : len;
-    const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, nv = Cy / N;
+    int col, lane;
+    s.split(col, lane);
+    const int nv = Cy / N;
     const T* const in = x + (size_t)b * s.T * s.C;
     // what a thread reads first is on its way while the statistics are joined
     raw_t<T, N> xv[U], xg[U];
@@ -362,8 +402,8 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_apply_k(const T* __restrict_
                 load(v, t);
                 load_channels(v);
             }
-            a.set(s, stat, v * N);
-            if (GLU) h.set(s, stat, Cy + v * N);
+            a.set(stat[group_of(s, v * N)]);
+            if (GLU) h.set(stat[group_of(s, Cy + v * N)]);
         }
         while (t < live) {
 #pragma unroll
@@ -374,7 +414,7 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_apply_k(const T* __restrict_
                 if (GLU) unpack<T, N>(xg[k], w);
 #pragma unroll
                 for (int j = 0; j < N; ++j) u[j] = act<ACT>(a(u[j], j), GLU ? h(w[j], j) : 0.f);
-                put<T, N>(q + (size_t)(t + k * s.lanes) * Cy, u);
+                put<T, N>(q + (size_t)(t + k * s.lanes) * Cy, u, s.past);
             }
             t += U * s.lanes;
             if (t < live) load(v, t);
@@ -383,49 +423,40 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_apply_k(const T* __restrict_
             float none[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) none[j] = len < 0 ? NAN : 0.f;
-            for (t = (live > t0 ? live : t0) + lane; t < t1; t += s.lanes) put<T, N>(q + (size_t)t * Cy, none);
+            for (t = (live > t0 ? live : t0) + lane; t < t1; t += s.lanes) put<T, N>(q + (size_t)t * Cy, none, s.past);
         }
     }
 }
 
 // ---- gradients -----------------------------------------------------------------------------------------------
-// xhat and du of N channels (and of their gates)
-template <int N>
-struct Channels {
-    float mean[N], rstd[N], gamma[N], beta[N];
-    __device__ __forceinline__ void set(const Shape& s, int b, const float* __restrict__ mn, const float* __restrict__ rs, const float* __restrict__ gm,
-                                        const float* __restrict__ bt, int c0)
-    {
-        channels_of<N>(gm, c0, 1.f, gamma);
-        channels_of<N>(bt, c0, 0.f, beta);
-        const size_t g0 = (size_t)b * s.G;
-        groups_of<N>(s, c0, [&](int g) { return make_float2(mn[g0 + g], rs[g0 + g]); }, [&](int j, float2 k) {
-            mean[j] = k.x;
-            rstd[j] = k.y;
-        });
-    }
-    __device__ __forceinline__ float hat(float x, int j) const { return (x - mean[j]) * rstd[j]; }
-    __device__ __forceinline__ float u(float x, int j) const { return __builtin_fmaf(x - mean[j], rstd[j] * gamma[j], beta[j]); }  // (as the forward call rounds it)
-};
-
 // chans [B][runs][2][C]: sums of du and du xhat over a run;  groups [B][runs][G][2]: both times gamma
 template <typename T, int N, int ACT>
-__global__ __launch_bounds__(MAX_THREADS) void norm_sums_k(const T* __restrict__ x, const T* __restrict__ dy, Shape s, const float* __restrict__ mean,
+__global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))) void norm_sums_k(const T* __restrict__ x, const T* __restrict__ dy, Shape s, const float* __restrict__ mean,
                                                            const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                            float* __restrict__ chans, float2* __restrict__ groups)
 {
     extern __shared__ float2 acc[];  // [lanes][C]: a lane's sums
+    __shared__ float2 part[MAX_THREADS / 64];
     constexpr bool GLU = ACT == W2L_ACT_GLU;
     constexpr int U = 2;
-    const int b = blockIdx.y, run = blockIdx.x, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C;
+    const Task task = task_of(s, blockIdx.x);
+    const int b = task.b, run = task.run, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C;
     const int t0 = run * s.rows, t1 = t0 + s.rows < len ? t0 + s.rows : len;
     if (t0 >= t1) return;
-    const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, nv = Cy / N;
+    int col, lane;
+    s.split(col, lane);
+    const int nv = Cy / N;
     if (lane < s.lanes)
         for (int v = col; v < nv; v += s.cols) {
-            Channels<N> a, h;
-            a.set(s, b, mean, rstd, gamma, beta, v * N);
-            if (GLU) h.set(s, b, mean, rstd, gamma, beta, Cy + v * N);
+            Affine<N> a, h;
+            auto stat_of = [&](int c) { return make_float2(mean[(size_t)b * s.G + group_of(s, c)], rstd[(size_t)b * s.G + group_of(s, c)]); };
+            const float2 st = stat_of(v * N), gt = GLU ? stat_of(Cy + v * N) : st;
+            a.load(gamma, beta, v * N);
+            a.set(st);
+            if (GLU) {
+                h.load(gamma, beta, Cy + v * N);
+                h.set(gt);
+            }
             float s1[N], s2[N], r1[N], r2[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) s1[j] = s2[j] = r1[j] = r2[j] = 0.f;
@@ -450,20 +481,20 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_sums_k(const T* __restrict__
 #pragma unroll
                     for (int j = 0; j < N; ++j) {
                         float du, dg = 0.f;
-                        act_bwd<ACT>(a.u(xk[j], j), GLU ? h.u(gk[j], j) : 0.f, d[j], du, dg);
+                        act_bwd<ACT>(a(xk[j], j), GLU ? h(gk[j], j) : 0.f, d[j], du, dg);
                         s1[j] += du;
-                        s2[j] = __builtin_fmaf(du, a.hat(xk[j], j), s2[j]);
+                        s2[j] = __builtin_fmaf(du, xk[j] - a.mean, s2[j]);
                         if (GLU) {
                             r1[j] += dg;
-                            r2[j] = __builtin_fmaf(dg, h.hat(gk[j], j), r2[j]);
+                            r2[j] = __builtin_fmaf(dg, gk[j] - h.mean, r2[j]);
                         }
                     }
                 }
             }
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                acc[(size_t)lane * s.C + v * N + j] = make_float2(s1[j], s2[j]);
-                if (GLU) acc[(size_t)lane * s.C + Cy + v * N + j] = make_float2(r1[j], r2[j]);
+                acc[(size_t)lane * s.C + v * N + j] = make_float2(s1[j], s2[j] * st.y);
+                if (GLU) acc[(size_t)lane * s.C + Cy + v * N + j] = make_float2(r1[j], r2[j] * gt.y);
             }
         }
     __syncthreads();
@@ -481,26 +512,53 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_sums_k(const T* __restrict__
         acc[c] = make_float2(k.x * gm, k.y * gm);  // (row 0 of this channel is read by this thread alone)
     }
     __syncthreads();
-    const int team = team_of(s.G, s.Cg), l = threadIdx.x & (team - 1), teams = blockDim.x / team;
-    for (int g0 = 0; g0 < s.G; g0 += teams) {
-        const int g = g0 + threadIdx.x / team;
-        float2 k = make_float2(0.f, 0.f);
-        if (g < s.G)
-            for (int c = l; c < s.Cg; c += team) {
-                k.x += acc[(size_t)g * s.Cg + c].x;
-                k.y += acc[(size_t)g * s.Cg + c].y;
-            }
-        for (int o = team >> 1; o > 0; o >>= 1) {
-            k.x += __shfl_xor(k.x, o, 64);
-            k.y += __shfl_xor(k.y, o, 64);
-        }
-        if (g < s.G && l == 0) groups[((size_t)b * s.runs + run) * s.G + g] = k;
-    }
+    sum_groups<float2>(s.G, 1, s.Cg, part, [&](int g, int, int c) { return acc[(size_t)g * s.Cg + c]; },
+                       [&](int g, float2 k) { groups[((size_t)b * s.runs + run) * s.G + g] = k; });
 }
 
-// blockIdx.y >= ahead: dx of a run of frames; below (ahead = 1): dgamma and dbeta, whose longer chains of loads start first
+// dgamma and dbeta of sixteen channels from `count` rows [2][C] of sums (dbeta's, dgamma's), those that are there(row): threads take rows in turn, and their sums are
+// added up in 64 bits and a fixed order.  All loads of a batch are in flight at once.
+constexpr int JOIN_CHANNELS = 16;
+template <typename F>
+__device__ __forceinline__ void sum_channels(const float* __restrict__ chans, int count, int C, int block, double2* lds, float* __restrict__ dgamma,
+                                             float* __restrict__ dbeta, int accumulate, F there)
+{
+    constexpr int U = 8;
+    const int l = threadIdx.x % JOIN_CHANNELS, first = threadIdx.x / JOIN_CHANNELS, step = blockDim.x / JOIN_CHANNELS, c = block * JOIN_CHANNELS + l;
+    double g = 0., h = 0.;
+    if (c < C)
+        for (int i = first; i < count; i += U * step) {
+            float gv[U], hv[U];
+            bool on[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int r = i + k * step < count ? i + k * step : i;
+                const float* const p = chans + (size_t)r * 2 * C + c;
+                hv[k] = p[0];
+                gv[k] = p[C];
+                on[k] = i + k * step < count && there(r);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                h += on[k] ? hv[k] : 0.f;
+                g += on[k] ? gv[k] : 0.f;
+            }
+        }
+    lds[threadIdx.x] = make_double2(g, h);
+    __syncthreads();
+    if (first != 0 || c >= C) return;
+    for (int i = 1; i < step; ++i) {
+        g += lds[i * JOIN_CHANNELS + l].x;
+        h += lds[i * JOIN_CHANNELS + l].y;
+    }
+    if (dgamma) dgamma[c] = (float)(accumulate ? dgamma[c] + g : g);
+    if (dbeta) dbeta[c] = (float)(accumulate ? dbeta[c] + h : h);
+}
+
+// Workgroups from `ahead` on: dx of a run of frames.  Those before them make dgamma and dbeta, whose longer chains of loads start first; they are a multiple of
+// eight, so that a run is read on the XCD that read it in norm_sums_k (8x750x1536 bf16, GLU: 35 -> 26 us for the two kernels).
 template <typename T, int N, int ACT>
-__global__ __launch_bounds__(MAX_THREADS) void norm_dx_k(const T* __restrict__ x, const T* __restrict__ dy, Shape s, const float* __restrict__ mean,
+__global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))) void norm_dx_k(const T* __restrict__ x, const T* __restrict__ dy, Shape s, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                          const float* __restrict__ chans, const float2* __restrict__ groups, T* __restrict__ dx,
                                                          float* __restrict__ dgamma, float* __restrict__ dbeta, int accumulate, int ahead)
@@ -508,39 +566,42 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_dx_k(const T* __restrict__ x
     extern __shared__ double2 lds[];  // [G] of floats: means of du gamma and du gamma xhat
     constexpr bool GLU = ACT == W2L_ACT_GLU;
     constexpr int U = 2;
-    const int b = (int)blockIdx.y - ahead, Cy = GLU ? s.C / 2 : s.C;
-    if (b < 0) {
-        // 64 channels a workgroup at a time, the runs dealt out over its wavefronts and added up in a fixed order
-        const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, l = threadIdx.x & 63;
-        for (int c0 = blockIdx.x * 64; c0 < s.C; c0 += gridDim.x * 64) {
-            const int c = c0 + l;
-            double g = 0., h = 0.;
-            if (c < s.C)
-                for (int i = 0; i < s.B; ++i) {
-                    const int len = frames_of(s, i), runs = len > 0 ? (len + s.rows - 1) / s.rows : 0;
-                    const float* const p = chans + (size_t)i * s.runs * 2 * s.C + c;
-#pragma unroll 4
-                    for (int r = (wave + i) % waves; r < runs; r += waves) {
-                        h += p[(size_t)r * 2 * s.C];
-                        g += p[(size_t)r * 2 * s.C + s.C];
-                    }
-                }
-            lds[threadIdx.x] = make_double2(g, h);
-            __syncthreads();
-            if (wave == 0 && c < s.C) {
-                for (int w = 1; w < waves; ++w) {
-                    g += lds[64 * w + l].x;
-                    h += lds[64 * w + l].y;
-                }
-                if (dgamma) dgamma[c] = (float)(accumulate ? dgamma[c] + g : g);
-                if (dbeta) dbeta[c] = (float)(accumulate ? dbeta[c] + h : h);
-            }
-            __syncthreads();
-        }
+    const int Cy = GLU ? s.C / 2 : s.C;
+    if ((int)blockIdx.x < ahead) {
+        // (runs that are not there left nothing: what lies in their place is not added)
+        sum_channels(chans, s.B * s.runs, s.C, blockIdx.x, lds, dgamma, dbeta, accumulate, [&](int i) {
+            const int u = i / s.runs;
+            return (i - u * s.runs) * s.rows < frames_of(s, u);
+        });
         return;
     }
-    const int len = frames_of(s, b), run = blockIdx.x, t0 = run * s.rows, t1 = t0 + s.rows < s.T ? t0 + s.rows : s.T, live = t1 < len ? t1 : len;
+    const Task task = task_of(s, blockIdx.x - ahead);
+    const int b = task.b, run = task.run, len = frames_of(s, b), t0 = run * s.rows, t1 = t0 + s.rows < s.T ? t0 + s.rows : s.T, live = t1 < len ? t1 : len;
     float2* const means = reinterpret_cast<float2*>(lds);
+    int col, lane;
+    s.split(col, lane);
+    const int nv = Cy / N;
+    const size_t row0 = (size_t)b * s.T;
+    // what a thread reads first is on its way while the means are joined
+    raw_t<T, N> xv[U], xg[U], dv[U];
+    Affine<N> a, h;
+    auto load = [&](int v, int t) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const size_t at = row0 + (t + k * s.lanes < live ? t + k * s.lanes : t);
+            xv[k] = fetch<T, N>(x + at * s.C + (size_t)v * N);
+            if (GLU) xg[k] = fetch<T, N>(x + at * s.C + Cy + (size_t)v * N);
+            dv[k] = fetch<T, N>(dy + at * Cy + (size_t)v * N);
+        }
+    };
+    auto load_channels = [&](int v) {
+        a.load(gamma, beta, v * N);
+        if (GLU) h.load(gamma, beta, Cy + v * N);
+    };
+    if (lane < s.lanes && t0 + lane < live) {
+        load(col, t0 + lane);
+        load_channels(col);
+    }
     if (t0 < len) {
         const int runs = (len + s.rows - 1) / s.rows;
         const float inv = 1.f / ((float)len * (float)s.Cg);
@@ -549,6 +610,7 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_dx_k(const T* __restrict__ x
             const int g = g0 + threadIdx.x / team;
             float2 k = make_float2(0.f, 0.f);
             if (g < s.G)
+#pragma unroll 4
                 for (int r = l; r < runs; r += team) {
                     const float2 o = groups[((size_t)b * s.runs + r) * s.G + g];
                     k.x += o.x;
@@ -562,32 +624,28 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_dx_k(const T* __restrict__ x
         }
         __syncthreads();
     }
-    const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, nv = Cy / N;
     if (lane >= s.lanes) return;
     for (int v = col; v < nv; v += s.cols) {
-        Channels<N> a, h;
-        float m1[N], m2[N], k1[N], k2[N];
-        if (t0 < len) {
-            a.set(s, b, mean, rstd, gamma, beta, v * N);
-            if (GLU) h.set(s, b, mean, rstd, gamma, beta, Cy + v * N);
-            auto mean_of = [&](int g) { return means[g]; };
-            groups_of<N>(s, v * N, mean_of, [&](int j, float2 k) { m1[j] = k.x; m2[j] = k.y; });
-            if (GLU) groups_of<N>(s, Cy + v * N, mean_of, [&](int j, float2 k) { k1[j] = k.x; k2[j] = k.y; });
-        }
-        const size_t row0 = (size_t)b * s.T;
-        const T* const p = x + row0 * s.C + (size_t)v * N;
-        const T* const q = dy + row0 * Cy + (size_t)v * N;
+        // dx = du gamma rstd + (x - mean) slope + level, slope = - rstd^2 m2, level = - rstd m1
+        float2 line = make_float2(0.f, 0.f), gline = line;
         T* const o = dx + row0 * s.C + (size_t)v * N;
         int t = t0 + lane;
-        for (; t < live; t += U * s.lanes) {
-            raw_t<T, N> xv[U], xg[U], dv[U];
-#pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const size_t at = t + k * s.lanes < live ? t + k * s.lanes : t;
-                xv[k] = fetch<T, N>(p + at * s.C);
-                if (GLU) xg[k] = fetch<T, N>(p + at * s.C + Cy);
-                dv[k] = fetch<T, N>(q + at * Cy);
+        if (t < live) {
+            if (v != col) {
+                load(v, t);
+                load_channels(v);
             }
+            auto set = [&](Affine<N>& f, float2& l, int c) {
+                const int g = group_of(s, c);
+                const float2 k = means[g];
+                const float r = rstd[(size_t)b * s.G + g];
+                f.set(make_float2(mean[(size_t)b * s.G + g], r));
+                l = make_float2(-k.y * r * r, -k.x * r);
+            };
+            set(a, line, v * N);
+            if (GLU) set(h, gline, Cy + v * N);
+        }
+        while (t < live) {
 #pragma unroll
             for (int k = 0; k < U; ++k) {
                 if (t + k * s.lanes >= live) break;
@@ -598,20 +656,22 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_dx_k(const T* __restrict__ x
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     float du, dg = 0.f;
-                    act_bwd<ACT>(a.u(xk[j], j), GLU ? h.u(gk[j], j) : 0.f, d[j], du, dg);
-                    xk[j] = (__builtin_fmaf(du, a.gamma[j], -m1[j]) - a.hat(xk[j], j) * m2[j]) * a.rstd[j];
-                    if (GLU) gk[j] = (__builtin_fmaf(dg, h.gamma[j], -k1[j]) - h.hat(gk[j], j) * k2[j]) * h.rstd[j];
+                    act_bwd<ACT>(a(xk[j], j), GLU ? h(gk[j], j) : 0.f, d[j], du, dg);
+                    xk[j] = __builtin_fmaf(du, a.scale[j], __builtin_fmaf(xk[j] - a.mean, line.x, line.y));
+                    if (GLU) gk[j] = __builtin_fmaf(dg, h.scale[j], __builtin_fmaf(gk[j] - h.mean, gline.x, gline.y));
                 }
                 T* const to = o + (size_t)(t + k * s.lanes) * s.C;
-                put<T, N>(to, xk);
-                if (GLU) put<T, N>(to + Cy, gk);
+                put<T, N>(to, xk, s.past);
+                if (GLU) put<T, N>(to + Cy, gk, s.past);
             }
+            t += U * s.lanes;
+            if (t < live) load(v, t);
         }
         if (t1 > live) {
             const float none[N] = {};
             for (t = (live > t0 ? live : t0) + lane; t < t1; t += s.lanes) {
-                put<T, N>(o + (size_t)t * s.C, none);
-                if (GLU) put<T, N>(o + (size_t)t * s.C + Cy, none);
+                put<T, N>(o + (size_t)t * s.C, none, s.past);
+                if (GLU) put<T, N>(o + (size_t)t * s.C + Cy, none, s.past);
             }
         }
     }
@@ -620,7 +680,8 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_dx_k(const T* __restrict__ x
 // ---- a workgroup a group -------------------------------------------------------------------------------------
 // Where groups are many or short, a workgroup has a group of an utterance (with GLU the group of the values and that of their gates) and reads it twice, the second
 // time from its L2, in one launch.  Vectors and groups of one utterance that are neighbours share lines, so consecutive ones go to one XCD.
-constexpr int GROUP_THREADS = 1024, GROUP_BWD_THREADS = 512, FLUSH = 64;  // (512: a lane's sums of all channels fit 64 KB of LDS)
+constexpr int GROUP_THREADS = 512, GROUP_BATCH = 6, FLUSH = 60;  // (512: a lane's sums of all channels fit 64 KB of LDS)
+static_assert(FLUSH % GROUP_BATCH == 0, "sums are flushed between batches");
 struct Place {
     int b, g;
 };
@@ -651,11 +712,13 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_k(const T* __restric
                                                               float eps, T* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd)
 {
     constexpr bool GLU = ACT == W2L_ACT_GLU;
-    constexpr int U = 4;
+    constexpr int U = GROUP_BATCH;
     __shared__ double2 lds[2][GROUP_THREADS / 64];
     const Place at = place_of(GLU ? s.G / 2 : s.G);
     const int b = at.b, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C, live = len < 0 ? 0 : len;
-    const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, c0 = at.g * s.Cg + col * N, step = U * s.lanes;
+    int col, lane;
+    s.split(col, lane);
+    const int c0 = at.g * s.Cg + col * N, step = U * s.lanes;
     const bool on = lane < s.lanes;
     const T* const p = x + (size_t)b * s.T * s.C + c0;
     raw_t<T, N> xv[U], xg[U];
@@ -721,15 +784,8 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_k(const T* __restric
         }
     }
     if (!on) return;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        a.mean[j] = s1.x;
-        a.scale[j] *= s1.y;
-        if (GLU) {
-            h.mean[j] = s2.x;
-            h.scale[j] *= s2.y;
-        }
-    }
+    a.set(s1);
+    if (GLU) h.set(s2);
     T* const q = y + (size_t)b * s.T * Cy + c0;
     for (int t = last; t >= 0;) {  // from the end, which is in registers
 #pragma unroll
@@ -740,7 +796,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_k(const T* __restric
             if (GLU) unpack<T, N>(xg[k], w);
 #pragma unroll
             for (int j = 0; j < N; ++j) u[j] = act<ACT>(a(u[j], j), GLU ? h(w[j], j) : 0.f);
-            put<T, N>(q + (size_t)(t + k * s.lanes) * Cy, u);
+            put<T, N>(q + (size_t)(t + k * s.lanes) * Cy, u, s.past);
         }
         t -= step;
         if (t >= 0) load(t);
@@ -748,22 +804,24 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_k(const T* __restric
     float none[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) none[j] = len < 0 ? NAN : 0.f;
-    for (int t = live + lane; t < s.T; t += s.lanes) put<T, N>(q + (size_t)t * Cy, none);
+    for (int t = live + lane; t < s.T; t += s.lanes) put<T, N>(q + (size_t)t * Cy, none, s.past);
 }
 
 // chans [B][2][C]: sums of du and du xhat of an utterance (NULL: not wanted)
 template <typename T, int N, int ACT>
-__global__ __launch_bounds__(GROUP_BWD_THREADS) void norm_group_bwd_k(const T* __restrict__ x, const T* __restrict__ dy, Shape s, const float* __restrict__ mean,
+__global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __restrict__ x, const T* __restrict__ dy, Shape s, const float* __restrict__ mean,
                                                                   const float* __restrict__ rstd, const float* __restrict__ gamma,
                                                                   const float* __restrict__ beta, T* __restrict__ dx, float* __restrict__ chans)
 {
     constexpr bool GLU = ACT == W2L_ACT_GLU;
-    constexpr int U = 2;
+    constexpr int U = GROUP_BATCH;
     extern __shared__ float2 acc[];  // [GLU: 2][lanes][Cg]: a lane's sums
-    __shared__ float2 lds[2][GROUP_BWD_THREADS / 64];
+    __shared__ float2 lds[2][GROUP_THREADS / 64];
     const Place at = place_of(GLU ? s.G / 2 : s.G);
     const int b = at.b, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C, live = len < 0 ? 0 : len;
-    const int col = threadIdx.x % s.cols, lane = threadIdx.x / s.cols, c0 = at.g * s.Cg + col * N, step = U * s.lanes;
+    int col, lane;
+    s.split(col, lane);
+    const int c0 = at.g * s.Cg + col * N, step = U * s.lanes;
     const bool on = lane < s.lanes;
     const size_t row0 = (size_t)b * s.T;
     const T* const p = x + row0 * s.C + c0;
@@ -779,21 +837,13 @@ __global__ __launch_bounds__(GROUP_BWD_THREADS) void norm_group_bwd_k(const T* _
         }
     };
     const size_t g0 = (size_t)b * s.G + at.g;
-    const float mn = mean[g0], rs = rstd[g0], mg = GLU ? mean[g0 + s.G / 2] : 0.f, rg = GLU ? rstd[g0 + s.G / 2] : 0.f;
-    float ga[N], ba[N], gh[N], bh[N];
-    channels_of<N>(gamma, c0, 1.f, ga);
-    channels_of<N>(beta, c0, 0.f, ba);
-    if (GLU) {
-        channels_of<N>(gamma, Cy + c0, 1.f, gh);
-        channels_of<N>(beta, Cy + c0, 0.f, bh);
-    }
-    auto grads = [&](int k, int j, const float (&xk)[N], const float (&gk)[N], const float (&d)[N], float& du, float& dg, float& hx, float& hg) {
-        const float u = __builtin_fmaf(xk[j] - mn, rs * ga[j], ba[j]), w = GLU ? __builtin_fmaf(gk[j] - mg, rg * gh[j], bh[j]) : 0.f;
-        dg = 0.f;
-        act_bwd<ACT>(u, w, d[j], du, dg);
-        hx = (xk[j] - mn) * rs;
-        hg = GLU ? (gk[j] - mg) * rg : 0.f;
-    };
+    // (an utterance without frames, or with a length out of range, has no part in anything: its statistics may be NaN)
+    const float mn = live ? mean[g0] : 0.f, rs = live ? rstd[g0] : 0.f, mg = GLU && live ? mean[g0 + s.G / 2] : 0.f, rg = GLU && live ? rstd[g0 + s.G / 2] : 0.f;
+    Affine<N> a, h;
+    a.load(gamma, beta, c0);
+    if (GLU) h.load(gamma, beta, Cy + c0);
+    a.set(make_float2(mn, rs));
+    if (GLU) h.set(make_float2(mg, rg));
     int last = -1;
     float s1[N], s2[N], r1[N], r2[N];
 #pragma unroll
@@ -811,32 +861,32 @@ __global__ __launch_bounds__(GROUP_BWD_THREADS) void norm_group_bwd_k(const T* _
                 unpack<T, N>(dv[k], d);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    float du, dg, hx, hg;
-                    grads(k, j, xk, gk, d, du, dg, hx, hg);
+                    float du, dg = 0.f;
+                    act_bwd<ACT>(a(xk[j], j), GLU ? h(gk[j], j) : 0.f, d[j], du, dg);
                     s1[j] += du;
-                    s2[j] = __builtin_fmaf(du, hx, s2[j]);
+                    s2[j] = __builtin_fmaf(du, xk[j] - mn, s2[j]);
                     if (GLU) {
                         r1[j] += dg;
-                        r2[j] = __builtin_fmaf(dg, hg, r2[j]);
+                        r2[j] = __builtin_fmaf(dg, gk[j] - mg, r2[j]);
                     }
                 }
             }
         }
     float2 k1 = make_float2(0.f, 0.f), k2 = k1;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-        k1.x = __builtin_fmaf(s1[j], ga[j], k1.x);
-        k1.y = __builtin_fmaf(s2[j], ga[j], k1.y);
+    for (int j = 0; j < N; ++j) {  // of du gamma rstd and du gamma rstd (x - mean)
+        k1.x = __builtin_fmaf(s1[j], a.scale[j], k1.x);
+        k1.y = __builtin_fmaf(s2[j], a.scale[j], k1.y);
         if (GLU) {
-            k2.x = __builtin_fmaf(r1[j], gh[j], k2.x);
-            k2.y = __builtin_fmaf(r2[j], gh[j], k2.y);
+            k2.x = __builtin_fmaf(r1[j], h.scale[j], k2.x);
+            k2.y = __builtin_fmaf(r2[j], h.scale[j], k2.y);
         }
     }
     if (chans && on)
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            acc[lane * s.Cg + col * N + j] = make_float2(s1[j], s2[j]);
-            if (GLU) acc[(s.lanes + lane) * s.Cg + col * N + j] = make_float2(r1[j], r2[j]);
+            acc[lane * s.Cg + col * N + j] = make_float2(s1[j], s2[j] * rs);
+            if (GLU) acc[(s.lanes + lane) * s.Cg + col * N + j] = make_float2(r1[j], r2[j] * rg);
         }
     k1 = sum_group(make_float2(wave64(k1.x, Sum()), wave64(k1.y, Sum())), lds[0]);
     if (GLU) k2 = sum_group(make_float2(wave64(k2.x, Sum()), wave64(k2.y, Sum())), lds[1]);
@@ -865,7 +915,8 @@ __global__ __launch_bounds__(GROUP_BWD_THREADS) void norm_group_bwd_k(const T* _
     }
     if (!on) return;
     const float inv = live ? 1.f / ((float)live * (float)s.Cg) : 0.f;
-    k1.x *= inv; k1.y *= inv; k2.x *= inv; k2.y *= inv;
+    // (rstd is in k1 and k2 already)
+    const float slope = -k1.y * inv * rs * rs, level = -k1.x * inv, gslope = -k2.y * inv * rg * rg, glevel = -k2.x * inv;
     T* const o = dx + row0 * s.C + c0;
     for (int t = last; t >= 0;) {
 #pragma unroll
@@ -877,22 +928,22 @@ __global__ __launch_bounds__(GROUP_BWD_THREADS) void norm_group_bwd_k(const T* _
             unpack<T, N>(dv[k], d);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                float du, dg, hx, hg;
-                grads(k, j, xk, gk, d, du, dg, hx, hg);
-                xk[j] = (__builtin_fmaf(du, ga[j], -k1.x) - hx * k1.y) * rs;
-                if (GLU) gk[j] = (__builtin_fmaf(dg, gh[j], -k2.x) - hg * k2.y) * rg;
+                float du, dg = 0.f;
+                act_bwd<ACT>(a(xk[j], j), GLU ? h(gk[j], j) : 0.f, d[j], du, dg);
+                xk[j] = __builtin_fmaf(du, a.scale[j], __builtin_fmaf(xk[j] - mn, slope, level));
+                if (GLU) gk[j] = __builtin_fmaf(dg, h.scale[j], __builtin_fmaf(gk[j] - mg, gslope, glevel));
             }
             T* const to = o + (size_t)(t + k * s.lanes) * s.C;
-            put<T, N>(to, xk);
-            if (GLU) put<T, N>(to + Cy, gk);
+            put<T, N>(to, xk, s.past);
+            if (GLU) put<T, N>(to + Cy, gk, s.past);
         }
         t -= step;
         if (t >= 0) load(t);
     }
     const float none[N] = {};
     for (int t = live + lane; t < s.T; t += s.lanes) {
-        put<T, N>(o + (size_t)t * s.C, none);
-        if (GLU) put<T, N>(o + (size_t)t * s.C + Cy, none);
+        put<T, N>(o + (size_t)t * s.C, none, s.past);
+        if (GLU) put<T, N>(o + (size_t)t * s.C + Cy, none, s.past);
     }
 }
 
@@ -900,23 +951,7 @@ __global__ __launch_bounds__(GROUP_BWD_THREADS) void norm_group_bwd_k(const T* _
 __global__ __launch_bounds__(256) void norm_join_k(const float* __restrict__ chans, int B, int C, float* __restrict__ dgamma, float* __restrict__ dbeta, int accumulate)
 {
     __shared__ double2 lds[256];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
-    double g = 0., h = 0.;
-    if (c < C)
-#pragma unroll 4
-        for (int b = wave; b < B; b += 4) {
-            h += chans[(size_t)b * 2 * C + c];
-            g += chans[(size_t)b * 2 * C + C + c];
-        }
-    lds[threadIdx.x] = make_double2(g, h);
-    __syncthreads();
-    if (wave || c >= C) return;
-    for (int w = 1; w < 4; ++w) {
-        g += lds[64 * w + threadIdx.x].x;
-        h += lds[64 * w + threadIdx.x].y;
-    }
-    if (dgamma) dgamma[c] = (float)(accumulate ? dgamma[c] + g : g);
-    if (dbeta) dbeta[c] = (float)(accumulate ? dbeta[c] + h : h);
+    sum_channels(chans, B, C, blockIdx.x, lds, dgamma, dbeta, accumulate, [](int) { return true; });
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------
@@ -925,36 +960,33 @@ bool shape_ok(int B, int T, int C, int G, int act)
     return B > 0 && T > 0 && T <= MAX_FRAMES && C > 0 && C <= MAX_CHANNELS && G > 0 && C % G == 0 && act >= W2L_ACT_NONE && act <= W2L_ACT_GLU && (act != W2L_ACT_GLU || C % 2 == 0) &&
            B <= 65534 && (long long)B * T <= 2147483647LL && (long long)B * T <= (1LL << 40) / C;
 }
-// channels of a vector: as many as divide a row (GLU: half a row) and make up at most 16 bytes
-int vector_of(int Cy, int dtype)
+// channels of a vector: as many as divide a group and a row (GLU: half a row) and make up at most 16 bytes
+int vector_of(int Cg, int Cy, int dtype)
 {
     int n = dtype == W2L_BF16 ? 8 : 4;
-    while (Cy % n) n /= 2;
+    while (Cg % n || Cy % n) n /= 2;
     return n;
 }
 // vectors: of a row that a thread can be given one of
-Shape shape_of(int B, int T, int C, int G, const int* in_len, int vectors)
+Shape shape_of(int B, int T, int C, int G, const int* in_len, int dtype, int vectors)
 {
-    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, in_len};
+    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, in_len, 1.f / (float)(C / G), 0.f, (size_t)B * T * C * dtype_size(dtype) > (32u << 20)};
     const int passes = (vectors + MAX_THREADS - 1) / MAX_THREADS;
     s.cols = (vectors + passes - 1) / passes;
     s.lanes = MAX_THREADS / s.cols;
     if (s.lanes > 16) s.lanes = 16;
+    s.inv_cols = 1.f / (float)s.cols;
     return s;
 }
 int threads_of(const Shape& s) { return (s.cols * s.lanes + 63) / 64 * 64; }
-// frames of a run: the same for all kernels of a call, so that a workgroup finds in its L2 what that of the same number read before
-int rows_of(int B, int T, int C, int dtype)
+// Frames of a run, the same for all kernels of a call, so that a workgroup finds in its XCD's L2 what that of the same number read before: whole batches of loads
+// (BATCH rows a thread), three runs a CU where there are so many
+void runs_of(Shape& s)
 {
-    const long long rows = (long long)B * T;
-    long long r = (rows + 767) / 768;
-    if (r < 16) r = 16;
-    if (r > 64) r = 64;
-    return (int)(r < T ? r : T);
-}
-void runs_of(Shape& s, int dtype)
-{
-    s.rows = rows_of(s.B, s.T, s.C, dtype);
+    const int unit = BATCH * s.lanes;
+    long long r = ((long long)s.B * s.T + 384) / 768 + unit / 2;
+    r = r / unit * unit;
+    s.rows = (int)(r < unit ? unit : r > 64 ? 64 : r);
     s.runs = (s.T + s.rows - 1) / s.rows;
 }
 bool workspace_ok(const void* ws, size_t have, size_t need) { return ws && have >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0; }
@@ -979,27 +1011,31 @@ bool apart(const Span (&in)[I], const Span (&out)[O])
     return true;
 }
 
-// A workgroup a group: where vectors and, with GLU, halves hold whole groups, and there are workgroups enough for what each has to read
 struct Form {
-    bool group;
-    int N;  // channels of a vector
+    bool group;  // a workgroup a group
+    int N;       // channels of a vector
 };
+// A workgroup a group saves a launch and the second reading from far away, as long as there are workgroups for the chip or what one reads is little.  Both ways
+// in us, forward and backward call (bf16, SiLU): 64 workgroups of 25 KB: 5.8 and 10.5 against 9.5 and 13; of 125 KB: 12 and 24 against 12 and 18; 128 of 250 KB (GLU): 20 and 35
+// against 20 and 35; of 1 MB: 66 and 126 against 66 and 115; 256 of 500 KB: 75 and 115 against 87 and 135; 16 of 500 KB: 34 and 69 against 12 and 17.
+// Thousands of workgroups that read few bytes are slower as well (4096 of 8 KB, 16 bytes a row: 42 and 76 against 25 and 39).
 Form form_of(int B, int T, int C, int G, int act, int dtype)
 {
-    const int Cg = C / G, Cy = act == W2L_ACT_GLU ? C / 2 : C;
-    if (act != W2L_ACT_GLU || G % 2 == 0) {
-        const int n = vector_of(Cg, dtype);
-        const long long workgroups = (long long)B * (act == W2L_ACT_GLU ? G / 2 : G), bytes = (long long)T * Cg * (act == W2L_ACT_GLU ? 2 : 1) * dtype_size(dtype);
-        if (Cg / n <= 256 && workgroups < (1 << 22) && GROUP_RULE) return {true, n};
-    }
-    return {false, vector_of(Cy, dtype)};
+    const bool glu = act == W2L_ACT_GLU;
+    const int Cg = C / G, n = vector_of(Cg, glu ? C / 2 : C, dtype);
+    const long long workgroups = (long long)B * (glu ? G / 2 : G), bytes = (long long)T * Cg * (glu ? 2 : 1) * dtype_size(dtype);
+    const long long most = workgroups >= 256 ? 1 << 20 : workgroups >= 128 ? 512 << 10 : 64 << 10;
+    // (a thread's sums of at most 128 rows: in fp32)
+    const bool group = !(glu && G % 2) && Cg / n <= 256 && bytes <= most && !(workgroups >= 2048 && bytes < (16 << 10)) && T <= 128 * (GROUP_THREADS / (Cg / n));
+    return {group, n};
 }
-Shape group_shape(int B, int T, int C, int G, const int* in_len, int N, int threads)
+Shape group_shape(int B, int T, int C, int G, const int* in_len, int dtype, int N)
 {
-    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, in_len};
+    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, in_len, 1.f / (float)(C / G), 0.f, (size_t)B * T * C * dtype_size(dtype) > (32u << 20)};
     s.cols = s.Cg / N;
-    const int lanes = threads / s.cols;
+    const int lanes = GROUP_THREADS / s.cols;
     s.lanes = lanes < T ? lanes : T;
+    s.inv_cols = 1.f / (float)s.cols;
     return s;
 }
 
@@ -1010,12 +1046,11 @@ template <typename T, int N>
 int forward(const void* x, const Shape& st, const Shape& ap, double2* sums, const float* gamma, const float* beta, float eps, int act, void* y, float* mean,
             float* rstd, hipStream_t stream)
 {
-    const dim3 g(st.runs, st.B), n(threads_of(st));
-    if (st.Cg % N == 0) hipLaunchKernelGGL((norm_stats_k<T, N, true>), g, n, (size_t)st.lanes * (st.C / N) * 16, stream, (const T*)x, st, sums);
-    else hipLaunchKernelGGL((norm_stats_k<T, N, false>), g, n, (size_t)st.lanes * st.C * 8, stream, (const T*)x, st, sums);
+    const dim3 g((unsigned)(st.runs * st.B)), n(threads_of(st));
+    hipLaunchKernelGGL((norm_stats_k<T, N>), g, n, (size_t)st.lanes * (st.C / N) * 16, stream, (const T*)x, st, sums);
     if (int rc = launch_status()) return rc;
 #define W2L_APPLY(A_)                                                                                                                         \
-    hipLaunchKernelGGL((norm_apply_k<T, N, A_>), dim3(ap.runs, ap.B), dim3(threads_of(ap)), (size_t)ap.G * 8, stream, (const T*)x, ap, sums, gamma, beta, \
+    hipLaunchKernelGGL((norm_apply_k<T, N, A_>), dim3((unsigned)(ap.runs * ap.B)), dim3(threads_of(ap)), (size_t)ap.G * 8, stream, (const T*)x, ap, sums, gamma, beta, \
                        eps, (T*)y, mean, rstd)
     if (act == W2L_ACT_NONE) W2L_APPLY(W2L_ACT_NONE);
     else if (act == W2L_ACT_RELU) W2L_APPLY(W2L_ACT_RELU);
@@ -1045,18 +1080,18 @@ int backward_group(const void* x, const void* dy, const Shape& s, const float* m
                        want ? (size_t)(GLU ? 2 : 1) * s.lanes * s.Cg * 8 : 0, stream, (const T*)x, (const T*)dy, s, mean, rstd, gamma, beta, (T*)dx, want ? chans : nullptr);
     if (int rc = launch_status()) return rc;
     if (!want) return W2L_OK;
-    hipLaunchKernelGGL(norm_join_k, dim3((s.C + 63) / 64), dim3(256), 0, stream, chans, s.B, s.C, dgamma, dbeta, accumulate);
+    hipLaunchKernelGGL(norm_join_k, dim3((s.C + JOIN_CHANNELS - 1) / JOIN_CHANNELS), dim3(256), 0, stream, chans, s.B, s.C, dgamma, dbeta, accumulate);
     return launch_status();
 }
 template <typename T, int N, int ACT>
 int backward(const void* x, const void* dy, const Shape& s, const float* mean, const float* rstd, const float* gamma, const float* beta, float* chans,
              float2* groups, void* dx, float* dgamma, float* dbeta, int accumulate, hipStream_t stream)
 {
-    hipLaunchKernelGGL((norm_sums_k<T, N, ACT>), dim3(s.runs, s.B), dim3(threads_of(s)), (size_t)s.lanes * s.C * 8, stream, (const T*)x, (const T*)dy, s,
+    hipLaunchKernelGGL((norm_sums_k<T, N, ACT>), dim3((unsigned)(s.runs * s.B)), dim3(threads_of(s)), (size_t)s.lanes * s.C * 8, stream, (const T*)x, (const T*)dy, s,
                        mean, rstd, gamma, beta, chans, groups);
     if (int rc = launch_status()) return rc;
-    const int ahead = dgamma || dbeta ? 1 : 0;
-    hipLaunchKernelGGL((norm_dx_k<T, N, ACT>), dim3(s.runs, s.B + ahead), dim3(threads_of(s)),
+    const int ahead = dgamma || dbeta ? ((s.C + JOIN_CHANNELS - 1) / JOIN_CHANNELS + 7) / 8 * 8 : 0;
+    hipLaunchKernelGGL((norm_dx_k<T, N, ACT>), dim3((unsigned)(ahead + (long long)s.runs * s.B)), dim3(threads_of(s)),
                        (size_t)(s.G > 2 * threads_of(s) ? s.G : 2 * threads_of(s)) * 8, stream, (const T*)x,
                        (const T*)dy, s, mean, rstd, gamma, beta, chans, groups, (T*)dx, dgamma, dbeta, accumulate, ahead);
     return launch_status();
@@ -1086,8 +1121,8 @@ extern "C" size_t w2l_groupnorm_workspace_bytes(int B, int T, int C, int G, int 
     if (!shape_ok(B, T, C, G, act) || !valid_dtype(dtype)) return 0;
     const Form form = form_of(B, T, C, G, act, dtype);
     if (form.group) return round_up((size_t)B * C * 8, 256);
-    Shape s = shape_of(B, T, C, G, nullptr, (act == W2L_ACT_GLU ? C / 2 : C) / form.N);
-    runs_of(s, dtype);
+    Shape s = shape_of(B, T, C, G, nullptr, dtype, (act == W2L_ACT_GLU ? C / 2 : C) / form.N);
+    runs_of(s);
     const size_t a = stat_bytes(s), b = sum_bytes(s);
     return a > b ? a : b;
 }
@@ -1110,11 +1145,12 @@ extern "C" int w2l_groupnorm_fwd(const void* x, const float* gamma, const float*
     if (form.group)
         return with_vector(dtype, n, [&](auto* t, auto n) {
             using T_ = std::remove_pointer_t<decltype(t)>;
-            return forward_group<T_, decltype(n)::value>(x, group_shape(B, T, C, G, in_len, decltype(n)::value, GROUP_THREADS), gamma, beta, eps, act, y, mean, rstd, (hipStream_t)stream);
+            return forward_group<T_, decltype(n)::value>(x, group_shape(B, T, C, G, in_len, dtype, decltype(n)::value), gamma, beta, eps, act, y, mean, rstd, (hipStream_t)stream);
         });
-    Shape ap = shape_of(B, T, C, G, in_len, Cy / n), st = shape_of(B, T, C, G, in_len, C / n);
-    runs_of(ap, dtype);
-    runs_of(st, dtype);
+    Shape ap = shape_of(B, T, C, G, in_len, dtype, Cy / n), st = shape_of(B, T, C, G, in_len, dtype, C / n);
+    runs_of(ap);
+    st.rows = ap.rows;
+    st.runs = ap.runs;
     return with_vector(dtype, n, [&](auto* t, auto n) {
         using T_ = std::remove_pointer_t<decltype(t)>;
         return forward<T_, decltype(n)::value>(x, st, ap, (double2*)workspace, gamma, beta, eps, act, y, mean, rstd, (hipStream_t)stream);
@@ -1140,8 +1176,8 @@ extern "C" int w2l_groupnorm_bwd(const void* x, const void* dy, const float* mea
     if (!apart(in, out)) return W2L_ERR_OVERLAP;
     const Form form = form_of(B, T, C, G, act, dtype);
     const int n = form.N;
-    Shape s = form.group ? group_shape(B, T, C, G, in_len, n, GROUP_BWD_THREADS) : shape_of(B, T, C, G, in_len, Cy / n);
-    if (!form.group) runs_of(s, dtype);
+    Shape s = form.group ? group_shape(B, T, C, G, in_len, dtype, n) : shape_of(B, T, C, G, in_len, dtype, Cy / n);
+    if (!form.group) runs_of(s);
     float* const chans = (float*)workspace;
     float2* const groups = (float2*)((char*)workspace + round_up((size_t)B * s.runs * C * 8, 256));
     return with_vector(dtype, n, [&](auto* t, auto n) {
@@ -1156,4 +1192,15 @@ extern "C" int w2l_groupnorm_bwd(const void* x, const void* dy, const float* mea
         W2L_BACKWARD(W2L_ACT_GLU);
 #undef W2L_BACKWARD
     });
+}
+
+extern "C" int w2l_groupnorm_launch_config(int B, int T, int C, int G, int act, int dtype, int* group, int* vector)
+{
+    if (!group || !vector) return W2L_ERR_NULL;
+    if (!shape_ok(B, T, C, G, act)) return W2L_ERR_SHAPE;
+    if (!valid_dtype(dtype)) return W2L_ERR_DTYPE;
+    const Form f = form_of(B, T, C, G, act, dtype);
+    *group = f.group;
+    *vector = f.N;
+    return W2L_OK;
 }

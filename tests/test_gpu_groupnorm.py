@@ -10,7 +10,7 @@ Bounds, in units of U = 2^-24 (half a step of fp32, relative); for a group, R is
   y         the activation's slope (at most 1.1 for SiLU, 1 and |a| / 4 for GLU) times u's error, and 12 U |y|
   du        the slope's own slope (1/2 for SiLU; GLU 1/4 for the value, 1/4 and |a| / 10 for the gate) times u's error, 16 U |du|.  ReLU: where |u| is
             below its error either slope is right
-  sums      of n values by threads of up to 64, then lanes, then runs of frames: (64 + 16 + 2 log2 n) U of the sum of magnitudes
+  sums      of n values by threads of up to 128, then lanes, then runs of frames: (128 + 16 + 2 log2 n) U of the sum of magnitudes
 bf16 outputs add 2^-8 of the value.  Every element is held to its own bound, and whole tensors to the relative L2 of 1e-5 (bf16 3e-3) that the repository's single
 kernels have."""
 import numpy as np
@@ -19,10 +19,10 @@ import torch
 
 import oracle
 from gpu_util import BF16_L2, DEV, to_dev, to_host
+from norm_cases import ACTS, SHAPES, code, fits
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
-ACTS = ("none", "relu", "silu", "glu")
 
 
 @pytest.fixture(scope="module")
@@ -50,10 +50,6 @@ def held(x, dtype):
 def on_gpu(x, dtype):
     t = torch.from_numpy(np.asarray(x, dtype=np.float32)).to(DEV)
     return t.bfloat16() if dtype == "bf16" else t
-
-
-def code(P, act):
-    return (P.W2L_ACT_NONE, P.W2L_ACT_RELU, P.W2L_ACT_SILU, P.W2L_ACT_GLU)[ACTS.index(act)]
 
 
 def run(P, x, G, gamma, beta, n, act, dtype, dy=None, eps=1e-5, accumulate=None, stream=None):
@@ -146,7 +142,7 @@ def check(got, x, G, gamma, beta, n, act, dtype, dy=None, eps=1e-5, accumulate=N
     else:
         e_du = np.zeros(u.shape)
     e_du = np.where(live[..., None], e_du + 16 * U * np.abs(du), 0)
-    k = lambda m: 80 + 2 * np.log2(m + 1)
+    k = lambda m: 144 + 2 * np.log2(m + 1)
     s1, s2 = np.abs(du), np.abs(du * hat)
     e1, e2 = e_du, e_du * np.abs(hat) + s1 * e_hat
     total = live.sum()
@@ -173,17 +169,13 @@ def case(seed, B, T, C, act, dtype, level=1.0):
     return x, f(1 + 0.3 * rng.standard_normal(C)), f(0.3 * rng.standard_normal(C)), dy
 
 
-# (B, T, C, G): vectors of 16, 8, 4 and 2 bytes; groups within a vector and across vectors; one frame; runs of frames with and without a rest; more channels than a
-# workgroup has vectors for; the widest
-SHAPES = [(1, 1, 16, 2), (2, 5, 8, 8), (3, 17, 12, 3), (2, 33, 18, 3), (1, 70, 30, 1), (2, 100, 500, 20), (5, 64, 48, 4), (1, 333, 96, 96), (2, 129, 1536, 32), (1, 40, 2048, 1), (1, 20, 8192, 64),
-          (1, 3, 8192, 8192), (1, 19, 4104, 27), (3, 1000, 64, 4), (40, 3, 130, 5)]
-
-
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
 def test_both_directions(P, shape, dtype, act):
     B, T, C, G = shape
+    if not fits(shape, act):
+        pytest.skip("GLU halves the channels")
     x, gamma, beta, dy = case(C + T, B, T, C, act, dtype)
     few = T * C // G < 64                                                 # groups of few values: their gradients cancel, and have their own bounds alone
     n = np.maximum(T - 7 * np.arange(B), 1)
