@@ -309,7 +309,7 @@ int w2l_sgd_momentum_step(float *w, float *v, const float *grad, void *w_lowp, l
  * otherwise.  1 <= n_tensors <= W2L_ADAMW_MAX_TENSORS, n <= W2L_ADAMW_MAX_VALUES, step >= 1, lr, weight_decay, max_norm >= 0, 0 <= beta <= 1 - 1e-7,
  * 1e-37 <= eps, all finite. */
 #define W2L_ADAMW_MAX_TENSORS 65536
-#define W2L_ADAMW_MAX_VALUES (1LL << 36)
+#define W2L_ADAMW_MAX_VALUES (1LL << 33)
 typedef struct {
     float *w;
     const void *grad;

@@ -1,6 +1,6 @@
 // AdamW over many tensors at once (w2l_adamw_step): one launch for up to 48 tensors, moments in 32 bits or in 8, the gradients clipped by their
-// joint norm.  A value costs a few dozen instructions and 26 to 46 bytes, each touched once: memory bounds it, but for the gradients, which the norm
-// reads first.
+// joint norm.  A value costs 18 to 30 bytes, each touched once, and 4 more where the norm reads the gradients first: memory bounds it.  107 M values with a bf16 copy,
+// clipped: 600 us with moments in 32 bits (6.1 TB/s), of which the norm takes 75, and 427 in 8 (5.5 TB/s); a copy of 4 GB moves 4.8.
 #include "lanes.h"
 
 #include <algorithm>
@@ -11,8 +11,10 @@ using namespace w2l;
 namespace {
 
 constexpr int THREADS = 256, MOST = 48;           // MOST tensors a launch: their table is a kernel argument, of which 4 KB are to be had
-constexpr int BLOCK = 256, CHUNK = 4096;          // values that share an exponent, and values of a workgroup
-constexpr int NORM_GROUPS = 1024, NORM_CHUNK = 8192;
+// Values that share an exponent; values of a workgroup, with moments in 32 and in 8 bits (32 bits: 4096 values take 621 us at 107 M, 2048 611, 1024 600)
+constexpr int BLOCK = 256, CHUNK32 = 4 * THREADS, CHUNK8 = 16 * THREADS;
+constexpr long long MOST_GROUPS = W2L_ADAMW_MAX_VALUES / CHUNK32;  // of a launch: 2^31 threads
+constexpr int NORM_GROUPS = 256, NORM_CHUNK = 4096;  // workgroups a tensor's norm has at most, and values for which it has one more
 
 struct Entry {
     float* w;
@@ -53,13 +55,14 @@ __host__ __device__ __forceinline__ unsigned mix(unsigned x)
     x *= 0xC2B2AE35u;
     return x ^ x >> 16;
 }
-__host__ __device__ inline Scalars scalars_of(const Hyper& h, double coef)
+// power1, power2: beta1 and beta2 to the step
+__host__ __device__ inline Scalars scalars_of(const Hyper& h, double power1, double power2)
 {
     Scalars s;
     s.lr = h.lr;
-    s.factor = (float)(h.grad_scale * coef);
-    s.rate = (float)(h.lr / (1. - pow(h.beta1, (double)h.step)));
-    s.inv_root = (float)(1. / sqrt(1. - pow(h.beta2, (double)h.step)));
+    s.factor = (float)h.grad_scale;
+    s.rate = (float)(h.lr / (1. - power1));
+    s.inv_root = (float)(1. / sqrt(1. - power2));
     s.eps = (float)h.eps;
     s.key = mix(mix(h.seed) ^ (unsigned)h.step);
     s.skip = h.step < 1;
@@ -76,22 +79,37 @@ __device__ __forceinline__ int entry_of(const Table& t, unsigned& within)
     return i;
 }
 
+// Loads and stores past the caches, for what a step touches once: 107 M values with moments in 32 bits 578 -> 528 us, in 8 bits 332 -> 289 where the moments' bytes, of
+// which a wavefront's instruction takes quarter lines, stay ordinary (321 if not); the norm after it 116 -> 75, which had waited for what was to be written back.  The
+// norm's own loads stay ordinary: up to 256 MB the step finds the gradients in the memory-side cache (and beyond: 600 us, 640 past it).
+template <bool PAST, typename V>
+__device__ __forceinline__ V get(const void* p)
+{
+    if (PAST) return __builtin_nontemporal_load(static_cast<const V*>(p));
+    return *static_cast<const V*>(p);
+}
+template <bool PAST, typename V>
+__device__ __forceinline__ void set(void* p, V v)
+{
+    if (PAST) __builtin_nontemporal_store(v, static_cast<V*>(p));
+    else *static_cast<V*>(p) = v;
+}
+typedef float f4_t __attribute__((ext_vector_type(4)));
+typedef unsigned u2_t __attribute__((ext_vector_type(2)));
+
 // ---- the gradients' norm -------------------------------------------------------------------------------------
 // Squares of fp32 values are exact in 64 bits, and so is their sum to 2^-53 of itself a term: what is clipped by it does not depend on the order
-template <typename G>
-__device__ __forceinline__ void four(const G* p, long long i, float (&g)[4]);
-template <>
-__device__ __forceinline__ void four<float>(const float* p, long long i, float (&g)[4])
+template <typename G, bool PAST = false>
+__device__ __forceinline__ void four(const G* p, long long i, float (&g)[4])
 {
-    const float4 q = *reinterpret_cast<const float4*>(p + i);
-    g[0] = q.x; g[1] = q.y; g[2] = q.z; g[3] = q.w;
-}
-template <>
-__device__ __forceinline__ void four<bf16_t>(const bf16_t* p, long long i, float (&g)[4])
-{
-    const uint2 q = *reinterpret_cast<const uint2*>(p + i);
-    g[0] = __uint_as_float(q.x << 16); g[1] = __uint_as_float(q.x & 0xffff0000u);
-    g[2] = __uint_as_float(q.y << 16); g[3] = __uint_as_float(q.y & 0xffff0000u);
+    if constexpr (sizeof(G) == 4) {
+        const f4_t q = get<PAST, f4_t>(p + i);
+        g[0] = q.x; g[1] = q.y; g[2] = q.z; g[3] = q.w;
+    } else {
+        const u2_t q = get<PAST, u2_t>(p + i);
+        g[0] = __uint_as_float(q.x << 16); g[1] = __uint_as_float(q.x & 0xffff0000u);
+        g[2] = __uint_as_float(q.y << 16); g[3] = __uint_as_float(q.y & 0xffff0000u);
+    }
 }
 
 // sum over the workgroup, in lane 0 of its first wavefront
@@ -140,17 +158,25 @@ __global__ __launch_bounds__(THREADS) void adamw_norm_k(const Table t, double* _
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
 
-// The step's scalars, where they depend on what the device alone knows
-__global__ __launch_bounds__(THREADS) void adamw_now_k(Hyper h, const float* lr, const int* step, const double* __restrict__ sums, int count,
-                                                       float* __restrict__ grad_norm, Scalars* __restrict__ out)
+// The step's scalars, where they depend on what the device alone knows.  The powers of a step that only the device knows are made by a wavefront each, while the
+// others sum.
+__global__ __launch_bounds__(1024) void adamw_now_k(Hyper h, Scalars now, const float* lr, const int* step, const double* __restrict__ sums, int count,
+                                                    float* __restrict__ grad_norm, Scalars* __restrict__ out)
 {
-    __shared__ double lds[THREADS / 64];
+    __shared__ double lds[16], powers[2];
     double s = 0.;
-    for (int i = threadIdx.x; i < count; i += THREADS) s += sums[i];
-    s = sum_all(s, lds);
-    if (threadIdx.x != 0) return;
     if (lr) h.lr = *lr;
     if (step) h.step = *step;
+    if ((lr || step) && (threadIdx.x == 64 || threadIdx.x == 128)) powers[threadIdx.x == 128] = pow(threadIdx.x == 64 ? h.beta1 : h.beta2, (double)h.step);
+    for (int i = threadIdx.x; i < count; i += 4 * 1024) {
+        double v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = i + k * 1024 < count ? sums[i + k * 1024] : 0.;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s += v[k];
+    }
+    s = sum_all(s, lds);
+    if (threadIdx.x != 0) return;
     double coef = 1.;
     bool finite = true;
     if (count) {
@@ -159,7 +185,8 @@ __global__ __launch_bounds__(THREADS) void adamw_now_k(Hyper h, const float* lr,
         if (grad_norm) *grad_norm = (float)norm;
         if (h.max_norm > 0. && h.max_norm < norm + 1e-6) coef = h.max_norm / (norm + 1e-6);
     }
-    Scalars now = scalars_of(h, coef);
+    if (lr || step) now = scalars_of(h, powers[0], powers[1]);
+    now.factor = (float)(h.grad_scale * coef);
     if (!finite) now.skip = 1;
     *out = now;
 }
@@ -207,6 +234,14 @@ __device__ __forceinline__ float moved(float w, float m, float root, float keep,
     return __builtin_fmaf(-s.rate * m, __builtin_amdgcn_rcpf(__builtin_fmaf(root, s.inv_root, s.eps)), w * keep);  // (the reciprocal to an ulp)
 }
 
+__device__ __forceinline__ u2_t low_of(f4_t x)
+{
+    typedef float float2_t __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    return (u2_t){__builtin_bit_cast(unsigned, __builtin_convertvector((float2_t){x.x, x.y}, bf16x2_t)),
+                  __builtin_bit_cast(unsigned, __builtin_convertvector((float2_t){x.z, x.w}, bf16x2_t))};
+}
+
 template <typename G>
 __global__ __launch_bounds__(THREADS) void adamw32_k(const Table t, const Scalars by_value, const Scalars* __restrict__ now, Moments o)
 {
@@ -218,40 +253,33 @@ __global__ __launch_bounds__(THREADS) void adamw32_k(const Table t, const Scalar
     const float keep = (float)(1. - s.lr * e.decay);
     const G* const grad = static_cast<const G*>(e.grad);
     float *const w = e.w, *const m = static_cast<float*>(e.m), *const v = static_cast<float*>(e.v);
-    const long long base = (long long)within * CHUNK;
-    typedef float f4 __attribute__((ext_vector_type(4)));
+    const long long at = (long long)within * CHUNK32 + threadIdx.x * 4;
+    if (at + 4 <= e.n) {
+        f4_t wq = get<true, f4_t>(w + at), mq = get<true, f4_t>(m + at), vq = get<true, f4_t>(v + at);
+        float g[4];
+        four<G, true>(grad, at, g);
 #pragma unroll
-    for (int u = 0; u < CHUNK / (4 * THREADS); ++u) {
-        const long long at = base + (u * THREADS + (int)threadIdx.x) * 4;
-        if (at + 4 <= e.n) {
-            f4 wq = *reinterpret_cast<f4*>(w + at), mq = *reinterpret_cast<f4*>(m + at), vq = *reinterpret_cast<f4*>(v + at);
-            float g[4];
-            four<G>(grad, at, g);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float mj = mq[j], vj = vq[j];
-                advance(g[j] * s.factor, mj, vj, o);
-                mq[j] = mj;
-                vq[j] = vj;
-                wq[j] = moved(wq[j], mj, sqrtf(vj), keep, s);
-            }
-            *reinterpret_cast<f4*>(w + at) = wq;
-            *reinterpret_cast<f4*>(m + at) = mq;
-            *reinterpret_cast<f4*>(v + at) = vq;
-            if (e.lowp)
-                *reinterpret_cast<uint2*>(e.lowp + at) = make_uint2((unsigned)f32_to_bf16(wq[0]) | (unsigned)f32_to_bf16(wq[1]) << 16,
-                                                                    (unsigned)f32_to_bf16(wq[2]) | (unsigned)f32_to_bf16(wq[3]) << 16);
-        } else
-            for (long long k = at; k < e.n; ++k) {
-                float mk = m[k], vk = v[k];
-                advance(Elem<G>::load(grad, (size_t)k) * s.factor, mk, vk, o);
-                const float wk = moved(w[k], mk, sqrtf(vk), keep, s);
-                m[k] = mk;
-                v[k] = vk;
-                w[k] = wk;
-                if (e.lowp) e.lowp[k] = f32_to_bf16(wk);
-            }
-    }
+        for (int j = 0; j < 4; ++j) {
+            float mj = mq[j], vj = vq[j];
+            advance(g[j] * s.factor, mj, vj, o);
+            mq[j] = mj;
+            vq[j] = vj;
+            wq[j] = moved(wq[j], mj, sqrtf(vj), keep, s);
+        }
+        set<true>(w + at, wq);
+        set<true>(m + at, mq);
+        set<true>(v + at, vq);
+        if (e.lowp) set<true>(e.lowp + at, low_of(wq));
+    } else
+        for (long long k = at; k < e.n; ++k) {
+            float mk = m[k], vk = v[k];
+            advance(Elem<G>::load(grad, (size_t)k) * s.factor, mk, vk, o);
+            const float wk = moved(w[k], mk, sqrtf(vk), keep, s);
+            m[k] = mk;
+            v[k] = vk;
+            w[k] = wk;
+            if (e.lowp) e.lowp[k] = f32_to_bf16(wk);
+        }
 }
 
 // Sixteen lanes have a block: four values at each of four places 64 apart a lane, so that a wavefront's loads are of whole lines
@@ -268,7 +296,7 @@ __global__ __launch_bounds__(THREADS) void adamw8_k(const Table t, const Scalars
     const G* const grad = static_cast<const G*>(e.grad);
     float* const w = e.w;
     unsigned char *const mc = static_cast<unsigned char*>(e.m), *const vc = static_cast<unsigned char*>(e.v);
-    const long long base = (long long)within * CHUNK + (threadIdx.x >> 4) * BLOCK, block = base / BLOCK;
+    const long long base = (long long)within * CHUNK8 + (threadIdx.x >> 4) * BLOCK, block = base / BLOCK;
     const int l = threadIdx.x & 15;
     const bool there = base < e.n, whole = base + BLOCK <= e.n;
     float wx[16], mx[16], vx[16];
@@ -280,14 +308,14 @@ __global__ __launch_bounds__(THREADS) void adamw8_k(const Table t, const Scalars
         for (int j = 0; j < 4; ++j) {
             const long long at = base + j * 64 + l * 4;
             if (whole) {
-                const float4 q = *reinterpret_cast<const float4*>(w + at);
+                const f4_t q = get<true, f4_t>(w + at);
                 wx[4 * j] = q.x; wx[4 * j + 1] = q.y; wx[4 * j + 2] = q.z; wx[4 * j + 3] = q.w;
                 float gj[4];
-                four<G>(grad, at, gj);
+                four<G, true>(grad, at, gj);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) g[4 * j + k] = gj[k];
-                mq[j] = *reinterpret_cast<const unsigned*>(mc + at);
-                vq[j] = *reinterpret_cast<const unsigned*>(vc + at);
+                mq[j] = get<false, unsigned>(mc + at);
+                vq[j] = get<false, unsigned>(vc + at);
             } else {
                 mq[j] = vq[j] = 0;
 #pragma unroll
@@ -353,12 +381,11 @@ __global__ __launch_bounds__(THREADS) void adamw8_k(const Table t, const Scalars
         }
         const float* const x = wx + 4 * j;
         if (whole) {
-            *reinterpret_cast<unsigned*>(mc + at) = mq;
-            *reinterpret_cast<unsigned*>(vc + at) = vq;
-            *reinterpret_cast<float4*>(w + at) = make_float4(x[0], x[1], x[2], x[3]);
-            if (e.lowp)
-                *reinterpret_cast<uint2*>(e.lowp + at) = make_uint2((unsigned)f32_to_bf16(x[0]) | (unsigned)f32_to_bf16(x[1]) << 16,
-                                                                    (unsigned)f32_to_bf16(x[2]) | (unsigned)f32_to_bf16(x[3]) << 16);
+            const f4_t wq = {x[0], x[1], x[2], x[3]};
+            set<false>(mc + at, mq);
+            set<false>(vc + at, vq);
+            set<true>(w + at, wq);
+            if (e.lowp) set<true>(e.lowp + at, low_of(wq));
         } else
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -429,7 +456,7 @@ int launch(const w2l_adamw_tensor* t, int n, int bits, const Hyper& h, const flo
     Scalars* now = nullptr;
     const bool norm = h.max_norm > 0. || grad_norm;
     const Moments o{(float)h.beta1, (float)(1. - h.beta1), (float)h.beta2, (float)(1. - h.beta2)};
-    Scalars by_value{};
+    const Scalars by_value = scalars_of(h, pow(h.beta1, (double)h.step), pow(h.beta2, (double)h.step));
     size_t count = 0;
     if (norm || lr || step) {
         now = static_cast<Scalars*>(ws);
@@ -449,20 +476,21 @@ int launch(const w2l_adamw_tensor* t, int n, int bits, const Hyper& h, const flo
             if (int rc = launch_status()) return rc;
             count += groups;
         }
-        hipLaunchKernelGGL(adamw_now_k, dim3(1), dim3(THREADS), 0, st, h, lr, step, sums, (int)count, grad_norm, now);
+        hipLaunchKernelGGL(adamw_now_k, dim3(1), dim3(1024), 0, st, h, by_value, lr, step, sums, (int)count, grad_norm, now);
         if (int rc = launch_status()) return rc;
-    } else
-        by_value = scalars_of(h, 1.);
-    for (int i = 0; i < n; i += MOST) {
+    }
+    const long long chunk = bits == 32 ? CHUNK32 : CHUNK8;
+    for (int i = 0; i < n;) {
         Table tab{};
         unsigned groups = 0;
         tab.number = i;
-        tab.count = n - i < MOST ? n - i : MOST;
-        for (int j = 0; j < tab.count; ++j) {
-            const w2l_adamw_tensor& a = t[i + j];
-            tab.e[j] = {a.w, a.grad, a.m, a.v, a.m_exp, a.v_exp, static_cast<bf16_t*>(a.w_lowp), a.n, a.weight_decay};
-            tab.first[j] = groups;
-            groups += (unsigned)((a.n + CHUNK - 1) / CHUNK);
+        for (; tab.count < MOST && i < n; ++i, ++tab.count) {  // (a tensor has at most MOST_GROUPS by itself)
+            const w2l_adamw_tensor& a = t[i];
+            const long long more = (a.n + chunk - 1) / chunk;
+            if (groups + more > MOST_GROUPS) break;
+            tab.e[tab.count] = {a.w, a.grad, a.m, a.v, a.m_exp, a.v_exp, static_cast<bf16_t*>(a.w_lowp), a.n, a.weight_decay};
+            tab.first[tab.count] = groups;
+            groups += (unsigned)more;
         }
         tab.first[tab.count] = groups;
         if (!groups) continue;
