@@ -48,8 +48,10 @@ __device__ __forceinline__ void unpack(raw_t<T, N> q, float (&x)[N])
             x[2 * j + 1] = __uint_as_float(w & 0xffff0000u);
         }
 }
-template <typename T, int N>
-__device__ __forceinline__ void put(T* p, const float (&x)[N], bool past)
+// PAST: past the caches.  Outputs of runs of frames (16x1500x1536 bf16, SiLU: 52 -> 41 us, 77 -> 71 with a pass behind it that reads them), not of a workgroup a group,
+// whose stores fill lines in parts (8x750x1536 in 32 groups: 13.6, 16.6 past them).
+template <typename T, int N, bool PAST>
+__device__ __forceinline__ void put(T* p, const float (&x)[N])
 {
     raw_t<T, N> q;
     if constexpr (sizeof(T) == 4) {
@@ -67,18 +69,17 @@ __device__ __forceinline__ void put(T* p, const float (&x)[N], bool past)
             if constexpr (N == 2) q = w;
             else q[j] = w;
         }
-    if (past) __builtin_nontemporal_store(q, reinterpret_cast<raw_t<T, N>*>(p));
+    if (PAST) __builtin_nontemporal_store(q, reinterpret_cast<raw_t<T, N>*>(p));
     else *reinterpret_cast<raw_t<T, N>*>(p) = q;
 }
 
 // How a workgroup takes a run of `rows` frames: `cols` threads side by side, `lanes` rows at a time
 struct Shape {
-    int B, T, C, G, Cg, rows, runs, cols, lanes;
+    int B, T, C, G, Cg, rows, runs, cols, lanes, split;
     const int* in_len;
     float inv_Cg, inv_cols;
-    bool past;  // outputs go past the L2s: they are more than these hold (16x1500x2048 bf16 and its gradient: 150 -> 144 us)
     // column and row of a thread (a thousand of them at most: see group_of)
-    __device__ __forceinline__ void split(int& col, int& lane) const
+    __device__ __forceinline__ void place(int& col, int& lane) const
     {
         lane = (int)(((float)threadIdx.x + 0.5f) * inv_cols);
         col = (int)threadIdx.x - lane * cols;
@@ -261,7 +262,7 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_stats_k(const T* __restrict_
     const int t0 = run * s.rows, t1 = t0 + s.rows < len ? t0 + s.rows : len;
     if (t0 >= t1) return;  // (what reads the sums knows that there are none)
     int col, lane;
-    s.split(col, lane);
+    s.place(col, lane);
     const int nv = s.C / N, here = t1 - t0;
     if (lane < s.lanes)
         for (int v = col; v < nv; v += s.cols) {
@@ -365,7 +366,7 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
     const int b = task.b, run = task.run, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C;
     const int t0 = run * s.rows, t1 = t0 + s.rows < s.T ? t0 + s.rows : s.T, live = t1 < len ? t1 : len;
     int col, lane;
-    s.split(col, lane);
+    s.place(col, lane);
     const int nv = Cy / N;
     const T* const in = x + (size_t)b * s.T * s.C;
     // what a thread reads first is on its way while the statistics are joined
@@ -414,7 +415,7 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
                 if (GLU) unpack<T, N>(xg[k], w);
 #pragma unroll
                 for (int j = 0; j < N; ++j) u[j] = act<ACT>(a(u[j], j), GLU ? h(w[j], j) : 0.f);
-                put<T, N>(q + (size_t)(t + k * s.lanes) * Cy, u, s.past);
+                put<T, N, true>(q + (size_t)(t + k * s.lanes) * Cy, u);
             }
             t += U * s.lanes;
             if (t < live) load(v, t);
@@ -423,7 +424,7 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
             float none[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) none[j] = len < 0 ? NAN : 0.f;
-            for (t = (live > t0 ? live : t0) + lane; t < t1; t += s.lanes) put<T, N>(q + (size_t)t * Cy, none, s.past);
+            for (t = (live > t0 ? live : t0) + lane; t < t1; t += s.lanes) put<T, N, true>(q + (size_t)t * Cy, none);
         }
     }
 }
@@ -444,7 +445,7 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
     const int t0 = run * s.rows, t1 = t0 + s.rows < len ? t0 + s.rows : len;
     if (t0 >= t1) return;
     int col, lane;
-    s.split(col, lane);
+    s.place(col, lane);
     const int nv = Cy / N;
     if (lane < s.lanes)
         for (int v = col; v < nv; v += s.cols) {
@@ -579,7 +580,7 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
     const int b = task.b, run = task.run, len = frames_of(s, b), t0 = run * s.rows, t1 = t0 + s.rows < s.T ? t0 + s.rows : s.T, live = t1 < len ? t1 : len;
     float2* const means = reinterpret_cast<float2*>(lds);
     int col, lane;
-    s.split(col, lane);
+    s.place(col, lane);
     const int nv = Cy / N;
     const size_t row0 = (size_t)b * s.T;
     // what a thread reads first is on its way while the means are joined
@@ -661,8 +662,8 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
                     if (GLU) gk[j] = __builtin_fmaf(dg, h.scale[j], __builtin_fmaf(gk[j] - h.mean, gline.x, gline.y));
                 }
                 T* const to = o + (size_t)(t + k * s.lanes) * s.C;
-                put<T, N>(to, xk, s.past);
-                if (GLU) put<T, N>(to + Cy, gk, s.past);
+                put<T, N, true>(to, xk);
+                if (GLU) put<T, N, true>(to + Cy, gk);
             }
             t += U * s.lanes;
             if (t < live) load(v, t);
@@ -670,8 +671,8 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
         if (t1 > live) {
             const float none[N] = {};
             for (t = (live > t0 ? live : t0) + lane; t < t1; t += s.lanes) {
-                put<T, N>(o + (size_t)t * s.C, none, s.past);
-                if (GLU) put<T, N>(o + (size_t)t * s.C + Cy, none, s.past);
+                put<T, N, true>(o + (size_t)t * s.C, none);
+                if (GLU) put<T, N, true>(o + (size_t)t * s.C + Cy, none);
             }
         }
     }
@@ -682,14 +683,21 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
 // time from its L2, in one launch.  Vectors and groups of one utterance that are neighbours share lines, so consecutive ones go to one XCD.
 constexpr int GROUP_THREADS = 512, GROUP_BATCH = 6, FLUSH = 60;  // (512: a lane's sums of all channels fit 64 KB of LDS)
 static_assert(FLUSH % GROUP_BATCH == 0, "sums are flushed between batches");
+// Where groups are fewer than CUs, two workgroups (split) each read a whole group and write half of its frames (8x750x1536 bf16 with GLU, 128 pairs of groups: 15.0 -> 14.7 us, with its
+// gradient 39.5 -> 37.1; 5x333x500 fp32, SiLU, and its gradient 17.0 -> 16.5; four or eight of them gain nothing more).
 struct Place {
-    int b, g;
+    int b, g, part, from, to;  // frames from .. to of the utterance's are written
 };
-__device__ __forceinline__ Place place_of(int per)  // per: workgroups an utterance
+__device__ __forceinline__ Place place_of(const Shape& s, int per)  // per: groups (pairs) of an utterance
 {
     const unsigned total = gridDim.x, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, q = total >> 3, r = total & 7;
-    const unsigned i = xcd * q + (xcd < r ? xcd : r) + slot;
-    return {(int)(i / per), (int)(i % per)};
+    const unsigned i = xcd * q + (xcd < r ? xcd : r) + slot, j = i / s.split;
+    return {(int)(j / per), (int)(j % per), (int)(i - j * s.split), 0, 0};
+}
+__device__ __forceinline__ void part_of(const Shape& s, Place& at, int live)
+{
+    at.from = (int)((long long)live * at.part / s.split);
+    at.to = (int)((long long)live * (at.part + 1) / s.split);
 }
 // over the workgroup; lds: a value a wavefront
 template <typename V>
@@ -714,10 +722,11 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_k(const T* __restric
     constexpr bool GLU = ACT == W2L_ACT_GLU;
     constexpr int U = GROUP_BATCH;
     __shared__ double2 lds[2][GROUP_THREADS / 64];
-    const Place at = place_of(GLU ? s.G / 2 : s.G);
+    Place at = place_of(s, GLU ? s.G / 2 : s.G);
     const int b = at.b, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C, live = len < 0 ? 0 : len;
+    part_of(s, at, live);
     int col, lane;
-    s.split(col, lane);
+    s.place(col, lane);
     const int c0 = at.g * s.Cg + col * N, step = U * s.lanes;
     const bool on = lane < s.lanes;
     const T* const p = x + (size_t)b * s.T * s.C + c0;
@@ -774,7 +783,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_k(const T* __restric
     if (GLU) k2 = sum_group(sum64(k2, 64), lds[1]);
     const double inv = live ? 1. / ((double)live * s.Cg) : 0.;
     const float2 s1 = stat_of(k1, inv, eps), s2 = GLU ? stat_of(k2, inv, eps) : s1;
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && at.part == 0) {
         const size_t o = (size_t)b * s.G + at.g;
         mean[o] = len < 0 ? NAN : s1.x;
         rstd[o] = len < 0 ? NAN : s1.y;
@@ -787,24 +796,27 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_k(const T* __restric
     a.set(s1);
     if (GLU) h.set(s2);
     T* const q = y + (size_t)b * s.T * Cy + c0;
-    for (int t = last; t >= 0;) {  // from the end, which is in registers
+    const int way = s.split > 1 ? step : -step;  // a workgroup alone goes from the end, which is in registers
+    int t = s.split > 1 ? at.from + lane : last;
+    if (s.split > 1 && t < at.to) load(t);
+    while (t >= 0 && t < at.to) {
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            if (t + k * s.lanes >= live) break;
+            if (t + k * s.lanes >= at.to) break;
             float u[N], w[N];
             unpack<T, N>(xv[k], u);
             if (GLU) unpack<T, N>(xg[k], w);
 #pragma unroll
             for (int j = 0; j < N; ++j) u[j] = act<ACT>(a(u[j], j), GLU ? h(w[j], j) : 0.f);
-            put<T, N>(q + (size_t)(t + k * s.lanes) * Cy, u, s.past);
+            put<T, N, false>(q + (size_t)(t + k * s.lanes) * Cy, u);
         }
-        t -= step;
-        if (t >= 0) load(t);
+        t += way;
+        if (t >= 0 && t < at.to) load(t);
     }
     float none[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) none[j] = len < 0 ? NAN : 0.f;
-    for (int t = live + lane; t < s.T; t += s.lanes) put<T, N>(q + (size_t)t * Cy, none, s.past);
+    for (t = live + at.part * s.lanes + lane; t < s.T; t += s.split * s.lanes) put<T, N, false>(q + (size_t)t * Cy, none);
 }
 
 // chans [B][2][C]: sums of du and du xhat of an utterance (NULL: not wanted)
@@ -817,10 +829,11 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __res
     constexpr int U = GROUP_BATCH;
     extern __shared__ float2 acc[];  // [GLU: 2][lanes][Cg]: a lane's sums
     __shared__ float2 lds[2][GROUP_THREADS / 64];
-    const Place at = place_of(GLU ? s.G / 2 : s.G);
+    Place at = place_of(s, GLU ? s.G / 2 : s.G);
     const int b = at.b, len = frames_of(s, b), Cy = GLU ? s.C / 2 : s.C, live = len < 0 ? 0 : len;
+    part_of(s, at, live);
     int col, lane;
-    s.split(col, lane);
+    s.place(col, lane);
     const int c0 = at.g * s.Cg + col * N, step = U * s.lanes;
     const bool on = lane < s.lanes;
     const size_t row0 = (size_t)b * s.T;
@@ -882,7 +895,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __res
             k2.y = __builtin_fmaf(r2[j], h.scale[j], k2.y);
         }
     }
-    if (chans && on)
+    if (chans && on && at.part == 0)
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             acc[lane * s.Cg + col * N + j] = make_float2(s1[j], s2[j] * rs);
@@ -890,7 +903,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __res
         }
     k1 = sum_group(make_float2(wave64(k1.x, Sum()), wave64(k1.y, Sum())), lds[0]);
     if (GLU) k2 = sum_group(make_float2(wave64(k2.x, Sum()), wave64(k2.y, Sum())), lds[1]);
-    if (chans) {
+    if (chans && at.part == 0) {
         if (blockDim.x == 64) __syncthreads();  // (sum_group's are the others')
         const int team = team_of(GLU ? 2 * s.Cg : s.Cg, s.lanes), l = threadIdx.x & (team - 1), teams = blockDim.x / team, count = GLU ? 2 * s.Cg : s.Cg;
         for (int i0 = 0; i0 < count; i0 += teams) {
@@ -918,10 +931,13 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __res
     // (rstd is in k1 and k2 already)
     const float slope = -k1.y * inv * rs * rs, level = -k1.x * inv, gslope = -k2.y * inv * rg * rg, glevel = -k2.x * inv;
     T* const o = dx + row0 * s.C + c0;
-    for (int t = last; t >= 0;) {
+    const int way = s.split > 1 ? step : -step;
+    int t = s.split > 1 ? at.from + lane : last;
+    if (s.split > 1 && t < at.to) load(t);
+    while (t >= 0 && t < at.to) {
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            if (t + k * s.lanes >= live) break;
+            if (t + k * s.lanes >= at.to) break;
             float xk[N], gk[N], d[N];
             unpack<T, N>(xv[k], xk);
             if (GLU) unpack<T, N>(xg[k], gk);
@@ -934,16 +950,16 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __res
                 if (GLU) gk[j] = __builtin_fmaf(dg, h.scale[j], __builtin_fmaf(gk[j] - mg, gslope, glevel));
             }
             T* const to = o + (size_t)(t + k * s.lanes) * s.C;
-            put<T, N>(to, xk, s.past);
-            if (GLU) put<T, N>(to + Cy, gk, s.past);
+            put<T, N, false>(to, xk);
+            if (GLU) put<T, N, false>(to + Cy, gk);
         }
-        t -= step;
-        if (t >= 0) load(t);
+        t += way;
+        if (t >= 0 && t < at.to) load(t);
     }
     const float none[N] = {};
-    for (int t = live + lane; t < s.T; t += s.lanes) {
-        put<T, N>(o + (size_t)t * s.C, none, s.past);
-        if (GLU) put<T, N>(o + (size_t)t * s.C + Cy, none, s.past);
+    for (t = live + at.part * s.lanes + lane; t < s.T; t += s.split * s.lanes) {
+        put<T, N, false>(o + (size_t)t * s.C, none);
+        if (GLU) put<T, N, false>(o + (size_t)t * s.C + Cy, none);
     }
 }
 
@@ -968,9 +984,9 @@ int vector_of(int Cg, int Cy, int dtype)
     return n;
 }
 // vectors: of a row that a thread can be given one of
-Shape shape_of(int B, int T, int C, int G, const int* in_len, int dtype, int vectors)
+Shape shape_of(int B, int T, int C, int G, const int* in_len, int vectors)
 {
-    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, in_len, 1.f / (float)(C / G), 0.f, (size_t)B * T * C * dtype_size(dtype) > (32u << 20)};
+    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, 1, in_len, 1.f / (float)(C / G), 0.f};
     const int passes = (vectors + MAX_THREADS - 1) / MAX_THREADS;
     s.cols = (vectors + passes - 1) / passes;
     s.lanes = MAX_THREADS / s.cols;
@@ -1012,8 +1028,9 @@ bool apart(const Span (&in)[I], const Span (&out)[O])
 }
 
 struct Form {
-    bool group;  // a workgroup a group
+    bool group;  // a workgroup a group, or `split` of them
     int N;       // channels of a vector
+    int split;
 };
 // A workgroup a group saves a launch and the second reading from far away, as long as there are workgroups for the chip or what one reads is little.  Both ways
 // in us, forward and backward call (bf16, SiLU): 64 workgroups of 25 KB: 5.8 and 10.5 against 9.5 and 13; of 125 KB: 12 and 24 against 12 and 18; 128 of 250 KB (GLU): 20 and 35
@@ -1027,12 +1044,14 @@ Form form_of(int B, int T, int C, int G, int act, int dtype)
     const long long most = workgroups >= 256 ? 1 << 20 : workgroups >= 128 ? 512 << 10 : 64 << 10;
     // (a thread's sums of at most 128 rows: in fp32)
     const bool group = !(glu && G % 2) && Cg / n <= 256 && bytes <= most && !(workgroups >= 2048 && bytes < (16 << 10)) && T <= 128 * (GROUP_THREADS / (Cg / n));
-    return {group, n};
+    const int split = group && workgroups <= 128 && bytes >= (16 << 10) ? 2 : 1;
+    return {group, n, split};
 }
-Shape group_shape(int B, int T, int C, int G, const int* in_len, int dtype, int N)
+Shape group_shape(int B, int T, int C, int G, const int* in_len, int N, int split)
 {
-    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, in_len, 1.f / (float)(C / G), 0.f, (size_t)B * T * C * dtype_size(dtype) > (32u << 20)};
+    Shape s{B, T, C, G, C / G, 0, 0, 0, 0, 1, in_len, 1.f / (float)(C / G), 0.f};
     s.cols = s.Cg / N;
+    s.split = split;
     const int lanes = GROUP_THREADS / s.cols;
     s.lanes = lanes < T ? lanes : T;
     s.inv_cols = 1.f / (float)s.cols;
@@ -1062,7 +1081,7 @@ int forward(const void* x, const Shape& st, const Shape& ap, double2* sums, cons
 template <typename T, int N>
 int forward_group(const void* x, const Shape& s, const float* gamma, const float* beta, float eps, int act, void* y, float* mean, float* rstd, hipStream_t stream)
 {
-    const dim3 g((unsigned)(s.B * (act == W2L_ACT_GLU ? s.G / 2 : s.G))), n(threads_of(s));
+    const dim3 g((unsigned)(s.B * (act == W2L_ACT_GLU ? s.G / 2 : s.G) * s.split)), n(threads_of(s));
 #define W2L_GROUP(A_) hipLaunchKernelGGL((norm_group_k<T, N, A_>), g, n, 0, stream, (const T*)x, s, gamma, beta, eps, (T*)y, mean, rstd)
     if (act == W2L_ACT_NONE) W2L_GROUP(W2L_ACT_NONE);
     else if (act == W2L_ACT_RELU) W2L_GROUP(W2L_ACT_RELU);
@@ -1076,7 +1095,7 @@ int backward_group(const void* x, const void* dy, const Shape& s, const float* m
                    void* dx, float* dgamma, float* dbeta, int accumulate, hipStream_t stream)
 {
     const bool GLU = ACT == W2L_ACT_GLU, want = dgamma || dbeta;
-    hipLaunchKernelGGL((norm_group_bwd_k<T, N, ACT>), dim3((unsigned)(s.B * (GLU ? s.G / 2 : s.G))), dim3(threads_of(s)),
+    hipLaunchKernelGGL((norm_group_bwd_k<T, N, ACT>), dim3((unsigned)(s.B * (GLU ? s.G / 2 : s.G) * s.split)), dim3(threads_of(s)),
                        want ? (size_t)(GLU ? 2 : 1) * s.lanes * s.Cg * 8 : 0, stream, (const T*)x, (const T*)dy, s, mean, rstd, gamma, beta, (T*)dx, want ? chans : nullptr);
     if (int rc = launch_status()) return rc;
     if (!want) return W2L_OK;
@@ -1121,7 +1140,7 @@ extern "C" size_t w2l_groupnorm_workspace_bytes(int B, int T, int C, int G, int 
     if (!shape_ok(B, T, C, G, act) || !valid_dtype(dtype)) return 0;
     const Form form = form_of(B, T, C, G, act, dtype);
     if (form.group) return round_up((size_t)B * C * 8, 256);
-    Shape s = shape_of(B, T, C, G, nullptr, dtype, (act == W2L_ACT_GLU ? C / 2 : C) / form.N);
+    Shape s = shape_of(B, T, C, G, nullptr, (act == W2L_ACT_GLU ? C / 2 : C) / form.N);
     runs_of(s);
     const size_t a = stat_bytes(s), b = sum_bytes(s);
     return a > b ? a : b;
@@ -1145,9 +1164,9 @@ extern "C" int w2l_groupnorm_fwd(const void* x, const float* gamma, const float*
     if (form.group)
         return with_vector(dtype, n, [&](auto* t, auto n) {
             using T_ = std::remove_pointer_t<decltype(t)>;
-            return forward_group<T_, decltype(n)::value>(x, group_shape(B, T, C, G, in_len, dtype, decltype(n)::value), gamma, beta, eps, act, y, mean, rstd, (hipStream_t)stream);
+            return forward_group<T_, decltype(n)::value>(x, group_shape(B, T, C, G, in_len, decltype(n)::value, form.split), gamma, beta, eps, act, y, mean, rstd, (hipStream_t)stream);
         });
-    Shape ap = shape_of(B, T, C, G, in_len, dtype, Cy / n), st = shape_of(B, T, C, G, in_len, dtype, C / n);
+    Shape ap = shape_of(B, T, C, G, in_len, Cy / n), st = shape_of(B, T, C, G, in_len, C / n);
     runs_of(ap);
     st.rows = ap.rows;
     st.runs = ap.runs;
@@ -1176,7 +1195,7 @@ extern "C" int w2l_groupnorm_bwd(const void* x, const void* dy, const float* mea
     if (!apart(in, out)) return W2L_ERR_OVERLAP;
     const Form form = form_of(B, T, C, G, act, dtype);
     const int n = form.N;
-    Shape s = form.group ? group_shape(B, T, C, G, in_len, dtype, n) : shape_of(B, T, C, G, in_len, dtype, Cy / n);
+    Shape s = form.group ? group_shape(B, T, C, G, in_len, n, form.split) : shape_of(B, T, C, G, in_len, Cy / n);
     if (!form.group) runs_of(s);
     float* const chans = (float*)workspace;
     float2* const groups = (float2*)((char*)workspace + round_up((size_t)B * s.runs * C * 8, 256));
