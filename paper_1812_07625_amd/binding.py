@@ -424,11 +424,12 @@ def w2l_policy_fwd_bwd(z, tokens, old_logprob, advantage, frame_loss, loss=None,
     BT = (B, T)
     per_frame = advantage.dim() == 2
     ptr = _pointers(dev, (("scores", z, shape, z.dtype), ("tokens", tokens, BT, _I32), ("old_logprob", old_logprob, BT, _F32),
-                          ("ref_logprob", ref_logprob, BT, _F32), ("advantage", advantage, BT if per_frame else (B,), _F32)))
-    out = _pointers(dev, (("weight", weight, BT, _F32), ("in_len", in_len, (B,), _I32), ("frame_loss", frame_loss, BT, _F32), ("loss", loss, (B,), _F32),
-                          ("logprob", logprob, BT, _F32), ("dz", dz, shape, gtype)))
-    _call(raw.w2l_policy_fwd_bwd, "w2l_policy_fwd_bwd", dev, (*ptr, int(per_frame), *out, B, T, Cc, clip_low, clip_high, kl_coef, grad_scale, dt, gt,
-                                                              1 if accumulate else 0, *_scratch(workspace, dev)), stream)
+                          ("ref_logprob", ref_logprob, BT, _F32), ("advantage", advantage, BT if per_frame else (B,), _F32), ("weight", weight, BT, _F32),
+                          ("in_len", in_len, (B,), _I32), ("frame_loss", frame_loss, BT, _F32), ("loss", loss, (B,), _F32), ("logprob", logprob, BT, _F32),
+                          ("dz", dz, shape, gtype)))
+    ptr.insert(5, 1 if per_frame else 0)
+    _call(raw.w2l_policy_fwd_bwd, "w2l_policy_fwd_bwd", dev,
+          (*ptr, B, T, Cc, clip_low, clip_high, kl_coef, grad_scale, dt, gt, 1 if accumulate else 0, *_scratch(workspace, dev)), stream)
     return frame_loss, loss, dz
 
 
