@@ -148,7 +148,8 @@ int w2l_glu_bwd(const void *y, const void *dh, void *dy, long long rows, int Cou
  * G = 1 normalises an utterance as a whole, G = C every channel over time.  x, y share `dtype`; gamma, beta [C] fp32 or NULL (1, 0);
  * mean, rstd [B,G] fp32; in_len [B] int32 (0..T) or NULL: all frames.  The arithmetic is fp32, y is rounded once.
  * Frames t >= in_len[b] are not read, whatever they hold; y is 0 there.  An utterance of no frames has mean = rstd = 0.  An in_len
- * outside its range: y, mean and rstd of that utterance are NaN.  NaN or an infinity in a live frame makes its group NaN.
+ * outside its range: y, mean and rstd of that utterance are NaN.  NaN or an infinity in a live frame makes its group NaN; so may values
+ * beyond 2^60, whose squares fp32 does not hold.
  * Limits: C <= 8192, T <= 2^24, B <= 65534, B * T < 2^31, B * T * C <= 2^40; C divisible by G (and by 2 with GLU); eps > 0.  Workspace: the queried
  * bytes (one query for both calls), 256-byte aligned.  No output nor the workspace may overlap an input or another output (W2L_ERR_OVERLAP).
  * Results are bit-reproducible and do not depend on the other utterances of the batch beyond the rounding of fp32 sums. */
@@ -266,7 +267,7 @@ int w2l_frame_ids_check_host(const int *ids, const int *in_len, int B, int Tp, i
  * advantage of 0 leaves the KL term alone.  NaN or +inf in the frame's z, a token other than -1 outside [0,C), an in_len outside its range: loss and
  * logprob are NaN (of the whole utterance in the last case); nothing but -inf: logprob -inf.  A frame whose loss is no finite fp32 number has zero gradient.
  * 0 <= clip_low <= 1, clip_high >= 0 (+inf: no bound), kl_coef >= 0 finite, weight * grad_scale * f finite.  Limits and workspace as
- * w2l_token_logprob_fwd; no output nor the workspace may overlap an input (W2L_ERR_OVERLAP). */
+ * w2l_token_logprob_fwd; no output nor the workspace may overlap an input or another output (W2L_ERR_OVERLAP). */
 size_t w2l_policy_workspace_bytes(int B, int Tp, int C, int z_dtype);
 int w2l_policy_fwd_bwd(const void *z, const int *tokens, const float *old_logprob, const float *ref_logprob,
                        const float *advantage, int advantage_per_frame, const float *weight, const int *in_len,
@@ -303,7 +304,7 @@ int w2l_sgd_momentum_step(float *w, float *v, const float *grad, void *w_lowp, l
  *       infinities are kept as NaN.  All bytes and exponents zero: moments of zero.
  * Arithmetic is fp32 (the moments with each product and sum rounded as written, the norm's sum and the step's constants in 64 bits), w is
  * off by a few half steps.  lr_dev, step_dev [1] (nullable): fp32 lr and int32 step, read on the device in place of lr and step, so that a captured graph
- * steps on; a step below 1 there changes nothing.  They, grad_norm and the exponents need natural alignment only.
+ * steps on; a step below 1 there changes nothing, lr is not checked there.  They, grad_norm and the exponents need natural alignment only.
  * tensors: HOST array, its pointers DEVICE pointers; n = 0: skipped.  Nothing the call writes may overlap anything else it reads or writes
  * (W2L_ERR_OVERLAP: a tensor listed twice, say).  Workspace (queried bytes, 256-byte aligned) where the norm, lr_dev or step_dev is asked for; NULL will do
  * otherwise.  1 <= n_tensors <= W2L_ADAMW_MAX_TENSORS, n <= W2L_ADAMW_MAX_VALUES, step >= 1, lr, weight_decay, max_norm >= 0, 0 <= beta <= 1 - 1e-7,

@@ -819,14 +819,16 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_k(const T* __restric
     for (t = live + at.part * s.lanes + lane; t < s.T; t += s.split * s.lanes) put<T, N, false>(q + (size_t)t * Cy, none);
 }
 
-// chans [B][2][C]: sums of du and du xhat of an utterance (NULL: not wanted)
+// chans [B][2][C]: sums of du and du xhat of an utterance (NULL: not wanted).  One utterance alone has dgamma and dbeta in their place, and no launch after this.
 template <typename T, int N, int ACT>
 __global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __restrict__ x, const T* __restrict__ dy, Shape s, const float* __restrict__ mean,
                                                                   const float* __restrict__ rstd, const float* __restrict__ gamma,
-                                                                  const float* __restrict__ beta, T* __restrict__ dx, float* __restrict__ chans)
+                                                                  const float* __restrict__ beta, T* __restrict__ dx, float* __restrict__ chans,
+                                                                  float* __restrict__ dgamma, float* __restrict__ dbeta, int accumulate)
 {
     constexpr bool GLU = ACT == W2L_ACT_GLU;
     constexpr int U = GROUP_BATCH;
+    const bool sums = chans || dgamma || dbeta;
     extern __shared__ float2 acc[];  // [GLU: 2][lanes][Cg]: a lane's sums
     __shared__ float2 lds[2][GROUP_THREADS / 64];
     Place at = place_of(s, GLU ? s.G / 2 : s.G);
@@ -895,7 +897,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __res
             k2.y = __builtin_fmaf(r2[j], h.scale[j], k2.y);
         }
     }
-    if (chans && on && at.part == 0)
+    if (sums && on && at.part == 0)
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             acc[lane * s.Cg + col * N + j] = make_float2(s1[j], s2[j] * rs);
@@ -903,7 +905,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __res
         }
     k1 = sum_group(make_float2(wave64(k1.x, Sum()), wave64(k1.y, Sum())), lds[0]);
     if (GLU) k2 = sum_group(make_float2(wave64(k2.x, Sum()), wave64(k2.y, Sum())), lds[1]);
-    if (chans && at.part == 0) {
+    if (sums && at.part == 0) {
         if (blockDim.x == 64) __syncthreads();  // (sum_group's are the others')
         const int team = team_of(GLU ? 2 * s.Cg : s.Cg, s.lanes), l = threadIdx.x & (team - 1), teams = blockDim.x / team, count = GLU ? 2 * s.Cg : s.Cg;
         for (int i0 = 0; i0 < count; i0 += teams) {
@@ -920,9 +922,14 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __res
                 k.y += __shfl_xor(k.y, o, 64);
             }
             if (i < count && l == 0) {
-                float* const o = chans + (size_t)b * 2 * s.C + at.g * s.Cg + half * Cy + c;
-                o[0] = k.x;
-                o[s.C] = k.y;
+                const int to = at.g * s.Cg + half * Cy + c;
+                if (chans) {
+                    float* const o = chans + (size_t)b * 2 * s.C + to;
+                    o[0] = k.x;
+                    o[s.C] = k.y;
+                }
+                if (dgamma) dgamma[to] = accumulate ? dgamma[to] + k.y : k.y;
+                if (dbeta) dbeta[to] = accumulate ? dbeta[to] + k.x : k.x;
             }
         }
     }
@@ -1094,11 +1101,12 @@ template <typename T, int N, int ACT>
 int backward_group(const void* x, const void* dy, const Shape& s, const float* mean, const float* rstd, const float* gamma, const float* beta, float* chans,
                    void* dx, float* dgamma, float* dbeta, int accumulate, hipStream_t stream)
 {
-    const bool GLU = ACT == W2L_ACT_GLU, want = dgamma || dbeta;
+    const bool GLU = ACT == W2L_ACT_GLU, want = dgamma || dbeta, alone = s.B == 1;
     hipLaunchKernelGGL((norm_group_bwd_k<T, N, ACT>), dim3((unsigned)(s.B * (GLU ? s.G / 2 : s.G) * s.split)), dim3(threads_of(s)),
-                       want ? (size_t)(GLU ? 2 : 1) * s.lanes * s.Cg * 8 : 0, stream, (const T*)x, (const T*)dy, s, mean, rstd, gamma, beta, (T*)dx, want ? chans : nullptr);
+                       want ? (size_t)(GLU ? 2 : 1) * s.lanes * s.Cg * 8 : 0, stream, (const T*)x, (const T*)dy, s, mean, rstd, gamma, beta, (T*)dx,
+                       want && !alone ? chans : nullptr, alone ? dgamma : nullptr, alone ? dbeta : nullptr, accumulate);
     if (int rc = launch_status()) return rc;
-    if (!want) return W2L_OK;
+    if (!want || alone) return W2L_OK;
     hipLaunchKernelGGL(norm_join_k, dim3((s.C + JOIN_CHANNELS - 1) / JOIN_CHANNELS), dim3(256), 0, stream, chans, s.B, s.C, dgamma, dbeta, accumulate);
     return launch_status();
 }

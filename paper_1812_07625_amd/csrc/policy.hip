@@ -315,9 +315,11 @@ extern "C" int w2l_policy_fwd_bwd(const void* z, const int* tokens, const float*
         return W2L_ERR_ALIGN;
     const size_t rows = (size_t)B * Tp, need = w2l_policy_workspace_bytes(B, Tp, C, z_dtype);
     if (!workspace_ok(workspace, ws_bytes, need)) return W2L_ERR_WORKSPACE;
+    const Span frame{frame_loss, rows * 4}, sums{loss, (size_t)B * 4}, lps{logprob, rows * 4}, grad{dz, rows * C * dtype_size(dz_dtype)}, ws{workspace, need};
     if (!apart({{z, rows * C * dtype_size(z_dtype)}, {tokens, rows * 4}, {old_logprob, rows * 4}, {ref_logprob, rows * 4},
                 {advantage, advantage_per_frame ? rows * 4 : (size_t)B * 4}, {weight, rows * 4}, {in_len, (size_t)B * 4}},
-               {{frame_loss, rows * 4}, {loss, (size_t)B * 4}, {logprob, rows * 4}, {dz, rows * C * dtype_size(dz_dtype)}, {workspace, need}}))
+               {frame, sums, lps, grad, ws}) ||
+        !apart({frame}, {sums, lps, grad, ws}) || !apart({sums}, {lps, grad, ws}) || !apart({lps}, {grad, ws}) || !apart({grad}, {ws}))
         return W2L_ERR_OVERLAP;
     const Frames fr = frames_of(in_len, B, Tp);
     const Policy po{tokens, old_logprob, ref_logprob, advantage, weight, frame_loss, logprob, 1.f - clip_low, 1.f + clip_high, kl_coef, grad_scale, advantage_per_frame};

@@ -249,19 +249,20 @@ def test_values_without_deviation(P):
     assert np.array_equal(got["y"], np.full(x.shape, 0.5)) and np.allclose(got["rstd"], 1e-3 ** -0.5, rtol=1e-6) and np.abs(got["dx"]).max() < 1e-4
 
 
-def test_gradients_are_added(P):
-    x, gamma, beta, dy = case(14, 3, 90, 48, "glu", "bf16")
-    before = np.random.default_rng(15).standard_normal(48).astype(np.float32).astype(np.float64)
-    n = [90, 10, 55]
-    check(run(P, x, 6, gamma, beta, n, "glu", "bf16", dy, accumulate=before), x, 6, gamma, beta, n, "glu", "bf16", dy, accumulate=before)
+@pytest.mark.parametrize("T,C,G,lengths", [(90, 48, 6, [90, 10, 55]), (90, 48, 6, [71]), (2500, 58, 1, [2500, 800]), (2500, 58, 1, [2000])], ids=str)
+def test_gradients_are_added(P, T, C, G, lengths):
+    x, gamma, beta, dy = case(14, len(lengths), T, C, "glu", "bf16")
+    before = np.random.default_rng(15).standard_normal(C).astype(np.float32).astype(np.float64)
+    check(run(P, x, G, gamma, beta, lengths, "glu", "bf16", dy, accumulate=before), x, G, gamma, beta, lengths, "glu", "bf16", dy, accumulate=before)
 
 
-def test_one_gradient_alone(P):
-    x, gamma, beta, dy = case(16, 2, 30, 24, "silu", "fp32")
-    full = run(P, x, 3, gamma, beta, None, "silu", "fp32", dy)
+@pytest.mark.parametrize("B,T,G", [(2, 30, 3), (1, 30, 3), (2, 3000, 1)])
+def test_one_gradient_alone(P, B, T, G):
+    x, gamma, beta, dy = case(16, B, T, 24, "silu", "fp32")
+    full = run(P, x, G, gamma, beta, None, "silu", "fp32", dy)
     xd, dyd, gd, bd = to_dev(x), to_dev(dy), to_dev(gamma), to_dev(beta)
-    y, mean, rstd = torch.empty_like(xd), torch.empty(2, 3, device=DEV), torch.empty(2, 3, device=DEV)
-    ws = P.workspace(P.w2l_groupnorm_workspace_bytes(2, 30, 24, 3, P.W2L_ACT_SILU, P.W2L_F32))
+    y, mean, rstd = torch.empty_like(xd), torch.empty(B, G, device=DEV), torch.empty(B, G, device=DEV)
+    ws = P.workspace(P.w2l_groupnorm_workspace_bytes(B, T, 24, G, P.W2L_ACT_SILU, P.W2L_F32))
     P.w2l_groupnorm_fwd(xd, y, mean, rstd, gd, bd, act=P.W2L_ACT_SILU, workspace=ws)
     for which in ("dgamma", "dbeta", None):
         out = torch.empty(24, device=DEV)
@@ -352,3 +353,53 @@ def test_a_tensor_beyond_2_31_values(P):
     torch.cuda.synchronize()
     assert float((dx[-2:].float() - dx2.float()).abs().max()) < 0.05 and not bool(dx[:-2].any())
     assert float((db - db2).norm() / db2.norm()) < 1e-3 and float((dg - dg2).norm() / dg2.norm()) < 1e-3
+
+
+def test_tensors_of_another_shape_or_place(P):
+    x, s = torch.zeros(2, 5, 8, device=DEV), torch.zeros(2, 2, device=DEV)
+    y, ws = torch.zeros_like(x), P.workspace(1 << 20)
+    with pytest.raises(ValueError, match="y must have shape"):
+        P.w2l_groupnorm_fwd(x, y, s, s.clone(), act=P.W2L_ACT_GLU, workspace=ws)
+    with pytest.raises(TypeError, match="y must be"):
+        P.w2l_groupnorm_fwd(x, y.bfloat16(), s, s.clone(), workspace=ws)
+    with pytest.raises(TypeError, match="unsupported"):
+        P.w2l_groupnorm_fwd(x.half(), y.half(), s, s.clone(), workspace=ws)
+    with pytest.raises(ValueError, match="rstd must have shape"):
+        P.w2l_groupnorm_fwd(x, y, s, torch.zeros(2, 4, device=DEV), workspace=ws)
+    with pytest.raises(ValueError, match="gamma must have shape"):
+        P.w2l_groupnorm_fwd(x, y, s, s.clone(), torch.zeros(7, device=DEV), workspace=ws)
+    with pytest.raises(ValueError, match="x must be contiguous"):
+        P.w2l_groupnorm_fwd(x.transpose(1, 2).contiguous().transpose(1, 2), y, s, s.clone(), workspace=ws)
+    with pytest.raises(ValueError, match="in_len is on cpu"):
+        P.w2l_groupnorm_fwd(x, y, s, s.clone(), in_len=torch.zeros(2, dtype=torch.int32), workspace=ws)
+    with pytest.raises(P.W2LError, match="-5"):
+        P.w2l_groupnorm_fwd(x, y, s, s.clone())
+    with pytest.raises(P.W2LError, match="-8"):
+        P.w2l_groupnorm_fwd(x, x, s, s.clone(), workspace=ws)
+    with pytest.raises(P.W2LError, match="-8"):
+        P.w2l_groupnorm_fwd(x, y, s, s, workspace=ws)
+    with pytest.raises(ValueError, match="dgamma must have shape"):
+        P.w2l_groupnorm_bwd(x, y, s, s.clone(), torch.zeros_like(x), dgamma=s, workspace=ws)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_gradients_by_differences(P, act):
+    """The kernel's gradients against central differences of its own forward pass in fp32: a step of 2^-7 leaves 2^-14 / 6 of the third derivative (a few units here) and
+    the forward pass's own rounding over the step, 2^7 * 50 U * sum |dy|, a quarter of a percent of a gradient of one."""
+    rng = np.random.default_rng(40)
+    B, T, C, G = 1, 6, 8, 2
+    x = held(rng.standard_normal((B, T, C)), "fp32")
+    gamma, beta = held(1 + 0.3 * rng.standard_normal(C), "fp32"), held(0.5 + 0.3 * rng.standard_normal(C), "fp32")
+    dy = held(rng.standard_normal((B, T, C // 2 if act == "glu" else C)), "fp32")
+    got = run(P, x, G, gamma, beta, None, act, "fp32", dy, eps=0.1)
+    near_kink = (np.abs(oracle.groupnorm(x, G, gamma, beta, None, 0.1, act)["u"]) < 0.1).any() if act == "relu" else False
+    h = 2.0 ** -7
+    loss = lambda a: (run(P, a, G, gamma, beta, None, act, "fp32", eps=0.1)["y"] * dy).sum()  # noqa: E731
+    for i in [(0, 0, 0), (0, 3, 5), (0, 5, 7), (0, 2, 2)]:
+        up, dn = x.copy(), x.copy()
+        up[i] += h
+        dn[i] -= h
+        num = (loss(held(up, "fp32")) - loss(held(dn, "fp32"))) / (held(up, "fp32") - held(dn, "fp32"))[i]
+        most = h * h * 8 + 50 * U * np.abs(dy).sum() / h
+        # a rectifier's kink within the step is worth up to the step times the slope's jump
+        assert abs(num - got["dx"][i]) <= most + (2 * h * np.abs(dy).max() * 4 if near_kink else 0), (i, num, got["dx"][i])

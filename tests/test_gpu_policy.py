@@ -278,3 +278,22 @@ def test_tensors_of_another_shape_or_place(P):
         P.w2l_policy_fwd_bwd(z, tok, old, A.cpu(), frame)
     with pytest.raises(P.W2LError):
         P.w2l_policy_fwd_bwd(z, tok, old, A, frame, kl_coef=0.1)          # a KL term without a reference
+
+
+def test_scores_beyond_2_31(P):
+    """Offsets that pass 32 bits: the last frames are as they are alone."""
+    T, C = 8400, 262144                                                    # 2.2e9 scores
+    free, _ = torch.cuda.mem_get_info()
+    if free < 24 << 30:
+        pytest.skip("needs 24 GiB")
+    c = case(12, 1, 3, C, "bf16")
+    z = torch.zeros((1, T, C), dtype=torch.bfloat16, device=DEV)
+    z[:, -3:] = dev(c["z"], "bf16")
+    far = lambda k: torch.cat((torch.zeros((1, T - 3), dtype=torch.from_numpy(c[k]).dtype), torch.from_numpy(c[k])), 1).to(torch.int32 if k == "tokens" else torch.float32).to(DEV)  # noqa: E731
+    frame, dz = torch.empty(1, T, device=DEV), torch.empty_like(z)
+    ws = P.workspace(P.w2l_policy_workspace_bytes(1, T, C, P.W2L_BF16))
+    P.w2l_policy_fwd_bwd(z, far("tokens"), far("old"), far("A"), frame, dz=dz, ref_logprob=far("ref"), weight=far("w"), clip_low=LOW, clip_high=HIGH, kl_coef=0.1, grad_scale=0.5,
+                         workspace=ws)
+    torch.cuda.synchronize()
+    check({"frame": to_host(frame[:, -3:]), "dz": to_host(dz[:, -3:])}, c, gtype="bf16")
+    assert not bool(dz[:, :-3].any()) and not bool(frame[:, :-3].any())    # weights of 0

@@ -97,8 +97,9 @@ def test_policy_arguments():
 
 def test_policy_outputs_on_inputs():
     at = places(POLICY)
-    for o, i in itertools.product(POLICY[7:], POLICY[:7]):
-        assert policy(**{o: at[i]}) == -8, (o, i)
+    for o, i in itertools.product(POLICY[7:], POLICY):
+        if o != i:
+            assert policy(**{o: at[i]}) == -8, (o, i)
 
 
 # ---- AdamW
