@@ -10,13 +10,14 @@
 // knows of its channels stays in registers from row to row.
 #include "lanes.h"
 
+#include <algorithm>
 #include <type_traits>
 
 using namespace w2l;
 
 namespace {
 
-constexpr int MAX_CHANNELS = 8192, MAX_FRAMES = 1 << 24, MAX_THREADS = 512, BATCH = 4;  // (8192: a pair of floats a channel fits 64 KB of LDS)
+constexpr int MAX_CHANNELS = 8192, MAX_FRAMES = 1 << 24, MAX_THREADS = 512, BATCH = 4, JOIN_CHANNELS = 16, JOIN_THREADS = 256;  // (8192: a pair of floats a channel fits 64 KB of LDS)
 
 // A vector of N neighbouring channels as it lies in memory, and its values
 template <typename T, int N> struct Vec {
@@ -296,6 +297,32 @@ __device__ __forceinline__ float2 stat_of(double2 k, double inv, float eps)
     const double mean = k.x * inv, var = k.y * inv - mean * mean;
     return make_float2((float)mean, inv > 0. ? 1.f / sqrtf((var < 0. ? 0.f : (float)var) + eps) : 0.f);
 }
+// A lane's share of the sums of a group's runs, from p on, a row of G groups each.  Where they are many, eight loads are in flight at once (in one utterance of
+// 2000x2048 with 64 groups, fp32, 39 -> 17 us for the forward call, together with the longer runs of runs_of); where they are few, the masked ones would cost 1 us.
+template <typename V>
+__device__ __forceinline__ V sum_runs(const V* __restrict__ p, int G, int runs, int l, int team)
+{
+    constexpr int U = 8;
+    V k{};
+    int r = l;
+    for (; r + (U - 1) * team < runs; r += U * team) {
+        V o[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) o[i] = p[(size_t)(r + i * team) * G];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            k.x += o[i].x;
+            k.y += o[i].y;
+        }
+    }
+#pragma unroll 4
+    for (; r < runs; r += team) {
+        const V o = p[(size_t)r * G];
+        k.x += o.x;
+        k.y += o.y;
+    }
+    return k;
+}
 // of every group of utterance b, into LDS
 __device__ __forceinline__ void join_stats(const Shape& s, const double2* __restrict__ sums, int b, int len, float eps, float2* stat)
 {
@@ -304,13 +331,7 @@ __device__ __forceinline__ void join_stats(const Shape& s, const double2* __rest
     for (int g0 = 0; g0 < s.G; g0 += teams) {
         const int g = g0 + threadIdx.x / team;
         double2 k = make_double2(0., 0.);
-        if (g < s.G)
-#pragma unroll 4
-            for (int r = l; r < runs; r += team) {
-                const double2 o = sums[((size_t)b * s.runs + r) * s.G + g];
-                k.x += o.x;
-                k.y += o.y;
-            }
+        if (g < s.G) k = sum_runs(sums + (size_t)b * s.runs * s.G + g, s.G, runs, l, team);
         k = sum64(k, team);
         if (g < s.G && l == 0) stat[g] = stat_of(k, inv, eps);
     }
@@ -517,43 +538,47 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
                        [&](int g, float2 k) { groups[((size_t)b * s.runs + run) * s.G + g] = k; });
 }
 
-// dgamma and dbeta of sixteen channels from `count` rows [2][C] of sums (dbeta's, dgamma's), those that are there(row): threads take rows in turn, and their sums are
+// dgamma and dbeta of `width` channels from `count` rows [2][C] of sums (dbeta's, dgamma's), those that are there(row): threads take rows in turn, and their sums are
 // added up in 64 bits and a fixed order.  All loads of a batch are in flight at once.
-constexpr int JOIN_CHANNELS = 16;
 template <typename F>
-__device__ __forceinline__ void sum_channels(const float* __restrict__ chans, int count, int C, int block, double2* lds, float* __restrict__ dgamma,
+__device__ __forceinline__ void sum_channels(const float* __restrict__ chans, int count, int C, int block, int width, double2* lds, float* __restrict__ dgamma,
                                              float* __restrict__ dbeta, int accumulate, F there)
 {
     constexpr int U = 8;
-    const int l = threadIdx.x % JOIN_CHANNELS, first = threadIdx.x / JOIN_CHANNELS, step = blockDim.x / JOIN_CHANNELS, c = block * JOIN_CHANNELS + l;
-    double g = 0., h = 0.;
+    const int l = threadIdx.x & (width - 1), first = threadIdx.x / width, step = blockDim.x / width, c = block * width + l;
+    double2 k = make_double2(0., 0.);
     if (c < C)
         for (int i = first; i < count; i += U * step) {
             float gv[U], hv[U];
             bool on[U];
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const int r = i + k * step < count ? i + k * step : i;
+            for (int j = 0; j < U; ++j) {
+                const int r = i + j * step < count ? i + j * step : i;
                 const float* const p = chans + (size_t)r * 2 * C + c;
-                hv[k] = p[0];
-                gv[k] = p[C];
-                on[k] = i + k * step < count && there(r);
+                hv[j] = p[0];
+                gv[j] = p[C];
+                on[j] = i + j * step < count && there(r);
             }
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                h += on[k] ? hv[k] : 0.f;
-                g += on[k] ? gv[k] : 0.f;
+            for (int j = 0; j < U; ++j) {
+                k.x += on[j] ? gv[j] : 0.f;
+                k.y += on[j] ? hv[j] : 0.f;
             }
         }
-    lds[threadIdx.x] = make_double2(g, h);
+    for (int o = 32; o >= width; o >>= 1) {
+        k.x += __shfl_xor(k.x, o, 64);
+        k.y += __shfl_xor(k.y, o, 64);
+    }
+    const int waves = blockDim.x / 64, wave = threadIdx.x / 64;
+    if ((int)(threadIdx.x & 63) < width) lds[wave * width + l] = k;
     __syncthreads();
     if (first != 0 || c >= C) return;
-    for (int i = 1; i < step; ++i) {
-        g += lds[i * JOIN_CHANNELS + l].x;
-        h += lds[i * JOIN_CHANNELS + l].y;
+    for (int i = 1; i < waves; ++i) {
+        k.x += lds[i * width + l].x;
+        k.y += lds[i * width + l].y;
     }
-    if (dgamma) dgamma[c] = (float)(accumulate ? dgamma[c] + g : g);
-    if (dbeta) dbeta[c] = (float)(accumulate ? dbeta[c] + h : h);
+    if (dgamma) dgamma[c] = (float)(accumulate ? dgamma[c] + k.x : k.x);
+    if (dbeta) dbeta[c] = (float)(accumulate ? dbeta[c] + k.y : k.y);
 }
 
 // Workgroups from `ahead` on: dx of a run of frames.  Those before them make dgamma and dbeta, whose longer chains of loads start first; they are a multiple of
@@ -562,7 +587,7 @@ template <typename T, int N, int ACT>
 __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))) void norm_dx_k(const T* __restrict__ x, const T* __restrict__ dy, Shape s, const float* __restrict__ mean,
                                                          const float* __restrict__ rstd, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                          const float* __restrict__ chans, const float2* __restrict__ groups, T* __restrict__ dx,
-                                                         float* __restrict__ dgamma, float* __restrict__ dbeta, int accumulate, int ahead)
+                                                         float* __restrict__ dgamma, float* __restrict__ dbeta, int accumulate, int ahead, int width)
 {
     extern __shared__ double2 lds[];  // [G] of floats: means of du gamma and du gamma xhat
     constexpr bool GLU = ACT == W2L_ACT_GLU;
@@ -570,7 +595,7 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
     const int Cy = GLU ? s.C / 2 : s.C;
     if ((int)blockIdx.x < ahead) {
         // (runs that are not there left nothing: what lies in their place is not added)
-        sum_channels(chans, s.B * s.runs, s.C, blockIdx.x, lds, dgamma, dbeta, accumulate, [&](int i) {
+        sum_channels(chans, s.B * s.runs, s.C, blockIdx.x, width, lds, dgamma, dbeta, accumulate, [&](int i) {
             const int u = i / s.runs;
             return (i - u * s.runs) * s.rows < frames_of(s, u);
         });
@@ -610,17 +635,8 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
         for (int g0 = 0; g0 < s.G; g0 += teams) {
             const int g = g0 + threadIdx.x / team;
             float2 k = make_float2(0.f, 0.f);
-            if (g < s.G)
-#pragma unroll 4
-                for (int r = l; r < runs; r += team) {
-                    const float2 o = groups[((size_t)b * s.runs + r) * s.G + g];
-                    k.x += o.x;
-                    k.y += o.y;
-                }
-            for (int o = team >> 1; o > 0; o >>= 1) {
-                k.x += __shfl_xor(k.x, o, 64);
-                k.y += __shfl_xor(k.y, o, 64);
-            }
+            if (g < s.G) k = sum_runs(groups + (size_t)b * s.runs * s.G + g, s.G, runs, l, team);
+            k = sum64(k, team);
             if (g < s.G && l == 0) means[g] = make_float2(k.x * inv, k.y * inv);
         }
         __syncthreads();
@@ -681,9 +697,9 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
 // ---- a workgroup a group -------------------------------------------------------------------------------------
 // Where groups are many or short, a workgroup has a group of an utterance (with GLU the group of the values and that of their gates) and reads it twice, the second
 // time from its L2, in one launch.  Vectors and groups of one utterance that are neighbours share lines, so consecutive ones go to one XCD.
-constexpr int GROUP_THREADS = 512, GROUP_BATCH = 6, FLUSH = 60;  // (512: a lane's sums of all channels fit 64 KB of LDS)
+constexpr int GROUP_THREADS = 512, GROUP_BATCH = 4, FLUSH = 64;  // (512: a lane's sums of all channels fit 64 KB of LDS; batches of 4: 35.4 us, of 3 35.6, 6 37.3, 10 40.8 for 8x750x1536 with GLU and its gradient)
 static_assert(FLUSH % GROUP_BATCH == 0, "sums are flushed between batches");
-// Where groups are fewer than CUs, two workgroups (split) each read a whole group and write half of its frames (8x750x1536 bf16 with GLU, 128 pairs of groups: 15.0 -> 14.7 us, with its
+// Where groups are fewer than CUs, two workgroups (split) each read a whole group and write half of its frames (8x750x1536 bf16 with GLU, 128 pairs of groups, at batches of 6: 15.0 -> 14.7 us, with its
 // gradient 39.5 -> 37.1; 5x333x500 fp32, SiLU, and its gradient 17.0 -> 16.5; four or eight of them gain nothing more).
 struct Place {
     int b, g, part, from, to;  // frames from .. to of the utterance's are written
@@ -971,10 +987,10 @@ __global__ __launch_bounds__(GROUP_THREADS) void norm_group_bwd_k(const T* __res
 }
 
 // dgamma and dbeta from the utterances' sums
-__global__ __launch_bounds__(256) void norm_join_k(const float* __restrict__ chans, int B, int C, float* __restrict__ dgamma, float* __restrict__ dbeta, int accumulate)
+__global__ __launch_bounds__(JOIN_THREADS) void norm_join_k(const float* __restrict__ chans, int B, int C, float* __restrict__ dgamma, float* __restrict__ dbeta, int accumulate, int width)
 {
-    __shared__ double2 lds[256];
-    sum_channels(chans, B, C, blockIdx.x, lds, dgamma, dbeta, accumulate, [](int) { return true; });
+    __shared__ double2 lds[JOIN_THREADS / 64 * JOIN_CHANNELS];
+    sum_channels(chans, B, C, blockIdx.x, width, lds, dgamma, dbeta, accumulate, [](int) { return true; });
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------
@@ -1001,6 +1017,8 @@ Shape shape_of(int B, int T, int C, int G, const int* in_len, int vectors)
     s.inv_cols = 1.f / (float)s.cols;
     return s;
 }
+// channels whose sums a workgroup joins: fewer where rows are so many that a thread had more than four batches of them (64x2000x32 fp32, SiLU, the backward call 58 -> 26 us)
+int join_width(long long rows, int threads) { return rows > 4LL * 8 * (threads / JOIN_CHANNELS) ? JOIN_CHANNELS / 4 : JOIN_CHANNELS; }
 int threads_of(const Shape& s) { return (s.cols * s.lanes + 63) / 64 * 64; }
 // Frames of a run, the same for all kernels of a call, so that a workgroup finds in its XCD's L2 what that of the same number read before: whole batches of loads
 // (BATCH rows a thread), three runs a CU where there are so many
@@ -1010,6 +1028,8 @@ void runs_of(Shape& s)
     long long r = ((long long)s.B * s.T + 384) / 768 + unit / 2;
     r = r / unit * unit;
     s.rows = (int)(r < unit ? unit : r > 64 ? 64 : r);
+    // (longer ones where joining an utterance's runs costs a workgroup more than its own rows)
+    while (s.rows < 64 && (long long)(s.T / s.rows) * s.G * 2 > (long long)s.rows * s.C) s.rows += unit;
     s.runs = (s.T + s.rows - 1) / s.rows;
 }
 bool workspace_ok(const void* ws, size_t have, size_t need) { return ws && have >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0; }
@@ -1040,15 +1060,17 @@ struct Form {
     int split;
 };
 // A workgroup a group saves a launch and the second reading from far away, as long as there are workgroups for the chip or what one reads is little.  Both ways
-// in us, forward and backward call (bf16, SiLU): 64 workgroups of 25 KB: 5.8 and 10.5 against 9.5 and 13; of 125 KB: 12 and 24 against 12 and 18; 128 of 250 KB (GLU): 20 and 35
-// against 20 and 35; of 1 MB: 66 and 126 against 66 and 115; 256 of 500 KB: 75 and 115 against 87 and 135; 16 of 500 KB: 34 and 69 against 12 and 17.
-// Thousands of workgroups that read few bytes are slower as well (4096 of 8 KB, 16 bytes a row: 42 and 76 against 25 and 39).
+// in us, forward and backward call (SiLU unless said): 64 workgroups of 62 KB (fp32): 6.1 and 10.4 against 9.0 and 9.8; of 125 KB (bf16): 10.5 and 21 against 10.7 and 16.1; 128 of 144 KB
+// (bf16, GLU): 14.0 and 24.2 against 17.3 and 25.3; 256 of 125 KB (bf16): 17.7 and 31 against 23.2 and 42; of 500 KB: 80 and 121 against 74 and 121; 1024 of 100 KB: 53 and 81 against
+// 55 and 134; 16 of 500 KB: 25 and 53 against 10.9 and 16.7.  Rows of more vectors than a workgroup's threads make few and slow runs (1x500x8192 bf16, 64 of 125 KB: 10.2 and 18
+// against 17.8 and 42).  Thousands of workgroups that read few bytes are slower as well (4096 of 8 KB, 16 bytes a row: 36 and 69 against 23 and 40).
 Form form_of(int B, int T, int C, int G, int act, int dtype)
 {
     const bool glu = act == W2L_ACT_GLU;
     const int Cg = C / G, n = vector_of(Cg, glu ? C / 2 : C, dtype);
     const long long workgroups = (long long)B * (glu ? G / 2 : G), bytes = (long long)T * Cg * (glu ? 2 : 1) * dtype_size(dtype);
-    const long long most = workgroups >= 256 ? 1 << 20 : workgroups >= 128 ? 512 << 10 : 64 << 10;
+    const bool wide = (glu ? C / 2 : C) / n > MAX_THREADS;
+    const long long most = workgroups >= 256 ? 1 << 20 : workgroups >= 128 ? 512 << 10 : wide ? 256 << 10 : 64 << 10;
     // (a thread's sums of at most 128 rows: in fp32)
     const bool group = !(glu && G % 2) && Cg / n <= 256 && bytes <= most && !(workgroups >= 2048 && bytes < (16 << 10)) && T <= 128 * (GROUP_THREADS / (Cg / n));
     const int split = group && workgroups <= 128 && bytes >= (16 << 10) ? 2 : 1;
@@ -1107,7 +1129,8 @@ int backward_group(const void* x, const void* dy, const Shape& s, const float* m
                        want && !alone ? chans : nullptr, alone ? dgamma : nullptr, alone ? dbeta : nullptr, accumulate);
     if (int rc = launch_status()) return rc;
     if (!want || alone) return W2L_OK;
-    hipLaunchKernelGGL(norm_join_k, dim3((s.C + JOIN_CHANNELS - 1) / JOIN_CHANNELS), dim3(256), 0, stream, chans, s.B, s.C, dgamma, dbeta, accumulate);
+    const int width = join_width(s.B, JOIN_THREADS);
+    hipLaunchKernelGGL(norm_join_k, dim3((s.C + width - 1) / width), dim3(JOIN_THREADS), 0, stream, chans, s.B, s.C, dgamma, dbeta, accumulate, width);
     return launch_status();
 }
 template <typename T, int N, int ACT>
@@ -1117,10 +1140,10 @@ int backward(const void* x, const void* dy, const Shape& s, const float* mean, c
     hipLaunchKernelGGL((norm_sums_k<T, N, ACT>), dim3((unsigned)(s.runs * s.B)), dim3(threads_of(s)), (size_t)s.lanes * s.C * 8, stream, (const T*)x, (const T*)dy, s,
                        mean, rstd, gamma, beta, chans, groups);
     if (int rc = launch_status()) return rc;
-    const int ahead = dgamma || dbeta ? ((s.C + JOIN_CHANNELS - 1) / JOIN_CHANNELS + 7) / 8 * 8 : 0;
+    const int width = join_width((long long)s.runs * s.B, threads_of(s)), ahead = dgamma || dbeta ? ((s.C + width - 1) / width + 7) / 8 * 8 : 0;
     hipLaunchKernelGGL((norm_dx_k<T, N, ACT>), dim3((unsigned)(ahead + (long long)s.runs * s.B)), dim3(threads_of(s)),
-                       (size_t)(s.G > 2 * threads_of(s) ? s.G : 2 * threads_of(s)) * 8, stream, (const T*)x,
-                       (const T*)dy, s, mean, rstd, gamma, beta, chans, groups, (T*)dx, dgamma, dbeta, accumulate, ahead);
+                       std::max((size_t)s.G * 8, (size_t)threads_of(s) / 64 * JOIN_CHANNELS * 16), stream, (const T*)x,
+                       (const T*)dy, s, mean, rstd, gamma, beta, chans, groups, (T*)dx, dgamma, dbeta, accumulate, ahead, width);
     return launch_status();
 }
 

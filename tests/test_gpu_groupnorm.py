@@ -182,6 +182,16 @@ def test_both_directions(P, shape, dtype, act):
     check(run(P, x, G, gamma, beta, n, act, dtype, dy), x, G, gamma, beta, n, act, dtype, dy, l2=not few)
 
 
+# utterances whose sums are joined a few channels at a time; runs so many that a lane joins batches of them; groups of rows wider than a workgroup's vectors
+@pytest.mark.parametrize("shape,group", [((600, 9, 24, 3), 1), ((1, 3000, 2048, 64), 0), ((1, 300, 8192, 64), 1)], ids=str)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_long_joins(P, shape, group, dtype):
+    B, T, C, G = shape
+    assert P.w2l_groupnorm_launch_config(*shape, P.W2L_ACT_SILU, P.W2L_BF16 if dtype == "bf16" else P.W2L_F32)[0] == group
+    x, gamma, beta, dy = case(C + B, B, T, C, "silu", dtype)
+    check(run(P, x, G, gamma, beta, None, "silu", dtype, dy), x, G, gamma, beta, None, "silu", dtype, dy)
+
+
 @pytest.mark.parametrize("C", [7, 9, 31, 255])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_odd_channels(P, C, dtype):
