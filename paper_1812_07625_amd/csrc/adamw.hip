@@ -1,6 +1,6 @@
 // AdamW over many tensors at once (w2l_adamw_step): one launch for up to 48 tensors, moments in 32 bits or in 8, the gradients clipped by their
 // joint norm.  A value costs 18 to 30 bytes, each touched once, and 4 more where the norm reads the gradients first: memory bounds it.  107 M values with a bf16 copy,
-// clipped: 600 us with moments in 32 bits (6.1 TB/s), of which the norm takes 75, and 427 in 8 (5.5 TB/s); a copy of 4 GB moves 4.8.
+// clipped: 584 us with moments in 32 bits (6.2 TB/s), of which the norm takes 75, and 400 in 8 (5.9 TB/s); a copy of 4 GB moves 4.8.
 #include "lanes.h"
 
 #include <algorithm>
@@ -11,7 +11,7 @@ using namespace w2l;
 namespace {
 
 constexpr int THREADS = 256, MOST = 48;           // MOST tensors a launch: their table is a kernel argument, of which 4 KB are to be had
-// Values that share an exponent; values of a workgroup, with moments in 32 and in 8 bits (32 bits: 4096 values take 621 us at 107 M, 2048 611, 1024 600)
+// Values that share an exponent; values of a workgroup, with moments in 32 and in 8 bits (32 bits, through the caches: 4096 values take 621 us at 107 M, 2048 611, 1024 600)
 constexpr int BLOCK = 256, CHUNK32 = 4 * THREADS, CHUNK8 = 16 * THREADS;
 constexpr long long MOST_GROUPS = W2L_ADAMW_MAX_VALUES / CHUNK32;  // of a launch: 2^31 threads
 constexpr int NORM_GROUPS = 256, NORM_CHUNK = 4096;  // workgroups a tensor's norm has at most, and values for which it has one more

@@ -4,7 +4,7 @@
 //                      norm_sums_k: sums over a run of du and du xhat of every channel, and of both times gamma of every group;
 //                      norm_dx_k: joins them and writes dx; workgroups of its own add up dgamma and dbeta
 //   a workgroup a group  norm_group_k, norm_group_bwd_k (and norm_join_k for dgamma and dbeta): groups that one workgroup reads twice
-// What bounds them is memory where a batch is large (16x1500x2048 bf16, one group, 20000 live frames: both calls together move 656 MB in 144 us, 4.6 TB/s), and where
+// What bounds them is memory where a batch is large (16x1500x2048 bf16, one group, 20000 live frames: both calls together move 656 MB in 140 us, 4.7 TB/s), and where
 // it is small the launches and a chain of loads, sums over lanes, and stores (3.6 us a launch).  The second reading finds in the caches what they hold.
 // A thread has a vector of N neighbouring channels (16 bytes where groups are whole vectors, less where they are not) in some rows; what it
 // knows of its channels stays in registers from row to row.
