@@ -60,7 +60,7 @@ __device__ __forceinline__ float loss_of(const Policy& po, const Sample& a, floa
     return loss;
 }
 
-// 2700 rows of 10001 bf16 (108 MB read and written): 28 us = 3.9 TB/s; 2900 of 32000 bf16 (371 MB): 76 us = 4.9 TB/s.
+// 2700 rows of 10001 bf16 (108 MB read and written): 26 us = 4.2 TB/s; 2900 of 32000 bf16 (371 MB): 76 us = 4.9 TB/s.
 // One row by a wavefront (!MULTI, four rows a workgroup), by a workgroup, or by G workgroups; then, and where rows are few, sums has (m or -inf, s, ., .) of
 // the `parts` that the row was read in before.
 template <typename T, typename D, int V, bool MULTI>
@@ -247,11 +247,15 @@ __global__ __launch_bounds__(1024) void policy_narrow_k(const T* __restrict__ z,
 }
 
 // As a distillation's rows, but for those of 17 to 24 slots, which three wavefronts take here however many there are (2700 of 10001 bf16: 31 -> 28 us, 6000 of 12000 65 -> 58,
-// 6000 of 6000 fp32 59 -> 52; of 16 slots 38 and 40, of 8 23 and 25)
+// 6000 of 6000 fp32 59 -> 52; of 16 slots 38 and 40, of 8 23 and 25).  Vector instructions take three quarters of such a row's time, so wavefronts have slots for the row and
+// hardly more: with six, seven and fourteen among their numbers, and not only 4, 8 and 16, 2700 of 9000 29.3 -> 25.1 us, of 10001 30.6 -> 27.6, of 17000 47.5 -> 41.4, 400 of 50000 27 -> 24.5.
 Plan plan_policy(long long rows, int C, int dtype)
 {
-    const Plan p = plan_distill(rows, C, dtype);
-    return p.W == 1 && slots_of(C, dtype) > 16 ? Plan{3, 1, 8} : p;
+    Plan p = plan_distill(rows, C, dtype);
+    const int slots = slots_of(C, dtype);
+    if (p.W == 1 && slots > 16) p.W = 3;
+    if (p.W > 1) p.V = tight((slots + p.W * p.G - 1) / (p.W * p.G), {2, 4, 6, 7, 8, 10, 14, 16});
+    return p;
 }
 
 template <typename T, typename D>
@@ -275,7 +279,7 @@ int launch(hipStream_t st, const void* z, const Policy& po, const Frames& fr, fl
             sums = (const float4*)ws;
         }
         if (p.W > 1)
-            known = with_slots<2, 4, 8, 12, 16>(p.V, [&](auto v) {
+            known = with_slots<2, 4, 6, 7, 8, 10, 14, 16>(p.V, [&](auto v) {
                 hipLaunchKernelGGL((policy_rows_k<T, D, decltype(v)::value, true>), dim3(grid_of((long long)fr.rows * p.G)), dim3(64 * p.W), 0, st, (const T*)z,
                                    po, fr, sums, parts, (D*)dz, C, p.G, how);
             });

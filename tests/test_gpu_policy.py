@@ -147,6 +147,19 @@ def test_every_form(P):
             check(run(P, c, dtype), c, gtype=dtype)
 
 
+# six, seven and fourteen slots a wavefront, two to seven wavefronts; seven and ten with a row in sixteen workgroups
+@pytest.mark.parametrize("rows,C,dtype", [(1100, 2801, "fp32"), (1100, 5631, "bf16"), (2056, 4500, "fp32"), (2056, 8999, "bf16"), (2056, 5101, "fp32"), (2056, 10001, "bf16"),
+                                          (416, 8500, "fp32"), (416, 17001, "bf16"), (136, 16601, "fp32"), (136, 33203, "bf16"), (8, 200001, "fp32"), (8, 262143, "fp32")],
+                         ids=str)
+def test_wavefronts_that_fit_the_row(P, rows, C, dtype):
+    c = case(rows + C, 1, 8, C, dtype)  # eight frames in turn: they begin alike within a vector
+    got = run(P, {k: np.concatenate([v] * (rows // 8), 1) for k, v in c.items()} if rows > 8 else c, dtype)
+    for k in ("frame", "logprob", "dz"):
+        for i in range(0, rows // 8 * 8, 8):
+            assert np.array_equal(got[k][:, i:i + 8], got[k][:, :8]), (k, i)
+    check({k: v[:, :8] for k, v in got.items() if k != "loss"}, c, gtype=dtype)
+
+
 @pytest.mark.parametrize("C,dtype,gtype", [(29, "fp32", "fp32"), (29, "bf16", "bf16"), (29, "bf16", "fp32"), (1000, "bf16", "fp32"), (20001, "bf16", "fp32")])
 def test_types_and_added_gradients(P, C, dtype, gtype):
     c = case(3, 3, 21, C, dtype)
