@@ -322,6 +322,36 @@ def test_captured_and_replayed_with_new_values(P):
             assert np.array_equal(got[a], to_host(b)), (k, a)
 
 
+def test_runs_of_frames_captured_and_replayed(P):
+    B, T, C, G = 2, 1300, 58, 2
+    assert P.w2l_groupnorm_launch_config(B, T, C, G, P.W2L_ACT_GLU, P.W2L_BF16)[0] == 0
+    x, gamma, beta, dy = case(38, B, T, C, "glu", "bf16")
+    xd, dyd, gd, bd = on_gpu(x, "bf16"), on_gpu(dy, "bf16"), to_dev(gamma), to_dev(beta)
+    n = to_dev(np.array([1300, 77], np.int32))
+    o = dict(y=torch.empty(B, T, C // 2, dtype=torch.bfloat16, device=DEV), mean=torch.empty(B, G, device=DEV), rstd=torch.empty(B, G, device=DEV))
+    g = dict(dx=torch.empty_like(xd), dgamma=torch.empty(C, device=DEV), dbeta=torch.empty(C, device=DEV))
+    ws = P.workspace(P.w2l_groupnorm_workspace_bytes(B, T, C, G, P.W2L_ACT_GLU, P.W2L_BF16))
+
+    def step():
+        P.w2l_groupnorm_fwd(xd, o["y"], o["mean"], o["rstd"], gd, bd, in_len=n, act=P.W2L_ACT_GLU, workspace=ws)
+        P.w2l_groupnorm_bwd(xd, dyd, o["mean"], o["rstd"], g["dx"], gd, bd, g["dgamma"], g["dbeta"], in_len=n, act=P.W2L_ACT_GLU, workspace=ws)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        xd.copy_(on_gpu(case(40 + k, B, T, C, "glu", "bf16")[0], "bf16"))
+        n.copy_(to_dev(np.array([1300 - k, 300 * k], np.int32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {a: to_host(b) for a, b in {**o, **g}.items()}
+        step()
+        torch.cuda.synchronize()
+        for a, b in {**o, **g}.items():
+            assert np.array_equal(got[a], to_host(b)), (k, a)
+
+
 def test_on_another_stream(P):
     x, gamma, beta, dy = case(19, 2, 100, 32, "silu", "fp32")
     want = run(P, x, 4, gamma, beta, None, "silu", "fp32")

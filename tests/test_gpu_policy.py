@@ -23,6 +23,7 @@ from test_gpu_scores import close, dev, guarded, rounded, spread
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 LOW, HIGH = 0.2, 0.3
+F32 = np.float32
 
 
 @pytest.fixture(scope="module")
@@ -310,3 +311,28 @@ def test_scores_beyond_2_31(P):
     torch.cuda.synchronize()
     check({"frame": to_host(frame[:, -3:]), "dz": to_host(dz[:, -3:])}, c, gtype="bf16")
     assert not bool(dz[:, :-3].any()) and not bool(frame[:, :-3].any())    # weights of 0
+
+
+@pytest.mark.parametrize("C", [29, 700])
+def test_ratios_beyond_fp32(P, C):
+    c = case(31, 2, 40, C, "fp32")
+    c["old"] = c["old"] - 200                                              # the ratio is +inf in fp32
+    c["A"] = np.abs(c["A"])
+    got = run(P, c, kl=0.0)                                                # bounded: (1 + clip_high) A, and no gradient
+    assert np.array_equal(got["frame"], (-(F32(1) + F32(HIGH)) * c["A"].astype(F32) * c["w"].astype(F32)).astype(np.float64)) and not got["dz"].any()
+    got = run(P, {**c, "A": -c["A"]}, kl=0.0)                              # not bounded from above: no finite number, and no gradient
+    assert np.all(got["frame"] == np.inf) and np.all(got["loss"] == np.inf) and not got["dz"].any()
+
+
+def test_on_another_stream(P):
+    c = case(32, 2, 60, 700, "fp32")
+    want = run(P, c)
+    z, tok, old, A, w, ref = (dev(c["z"], "fp32"), *(to_dev(c[k]) for k in ("tokens", "old", "A", "w", "ref")))
+    frame, loss, dz = torch.zeros(2, 60, device=DEV), torch.zeros(2, device=DEV), torch.zeros_like(z)
+    ws = P.workspace(P.w2l_policy_workspace_bytes(2, 60, 700, P.W2L_F32))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    P.w2l_policy_fwd_bwd(z, tok, old, A, frame, loss, dz, ref_logprob=ref, weight=w, clip_low=LOW, clip_high=HIGH, kl_coef=0.1, grad_scale=0.5, workspace=ws, stream=side)
+    side.synchronize()
+    for k, t in (("frame", frame), ("loss", loss), ("dz", dz)):
+        assert np.array_equal(to_host(t), want[k]), k
