@@ -148,8 +148,8 @@ int w2l_glu_bwd(const void *y, const void *dh, void *dy, long long rows, int Cou
  * G = 1 normalises an utterance as a whole, G = C every channel over time.  x, y share `dtype`; gamma, beta [C] fp32 or NULL (1, 0);
  * mean, rstd [B,G] fp32; in_len [B] int32 (0..T) or NULL: all frames.  The arithmetic is fp32, y is rounded once.
  * Frames t >= in_len[b] are not read, whatever they hold; y is 0 there.  An utterance of no frames has mean = rstd = 0.  An in_len
- * outside its range: y, mean and rstd of that utterance are NaN.  NaN or an infinity in a live frame makes its group NaN; so may values
- * beyond 2^60, whose squares fp32 does not hold.
+ * outside its range: y, mean and rstd of that utterance are NaN.  NaN or an infinity in a live frame makes its group NaN (mean, rstd, y and dx); so may
+ * deviations beyond 2^60, and so does a variance that fp32 does not hold.
  * Limits: C <= 8192, T <= 2^24, B <= 65534, B * T < 2^31, B * T * C <= 2^40; C divisible by G (and by 2 with GLU); eps > 0.  Workspace: the queried
  * bytes (one query for both calls), 256-byte aligned.  No output nor the workspace may overlap an input or another output (W2L_ERR_OVERLAP).
  * Results are bit-reproducible and do not depend on the other utterances of the batch beyond the rounding of fp32 sums. */

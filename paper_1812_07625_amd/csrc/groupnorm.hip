@@ -291,11 +291,14 @@ __global__ __launch_bounds__(MAX_THREADS) void norm_stats_k(const T* __restrict_
                         [&](int g, double2 k) { sums[((size_t)b * s.runs + run) * s.G + g] = k; });
 }
 
-// mean and 1 / deviation from a group's sums; inv: 1 / its values (0: it has none)
+// mean and 1 / deviation from a group's sums; inv: 1 / its values (0: it has none).  A variance that fp32 does not hold (a thread's squares are fp32 too) is none: 1 / sqrt(inf)
+// would be 0, every value would become beta, and every gradient 0.
 __device__ __forceinline__ float2 stat_of(double2 k, double inv, float eps)
 {
     const double mean = k.x * inv, var = k.y * inv - mean * mean;
-    return make_float2((float)mean, inv > 0. ? 1.f / sqrtf((var < 0. ? 0.f : (float)var) + eps) : 0.f);
+    const float sum = (var < 0. ? 0.f : (float)var) + eps;
+    if (!(sum < INFINITY)) return make_float2(NAN, NAN);
+    return make_float2((float)mean, inv > 0. ? 1.f / sqrtf(sum) : 0.f);
 }
 // A lane's share of the sums of a group's runs, from p on, a row of G groups each.  Where they are many, eight loads are in flight at once (in one utterance of
 // 2000x2048 with 64 groups, fp32, 39 -> 17 us for the forward call, together with the longer runs of runs_of); where they are few, the masked ones would cost 1 us.
