@@ -1090,6 +1090,21 @@ Shape group_shape(int B, int T, int C, int G, const int* in_len, int N, int spli
     return s;
 }
 
+// Utterances of a launch, which has to stay below 2^32 threads: of 2^22 workgroups, or one (whose runs are 2^24 / (4 lanes) at most, its groups 2^14)
+int utterances_of(const Shape& s, long long workgroups)
+{
+    const long long most = (1LL << 22) / workgroups;
+    return most < 1 ? 1 : most < s.B ? (int)most : s.B;
+}
+// Utterances first .. first + count alone
+Shape part_of(const Shape& s, int first, int count)
+{
+    Shape p = s;
+    p.B = count;
+    if (p.in_len) p.in_len += first;
+    return p;
+}
+
 size_t stat_bytes(const Shape& s) { return round_up((size_t)s.B * s.runs * s.G * sizeof(double2), 256); }
 size_t sum_bytes(const Shape& s) { return round_up((size_t)s.B * s.runs * s.C * 8, 256) + round_up((size_t)s.B * s.runs * s.G * 8, 256); }
 
@@ -1097,40 +1112,57 @@ template <typename T, int N>
 int forward(const void* x, const Shape& st, const Shape& ap, double2* sums, const float* gamma, const float* beta, float eps, int act, void* y, float* mean,
             float* rstd, hipStream_t stream)
 {
-    const dim3 g((unsigned)(st.runs * st.B)), n(threads_of(st));
-    hipLaunchKernelGGL((norm_stats_k<T, N>), g, n, (size_t)st.lanes * (st.C / N) * 16, stream, (const T*)x, st, sums);
-    if (int rc = launch_status()) return rc;
+    const int most = utterances_of(st, st.runs), Cy = act == W2L_ACT_GLU ? st.C / 2 : st.C;
+    for (int b = 0; b < st.B; b += most) {
+        const Shape a = part_of(st, b, std::min(most, st.B - b)), p = part_of(ap, b, a.B);
+        const T* const in = (const T*)x + (size_t)b * st.T * st.C;
+        double2* const k = sums + (size_t)b * st.runs * st.G;
+        hipLaunchKernelGGL((norm_stats_k<T, N>), dim3((unsigned)(a.runs * a.B)), dim3(threads_of(a)), (size_t)a.lanes * (a.C / N) * 16, stream, in, a, k);
+        if (int rc = launch_status()) return rc;
 #define W2L_APPLY(A_)                                                                                                                         \
-    hipLaunchKernelGGL((norm_apply_k<T, N, A_>), dim3((unsigned)(ap.runs * ap.B)), dim3(threads_of(ap)), (size_t)ap.G * 8, stream, (const T*)x, ap, sums, gamma, beta, \
-                       eps, (T*)y, mean, rstd)
-    if (act == W2L_ACT_NONE) W2L_APPLY(W2L_ACT_NONE);
-    else if (act == W2L_ACT_RELU) W2L_APPLY(W2L_ACT_RELU);
-    else if (act == W2L_ACT_SILU) W2L_APPLY(W2L_ACT_SILU);
-    else W2L_APPLY(W2L_ACT_GLU);
+    hipLaunchKernelGGL((norm_apply_k<T, N, A_>), dim3((unsigned)(p.runs * p.B)), dim3(threads_of(p)), (size_t)p.G * 8, stream, in, p, k, gamma, beta, eps, \
+                       (T*)y + (size_t)b * p.T * Cy, mean + (size_t)b * p.G, rstd + (size_t)b * p.G)
+        if (act == W2L_ACT_NONE) W2L_APPLY(W2L_ACT_NONE);
+        else if (act == W2L_ACT_RELU) W2L_APPLY(W2L_ACT_RELU);
+        else if (act == W2L_ACT_SILU) W2L_APPLY(W2L_ACT_SILU);
+        else W2L_APPLY(W2L_ACT_GLU);
 #undef W2L_APPLY
-    return launch_status();
+        if (int rc = launch_status()) return rc;
+    }
+    return W2L_OK;
 }
 template <typename T, int N>
 int forward_group(const void* x, const Shape& s, const float* gamma, const float* beta, float eps, int act, void* y, float* mean, float* rstd, hipStream_t stream)
 {
-    const dim3 g((unsigned)(s.B * (act == W2L_ACT_GLU ? s.G / 2 : s.G) * s.split)), n(threads_of(s));
-#define W2L_GROUP(A_) hipLaunchKernelGGL((norm_group_k<T, N, A_>), g, n, 0, stream, (const T*)x, s, gamma, beta, eps, (T*)y, mean, rstd)
-    if (act == W2L_ACT_NONE) W2L_GROUP(W2L_ACT_NONE);
-    else if (act == W2L_ACT_RELU) W2L_GROUP(W2L_ACT_RELU);
-    else if (act == W2L_ACT_SILU) W2L_GROUP(W2L_ACT_SILU);
-    else W2L_GROUP(W2L_ACT_GLU);
+    const int each = (act == W2L_ACT_GLU ? s.G / 2 : s.G) * s.split, most = utterances_of(s, each), Cy = act == W2L_ACT_GLU ? s.C / 2 : s.C;
+    for (int b = 0; b < s.B; b += most) {
+        const Shape p = part_of(s, b, std::min(most, s.B - b));
+#define W2L_GROUP(A_)                                                                                                                              \
+    hipLaunchKernelGGL((norm_group_k<T, N, A_>), dim3((unsigned)(p.B * each)), dim3(threads_of(p)), 0, stream, (const T*)x + (size_t)b * p.T * p.C, p, gamma, beta, eps, \
+                       (T*)y + (size_t)b * p.T * Cy, mean + (size_t)b * p.G, rstd + (size_t)b * p.G)
+        if (act == W2L_ACT_NONE) W2L_GROUP(W2L_ACT_NONE);
+        else if (act == W2L_ACT_RELU) W2L_GROUP(W2L_ACT_RELU);
+        else if (act == W2L_ACT_SILU) W2L_GROUP(W2L_ACT_SILU);
+        else W2L_GROUP(W2L_ACT_GLU);
 #undef W2L_GROUP
-    return launch_status();
+        if (int rc = launch_status()) return rc;
+    }
+    return W2L_OK;
 }
 template <typename T, int N, int ACT>
 int backward_group(const void* x, const void* dy, const Shape& s, const float* mean, const float* rstd, const float* gamma, const float* beta, float* chans,
                    void* dx, float* dgamma, float* dbeta, int accumulate, hipStream_t stream)
 {
     const bool GLU = ACT == W2L_ACT_GLU, want = dgamma || dbeta, alone = s.B == 1;
-    hipLaunchKernelGGL((norm_group_bwd_k<T, N, ACT>), dim3((unsigned)(s.B * (GLU ? s.G / 2 : s.G) * s.split)), dim3(threads_of(s)),
-                       want ? (size_t)(GLU ? 2 : 1) * s.lanes * s.Cg * 8 : 0, stream, (const T*)x, (const T*)dy, s, mean, rstd, gamma, beta, (T*)dx,
-                       want && !alone ? chans : nullptr, alone ? dgamma : nullptr, alone ? dbeta : nullptr, accumulate);
-    if (int rc = launch_status()) return rc;
+    const int each = (GLU ? s.G / 2 : s.G) * s.split, most = utterances_of(s, each), Cy = GLU ? s.C / 2 : s.C;
+    for (int b = 0; b < s.B; b += most) {
+        const Shape p = part_of(s, b, std::min(most, s.B - b));
+        const size_t rows = (size_t)b * p.T;
+        hipLaunchKernelGGL((norm_group_bwd_k<T, N, ACT>), dim3((unsigned)(p.B * each)), dim3(threads_of(p)), want ? (size_t)(GLU ? 2 : 1) * p.lanes * p.Cg * 8 : 0, stream,
+                           (const T*)x + rows * p.C, (const T*)dy + rows * Cy, p, mean + (size_t)b * p.G, rstd + (size_t)b * p.G, gamma, beta, (T*)dx + rows * p.C,
+                           want && !alone ? chans + (size_t)b * 2 * p.C : nullptr, alone ? dgamma : nullptr, alone ? dbeta : nullptr, accumulate);
+        if (int rc = launch_status()) return rc;
+    }
     if (!want || alone) return W2L_OK;
     const int width = join_width(s.B, JOIN_THREADS);
     hipLaunchKernelGGL(norm_join_k, dim3((s.C + width - 1) / width), dim3(JOIN_THREADS), 0, stream, chans, s.B, s.C, dgamma, dbeta, accumulate, width);
@@ -1140,14 +1172,25 @@ template <typename T, int N, int ACT>
 int backward(const void* x, const void* dy, const Shape& s, const float* mean, const float* rstd, const float* gamma, const float* beta, float* chans,
              float2* groups, void* dx, float* dgamma, float* dbeta, int accumulate, hipStream_t stream)
 {
-    hipLaunchKernelGGL((norm_sums_k<T, N, ACT>), dim3((unsigned)(s.runs * s.B)), dim3(threads_of(s)), (size_t)s.lanes * s.C * 8, stream, (const T*)x, (const T*)dy, s,
-                       mean, rstd, gamma, beta, chans, groups);
-    if (int rc = launch_status()) return rc;
-    const int width = join_width((long long)s.runs * s.B, threads_of(s)), ahead = dgamma || dbeta ? ((s.C + width - 1) / width + 7) / 8 * 8 : 0;
-    hipLaunchKernelGGL((norm_dx_k<T, N, ACT>), dim3((unsigned)(ahead + (long long)s.runs * s.B)), dim3(threads_of(s)),
-                       std::max((size_t)s.G * 8, (size_t)threads_of(s) / 64 * JOIN_CHANNELS * 16), stream, (const T*)x,
-                       (const T*)dy, s, mean, rstd, gamma, beta, chans, groups, (T*)dx, dgamma, dbeta, accumulate, ahead, width);
-    return launch_status();
+    const int most = utterances_of(s, s.runs), Cy = ACT == W2L_ACT_GLU ? s.C / 2 : s.C;
+    for (int b = 0; b < s.B; b += most) {
+        const Shape p = part_of(s, b, std::min(most, s.B - b));
+        const size_t rows = (size_t)b * p.T, runs = (size_t)b * p.runs;
+        const T *const in = (const T*)x + rows * p.C, *const back = (const T*)dy + rows * Cy;
+        const float *const mn = mean + (size_t)b * p.G, *const rs = rstd + (size_t)b * p.G;
+        float* const ch = chans + runs * 2 * p.C;
+        float2* const gr = groups + runs * p.G;
+        hipLaunchKernelGGL((norm_sums_k<T, N, ACT>), dim3((unsigned)(p.runs * p.B)), dim3(threads_of(p)), (size_t)p.lanes * p.C * 8, stream, in, back, p, mn, rs, gamma, beta,
+                           ch, gr);
+        if (int rc = launch_status()) return rc;
+        const int width = join_width((long long)p.runs * p.B, threads_of(p)), ahead = dgamma || dbeta ? ((p.C + width - 1) / width + 7) / 8 * 8 : 0;
+        // (utterances of a launch after the first add to what those before left in dgamma and dbeta)
+        hipLaunchKernelGGL((norm_dx_k<T, N, ACT>), dim3((unsigned)(ahead + (long long)p.runs * p.B)), dim3(threads_of(p)),
+                           std::max((size_t)p.G * 8, (size_t)threads_of(p) / 64 * JOIN_CHANNELS * 16), stream, in, back, p, mn, rs, gamma, beta, ch, gr,
+                           (T*)dx + rows * p.C, dgamma, dbeta, accumulate || b, ahead, width);
+        if (int rc = launch_status()) return rc;
+    }
+    return W2L_OK;
 }
 
 // f(a null pointer of the type, std::integral_constant of the vector length)

@@ -1,7 +1,9 @@
 """w2l_groupnorm_fwd / _bwd at the ends of what they take."""
 import numpy as np
 import pytest
+import torch
 
+from gpu_util import DEV
 from norm_cases import ACTS, code
 from test_gpu_groupnorm import case, check, held, run
 
@@ -52,3 +54,54 @@ def test_large_values_whose_variance_fp32_holds(P):
             x, gamma, beta, dy = case(22, 2, T, C, "none", dtype)
             x = x * 2.0 ** 56
             check(run(P, x, G, gamma, beta, None, "none", dtype, dy), x, G, gamma, beta, None, "none", dtype, dy, l2=False)
+
+
+# (T, C, G, form, memory): 65534 utterances, most without frames, in more workgroups than one launch has; parts end at utterance 2^22 / workgroups of one
+@pytest.mark.parametrize("T,C,G,form,part,need", [(8190, 4, 4, 0, 32768, 30), (1040, 520, 65, 1, 64527, 160)], ids=["runs of frames", "a workgroup a group"])
+def test_more_workgroups_than_a_launch_has(P, T, C, G, form, part, need):
+    """The utterances with frames are, bit for bit, what a batch of them alone is.  dgamma and dbeta are sums of the same fp32 numbers in 64 bits, rounded once, or once a part
+    and added up in fp32: within 4 half steps of the parts' magnitudes."""
+    B, act, U = 65534, P.W2L_ACT_SILU, 2.0 ** -24
+    assert all(P.w2l_groupnorm_launch_config(b, T, C, G, act, P.W2L_BF16)[0] == form for b in (B, 600, 1200))
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < need << 30:
+        pytest.skip("needs %d GiB" % need)
+    rng = np.random.default_rng(41)
+    live = np.sort(np.concatenate((rng.choice(part - 1, 599, False), [part - 1, part], part + 1 + rng.choice(B - part - 2, 598, False), [B - 1])))
+    few = len(live)
+    lengths = rng.integers(1, 200, few)
+    lengths[[0, 598, 600, -1]] = T, T, T - 1, T
+    n, at = torch.zeros(B, dtype=torch.int32, device=DEV), torch.from_numpy(live).to(DEV)
+    n[at] = torch.from_numpy(lengths.astype(np.int32)).to(DEV)
+    small = torch.randn(few, T, C, device=DEV, generator=torch.Generator(device=DEV).manual_seed(42)).bfloat16()
+    gamma, beta = torch.linspace(0.5, 1.5, C, device=DEV), torch.linspace(-1, 1, C, device=DEV)
+    x = torch.empty(B, T, C, dtype=torch.bfloat16, device=DEV)             # (frames behind an end are not read, whatever is there)
+    for i, b in enumerate(live):
+        x[b] = small[i]
+
+    def both(x, n):
+        b = len(x)
+        y, mean, rstd = torch.empty_like(x), torch.empty(b, G, device=DEV), torch.empty(b, G, device=DEV)
+        ws = P.workspace(P.w2l_groupnorm_workspace_bytes(b, T, C, G, act, P.W2L_BF16))
+        P.w2l_groupnorm_fwd(x, y, mean, rstd, gamma, beta, in_len=n, act=act, workspace=ws)
+        rows = at if b == B else torch.arange(b, device=DEV)
+        o = dict(y=y[rows], mean=mean[rows], rstd=rstd[rows])
+        nothing = torch.ones(b, dtype=torch.bool, device=DEV)
+        nothing[rows] = False
+        zero = lambda t: all(not bool(p[k].any()) for p, k in zip(t.split(4096), nothing.split(4096)))  # noqa: E731
+        assert zero(y) and zero(mean) and zero(rstd)
+        del y
+        dx, dg, db = torch.empty_like(x), torch.empty(C, device=DEV), torch.empty(C, device=DEV)
+        P.w2l_groupnorm_bwd(x, x, mean, rstd, dx, gamma, beta, dg, db, in_len=n, act=act, workspace=ws)
+        assert zero(dx)
+        return {**o, "dx": dx[rows], "dgamma": dg, "dbeta": db}
+    got = both(x, n)
+    del x
+    torch.cuda.empty_cache()
+    m = torch.from_numpy(lengths.astype(np.int32)).to(DEV)
+    want = both(small, m)
+    for k in ("y", "mean", "rstd", "dx"):
+        assert torch.equal(got[k], want[k]), k
+    first, second = both(small[:600], m[:600]), both(small[600:], m[600:])
+    for k in ("dgamma", "dbeta"):
+        assert bool((got[k] - want[k]).abs().le(4 * U * (first[k].abs() + second[k].abs())).all()), k
