@@ -3,6 +3,7 @@
 //                      norm_apply_k: joins the runs of an utterance, normalises, applies the activation;
 //                      norm_sums_k: sums over a run of du and du xhat of every channel, and of both times gamma of every group;
 //                      norm_dx_k: joins them and writes dx; workgroups of its own add up dgamma and dbeta
+//                      (norm_join_runs_k before norm_apply_k and norm_dx_k where an utterance has so many runs that they are joined once)
 //   a workgroup a group  norm_group_k, norm_group_bwd_k (and norm_join_k for dgamma and dbeta): groups that one workgroup reads twice
 // What bounds them is memory where a batch is large (16x1500x2048 bf16, one group, 20000 live frames: both calls together move 656 MB in 140 us, 4.7 TB/s), and where
 // it is small the launches and a chain of loads, sums over lanes, and stores (3.6 us a launch).  The second reading finds in the caches what they hold.
@@ -17,7 +18,7 @@ using namespace w2l;
 
 namespace {
 
-constexpr int MAX_CHANNELS = 8192, MAX_FRAMES = 1 << 24, MAX_THREADS = 512, BATCH = 4, JOIN_CHANNELS = 16, JOIN_THREADS = 256;  // (8192: a pair of floats a channel fits 64 KB of LDS)
+constexpr int MAX_CHANNELS = 8192, MAX_FRAMES = 1 << 24, MAX_THREADS = 512, BATCH = 4, JOIN_CHANNELS = 16, JOIN_GROUPS = 8, JOIN_THREADS = 256;  // (8192: a pair of floats a channel fits 64 KB of LDS)
 
 // A vector of N neighbouring channels as it lies in memory, and its values
 template <typename T, int N> struct Vec {
@@ -79,6 +80,8 @@ struct Shape {
     int B, T, C, G, Cg, rows, runs, cols, lanes, split;
     const int* in_len;
     float inv_Cg, inv_cols;
+    int joined = 0;  // the sums of an utterance's runs are joined already, in the place of its first run's
+    __device__ __forceinline__ int runs_to_join(int len) const { return joined && len > 0 ? 1 : (len + rows - 1) / rows; }
     // column and row of a thread (a thousand of them at most: see group_of)
     __device__ __forceinline__ void place(int& col, int& lane) const
     {
@@ -302,11 +305,11 @@ __device__ __forceinline__ float2 stat_of(double2 k, double inv, float eps)
 }
 // A lane's share of the sums of a group's runs, from p on, a row of G groups each.  Where they are many, eight loads are in flight at once (in one utterance of
 // 2000x2048 with 64 groups, fp32, 39 -> 17 us for the forward call, together with the longer runs of runs_of); where they are few, the masked ones would cost 1 us.
-template <typename V>
-__device__ __forceinline__ V sum_runs(const V* __restrict__ p, int G, int runs, int l, int team)
+template <typename A, typename V>
+__device__ __forceinline__ A sum_runs(const V* __restrict__ p, int G, int runs, int l, int team)
 {
     constexpr int U = 8;
-    V k{};
+    A k{};
     int r = l;
     for (; r + (U - 1) * team < runs; r += U * team) {
         V o[U];
@@ -329,16 +332,43 @@ __device__ __forceinline__ V sum_runs(const V* __restrict__ p, int G, int runs, 
 // of every group of utterance b, into LDS
 __device__ __forceinline__ void join_stats(const Shape& s, const double2* __restrict__ sums, int b, int len, float eps, float2* stat)
 {
-    const int runs = (len + s.rows - 1) / s.rows, team = team_of(s.G, runs), l = threadIdx.x & (team - 1), teams = blockDim.x / team;
+    const int runs = s.runs_to_join(len), team = team_of(s.G, runs), l = threadIdx.x & (team - 1), teams = blockDim.x / team;
     const double inv = len > 0 ? 1. / ((double)len * s.Cg) : 0.;
     for (int g0 = 0; g0 < s.G; g0 += teams) {
         const int g = g0 + threadIdx.x / team;
         double2 k = make_double2(0., 0.);
-        if (g < s.G) k = sum_runs(sums + (size_t)b * s.runs * s.G + g, s.G, runs, l, team);
+        if (g < s.G) k = sum_runs<double2>(sums + (size_t)b * s.runs * s.G + g, s.G, runs, l, team);
         k = sum64(k, team);
         if (g < s.G && l == 0) stat[g] = stat_of(k, inv, eps);
     }
     __syncthreads();
+}
+
+// The sums of groups' runs in a launch of its own, into the place of the first run's, for kernels whose workgroups would each read them all: `width` neighbouring groups
+// a workgroup, whose threads take runs in turn and add up in 64 bits.
+template <typename V>
+__global__ __launch_bounds__(JOIN_THREADS) void norm_join_runs_k(Shape s, V* sums, int width)
+{
+    __shared__ double2 lds[JOIN_THREADS / 64 * JOIN_GROUPS];
+    const int len = frames_of(s, blockIdx.y), l = threadIdx.x & (width - 1), g = blockIdx.x * width + l, wave = threadIdx.x / 64;
+    V* const at = sums + (size_t)blockIdx.y * s.runs * s.G + g;
+    double2 k = make_double2(0., 0.);
+    if (g < s.G && len > 0) k = sum_runs<double2>((const V*)at, s.G, (len + s.rows - 1) / s.rows, threadIdx.x / width, JOIN_THREADS / width);
+    for (int o = 32; o >= width; o >>= 1) {
+        k.x += __shfl_xor(k.x, o, 64);
+        k.y += __shfl_xor(k.y, o, 64);
+    }
+    if ((int)(threadIdx.x & 63) < width) lds[wave * width + l] = k;
+    __syncthreads();  // (and all runs have been read)
+    if ((int)threadIdx.x >= width || g >= s.G || len <= 0) return;
+    for (int i = 1; i < JOIN_THREADS / 64; ++i) {
+        k.x += lds[i * width + l].x;
+        k.y += lds[i * width + l].y;
+    }
+    V o;
+    o.x = k.x;
+    o.y = k.y;
+    *at = o;
 }
 
 // Values of channels c0 .. c0 + N of a vector over channels; `none` where there is none
@@ -632,13 +662,13 @@ __global__ __launch_bounds__(MAX_THREADS) __attribute__((amdgpu_waves_per_eu(4))
         load_channels(col);
     }
     if (t0 < len) {
-        const int runs = (len + s.rows - 1) / s.rows;
+        const int runs = s.runs_to_join(len);
         const float inv = 1.f / ((float)len * (float)s.Cg);
         const int team = team_of(s.G, runs), l = threadIdx.x & (team - 1), teams = blockDim.x / team;
         for (int g0 = 0; g0 < s.G; g0 += teams) {
             const int g = g0 + threadIdx.x / team;
             float2 k = make_float2(0.f, 0.f);
-            if (g < s.G) k = sum_runs(groups + (size_t)b * s.runs * s.G + g, s.G, runs, l, team);
+            if (g < s.G) k = sum_runs<float2>(groups + (size_t)b * s.runs * s.G + g, s.G, runs, l, team);
             k = sum64(k, team);
             if (g < s.G && l == 0) means[g] = make_float2(k.x * inv, k.y * inv);
         }
@@ -1035,6 +1065,15 @@ void runs_of(Shape& s)
     while (s.rows < 64 && (long long)(s.T / s.rows) * s.G * 2 > (long long)s.rows * s.C) s.rows += unit;
     s.runs = (s.T + s.rows - 1) / s.rows;
 }
+// Whether the sums of an utterance's runs, of `size` bytes a group, are joined by a launch of their own: where they outweigh what a run reads and writes, `tensors` times its
+// frames.  Each workgroup's joining them is the square of an utterance's length, 3 us of launch less.  Both ways in us, forward and backward call: 1x131072x64 bf16 in 32
+// groups 239 and 244 -> 27 and 30; 1x60000x512 in 32 75 and 91 -> 38 and 59; 1x24000x512 with GLU 25 -> 18 (backward below the limit, 33 and 28);  below it 1x12000x1536 with
+// GLU 30 and 45, 26 and 42 apart;  1x6000x512 12.6 and 15.6, 12.0 and 15.2;  16x1500x2048 in one group 50 and 85, 52 and 88;  above it and slower: 1x400000x64 in one group,
+// backward, 76 -> 80 (forward 51 -> 36).
+bool joins_apart(const Shape& s, int size, int tensors, int dtype)
+{
+    return (long long)s.runs * s.G * size > (long long)tensors * s.rows * s.C * (long long)dtype_size(dtype);
+}
 bool workspace_ok(const void* ws, size_t have, size_t need) { return ws && have >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0; }
 bool meets(const void* a, size_t an, const void* b, size_t bn)
 {
@@ -1090,6 +1129,13 @@ Shape group_shape(int B, int T, int C, int G, const int* in_len, int N, int spli
     return s;
 }
 
+// neighbouring groups of a workgroup that joins runs: their sums lie in one line
+int groups_of_join(int G)
+{
+    int width = JOIN_GROUPS;
+    while (width > 1 && width / 2 >= G) width /= 2;
+    return width;
+}
 // Utterances of a launch, which has to stay below 2^32 threads: of 2^22 workgroups, or one (whose runs are 2^24 / (4 lanes) at most, its groups 2^14)
 int utterances_of(const Shape& s, long long workgroups)
 {
@@ -1119,6 +1165,11 @@ int forward(const void* x, const Shape& st, const Shape& ap, double2* sums, cons
         double2* const k = sums + (size_t)b * st.runs * st.G;
         hipLaunchKernelGGL((norm_stats_k<T, N>), dim3((unsigned)(a.runs * a.B)), dim3(threads_of(a)), (size_t)a.lanes * (a.C / N) * 16, stream, in, a, k);
         if (int rc = launch_status()) return rc;
+        if (p.joined) {
+            const int width = groups_of_join(p.G);
+            hipLaunchKernelGGL(norm_join_runs_k<double2>, dim3((p.G + width - 1) / width, p.B), dim3(JOIN_THREADS), 0, stream, p, k, width);
+            if (int rc = launch_status()) return rc;
+        }
 #define W2L_APPLY(A_)                                                                                                                         \
     hipLaunchKernelGGL((norm_apply_k<T, N, A_>), dim3((unsigned)(p.runs * p.B)), dim3(threads_of(p)), (size_t)p.G * 8, stream, in, p, k, gamma, beta, eps, \
                        (T*)y + (size_t)b * p.T * Cy, mean + (size_t)b * p.G, rstd + (size_t)b * p.G)
@@ -1183,6 +1234,11 @@ int backward(const void* x, const void* dy, const Shape& s, const float* mean, c
         hipLaunchKernelGGL((norm_sums_k<T, N, ACT>), dim3((unsigned)(p.runs * p.B)), dim3(threads_of(p)), (size_t)p.lanes * p.C * 8, stream, in, back, p, mn, rs, gamma, beta,
                            ch, gr);
         if (int rc = launch_status()) return rc;
+        if (p.joined) {
+            const int width = groups_of_join(p.G);
+            hipLaunchKernelGGL(norm_join_runs_k<float2>, dim3((p.G + width - 1) / width, p.B), dim3(JOIN_THREADS), 0, stream, p, gr, width);
+            if (int rc = launch_status()) return rc;
+        }
         const int width = join_width((long long)p.runs * p.B, threads_of(p)), ahead = dgamma || dbeta ? ((p.C + width - 1) / width + 7) / 8 * 8 : 0;
         // (utterances of a launch after the first add to what those before left in dgamma and dbeta)
         hipLaunchKernelGGL((norm_dx_k<T, N, ACT>), dim3((unsigned)(ahead + (long long)p.runs * p.B)), dim3(threads_of(p)),
@@ -1245,6 +1301,7 @@ extern "C" int w2l_groupnorm_fwd(const void* x, const float* gamma, const float*
         });
     Shape ap = shape_of(B, T, C, G, in_len, Cy / n), st = shape_of(B, T, C, G, in_len, C / n);
     runs_of(ap);
+    ap.joined = joins_apart(ap, sizeof(double2), 2, dtype);
     st.rows = ap.rows;
     st.runs = ap.runs;
     return with_vector(dtype, n, [&](auto* t, auto n) {
@@ -1273,7 +1330,10 @@ extern "C" int w2l_groupnorm_bwd(const void* x, const void* dy, const float* mea
     const Form form = form_of(B, T, C, G, act, dtype);
     const int n = form.N;
     Shape s = form.group ? group_shape(B, T, C, G, in_len, n, form.split) : shape_of(B, T, C, G, in_len, Cy / n);
-    if (!form.group) runs_of(s);
+    if (!form.group) {
+        runs_of(s);
+        s.joined = joins_apart(s, sizeof(float2), 3, dtype);
+    }
     float* const chans = (float*)workspace;
     float2* const groups = (float2*)((char*)workspace + round_up((size_t)B * s.runs * C * 8, 256));
     return with_vector(dtype, n, [&](auto* t, auto n) {

@@ -105,3 +105,57 @@ def test_more_workgroups_than_a_launch_has(P, T, C, G, form, part, need):
     first, second = both(small[:600], m[:600]), both(small[600:], m[600:])
     for k in ("dgamma", "dbeta"):
         assert bool((got[k] - want[k]).abs().le(4 * U * (first[k].abs() + second[k].abs())).all()), k
+
+
+# runs joined by a launch of their own, both ways: of 24, 32 and 64 groups, of one, of nine (not a whole number of workgroups), with vectors of every length
+LONG = [(4, 40000, 48, 24), (3, 50000, 8, 1), (2, 40000, 36, 9), (1, 70000, 64, 64), (1, 40000, 64, 32)]
+
+
+@pytest.mark.parametrize("act", ["silu", "glu"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", LONG, ids=str)
+def test_long_utterances_in_many_runs(P, shape, dtype, act):
+    B, T, C, G = shape
+    assert P.w2l_groupnorm_launch_config(*shape, code(P, act), P.W2L_BF16 if dtype == "bf16" else P.W2L_F32)[0] == 0
+    x, gamma, beta, dy = case(C + B, B, T, C, act, dtype)
+    n = [T, 17, 0, T + 1][:B]
+    clean = [k if k <= T else 0 for k in n]
+    x[np.arange(T)[None] >= np.array(n)[:, None]] = 0
+    got = run(P, x, G, gamma, beta, n, act, dtype, dy)
+    for k in ("y", "mean", "rstd"):
+        assert np.isnan(got[k][3:]).all(), k
+        got[k][3:] = 0
+    assert not got["dx"][3:].any()
+    check(got, x * (np.arange(B) < 3)[:, None, None], G, gamma, beta, clean, act, dtype, dy, l2=False)
+    before = np.linspace(-1, 1, C).astype(np.float32).astype(np.float64)
+    again, add = (run(P, x, G, gamma, beta, n, act, dtype, dy, accumulate=a) for a in (None, before))
+    for k in ("y", "mean", "rstd", "dx", "dgamma", "dbeta"):
+        assert np.array_equal(again[k][:3], got[k][:3]), k
+    check({**add, **{k: got[k] for k in ("y", "mean", "rstd")}}, x * (np.arange(B) < 3)[:, None, None], G, gamma, beta, clean, act, dtype, dy, accumulate=before, l2=False)
+
+
+def test_long_utterances_captured_and_replayed(P):
+    B, T, C, G = 2, 40000, 64, 32
+    x, gamma, beta, dy = (torch.from_numpy(a).float().to(DEV) for a in case(51, B, T, C, "glu", "bf16"))
+    x, dy, n = x.bfloat16(), dy.bfloat16(), torch.tensor([T, 30000], dtype=torch.int32, device=DEV)
+    new = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device=DEV)  # noqa: E731
+    y, mean, rstd, dx, dg, db = new(B, T, C // 2, t=torch.bfloat16), new(B, G), new(B, G), new(B, T, C, t=torch.bfloat16), new(C), new(C)
+    ws = P.workspace(P.w2l_groupnorm_workspace_bytes(B, T, C, G, P.W2L_ACT_GLU, P.W2L_BF16))
+
+    def step():
+        P.w2l_groupnorm_fwd(x, y, mean, rstd, gamma, beta, in_len=n, act=P.W2L_ACT_GLU, workspace=ws)
+        P.w2l_groupnorm_bwd(x, dy, mean, rstd, dx, gamma, beta, dg, db, in_len=n, act=P.W2L_ACT_GLU, workspace=ws)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        x.normal_()
+        n.copy_(torch.tensor([T - k, 10000 * k], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (y, mean, rstd, dx, dg, db)]
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (y, mean, rstd, dx, dg, db))), k
