@@ -298,8 +298,8 @@ int w2l_sgd_momentum_step(float *w, float *v, const float *grad, void *w_lowp, l
  * call changes no tensor.  w fp32; grad fp32 or bf16 (grad_dtype, one for all tensors); moment_bits 32 or 8, one for all:
  *   32: m and v [n] fp32.
  *   8:  m and v [n] bytes, m_exp and v_exp [ceil(n / 256)] int8.  Value i is the e4m3 number (OCP, no infinity) of its byte times 2^exp of block i / 256;
- *       m holds the first moment, v the ROOT of the second.  A block's exponent is the least, and at least -100, with which its largest magnitude
- *       is at most 448 * 2^exp (0 where all are 0).  Values are rounded up or down at random, in proportion to how near they are, with random bits of
+ *       m holds the first moment, v the ROOT of the second.  A block's exponent (any int8 is read) becomes the least, and at least -100, with which its largest
+ *       magnitude is at most 448 * 2^exp (0 where all are 0).  Values are rounded up or down at random, in proportion to how near they are, with random bits of
  *       (seed, t, index of the tensor, index of the value): the same call gives the same bits.  A root above 0 stays above 0.  NaN and
  *       infinities are kept as NaN.  All bytes and exponents zero: moments of zero.
  * Arithmetic is fp32 (the moments with each product and sum rounded as written, the norm's sum and the step's constants in 64 bits), w is

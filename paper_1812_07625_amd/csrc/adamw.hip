@@ -202,7 +202,7 @@ __device__ __forceinline__ int exponent_of(float most)
     const int E = (int)(u >> 23) - 135 + ((u & 0x7fffffu) > 0x600000u);  // 448 = 1.75 * 2^8
     return u == 0 ? 0 : E < -100 ? -100 : E;
 }
-__device__ __forceinline__ float two_to(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
+__device__ __forceinline__ float two_to(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }  // -126 <= e <= 127
 // |x| in units of the block's least number (scale = 2^(9 - E): 0 <= u <= 448 * 512), r: 16 random bits -> the magnitude's code
 __device__ __forceinline__ unsigned code_of(float u, unsigned r)
 {
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(THREADS) void adamw8_k(const Table t, const Scalars
     if (there) {
         float g[16];
         unsigned mq[4], vq[4];
-        const float ms = two_to(e.m_exp[block]), vs = two_to(e.v_exp[block]);
+        const float ms = __builtin_ldexpf(1.f, e.m_exp[block]), vs = __builtin_ldexpf(1.f, e.v_exp[block]);  // (-128 and -127 are exponents too: denormal numbers)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const long long at = base + j * 64 + l * 4;
