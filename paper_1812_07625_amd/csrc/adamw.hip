@@ -456,7 +456,7 @@ int overlap(const w2l_adamw_tensor* t, int n, size_t grad_size, int bits, const 
 template <typename G>
 int launch(const w2l_adamw_tensor* t, int n, int bits, const Hyper& h, const float* lr, const int* step, float* grad_norm, void* ws, hipStream_t st)
 {
-    double* const sums = reinterpret_cast<double*>(static_cast<char*>(ws) + 256);
+    double* const sums = ws ? reinterpret_cast<double*>(static_cast<char*>(ws) + 256) : nullptr;  // (none: neither norm nor scalars from the device)
     Scalars* now = nullptr;
     const bool norm = h.max_norm > 0. || grad_norm;
     const Moments o{(float)h.beta1, (float)(1. - h.beta1), (float)h.beta2, (float)(1. - h.beta2)};
