@@ -275,6 +275,9 @@ int w2l_policy_fwd_bwd(const void *z, const int *tokens, const float *old_logpro
                        float clip_high, float kl_coef, float grad_scale, int z_dtype, int dz_dtype, int accumulate,
                        void *workspace, size_t ws_bytes, void *stream);
 
+/* Host-only query: how w2l_policy_fwd_bwd deals out a row, as w2l_distill_launch_config.  For tests and tuning; launches nothing.  Errors as the call itself. */
+int w2l_policy_launch_config(int B, int Tp, int C, int z_dtype, int *wavefronts, int *groups, int *slots);
+
 /* ---- SGD with momentum (Sec. 4.1: the optimiser of every run in the paper) ---------
  * The paper names the optimiser and does not write the update out; this is the classical
  * heavy-ball form with optional L2 weight decay, elementwise over n values:

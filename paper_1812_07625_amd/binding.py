@@ -29,7 +29,7 @@ __all__ = [
     "w2l_token_logprob_launch_config", "w2l_distill_workspace_bytes", "w2l_distill_fwd_bwd", "w2l_distill_launch_config",
     "w2l_frame_ids_check_host",
     "W2L_ACT_NONE", "W2L_ACT_RELU", "W2L_ACT_SILU", "W2L_ACT_GLU", "w2l_groupnorm_workspace_bytes", "w2l_groupnorm_fwd", "w2l_groupnorm_bwd", "w2l_groupnorm_launch_config",
-    "w2l_policy_workspace_bytes", "w2l_policy_fwd_bwd",
+    "w2l_policy_workspace_bytes", "w2l_policy_fwd_bwd", "w2l_policy_launch_config",
     "w2l_adamw_tensor", "adamw_tensors", "w2l_adamw_workspace_bytes", "w2l_adamw_step",
     "w2l_train_step_workspace_bytes", "w2l_train_step", "w2l_train_step_asg_workspace_bytes", "w2l_train_step_asg",
     "w2l_train_step_launch_config", "w2l_train_step_layer_config", "w2l_sgd_momentum_step",
@@ -94,6 +94,7 @@ def _load():
         "w2l_groupnorm_launch_config": (i, [i] * 6 + [C.POINTER(C.c_int)] * 2),
         "w2l_policy_workspace_bytes": (sz, [i] * 4),
         "w2l_policy_fwd_bwd": (i, [vp] * 5 + [i] + [vp] * 6 + [i] * 3 + [f] * 4 + [i] * 3 + [vp, sz, vp]),
+        "w2l_policy_launch_config": (i, [i] * 4 + [C.POINTER(C.c_int)] * 3),
         "w2l_adamw_workspace_bytes": (sz, [vp, i]),
         "w2l_adamw_step": (i, [vp, i, i, i, ll] + [C.c_double] * 6 + [C.c_uint] + [vp] * 4 + [sz, vp]),
         "w2l_ctc_workspace_bytes": (sz, [i] * 4),
@@ -431,6 +432,13 @@ def w2l_policy_fwd_bwd(z, tokens, old_logprob, advantage, frame_loss, loss=None,
     _call(raw.w2l_policy_fwd_bwd, "w2l_policy_fwd_bwd", dev,
           (*ptr, B, T, Cc, clip_low, clip_high, kl_coef, grad_scale, dt, gt, 1 if accumulate else 0, *_scratch(workspace, dev)), stream)
     return frame_loss, loss, dz
+
+
+def w2l_policy_launch_config(B, Tp, Cc, dtype):
+    """(wavefronts, workgroups, slots) that w2l_policy_fwd_bwd gives a row; host only."""
+    out = [C.c_int() for _ in range(3)]
+    _check(raw.w2l_policy_launch_config(B, Tp, Cc, dtype, *[C.byref(o) for o in out]), "w2l_policy_launch_config")
+    return tuple(o.value for o in out)
 
 
 def w2l_groupnorm_workspace_bytes(B, T, Cc, groups, act, dtype) -> int:

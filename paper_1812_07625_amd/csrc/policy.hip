@@ -331,3 +331,15 @@ extern "C" int w2l_policy_fwd_bwd(const void* z, const int* tokens, const float*
     if (dz_dtype == W2L_F32) return launch<bf16_t, float>((hipStream_t)stream, z, po, fr, loss, dz, workspace, C, accumulate);
     return launch<bf16_t, bf16_t>((hipStream_t)stream, z, po, fr, loss, dz, workspace, C, accumulate);
 }
+
+extern "C" int w2l_policy_launch_config(int B, int Tp, int C, int z_dtype, int* wavefronts, int* groups, int* slots)
+{
+    if (!wavefronts || !groups || !slots) return W2L_ERR_NULL;
+    if (!shape_ok(B, Tp, C, 0, 0)) return W2L_ERR_SHAPE;
+    if (!valid_dtype(z_dtype)) return W2L_ERR_DTYPE;
+    const Plan p = plan_policy((long long)B * Tp, C, z_dtype);
+    *wavefronts = p.W;
+    *groups = p.G;
+    *slots = p.V;
+    return W2L_OK;
+}
