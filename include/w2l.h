@@ -146,7 +146,8 @@ int w2l_glu_bwd(const void *y, const void *dh, void *dy, long long rows, int Cou
  *   y = u (W2L_ACT_NONE), max(u, 0) (_RELU), u sigmoid(u) (_SILU): [B,T,C]
  *   y = u[:C/2] sigmoid(u[C/2:]) (_GLU, value half and gate half as in w2l_glu_fwd): [B,T,C/2]
  * G = 1 normalises an utterance as a whole, G = C every channel over time.  x, y share `dtype`; gamma, beta [C] fp32 or NULL (1, 0);
- * mean, rstd [B,G] fp32; in_len [B] int32 (0..T) or NULL: all frames.  The arithmetic is fp32, y is rounded once.
+ * mean, rstd [B,G] fp32; in_len [B] int32 (0..T) or NULL: all frames.  The arithmetic is fp32, y is rounded once: the mean, rounded to fp32 as it is returned, leaves
+ * xhat 2^-24 |mean| rstd off; squares of deviations below 2^-60 lose bits, which counts where eps is below 2^-100.
  * Frames t >= in_len[b] are not read, whatever they hold; y is 0 there.  An utterance of no frames has mean = rstd = 0.  An in_len
  * outside its range: y, mean and rstd of that utterance are NaN.  NaN or an infinity in a live frame makes its group NaN (mean, rstd, y and dx); so may
  * deviations beyond 2^60, and so does a variance that fp32 does not hold.
@@ -266,6 +267,8 @@ int w2l_frame_ids_check_host(const int *ids, const int *in_len, int B, int Tp, i
  * Frames t >= in_len[b], frames of token -1 and frames of weight 0, whatever they hold, have loss, logprob and gradient 0.  An
  * advantage of 0 leaves the KL term alone.  NaN or +inf in the frame's z, a token other than -1 outside [0,C), an in_len outside its range: loss and
  * logprob are NaN (of the whole utterance in the last case); nothing but -inf: logprob -inf.  A frame whose loss is no finite fp32 number has zero gradient.
+ * r, exp(e) and their products with A and kl_coef are fp32 numbers: where one that the loss takes is beyond fp32 (a difference of log-probabilities above 88), the loss is infinite
+ * whatever the weight.
  * 0 <= clip_low <= 1, clip_high >= 0 (+inf: no bound), kl_coef >= 0 finite, weight * grad_scale * f finite.  Limits and workspace as
  * w2l_token_logprob_fwd; no output nor the workspace may overlap an input or another output (W2L_ERR_OVERLAP). */
 size_t w2l_policy_workspace_bytes(int B, int Tp, int C, int z_dtype);
@@ -305,10 +308,10 @@ int w2l_sgd_momentum_step(float *w, float *v, const float *grad, void *w_lowp, l
  *       magnitude is at most 448 * 2^exp (0 where all are 0).  Values are rounded up or down at random, in proportion to how near they are, with random bits of
  *       (seed, t, index of the tensor, index of the value): the same call gives the same bits.  The expectation of the first moment and of the root is what
  *       was rounded.  The second moment has the rounding's variance more: with normal gradients it settles 3 to 6 % above its 32-bit value, and single roots scatter by
- *       12 to 17 %, whatever beta2 is.  A root above 0 stays above 0 while its square is above 0 in fp32 (from 2^-75 on): below the block's least number, 2^(exp - 9), it becomes
+ *       12 to 17 %, whatever beta2 is (1 - beta2 small: 4.0 and 15 % measured at 0.999, 2.9 and 14 at 0.98).  A root above 0 stays above 0 while its square is above 0 in fp32 (from 2^-75 on): below the block's least number, 2^(exp - 9), it becomes
  *       that.  NaN and infinities are kept as NaN.  All bytes and exponents zero: moments of zero.
  * Arithmetic is fp32 (the moments with each product and sum rounded as written, the norm's sum and the step's constants in 64 bits), w is
- * off by a few half steps.  lr_dev, step_dev [1] (nullable): fp32 lr and int32 step, read on the device in place of lr and step, so that a captured graph
+ * off by a few half steps (of numbers that fp32 holds as normal ones: lr / (1 - beta1^t) * m above 2^-126, the denominator below 2^126).  lr_dev, step_dev [1] (nullable): fp32 lr and int32 step, read on the device in place of lr and step, so that a captured graph
  * steps on; a step below 1 there changes nothing, lr is not checked there.  They, grad_norm and the exponents need natural alignment only.
  * tensors: HOST array, its pointers DEVICE pointers; n = 0: skipped.  Nothing the call writes may overlap anything else it reads or writes
  * (W2L_ERR_OVERLAP: a tensor listed twice, say).  Workspace (queried bytes, 256-byte aligned) where the norm, lr_dev or step_dev is asked for; NULL will do

@@ -5,7 +5,7 @@
 //                      norm_dx_k: joins them and writes dx; workgroups of its own add up dgamma and dbeta
 //                      (norm_join_runs_k before norm_apply_k and norm_dx_k where an utterance has so many runs that they are joined once)
 //   a workgroup a group  norm_group_k, norm_group_bwd_k (and norm_join_k for dgamma and dbeta): groups that one workgroup reads twice
-// What bounds them is memory where a batch is large (16x1500x2048 bf16, one group, 20000 live frames: both calls together move 656 MB in 140 us, 4.7 TB/s), and where
+// What bounds them is memory where a batch is large (16x1500x2048 bf16, one group, 20000 live frames: both calls together move 723 MB in 140 us, 5.2 TB/s), and where
 // it is small the launches and a chain of loads, sums over lanes, and stores (3.6 us a launch).  The second reading finds in the caches what they hold.
 // A thread has a vector of N neighbouring channels (16 bytes where groups are whole vectors, less where they are not) in some rows; what it
 // knows of its channels stays in registers from row to row.
@@ -18,7 +18,7 @@ using namespace w2l;
 
 namespace {
 
-constexpr int MAX_CHANNELS = 8192, MAX_FRAMES = 1 << 24, MAX_THREADS = 512, BATCH = 4, JOIN_CHANNELS = 16, JOIN_GROUPS = 8, JOIN_THREADS = 256;  // (8192: a pair of floats a channel fits 64 KB of LDS)
+constexpr int MAX_CHANNELS = 8192, MAX_FRAMES = 1 << 24, MAX_THREADS = 512, BATCH = 4, JOIN_CHANNELS = 16, JOIN_GROUPS = 8, JOIN_THREADS = 256;  // (8192: a lane's pairs of floats of all channels fit 64 KB of LDS; norm_stats_k's pairs of 64-bit sums, one a vector, are 128 of its 160 where vectors are of one channel)
 
 // A vector of N neighbouring channels as it lies in memory, and its values
 template <typename T, int N> struct Vec {
