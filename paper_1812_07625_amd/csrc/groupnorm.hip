@@ -1066,13 +1066,14 @@ void runs_of(Shape& s)
     s.runs = (s.T + s.rows - 1) / s.rows;
 }
 // Whether the sums of an utterance's runs, of `size` bytes a group, are joined by a launch of their own: where they outweigh what a run reads and writes, `tensors` times its
-// frames.  Each workgroup's joining them is the square of an utterance's length, 3 us of launch less.  Both ways in us, forward and backward call: 1x131072x64 bf16 in 32
-// groups 239 and 244 -> 27 and 30; 1x60000x512 in 32 75 and 91 -> 38 and 59; 1x24000x512 with GLU 25 -> 18 (backward below the limit, 33 and 28);  below it 1x12000x1536 with
-// GLU 30 and 45, 26 and 42 apart;  1x6000x512 12.6 and 15.6, 12.0 and 15.2;  16x1500x2048 in one group 50 and 85, 52 and 88;  above it and slower: 1x400000x64 in one group,
-// backward, 76 -> 80 (forward 51 -> 36).
+// frames, and all workgroups together would read 16 MB of them, which takes as long as a launch.  Each workgroup's joining them is the square of an utterance's length.  Both ways in us, forward and backward
+// call: 1x131072x64 bf16 in 32 groups 239 and 244 -> 27 and 30; 1x60000x512 in 32 75 and 91 -> 38 and 59; 1x24000x512 with GLU 25 -> 18 (backward below the first limit, 33 and 28);
+// below it 1x12000x1536 with GLU 30 and 45, 26 and 42 apart;  1x6000x512 12.6 and 15.6, 12.0 and 15.2;  16x1500x2048 in one group 50 and 85, 52 and 88;  below the second 32x700x80 in 80
+// 11.6, 12.3 apart;  above both and slower: 1x400000x64 in one group, backward, 76 -> 80 (forward 51 -> 36).
 bool joins_apart(const Shape& s, int size, int tensors, int dtype)
 {
-    return (long long)s.runs * s.G * size > (long long)tensors * s.rows * s.C * (long long)dtype_size(dtype);
+    const double sums = (double)s.runs * s.G * size;  // of an utterance
+    return sums > (double)tensors * s.rows * s.C * (double)dtype_size(dtype) && sums * s.runs * s.B > (double)(16 << 20);
 }
 bool workspace_ok(const void* ws, size_t have, size_t need) { return ws && have >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0; }
 bool meets(const void* a, size_t an, const void* b, size_t bn)

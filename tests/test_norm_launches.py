@@ -44,7 +44,7 @@ def test_one_launch_each_where_they_fit(recorder):
     assert P.w2l_groupnorm_launch_config(65, 1 << 23, 32, 32, 2, 1) == (0, 1)
 
 
-@pytest.mark.parametrize("size", [(1, 131072, 64, 32, 2, 1), (1, 1 << 24, 32, 32, 2, 1), (4, 60000, 512, 32, 3, 1), (1, 1 << 22, 512, 512, 2, 0), (2, 50000, 8, 1, 0, 0)], ids=str)
+@pytest.mark.parametrize("size", [(1, 131072, 64, 32, 2, 1), (1, 1 << 24, 32, 32, 2, 1), (4, 60000, 512, 32, 3, 1), (1, 1 << 22, 512, 512, 2, 0), (2, 100000, 8, 1, 0, 0)], ids=str)
 def test_runs_of_long_utterances_are_joined_once(recorder, size):
     """Not by each workgroup that needs their sums, which would be the square of an utterance's length: a launch that gives up to eight groups of an utterance a workgroup, each way."""
     B, T, C, G, act, dtype = size
@@ -53,3 +53,8 @@ def test_runs_of_long_utterances_are_joined_once(recorder, size):
     assert len(all_) == 6
     for grid, block, _ in (all_[1], all_[4]):
         assert grid == (-(-G // 8), B, 1) and block[0] == 256
+
+
+@pytest.mark.parametrize("size", [(32, 700, 80, 80, 2, 1), (1, 3000, 512, 32, 2, 1)], ids=str)
+def test_few_sums_cost_no_launch(recorder, size):
+    assert P.w2l_groupnorm_launch_config(*size)[0] == 0 and len(launches(recorder, call(*size))) == 4
